@@ -17,6 +17,9 @@
  *                          App. A.2)
  *   cast_block_step        the three in order at one attention residual site
  *
+ * and the history as a serving loop keeps it, a paged KV cache: cast_rotary,
+ * cast_cache_append, cast_cache_attention.
+ *
  * Conventions shared by every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller; `anchors` and
  *     `anchor_mask` are HOST arrays read during the call only.  The library
@@ -383,6 +386,144 @@ typedef struct {
 cast_status cast_select_frames(const cast_select_args* args, void* workspace,
                                size_t workspace_bytes, void* stream);
 size_t cast_select_workspace_size(const cast_select_args* args);
+
+/* ------------------------------------------------------------------------ */
+/* Paged KV cache: the history as a serving loop keeps it (no counterpart in */
+/* the paper, whose history is given): rotary positions, the append of new   */
+/* tokens, and attention over everything a token may still see.              */
+/* ------------------------------------------------------------------------ */
+#define CAST_F8E4M3 2             /* cache pages only: 8-bit floats (4 exponent, 3 mantissa bits,
+                                     no infinity), one scale for each (page, KV head) */
+
+#define CAST_ROTARY_HALF 0        /* pair i = channels (i, i + rot_dim / 2) */
+#define CAST_ROTARY_INTERLEAVED 1 /* pair i = channels (2 i, 2 i + 1) */
+#define CAST_ROTARY_PLAIN 0       /* f = base^(-k / n) for pair k of an axis' n pairs */
+#define CAST_ROTARY_LINEAR 1      /* f / factor */
+#define CAST_ROTARY_STRETCH 2     /* base -> base * factor^(n / (n - 1)) */
+#define CAST_ROTARY_PARTS 3       /* f (g + (1 - g) / factor), g = (r - 1) / 31 clamped to [0, 1],
+                                     r = original_length f / 2 pi turns; amplitude 1 + 0.1 ln factor */
+#define CAST_MAX_AXES 3
+#define CAST_MAX_ROTARY_PAIRS 128
+
+typedef struct {
+  int32_t rot_dim;                /* channels rotated, the first of each head: a multiple of 16, 16..256 */
+  int32_t layout;                 /* CAST_ROTARY_HALF | CAST_ROTARY_INTERLEAVED */
+  int32_t n_axes;                 /* position axes, 1..CAST_MAX_AXES (e.g. frame, row, column) */
+  int32_t pairs[CAST_MAX_AXES];   /* pairs of each axis, >= 1, in order; their sum is rot_dim / 2 */
+  int32_t scaling;                /* CAST_ROTARY_PLAIN | _LINEAR | _STRETCH | _PARTS */
+  double base, factor;            /* base > 1; factor >= 1 (unless _PLAIN) */
+  int32_t original_length;        /* _PARTS: the length the frequencies were learnt at, >= 1 */
+} cast_rotary_params;
+
+/* What the kernels take: made once by cast_rotary_table_init, kept by the caller, plain data. */
+typedef struct {
+  int32_t rot_dim, layout, n_axes;
+  float amplitude;
+  uint64_t turn[CAST_MAX_ROTARY_PAIRS];  /* turns that a position advances pair i by, in 2^-64 */
+  uint8_t axis[CAST_MAX_ROTARY_PAIRS];
+} cast_rotary_table;
+
+/* Host only.  Errors: INVALID_ARG for NULL pointers or a value outside the ranges above, and for
+ * _STRETCH with an axis of one pair; UNSUPPORTED for rot_dim not a multiple of 16 or above 256. */
+cast_status cast_rotary_table_init(const cast_rotary_params* params, cast_rotary_table* table);
+
+typedef struct {
+  const void* x;                  /* device [T, H, d], bf16 or f32 */
+  void* out;                      /* device [T, H, d] of the same dtype; may be x */
+  int64_t x_row_stride, out_row_stride;  /* elements between tokens: >= H*d, multiples of 8 */
+  int32_t T, H, d;                /* d a multiple of 16, rot_dim..256; T = 0 does nothing */
+  int32_t dtype;                  /* CAST_BF16 | CAST_F32 */
+  const int32_t* positions;       /* device [T, n_axes], any int32 */
+  const cast_rotary_table* table; /* HOST */
+  int32_t inverse;                /* nonzero: the transposed map, i.e. the gradient of the rotation */
+} cast_rotary_args;
+
+/* Each pair (a, b) of the first rot_dim channels becomes amplitude * (a cos - b sin, b cos + a sin)
+ * with the angle positions[t, axis] * f (inverse: -angle); the other channels are copied.  The
+ * angle is reduced exactly (integer turns), so it is good to f32 rounding at any position.
+ * f32 arithmetic, one rounding.  Errors: INVALID_ARG for NULL or misaligned pointers, bad shapes or
+ * strides, an unusable table; UNSUPPORTED for a head dim as above. */
+cast_status cast_rotary(const cast_rotary_args* args, void* stream);
+
+typedef struct {
+  int32_t dtype;                  /* CAST_BF16 or CAST_F8E4M3 */
+  int32_t n_pages, page_size;     /* page_size 16, 32, 64 or 128 tokens */
+  int32_t H, d;                   /* KV heads; d in {64, 128} */
+  void* k;                        /* device [n_pages, page_size, H, d].  With CAST_BF16 this is the */
+  void* v;                        /* layout of history blocks [M, B_v, H, d] (cast_route_args) */
+  int64_t row_stride;             /* elements between token rows: >= H*d, a multiple of 16; a page
+                                     is page_size consecutive rows */
+  float* k_scale;                 /* CAST_F8E4M3: device [n_pages, H], powers of two: a row holds */
+  float* v_scale;                 /* code * scale */
+} cast_kv_cache;
+
+/* The sequences of a call.  Sequence b has kv_len[b] tokens in the cache once its new ones are
+ * counted; position p lies in row p % page_size of page page_table[b, p / page_size]. */
+typedef struct {
+  const int32_t* page_table;      /* device [B, max_pages]; entries no row of the call needs are not read */
+  int64_t page_table_stride;      /* elements between sequences, >= max_pages */
+  int32_t max_pages;
+  const int32_t* kv_len;          /* device [B], >= 0 */
+  const int32_t* cu_new;          /* device [B + 1], ascending from 0 to T: sequence b's new tokens are
+                                     rows cu_new[b] .. cu_new[b + 1] - 1 of the call's T; NULL: T / B each */
+  int32_t B, T, max_new;          /* max_new: bound of a sequence's new tokens */
+} cast_cache_batch;
+
+typedef struct {
+  cast_kv_cache cache;
+  cast_cache_batch batch;
+  const void* k;                  /* device bf16 [T, H, d] */
+  const void* v;
+  int64_t k_row_stride, v_row_stride;    /* >= H*d, multiples of 8 */
+  const cast_rotary_table* rotary;       /* HOST; NULL: keys are stored as they are */
+  const int32_t* positions;       /* device [T, n_axes]; NULL: a token's place in its sequence (one axis) */
+  const void* q;                  /* optional device bf16 [T, H_q, d]: rotated into q_out in this launch */
+  void* q_out;                    /* device bf16 [T, H_q, d]; may be q */
+  int64_t q_row_stride, q_out_row_stride;
+  int32_t H_q;
+} cast_append_args;
+
+/* New token i of sequence b, at position p = kv_len[b] - new_b + i, has its key rotated (f32) and
+ * its key and value stored in the cache; at p < 0 nothing is stored and q_out is left as it is.  CAST_F8E4M3: of each page,
+ * head and K or V, e is the least integer with max |x| <= 448 * 2^e over the finite new values, in
+ * [-120, 120]; a page that the sequence only continues (its first new row is not row 0) keeps the
+ * larger of its scale and 2^e, and its earlier rows are rounded again at a scale that grew (a power
+ * of two: nothing but subnormal codes changes).  Codes are x / scale to nearest even; NaN and
+ * infinity become NaN.  The pages written by one call are distinct.
+ * One launch.  Errors: INVALID_ARG for NULL or misaligned pointers, bad shapes, strides or tables;
+ * UNSUPPORTED for d not 64/128, page_size not 16/32/64/128.  A page outside [0, n_pages), a position
+ * past max_pages pages or a new token past max_new is left out, recorded, and reported by
+ * cast_check_device() as INVALID_ARG. */
+cast_status cast_cache_append(const cast_append_args* args, void* stream);
+
+typedef struct {
+  cast_kv_cache cache;
+  cast_cache_batch batch;
+  const void* q;                  /* device bf16 [T, H_q, d]; query head h reads KV head h / (H_q / H) */
+  int64_t q_row_stride;           /* >= H_q*d, a multiple of 8 */
+  int32_t H_q;                    /* a multiple of cache.H, at most 128 times it */
+  int32_t causal;                 /* nonzero: a row sees positions up to its own; 0: up to kv_len - 1 */
+  int32_t window;                 /* > 0: a row at p sees positions > p - window only, and */
+  int32_t sinks;                  /* positions < sinks (which the window never hides); 0 = no window */
+  float scale;                    /* softmax scale; <= 0 means 1/sqrt(d) */
+  void* o;                        /* device [T, H_q*d], dtype o_dtype */
+  int32_t o_dtype;                /* CAST_BF16 or CAST_F32 */
+  float* lse;                     /* optional device f32 [T, H_q]: natural log-sum-exp of the row's logits */
+} cast_cache_attn_args;
+
+/* o[t, h] = sum_j softmax_j(scale * q_t,h . k_j) v_j over the positions j that row t sees; a row that
+ * sees none gives 0 (lse -inf).  The new tokens themselves are read from the cache: append first.
+ * bf16 products (8-bit rows are decoded to bf16, exactly), f32 softmax and sums.  What lies at
+ * positions that a row does not see never reaches it, whatever it holds.  The workspace
+ * (cast_cache_attention_workspace_size() bytes; NULL allowed when that is 0) holds partial results of
+ * rows whose keys are split over several SMs.
+ * Errors: as cast_cache_append, and INVALID_ARG for H_q not a multiple of cache.H, a negative window
+ * or sinks, a short workspace; UNSUPPORTED for H_q above 128 cache.H.  A page out of range reads as
+ * zeros and positions past max_pages pages as not there; they and new tokens past max_new (whose rows
+ * of o are not written) are recorded and reported as there. */
+cast_status cast_cache_attention(const cast_cache_attn_args* args, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* args);
 
 /* ------------------------------------------------------------------------ */
 /* Status                                                                    */

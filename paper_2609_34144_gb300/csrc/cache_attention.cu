@@ -1,0 +1,859 @@
+// Attention over the paged KV cache (cast_cache_attention).
+//
+// Few rows a sequence (single tokens, drafts): k_cache_rows.  A unit is 16 * MT rows of one sequence
+// and KV head, a row being (token, query head of the KV head's group), so that the group's heads
+// read a key once.  The keys that a unit's rows can see are a list of 16-token blocks (the sinks'
+// blocks, then the window's), and all units' blocks in a row are the work of the call: every CTA
+// takes an equal share of it, found from the lengths on the device, whatever they are.  A CTA whose
+// share begins or ends inside a unit leaves that part (unnormalised o, running maximum and sum) in
+// the workspace, and k_cache_merge joins the parts.
+//
+// Inside a CTA each warp works on its own blocks (w, w + 4, ...) with its own running maximum, sum
+// and o in registers, so that there is no barrier between the loads and the end of the unit: its
+// lanes fetch K and V rows with 16-byte asynchronous copies into a private ring of stages, in an
+// order of 16-byte chunks that ldmatrix reads without bank conflicts, and rows that no row of the
+// unit sees are filled with zeros instead of being read.  S = Q K^T and o += P V are m16n8k16
+// products: at 16 rows the tensor cores wait for memory anyway.
+//
+// 8-bit rows are decoded to bf16 on the way from shared memory to the products: a code's exponent
+// and mantissa moved to bf16's fields are code * 2^-120, a subnormal code included, so that one
+// multiplication by 2^120 * scale gives the value, exactly.  The order of channels inside a 16-wide
+// step of Q K^T, and of o's columns, is that in which the codes lie in their 32-bit words.
+#include <cmath>
+
+#include "cache.cuh"
+#include "ptx.cuh"
+
+namespace cast {
+namespace {
+
+constexpr float kRescale = 8.f;   // the running maximum is renewed when a logit exceeds it by 2^8
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kWarps = 4;
+
+struct RowsKArgs {
+  cast_cache_batch batch;
+  int n_pages, page_size, page_shift, H, H_q, group;   // page_size = 2^page_shift, group = H_q / H
+  int causal, window, sinks, o_f32;
+  int64_t row_stride, q_stride;
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  const __nv_bfloat16* q;
+  void* o;
+  float* lse;
+  float scale_log2;
+  unsigned* error;
+  int row_tiles;      // units of 16 * MT rows that a sequence may have
+  int least;          // blocks that a CTA takes at least
+  int whole;          // every CTA has one whole unit
+  float* part_o;      // [2 * grid][16 * MT][D]
+  float2* part_ml;    // [2 * grid][16 * MT]
+};
+
+// What the rows of one unit see: blocks [0, n_sink) and [first, end) of 16 positions, and within
+// them the positions below `sinks` or from lo on, below hi.
+struct Span {
+  int n_sink, first, end;
+  int lo, hi, sinks;
+  int p0;        // position of the sequence's first new token
+  int n_rows;    // rows of the sequence
+  int t0;
+  __device__ __forceinline__ int blocks() const { return n_sink + max(end - first, 0); }
+  __device__ __forceinline__ int block(int i) const { return i < n_sink ? i : first + (i - n_sink); }
+};
+__device__ __forceinline__ Span span_of(const RowsKArgs& a, int b, int row_tile, int rows) {
+  const Sequence s = sequence_of(a.batch, b);
+  Span z;
+  z.t0 = s.t0;
+  z.p0 = s.len - s.n_new;
+  const int kept = min(s.n_new, a.batch.max_new);
+  if (kept < s.n_new) atomicExch(a.error, kCacheBadInput);
+  z.n_rows = kept * a.group;
+  const int64_t room = (int64_t)a.batch.max_pages * a.page_size;
+  if (s.len > room) atomicExch(a.error, kCacheBadInput);
+  const int len = (int)min((int64_t)s.len, room);
+  const int r0 = row_tile * rows, r1 = min(r0 + rows, z.n_rows) - 1;
+  z.n_sink = z.first = z.end = z.lo = z.hi = z.sinks = 0;
+  if (r0 > r1) return z;
+  z.hi = a.causal ? min(len, max(z.p0 + r1 / a.group + 1, 0)) : len;
+  if (a.window > 0) {
+    z.lo = min(max(z.p0 + r0 / a.group - a.window + 1, 0), z.hi);
+    z.sinks = min(min(a.sinks, z.lo), z.hi);
+  }
+  z.first = z.lo / 16;
+  z.end = (z.hi + 15) / 16;
+  z.n_sink = min((z.sinks + 15) / 16, z.first);
+  return z;
+}
+
+// ---------------------------------------------------------------- warp-level pieces
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
+}
+
+// A page's scale as the two bf16 factors of the decoding: 2^120 * scale overflows bf16 from 2^8 on
+struct Factor {
+  uint32_t once, twice;   // bf16 pairs; `twice` is 1 unless the scale is above 128
+  bool two;
+};
+__device__ __forceinline__ Factor factor_of(float scale) {
+  Factor f;
+  f.two = scale > 128.f;
+  const float a = f.two ? 0x1p120f : scale * 0x1p120f;
+  f.once = pack2(a, a);
+  f.twice = pack2(scale, scale);
+  return f;
+}
+// Codes 0, 2 (even) and 1, 3 (odd) of a word as bf16 pairs
+__device__ __forceinline__ void decode4(uint32_t w, const Factor& f, uint32_t& even, uint32_t& odd) {
+  even = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
+  odd = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+  even = mul2(even, f.once);
+  odd = mul2(odd, f.once);
+  if (f.two) {
+    even = mul2(even, f.twice);
+    odd = mul2(odd, f.twice);
+  }
+  // the format's NaN (all seven bits set): the fields above make 480 of it
+  if ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u) {
+    if ((w & 0x0000007fu) == 0x0000007fu) even |= 0x00007fffu;
+    if ((w & 0x00007f00u) == 0x00007f00u) odd |= 0x00007fffu;
+    if ((w & 0x007f0000u) == 0x007f0000u) even |= 0x7fff0000u;
+    if ((w & 0x7f000000u) == 0x7f000000u) odd |= 0x7fff0000u;
+  }
+}
+
+template <int D, bool F8, int MT>
+struct Cfg {
+  static constexpr int ROWS = 16 * MT;
+  static constexpr int ROWB = D * (F8 ? 1 : 2);        // bytes of a key row
+  static constexpr int CHUNKS = ROWB / 16;
+  static constexpr int BLOCK = 16 * ROWB;              // K or V of a 16-token block
+  static constexpr int STAGES = (24 * 1024) / (2 * BLOCK) > 8 ? 8 : (24 * 1024) / (2 * BLOCK);
+  static constexpr int RING = STAGES * 2 * BLOCK;      // of one warp
+  static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
+  static constexpr int SMEM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
+  static_assert(STAGES >= 2, "a block is fetched while another is used");
+};
+
+// Where chunk c of row r of a block lies: rows of 128 bytes or more permute their eight chunks by
+// the row, so that the eight rows of an ldmatrix take eight bank groups; 64-byte rows by row pairs.
+template <int ROWB>
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+  if constexpr (ROWB >= 128) return r * ROWB + ((c ^ (r & 7)) << 4);
+  return r * ROWB + ((c ^ ((r >> 1) & 3)) << 4);
+}
+
+// Whether a 16-byte chunk of V holds a value that is not finite
+template <bool F8>
+__device__ __forceinline__ bool not_finite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F8) bad |= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
+    else bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+  }
+  return bad;
+}
+// Channel c of row r of a V block
+template <bool F8, int ROWB>
+__device__ __forceinline__ float value_at(const uint8_t* block, int r, int c, float scale) {
+  const uint8_t* p = block + chunk_at<ROWB>(r, c * (F8 ? 1 : 2) / 16) + c * (F8 ? 1 : 2) % 16;
+  if constexpr (F8) {
+    const __half h(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3));
+    return __half2float(h) * scale;
+  }
+  return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+}
+
+template <int D, bool F8, int MT>
+__global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_constant__ RowsKArgs a) {
+  using C = Cfg<D, F8, MT>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int s_work[kWarps], s_entry;
+  __shared__ int64_t s_before;
+  __shared__ float2 s_scale[kWarps][C::STAGES];   // K and V scale of a stage's page
+  __shared__ float s_prob[kWarps][C::ROWS][17];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, q4 = lane & 3;
+  const int entries = a.batch.B * a.row_tiles;
+
+  // Rows of units without any block get zeros (one CTA's threads do this)
+  auto zero_rows = [&](int e, int h0, int h1) {
+    const Span z = span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS);
+    const int r0 = (e % a.row_tiles) * C::ROWS, n = max(min(r0 + C::ROWS, z.n_rows) - r0, 0), heads = h1 - h0;
+    for (int i = threadIdx.x; i < n * heads * D; i += kWarps * 32) {
+      const int c = i % D, h = h0 + i / D % heads, r = r0 + i / (D * heads);
+      const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
+      if (a.o_f32) static_cast<float*>(a.o)[row * D + c] = 0.f;
+      else static_cast<__nv_bfloat16*>(a.o)[row * D + c] = __float2bfloat16_rn(0.f);
+      if (a.lse && c == 0) a.lse[row] = -INFINITY;
+    }
+  };
+
+  // ---- this CTA's share of the call's blocks: [at, stop), and the entry (sequence, row tile) it
+  // begins in, whose blocks begin at entry_at
+  int entry;
+  int64_t at, stop, entry_at = 0;
+  if (a.whole) {
+    entry = blockIdx.x / a.H;
+    const int h = blockIdx.x - entry * a.H;
+    const int nb = span_of(a, entry / a.row_tiles, entry % a.row_tiles, C::ROWS).blocks();
+    if (nb == 0) {
+      zero_rows(entry, h, h + 1);
+      return;
+    }
+    at = (int64_t)h * nb;
+    stop = at + nb;
+  } else {
+    int mine = 0, none = 0;
+    for (int e = threadIdx.x; e < entries; e += kWarps * 32) {
+      const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS).blocks();
+      mine += n;
+      none |= n == 0;
+    }
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) s_work[warp] = mine;
+    none = __syncthreads_or(none);
+    int64_t total = 0;
+    for (int w = 0; w < kWarps; ++w) total += s_work[w];
+    total *= a.H;
+    const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
+    at = blockIdx.x * share;
+    stop = min(at + share, total);
+    if (none && blockIdx.x == 0) {
+      for (int e = 0; e < entries; ++e)
+        if (span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS).blocks() == 0) zero_rows(e, 0, a.H);
+    }
+    if (at >= stop) return;
+    if (warp == 0) {
+      int64_t before = 0;
+      for (int e0 = 0; e0 < entries; e0 += 32) {
+        const int e = e0 + lane;
+        const int n = e < entries ? span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS).blocks() : 0;
+        int sum = n;
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * a.H > at);
+        if (hit) {
+          if (lane == __ffs(hit) - 1) {
+            s_entry = e;
+            s_before = before + sum - n;
+          }
+          break;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+      }
+    }
+    __syncthreads();
+    entry = s_entry;
+    entry_at = s_before * a.H;
+  }
+
+  uint8_t* ring = smem + warp * C::RING;
+  const uint32_t ring_at = smem_u32(ring);
+
+  for (; at < stop; ++entry) {
+    const int b = entry / a.row_tiles, tile = entry % a.row_tiles;
+    const Span z = span_of(a, b, tile, C::ROWS);
+    const int nb = z.blocks();
+    const int* table = a.batch.page_table + (int64_t)b * a.batch.page_table_stride;
+    for (int h = nb ? (int)((at - entry_at) / nb) : a.H; h < a.H && at < stop; ++h) {
+      // blocks k0 .. k1-1 of unit (b, tile, h)
+      const int64_t unit_at = entry_at + (int64_t)h * nb;
+      const int k0 = (int)(at - unit_at);
+      const int k1 = (int)min((int64_t)nb, stop - unit_at);
+
+      // Q fragments: rows g and g + 8 of each 16
+      uint32_t qf[MT][D / 16][4];
+      int pos[MT][2];   // the rows' positions
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = tile * C::ROWS + m * 16 + j * 8 + g;
+          const bool in = r < z.n_rows;
+          const int i = r / a.group;
+          pos[m][j] = in ? z.p0 + i : -1;
+          const __nv_bfloat16* src =
+              a.q + (int64_t)(z.t0 + (in ? i : 0)) * a.q_stride + (h * a.group + (in ? r - i * a.group : 0)) * D;
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s) {
+            uint32_t x, y;
+            if constexpr (F8) {
+              const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + s * 16 + q4 * 4));
+              x = __byte_perm(w.x, w.y, 0x5410);
+              y = __byte_perm(w.x, w.y, 0x7632);
+            } else {
+              x = __ldg(reinterpret_cast<const uint32_t*>(src + s * 16 + q4 * 2));
+              y = __ldg(reinterpret_cast<const uint32_t*>(src + s * 16 + q4 * 2 + 8));
+            }
+            qf[m][s][j] = in ? x : 0u;
+            qf[m][s][2 + j] = in ? y : 0u;
+          }
+        }
+      // positions that every row sees: [all_lo, all_hi); the others' blocks are masked
+      int all_lo = 0, all_hi = z.hi;
+      {
+        const int r1 = min(tile * C::ROWS + C::ROWS, z.n_rows) - 1;
+        if (a.causal) all_hi = min(z.hi, max(z.p0 + tile * C::ROWS / a.group + 1, 0));
+        if (a.window > 0) all_lo = max(z.p0 + r1 / a.group - a.window + 1, 0);
+      }
+
+      float o[MT][D / 8][4], m_ref[MT][2], l[MT][2];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+#pragma unroll
+        for (int t = 0; t < D / 8; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[m][t][e] = 0.f;
+        m_ref[m][0] = m_ref[m][1] = -INFINITY;
+        l[m][0] = l[m][1] = 0.f;
+      }
+
+      // The page of block i of the unit (-1: out of range, reads as zeros)
+      auto page_of = [&](int i) {
+        const int g0 = (z.block(i) * 16) >> a.page_shift;
+        int p = __ldg(table + g0);
+        if (p < 0 || p >= a.n_pages) {
+          if (lane == 0) atomicExch(a.error, kCacheBadInput);
+          p = -1;
+        }
+        return p;
+      };
+      // fetches block i of the unit into stage st
+      auto fetch = [&](int i, int st, int page) {
+        const int base = z.block(i) * 16;
+        const int64_t row0 = (int64_t)max(page, 0) * a.page_size + (base & (a.page_size - 1));
+        const uint8_t* ks = a.k + (row0 * a.row_stride + (int64_t)h * D) * (F8 ? 1 : 2);
+        const uint8_t* vs = a.v + (row0 * a.row_stride + (int64_t)h * D) * (F8 ? 1 : 2);
+        const uint32_t dst = ring_at + st * 2 * C::BLOCK;
+#pragma unroll
+        for (int c = 0; c < 16 * C::CHUNKS / 32; ++c) {
+          const int x = c * 32 + lane, r = x / C::CHUNKS, cc = x % C::CHUNKS;
+          const int p = base + r;
+          const bool in = page >= 0 && p < z.hi && (p >= z.lo || p < z.sinks);
+          const int64_t off = in ? (int64_t)r * a.row_stride * (F8 ? 1 : 2) + cc * 16 : 0;
+          copy16(dst + chunk_at<C::ROWB>(r, cc), ks + off, in);
+          copy16(dst + C::BLOCK + chunk_at<C::ROWB>(r, cc), vs + off, in);
+        }
+        if constexpr (F8) {
+          // lanes 0 and 1: the page's scales, 4 bytes behind the same group of copies
+          if (lane < 2) {
+            const float* src = (lane ? a.v_scale : a.k_scale) + (int64_t)max(page, 0) * a.H + h;
+            copy4(smem_u32(&s_scale[warp][st]) + 4 * lane, src);
+          }
+        }
+      };
+      const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) / kWarps : 0;   // blocks of this warp
+      const int i0 = k0 + warp;
+      __syncwarp();
+      for (int st = 0; st < C::STAGES - 1; ++st) {
+        if (st < n) fetch(i0 + st * kWarps, st, page_of(i0 + st * kWarps));
+        copy_commit();
+      }
+      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * kWarps) : -1;
+
+      int st = 0, into = C::STAGES - 1;
+      for (int it = 0; it < n; ++it) {
+        copy_wait<C::STAGES - 2>();
+        __syncwarp();
+        // the stage used one block ago takes the block STAGES - 1 ahead
+        const int ahead = it + C::STAGES - 1;
+        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_page);
+        copy_commit();
+        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * kWarps);
+        const uint32_t kt = ring_at + st * 2 * C::BLOCK, vt = kt + C::BLOCK;
+        float s[MT][2][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[m][t][e] = 0.f;
+        Factor fk, fv;
+        if constexpr (F8) {
+          const float2 sc = s_scale[warp][st];
+          fk = factor_of(sc.x);
+          fv = factor_of(sc.y);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < D / 16; c += 4) {
+              uint32_t w[4];
+              ldsm4(kt + chunk_at<C::ROWB>(t * 8 + (lane & 7), c + (lane >> 3)), w);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t b0, b1;
+                decode4(w[j], fk, b0, b1);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) mma16816(s[m][t], qf[m][c + j], b0, b1);
+              }
+            }
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t w[4];
+            ldsm4(kt + chunk_at<C::ROWB>((lane >> 4) * 8 + (lane & 7), 2 * c + ((lane >> 3) & 1)), w);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              mma16816(s[m][0], qf[m][c], w[0], w[1]);
+              mma16816(s[m][1], qf[m][c], w[2], w[3]);
+            }
+          }
+        }
+        const int base = z.block(i0 + it * kWarps) * 16;
+        const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
+        bool grows = false;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x = s[m][t][e] * a.scale_log2;
+              if (!whole) {
+                const int p = base + t * 8 + q4 * 2 + (e & 1), r = pos[m][e >> 1];
+                const bool see = p < z.hi && (!a.causal || p <= r) &&
+                                 (a.window <= 0 || p > r - a.window || p < a.sinks);
+                if (!see) x = -INFINITY;
+              }
+              s[m][t][e] = x;
+              grows = grows || x > m_ref[m][e >> 1] + kRescale;
+            }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float x = fmaxf(fmaxf(s[m][0][2 * j], s[m][0][2 * j + 1]), fmaxf(s[m][1][2 * j], s[m][1][2 * j + 1]));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+              if (x > m_ref[m][j]) {
+                const float f = exp2_fast(m_ref[m][j] - x);
+                m_ref[m][j] = x;
+                l[m][j] *= f;
+#pragma unroll
+                for (int t = 0; t < D / 8; ++t) {
+                  o[m][t][2 * j] *= f;
+                  o[m][t][2 * j + 1] *= f;
+                }
+              }
+            }
+        }
+        uint32_t pf[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            // a row that has seen nothing yet: exp2(-inf - 0) = 0
+            const float ref = m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float p = exp2_fast(s[m][t][2 * j + e] - ref);
+                s[m][t][2 * j + e] = p;
+                l[m][j] += p;
+              }
+          }
+          pf[m][0] = pack2(s[m][0][0], s[m][0][1]);
+          pf[m][1] = pack2(s[m][0][2], s[m][0][3]);
+          pf[m][2] = pack2(s[m][1][0], s[m][1][1]);
+          pf[m][3] = pack2(s[m][1][2], s[m][1][3]);
+        }
+        // A block that the rows do not all see, with a value that is not finite: 0 times it would
+        // reach the rows that do not see it, so its tokens are added one by one where they are seen.
+        bool apart = false;
+        if (!whole) {
+          for (int x = lane; x < C::BLOCK / 16; x += 32)
+            apart |= not_finite<F8>(*reinterpret_cast<const uint4*>(ring + st * 2 * C::BLOCK + C::BLOCK + x * 16));
+          apart = __any_sync(0xffffffffu, apart);
+        }
+        if (apart) {
+          const float scale = F8 ? s_scale[warp][st].y : 1.f;
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                s_prob[warp][m * 16 + (e >> 1) * 8 + g][t * 8 + q4 * 2 + (e & 1)] = s[m][t][e];
+          __syncwarp();
+#pragma unroll 1
+          for (int t = 0; t < 16; ++t) {
+            const int p = base + t;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const int r = pos[m][j];
+                const bool see = p < z.hi && (!a.causal || p <= r) && (a.window <= 0 || p > r - a.window || p < a.sinks);
+                if (!see) continue;
+                const float w = s_prob[warp][m * 16 + j * 8 + g][t];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const int n = F8 ? (c >> 1) * 16 + 2 * (q4 * 2 + e) + (c & 1) : c * 8 + q4 * 2 + e;
+                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, scale);
+                  }
+              }
+          }
+        } else if constexpr (F8) {
+#pragma unroll
+          for (int c = 0; c < D / 16; c += 2) {
+            uint32_t w[4];
+            ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              uint32_t e0, e1, d0, d1;
+              decode4(w[2 * j], fv, e0, d0);
+              decode4(w[2 * j + 1], fv, e1, d1);
+#pragma unroll
+              for (int m = 0; m < MT; ++m) {
+                mma16816(o[m][2 * (c + j)], pf[m], e0, e1);
+                mma16816(o[m][2 * (c + j) + 1], pf[m], d0, d1);
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t w[4];
+            ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), 2 * c + (lane >> 4)), w);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              mma16816(o[m][2 * c], pf[m], w[0], w[1]);
+              mma16816(o[m][2 * c + 1], pf[m], w[2], w[3]);
+            }
+          }
+        }
+        __syncwarp();
+        into = st;
+        st = st + 1 == C::STAGES ? 0 : st + 1;
+      }
+      copy_wait<0>();
+      __syncthreads();   // every warp is done with its ring: the merge takes the space
+
+      // ---- join the warps
+      float* mo = reinterpret_cast<float*>(smem);                        // [warp][row][D]
+      float2* ml = reinterpret_cast<float2*>(mo + kWarps * C::ROWS * D); // [warp][row]
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float x = l[m][j];
+          x += __shfl_xor_sync(0xffffffffu, x, 1);
+          x += __shfl_xor_sync(0xffffffffu, x, 2);
+          const int r = m * 16 + j * 8 + g;
+          if (q4 == 0) ml[warp * C::ROWS + r] = make_float2(m_ref[m][j], x);
+          float* dst = mo + (warp * C::ROWS + r) * D;
+          if constexpr (F8) {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c)
+              *reinterpret_cast<float4*>(dst + c * 16 + q4 * 4) =
+                  make_float4(o[m][2 * c][2 * j], o[m][2 * c + 1][2 * j], o[m][2 * c][2 * j + 1], o[m][2 * c + 1][2 * j + 1]);
+          } else {
+#pragma unroll
+            for (int t = 0; t < D / 8; ++t)
+              *reinterpret_cast<float2*>(dst + t * 8 + q4 * 2) = make_float2(o[m][t][2 * j], o[m][t][2 * j + 1]);
+          }
+        }
+      __syncthreads();
+      const bool complete = k0 == 0 && k1 == nb;
+      // a share that begins inside the unit leaves its part in the CTA's first place
+      const int slot = 2 * blockIdx.x + (k0 > 0 ? 0 : 1);
+      for (int x = threadIdx.x; x < C::ROWS * D / 4; x += kWarps * 32) {
+        const int rr = x / (D / 4), c = x % (D / 4) * 4;
+        const int r = tile * C::ROWS + rr;
+        if (r >= z.n_rows) continue;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * C::ROWS + rr].x);
+        float sum = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 v = ml[w * C::ROWS + rr];
+          const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+          sum += f * v.y;
+          const float4 y = *reinterpret_cast<const float4*>(mo + (w * C::ROWS + rr) * D + c);
+          acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+        }
+        if (complete) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
+          if (a.o_f32) {
+            *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c) =
+                make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+          } else {
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c) =
+                make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+          }
+          if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+        } else {
+          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * C::ROWS + rr) * D + c) = acc;
+          if (c == 0) a.part_ml[(int64_t)slot * C::ROWS + rr] = make_float2(top, sum);
+        }
+      }
+      __syncthreads();   // the space goes back to the rings
+      at = unit_at + k1;
+    }
+    entry_at += (int64_t)nb * a.H;
+  }
+}
+
+// Joins the parts of the units that no single CTA of k_cache_rows had whole: one CTA a unit.
+template <int D, int MT>
+__global__ void __launch_bounds__(128) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
+  constexpr int ROWS = 16 * MT;
+  __shared__ int s_sum[4], s_before[4];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int entries = a.batch.B * a.row_tiles;
+  const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  int sum = 0, before = 0;
+  for (int e = threadIdx.x; e < entries; e += 128) {
+    const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
+    sum += n;
+    before += e < entry ? n : 0;
+  }
+  sum = __reduce_add_sync(0xffffffffu, sum);
+  before = __reduce_add_sync(0xffffffffu, before);
+  if ((threadIdx.x & 31) == 0) {
+    s_sum[threadIdx.x >> 5] = sum;
+    s_before[threadIdx.x >> 5] = before;
+  }
+  __syncthreads();
+  int64_t total = 0, at = 0;
+  for (int w = 0; w < 4; ++w) {
+    total += s_sum[w];
+    at += s_before[w];
+  }
+  total *= a.H;
+  const int64_t share = max((int64_t)a.least, (total + ctas - 1) / ctas);
+  const int tile = entry % a.row_tiles;
+  const Span z = span_of(a, entry / a.row_tiles, tile, ROWS);
+  const int nb = z.blocks();
+  at = at * a.H + (int64_t)h * nb;
+  if (nb == 0) return;
+  const int c0 = (int)(at / share), c1 = (int)((at + nb - 1) / share);
+  if (c0 == c1) return;   // written whole
+  for (int x = threadIdx.x; x < ROWS * D / 4; x += 128) {
+    const int rr = x / (D / 4), c = x % (D / 4) * 4;
+    const int r = tile * ROWS + rr;
+    if (r >= z.n_rows) continue;
+    // CTA c0 began the unit (its second place), unless its share begins with the unit's first block,
+    // which is also k0 == 0; the others began inside it (their first place)
+    float top = -INFINITY;
+    for (int i = c0; i <= c1; ++i) {
+      const int64_t slot = 2 * i + (i == c0 ? 1 : 0);
+      top = fmaxf(top, a.part_ml[slot * ROWS + rr].x);
+    }
+    float l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = c0; i <= c1; ++i) {
+      const int64_t slot = 2 * i + (i == c0 ? 1 : 0);
+      const float2 v = a.part_ml[slot * ROWS + rr];
+      const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+      l += f * v.y;
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * ROWS + rr) * D + c);
+      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
+    if (a.o_f32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c) =
+          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c) =
+          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    }
+    if (a.lse && c == 0) a.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+  }
+}
+
+// ---------------------------------------------------------------- host side
+struct RowsPlan {
+  int mt, row_tiles, grid, least;
+  bool whole;            // a CTA takes a whole unit; else units may be split and are merged
+  size_t part_o_bytes, total_bytes;
+};
+RowsPlan rows_plan(const cast_cache_attn_args& a) {
+  RowsPlan p{};
+  const int group = a.H_q / a.cache.H;
+  const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
+  p.mt = 1;
+  const int rows = 16 * p.mt;
+  p.row_tiles = (int)(((int64_t)max_new * group + rows - 1) / rows);
+  int dev = 0, nsm = 152;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
+  p.grid = 2 * (nsm < 1 ? 1 : nsm);
+  p.least = 16;
+  // Blocks that a unit has at most.  Up to 64 (a thousand tokens: four blocks' latency a warp's ring)
+  // a CTA takes a whole unit and nothing is joined.
+  const int64_t room = (int64_t)a.batch.max_pages * a.cache.page_size;
+  int64_t most = room / 16;
+  if (a.window > 0) {
+    const int64_t seen = ((int64_t)a.window + rows) / 16 + 2 + ((int64_t)a.sinks + 15) / 16;
+    if (seen < most) most = seen;
+  }
+  p.whole = most <= 64;
+  if (p.whole) {
+    const int64_t units = (int64_t)a.batch.B * p.row_tiles * a.cache.H;
+    p.grid = units > 0x7fffffff ? 0 : (int)units;
+    return p;
+  }
+  p.part_o_bytes = align_up((size_t)2 * p.grid * rows * a.cache.d * sizeof(float));
+  p.total_bytes = p.part_o_bytes + align_up((size_t)2 * p.grid * rows * sizeof(float2));
+  return p;
+}
+
+cast_status validate_attention(const cast_cache_attn_args* a, const char* who) {
+  if (!a) return fail(CAST_ERR_INVALID_ARG, "%s: args is NULL", who);
+  cast_status s = validate_cache(a->cache, who);
+  if (s) return s;
+  if ((s = validate_batch(a->batch, who))) return s;
+  if (a->H_q < 1 || a->H_q % a->cache.H)
+    return fail(CAST_ERR_INVALID_ARG, "%s: H_q %d is not a multiple of the cache's %d heads", who, a->H_q, a->cache.H);
+  if (a->H_q / a->cache.H > 128) return fail(CAST_ERR_UNSUPPORTED, "%s: %d query heads a KV head", who, a->H_q / a->cache.H);
+  if (a->window < 0 || a->sinks < 0)
+    return fail(CAST_ERR_INVALID_ARG, "%s: window %d and sinks %d must be >= 0", who, a->window, a->sinks);
+  if (!std::isfinite(a->scale)) return fail(CAST_ERR_INVALID_ARG, "%s: scale is not finite", who);
+  if (a->o_dtype != CAST_BF16 && a->o_dtype != CAST_F32)
+    return fail(CAST_ERR_INVALID_ARG, "%s: o_dtype %d", who, a->o_dtype);
+  if (a->batch.T == 0) return CAST_OK;
+  if (!a->q || !aligned16(a->q) || !a->o || !aligned16(a->o))
+    return fail(CAST_ERR_INVALID_ARG, "%s: q or o is NULL or not 16-byte aligned", who);
+  if (a->q_row_stride < (int64_t)a->H_q * a->cache.d || a->q_row_stride % 8)
+    return fail(CAST_ERR_INVALID_ARG, "%s: q row stride %lld must be >= H_q*d and a multiple of 8", who,
+                (long long)a->q_row_stride);
+  return CAST_OK;
+}
+
+template <int D, bool F8, int MT>
+cast_status launch_rows(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
+  using C = Cfg<D, F8, MT>;
+  static std::atomic<uint64_t> attr_done{0};
+  if (!once_per_device(attr_done, [&] {
+        return cudaFuncSetAttribute(k_cache_rows<D, F8, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) ==
+               cudaSuccess;
+      }))
+    return check_launch("cache attention smem attribute");
+  k_cache_rows<D, F8, MT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
+  cast_status s = check_launch("cache attention");
+  if (s || p.whole) return s;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(k.batch.B * k.row_tiles * k.H), 1, 1);
+  cfg.blockDim = dim3(128, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, k_cache_merge<D, MT>, k, p.grid) != cudaSuccess) return check_launch("cache attention merge");
+  return check_launch("cache attention merge");
+}
+
+}  // namespace
+}  // namespace cast
+
+using namespace cast;
+
+extern "C" {
+
+size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {
+  if (!a || a->batch.T < 1 || a->cache.H < 1 || a->H_q < a->cache.H || (a->cache.d != 64 && a->cache.d != 128)) return 0;
+  return rows_plan(*a).total_bytes;
+}
+
+cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t ws_bytes, void* stream) {
+  clear_error_detail();
+  const char* who = "cast_cache_attention";
+  cast_status s = validate_attention(a, who);
+  if (s) return s;
+  if (a->batch.T == 0) return CAST_OK;
+  const RowsPlan p = rows_plan(*a);
+  if (ws_bytes < p.total_bytes || (p.total_bytes && !ws))
+    return fail(CAST_ERR_INVALID_ARG, "%s: workspace %zu B < %zu B", who, ws_bytes, p.total_bytes);
+  if (reinterpret_cast<uintptr_t>(ws) % kWsAlign)
+    return fail(CAST_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", who);
+  const cast_kv_cache& c = a->cache;
+  if ((int64_t)a->batch.B * p.row_tiles * c.H > 0x7fffffff)
+    return fail(CAST_ERR_UNSUPPORTED, "%s: too many units", who);
+  RowsKArgs k{};
+  k.batch = a->batch;
+  k.n_pages = c.n_pages;
+  k.page_size = c.page_size;
+  while ((1 << k.page_shift) < c.page_size) ++k.page_shift;
+  k.H = c.H;
+  k.H_q = a->H_q;
+  k.group = a->H_q / c.H;
+  k.causal = a->causal ? 1 : 0;
+  // a window as long as a sequence can be hides nothing
+  k.window = a->window < (int64_t)a->batch.max_pages * c.page_size ? a->window : 0;
+  k.sinks = k.window > 0 ? a->sinks : 0;
+  k.o_f32 = a->o_dtype == CAST_F32;
+  k.row_stride = c.row_stride;
+  k.q_stride = a->q_row_stride;
+  k.k = static_cast<const uint8_t*>(c.k);
+  k.v = static_cast<const uint8_t*>(c.v);
+  k.k_scale = c.k_scale;
+  k.v_scale = c.v_scale;
+  k.q = static_cast<const __nv_bfloat16*>(a->q);
+  k.o = a->o;
+  k.lse = a->lse;
+  k.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;
+  if (!(k.error = cache_error_address())) return check_launch("cache error word");
+  k.row_tiles = p.row_tiles;
+  k.least = p.least;
+  k.whole = p.whole;
+  k.part_o = static_cast<float*>(ws);
+  k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (c.dtype == CAST_F8E4M3)
+    return c.d == 128 ? launch_rows<128, true, 1>(k, p, st) : launch_rows<64, true, 1>(k, p, st);
+  return c.d == 128 ? launch_rows<128, false, 1>(k, p, st) : launch_rows<64, false, 1>(k, p, st);
+}
+
+}  // extern "C"

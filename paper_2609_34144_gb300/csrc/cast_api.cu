@@ -73,8 +73,6 @@ __global__ void k_residual_add_bf16(__nv_bfloat16* __restrict__ x,
     x[n - 1] = __float2bfloat16_rn(__bfloat162float(x[n - 1]) + __bfloat162float(r[n - 1]));
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 cast_status validate_anchors(const int32_t* anchors, int n_anchors, int n_frames, const char* who) {
   if (!anchors) return fail(CAST_ERR_INVALID_ARG, "%s: anchors is NULL", who);
   if (n_anchors < 1 || n_anchors > CAST_MAX_ANCHORS)
@@ -636,9 +634,14 @@ cast_status cast_check_device(void* stream) {
   const unsigned int wp = par_error_word(st, true);
   const unsigned int wr = route_error_word(st, true);
   const unsigned int wd = dense_error_word(st, true);
+  const unsigned int wc = cache_error_word(st, true);
   if (wa == 1u || wp || wd || wr == 2u) return fail(CAST_ERR_DEVICE_TIMEOUT, "a kernel gave up on a bounded wait");
   if (wa == 2u) return fail(CAST_ERR_INVALID_ARG, "attention: a routed block index was outside [0, M)");
   if (wr) return fail(CAST_ERR_INVALID_ARG, "routing: a candidate index was outside [0, M) or repeated");
+  if (wc)
+    return fail(CAST_ERR_INVALID_ARG,
+                "cache: a page was outside [0, n_pages), a position past max_pages pages, or a sequence had "
+                "more than max_new new tokens");
   return check_launch("cast_check_device");
 }
 

@@ -142,6 +142,14 @@ struct AnchorGemm {
 cast_status gemm_anchor_rows(const AnchorGemm& g, cudaStream_t st);
 unsigned int dense_error_word(cudaStream_t st, bool clear);
 
+// ------------------------------------------------------------------ paged KV cache
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// host checks shared by the append and the attention (cache.cu)
+cast_status validate_cache(const cast_kv_cache& c, const char* who);
+cast_status validate_batch(const cast_cache_batch& b, const char* who);
+// Nonzero when a cache kernel left out a page, position or token that was out of range.
+unsigned int cache_error_word(cudaStream_t st, bool clear);
+
 // ------------------------------------------------------------------ residual update
 cast_status launch_residual_add(void* x, const void* r, int dtype, size_t n, cudaStream_t st);
 

@@ -20,7 +20,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_TIMEOUT = 0, 1, 2, 3, 4
-F32, BF16 = 0, 1
+F32, BF16, F8E4M3 = 0, 1, 2
 ROUTE_OMISSION, ROUTE_SIMILARITY = 0, 1
 HIST_BLOCKS, HIST_FRAMES = 0, 1
 GATE_PAPER, GATE_ZERO, GATE_ONE = 0, 1, 2
@@ -94,6 +94,56 @@ class SelectArgs(C.Structure):
                 ("mask_out", _vp), ("rms_out", _vp), ("score_out", _vp)]
 
 
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_STRETCH, ROTARY_PARTS = 0, 1, 2, 3
+MAX_AXES, MAX_ROTARY_PAIRS = 3, 128
+
+
+class RotaryParams(C.Structure):
+    _fields_ = [("rot_dim", _i32), ("layout", _i32), ("n_axes", _i32), ("pairs", _i32 * MAX_AXES),
+                ("scaling", _i32), ("base", C.c_double), ("factor", C.c_double),
+                ("original_length", _i32)]
+
+
+class RotaryTable(C.Structure):
+    _fields_ = [("rot_dim", _i32), ("layout", _i32), ("n_axes", _i32), ("amplitude", _f32),
+                ("turn", C.c_uint64 * MAX_ROTARY_PAIRS), ("axis", C.c_uint8 * MAX_ROTARY_PAIRS)]
+
+
+class RotaryArgs(C.Structure):
+    _fields_ = [("x", _vp), ("out", _vp), ("x_row_stride", _i64), ("out_row_stride", _i64), ("T", _i32),
+                ("H", _i32), ("d", _i32), ("dtype", _i32), ("positions", _vp),
+                ("table", C.POINTER(RotaryTable)), ("inverse", _i32)]
+
+
+class KvCache(C.Structure):
+    _fields_ = [("dtype", _i32), ("n_pages", _i32), ("page_size", _i32), ("H", _i32), ("d", _i32),
+                ("k", _vp), ("v", _vp), ("row_stride", _i64), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+class CacheBatch(C.Structure):
+    _fields_ = [("page_table", _vp), ("page_table_stride", _i64), ("max_pages", _i32), ("kv_len", _vp),
+                ("cu_new", _vp), ("B", _i32), ("T", _i32), ("max_new", _i32)]
+
+
+class AppendArgs(C.Structure):
+    _fields_ = [("cache", KvCache), ("batch", CacheBatch), ("k", _vp), ("v", _vp), ("k_row_stride", _i64),
+                ("v_row_stride", _i64), ("rotary", C.POINTER(RotaryTable)), ("positions", _vp), ("q", _vp),
+                ("q_out", _vp), ("q_row_stride", _i64), ("q_out_row_stride", _i64), ("H_q", _i32)]
+
+
+class CacheAttnArgs(C.Structure):
+    _fields_ = [("cache", KvCache), ("batch", CacheBatch), ("q", _vp), ("q_row_stride", _i64), ("H_q", _i32),
+                ("causal", _i32), ("window", _i32), ("sinks", _i32), ("scale", _f32), ("o", _vp),
+                ("o_dtype", _i32), ("lse", _vp)]
+
+
+_lib.cast_rotary_table_init.argtypes = [C.POINTER(RotaryParams), C.POINTER(RotaryTable)]
+_lib.cast_rotary.argtypes = [C.POINTER(RotaryArgs), _vp]
+_lib.cast_cache_append.argtypes = [C.POINTER(AppendArgs), _vp]
+_lib.cast_cache_attention.argtypes = [C.POINTER(CacheAttnArgs), _vp, C.c_size_t, _vp]
+_lib.cast_cache_attention_workspace_size.argtypes = [C.POINTER(CacheAttnArgs)]
+_lib.cast_cache_attention_workspace_size.restype = C.c_size_t
 _lib.cast_ffn_step.argtypes = [C.POINTER(FfnArgs), _vp, C.c_size_t, _vp]
 _lib.cast_ffn_workspace_size.argtypes = [C.POINTER(FfnArgs)]
 _lib.cast_ffn_workspace_size.restype = C.c_size_t
@@ -125,7 +175,9 @@ for _f in ("cast_route_topk", "cast_route_topk_noalloc", "cast_anchor_attention"
            "cast_check_device"):
     getattr(_lib, _f).restype = C.c_int
 
-EXPORTED = ["cast_select_frames", "cast_select_workspace_size", "cast_ffn_step",
+EXPORTED = ["cast_rotary_table_init", "cast_rotary", "cast_cache_append", "cast_cache_attention",
+            "cast_cache_attention_workspace_size",
+            "cast_select_frames", "cast_select_workspace_size", "cast_ffn_step",
             "cast_ffn_workspace_size",
             "cast_route_topk", "cast_route_workspace_size", "cast_route_topk_noalloc",
             "cast_anchor_attention", "cast_attention_workspace_size",
@@ -519,3 +571,162 @@ def cast_ffn_step(x, anchors, w1, b1, w2, b2, grid, r_out, channel_weight=None, 
 def ffn_workspace_size(x, anchors, w1, b1, w2, b2, grid, r_out):
     return _lib.cast_ffn_workspace_size(C.byref(ffn_args(x, anchors, w1, b1, w2, b2, grid, r_out)))
 
+
+
+# --------------------------------------------------------------------------- paged KV cache
+def rotary_table(rot_dim, layout="half", base=10000.0, sections=None, scaling=None):
+    """The table cast_rotary and cast_cache_append rotate by (host data, made once).  layout:
+    "half" (pairs i, i + rot_dim/2) or "interleaved" (2i, 2i+1); sections: pairs of each position
+    axis (default: one axis); scaling: None, ("linear", factor), ("stretch", factor) or
+    ("parts", factor, original_length)."""
+    p, t = RotaryParams(), RotaryTable()
+    sections = [rot_dim // 2] if sections is None else list(sections)
+    if not 1 <= len(sections) <= MAX_AXES:
+        raise ValueError(f"1 to {MAX_AXES} position axes")
+    p.rot_dim, p.n_axes, p.base, p.factor = rot_dim, len(sections), base, 1.0
+    p.layout = {"half": ROTARY_HALF, "interleaved": ROTARY_INTERLEAVED}[layout]
+    for a, n in enumerate(sections):
+        p.pairs[a] = n
+    if scaling is not None:
+        p.scaling = {"linear": ROTARY_LINEAR, "stretch": ROTARY_STRETCH, "parts": ROTARY_PARTS}[scaling[0]]
+        p.factor = scaling[1]
+        p.original_length = scaling[2] if len(scaling) > 2 else 0
+    _check(_lib.cast_rotary_table_init(C.byref(p), C.byref(t)))
+    return t
+
+
+def _heads_stride(t, name, dtype=torch.bfloat16):
+    """Token row stride of a [T, H, d] tensor whose (H, d) are contiguous."""
+    if t.dim() != 3 or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: expected [T, H, d] of {dtype}")
+    T, H, d = t.shape
+    s0, s1, s2 = t.stride()
+    if (d > 1 and s2 != 1) or (H > 1 and s1 != d):
+        raise ValueError(f"{name}: heads and channels must be contiguous")
+    return s0 if T > 1 else H * d
+
+
+def _int32(t, name, shape=None):
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor" + (f" of shape {shape}" if shape else ""))
+    return t.data_ptr()
+
+
+def _on_stream(stream, *tensors):
+    """Tensors allocated for a call on another stream than the current one stay alive until it is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
+    """Rotates x [T, H, d] (bf16 or f32) by int32 positions [T] or [T, n_axes]; inverse: the
+    transposed map (the rotation's gradient).  out may be x."""
+    stride = _heads_stride(x, "x", None)
+    T, H, d = x.shape
+    n = table.n_axes
+    pos = _int32(positions, "positions", (T,) if n == 1 and positions.dim() == 1 else (T, n))
+    o = torch.empty((T, H, d), dtype=x.dtype, device=x.device) if out is None else out
+    if out is not None and (o.shape != x.shape or o.dtype != x.dtype):
+        raise ValueError("out must have x's shape and dtype")
+    a = RotaryArgs(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
+                   _dtype_code(x), pos, C.pointer(table), inverse)
+    _check(_lib.cast_rotary(C.byref(a), _stream(stream)))
+    if out is None:
+        _on_stream(stream, o)
+    return o
+
+
+def kv_cache(k, v, k_scale=None, v_scale=None):
+    """Handle of a paged cache: k, v [n_pages, page_size, H, d], bf16 or float8_e4m3fn (or its bits
+    as uint8) with f32 scales [n_pages, H].  It keeps the tensors it describes."""
+    if k.shape != v.shape or k.dim() != 4 or k.dtype != v.dtype:
+        raise ValueError("k and v: [n_pages, page_size, H, d] of one shape and dtype")
+    n, ps, H, d = k.shape
+    if _row_stride(k) != _row_stride(v):
+        raise ValueError("k and v must have the same row stride")
+    f8 = k.dtype in (torch.float8_e4m3fn, torch.uint8)
+    if not f8 and k.dtype != torch.bfloat16:
+        raise TypeError(f"unsupported cache dtype {k.dtype}")
+    if f8:
+        for s in (k_scale, v_scale):
+            if s is None or s.dtype != torch.float32 or tuple(s.shape) != (n, H) or not s.is_contiguous():
+                raise ValueError("8-bit pages need contiguous f32 scales [n_pages, H]")
+    c = KvCache(F8E4M3 if f8 else BF16, n, ps, H, d, k.data_ptr(), v.data_ptr(), _row_stride(k),
+                k_scale.data_ptr() if f8 else None, v_scale.data_ptr() if f8 else None)
+    c._keep = (k, v, k_scale, v_scale)
+    return c
+
+
+def _batch(page_table, kv_len, cu_new, T, max_new):
+    if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table: expected int32 [B, max_pages]")
+    B, P = page_table.shape
+    cu = None if cu_new is None else _int32(cu_new, "cu_new", (B + 1,))
+    if max_new is None:
+        max_new = T if cu is not None else T // max(B, 1)
+    return CacheBatch(page_table.data_ptr(), max(page_table.stride(0), P), P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new)
+
+
+def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None, rotary=None, positions=None,
+                      q=None, q_out=None, stream=None):
+    """Stores new tokens' keys (rotated) and values [T, H, d] in the cache; kv_len [B] counts them
+    already.  cu_new [B + 1]: ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes]
+    (None: a token's place in its sequence).  With q [T, H_q, d] returns it rotated."""
+    T, H, d = k.shape
+    if v.shape != k.shape or H != cache.H or d != cache.d:
+        raise ValueError("k and v must be [T, H, d] of the cache's heads")
+    pos = None
+    if positions is not None and rotary is not None:
+        pos = _int32(positions, "positions", (T,) if positions.dim() == 1 and rotary.n_axes == 1 else (T, rotary.n_axes))
+    qp = qo = None
+    qs = qos = Hq = 0
+    o = None
+    if q is not None:
+        qs, Hq = _heads_stride(q, "q"), q.shape[1]
+        if q.shape[0] != T or q.shape[2] != d:
+            raise ValueError("q must be [T, H_q, d]")
+        o = torch.empty((T, Hq, d), dtype=q.dtype, device=q.device) if q_out is None else q_out
+        if o.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        qp, qo, qos = q.data_ptr(), o.data_ptr(), _heads_stride(o, "q_out")
+    a = AppendArgs(cache, _batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(), _heads_stride(k, "k"),
+                   _heads_stride(v, "v"), C.pointer(rotary) if rotary is not None else None, pos, qp, qo, qs, qos, Hq)
+    _check(_lib.cast_cache_append(C.byref(a), _stream(stream)))
+    if q_out is None:
+        _on_stream(stream, o)
+    return o
+
+
+def cache_attention_args(q, cache, page_table, kv_len, o, cu_new=None, max_new=None, causal=True, window=0, sinks=0,
+                         scale=0.0, lse=None):
+    T, Hq, d = q.shape
+    if d != cache.d:
+        raise ValueError("q must be [T, H_q, d] of the cache's head dim")
+    return CacheAttnArgs(cache, _batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
+                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), None if lse is None else lse.data_ptr())
+
+
+def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None, causal=True, window=0, sinks=0,
+                         scale=0.0, out=None, out_dtype=torch.bfloat16, want_lse=False, workspace=None, stream=None):
+    """Attention of the new tokens' queries q [T, H_q, d] over their sequences' cached tokens.
+    window > 0: a row sees the last `window` positions and the first `sinks`.  Returns
+    o [T, H_q*d] (and lse [T, H_q])."""
+    T, Hq, d = q.shape
+    dev = q.device
+    o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
+    if o.numel() != T * Hq * d or not o.is_contiguous():
+        raise ValueError("out must be contiguous [T, H_q*d]")
+    lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
+    a = cache_attention_args(q, cache, page_table, kv_len, o, cu_new, max_new, causal, window, sinks, scale, lse)
+    need = _lib.cast_cache_attention_workspace_size(C.byref(a))
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None and need else workspace
+    _check(_lib.cast_cache_attention(C.byref(a), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                     _stream(stream)))
+    _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
+    return (o, lse) if want_lse else o
+
+
+def cache_attention_workspace_size(args):
+    return _lib.cast_cache_attention_workspace_size(C.byref(args))
