@@ -272,7 +272,7 @@ cast_status validate_cache(const cast_kv_cache& c, const char* who) {
 }
 
 cast_status validate_batch(const cast_cache_batch& b, const char* who) {
-  if (b.B < 1 || b.T < 0 || b.max_pages < 0 || b.max_new < 0)
+  if (b.B < 1 || b.T < 0 || b.max_pages < 0 || b.max_new < (b.T > 0 ? 1 : 0))
     return fail(CAST_ERR_INVALID_ARG, "%s: bad batch (B %d, T %d, max_pages %d, max_new %d)", who, b.B, b.T,
                 b.max_pages, b.max_new);
   if (!b.page_table || !b.kv_len || !aligned4(b.page_table) || !aligned4(b.kv_len) || !aligned4(b.cu_new))
@@ -426,7 +426,7 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
       return fail(CAST_ERR_INVALID_ARG, "%s: a table of %d axes needs positions", who, a->rotary->n_axes);
     if (!aligned4(a->positions)) return fail(CAST_ERR_INVALID_ARG, "%s: positions misaligned", who);
   }
-  if (a->batch.T == 0 || a->batch.max_new == 0) return CAST_OK;
+  if (a->batch.T == 0) return CAST_OK;
   if ((s = check_rows(a->k, a->k_row_stride, (int64_t)c.H * c.d, "k", who))) return s;
   if ((s = check_rows(a->v, a->v_row_stride, (int64_t)c.H * c.d, "v", who))) return s;
   if (a->q) {

@@ -22,6 +22,7 @@
 #include <cmath>
 
 #include "cache.cuh"
+#include "cache_attention.cuh"
 #include "ptx.cuh"
 
 namespace cast {
@@ -117,48 +118,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&x);
-}
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-  uint32_t y;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
-  return y;
-}
-
-// A page's scale as the two bf16 factors of the decoding: 2^120 * scale overflows bf16 from 2^8 on
-struct Factor {
-  uint32_t once, twice;   // bf16 pairs; `twice` is 1 unless the scale is above 128
-  bool two;
-};
-__device__ __forceinline__ Factor factor_of(float scale) {
-  Factor f;
-  f.two = scale > 128.f;
-  const float a = f.two ? 0x1p120f : scale * 0x1p120f;
-  f.once = pack2(a, a);
-  f.twice = pack2(scale, scale);
-  return f;
-}
-// Codes 0, 2 (even) and 1, 3 (odd) of a word as bf16 pairs
-__device__ __forceinline__ void decode4(uint32_t w, const Factor& f, uint32_t& even, uint32_t& odd) {
-  even = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
-  odd = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
-  even = mul2(even, f.once);
-  odd = mul2(odd, f.once);
-  if (f.two) {
-    even = mul2(even, f.twice);
-    odd = mul2(odd, f.twice);
-  }
-  // the format's NaN (all seven bits set): the fields above make 480 of it
-  if ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u) {
-    if ((w & 0x0000007fu) == 0x0000007fu) even |= 0x00007fffu;
-    if ((w & 0x00007f00u) == 0x00007f00u) odd |= 0x00007fffu;
-    if ((w & 0x007f0000u) == 0x007f0000u) even |= 0x7fff0000u;
-    if ((w & 0x7f000000u) == 0x7f000000u) odd |= 0x7fff0000u;
-  }
-}
-
 template <int D, bool F8, int MT>
 struct Cfg {
   static constexpr int ROWS = 16 * MT;
@@ -180,18 +139,6 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return r * ROWB + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
-// Whether a 16-byte chunk of V holds a value that is not finite
-template <bool F8>
-__device__ __forceinline__ bool not_finite(const uint4& x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (F8) bad |= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
-    else bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  }
-  return bad;
-}
 // Channel c of row r of a V block
 template <bool F8, int ROWB>
 __device__ __forceinline__ float value_at(const uint8_t* block, int r, int c, float scale) {
@@ -802,9 +749,15 @@ using namespace cast;
 
 extern "C" {
 
+// Few rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu).
+static bool by_tiles(const cast_cache_attn_args& a) {
+  const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
+  return (int64_t)max_new * (a.H_q / a.cache.H) > 64;
+}
+
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {
   if (!a || a->batch.T < 1 || a->cache.H < 1 || a->H_q < a->cache.H || (a->cache.d != 64 && a->cache.d != 128)) return 0;
-  return rows_plan(*a).total_bytes;
+  return by_tiles(*a) ? tiles_plan(*a).total_bytes : rows_plan(*a).total_bytes;
 }
 
 cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t ws_bytes, void* stream) {
@@ -813,11 +766,15 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   cast_status s = validate_attention(a, who);
   if (s) return s;
   if (a->batch.T == 0) return CAST_OK;
-  const RowsPlan p = rows_plan(*a);
-  if (ws_bytes < p.total_bytes || (p.total_bytes && !ws))
-    return fail(CAST_ERR_INVALID_ARG, "%s: workspace %zu B < %zu B", who, ws_bytes, p.total_bytes);
+  const bool tiles = by_tiles(*a);
+  const TilesPlan tp = tiles ? tiles_plan(*a) : TilesPlan{};
+  const RowsPlan p = tiles ? RowsPlan{} : rows_plan(*a);
+  const size_t need = tiles ? tp.total_bytes : p.total_bytes;
+  if (ws_bytes < need || (need && !ws))
+    return fail(CAST_ERR_INVALID_ARG, "%s: workspace %zu B < %zu B", who, ws_bytes, need);
   if (reinterpret_cast<uintptr_t>(ws) % kWsAlign)
     return fail(CAST_ERR_INVALID_ARG, "%s: workspace not 256-byte aligned", who);
+  if (tiles) return launch_tiles(*a, tp, ws, static_cast<cudaStream_t>(stream));
   const cast_kv_cache& c = a->cache;
   if ((int64_t)a->batch.B * p.row_tiles * c.H > 0x7fffffff)
     return fail(CAST_ERR_UNSUPPORTED, "%s: too many units", who);

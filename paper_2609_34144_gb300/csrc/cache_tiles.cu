@@ -1,0 +1,870 @@
+// Attention over the paged KV cache for many rows a sequence (chunks of frames, prompts) on the
+// tensor cores' tcgen05 form.
+//
+// Rows of one KV head are (token, query head of the group) pairs, G of them a token: a tile of 128
+// rows holds 128 / G whole tokens, a unit two consecutive tiles (Q0, Q1) of one sequence, so that each
+// K/V tile of 128 positions fetched feeds 256 rows.  The positions a unit's rows can see are a list
+// of tiles (the sinks', then the window's); a call with few units cuts the list into n_split parts,
+// whose unnormalised o, maxima and sums k_tiles_merge joins.
+//
+// Roles (one CTA an SM): warp 0 fetches Q and the K pages, warp 2 the V pages (TMA boxes of one page x
+// 64 channels into a two-stage ring of 128-byte-swizzled tiles; a page that no row sees or that is
+// out of range is fetched from beyond the cache's end, which reads as zeros), warp 1 issues the
+// products in the order S0 S1 | PV0 S0' PV1 S1' | ..., and two warpgroups hold one query row a thread:
+// S from TMEM, mask, running maximum (renewed when a logit exceeds it by 2^8) and sum, P as bf16 back
+// to TMEM, where the P V product reads it.  The products of one thread complete in order, so a
+// thread that has S of tile j may change o, which holds tiles 0 .. j-1, before it hands over P.
+//
+// 0 times a value that is not finite is not 0: rows of V that no row of the unit sees are zeroed in
+// shared memory (warp 3), and in tiles that the rows do not all see alike a V row holding NaN or
+// infinity is zeroed too and its token added by the rows that do see it, one by one.
+//
+// 8-bit pages: the same boxes land in a raw tile, and a fourth warpgroup decodes them to the bf16
+// tiles (exactly: the scales are powers of two), with the zeroing on the way.
+#include <cmath>
+
+#include "cache.cuh"
+#include "cache_attention.cuh"
+#include "ptx.cuh"
+
+namespace cast {
+namespace {
+
+__device__ unsigned int g_tiles_error;
+
+constexpr int BM = 128, BN = 128, kStages = 2;
+constexpr int kTmemCols = 512;   // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
+
+template <int HD, bool F8>
+struct Cfg {
+  static constexpr int THREADS = F8 ? 512 : 384;
+  // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
+  static constexpr int LAUNCH = F8 ? 128 : 168;
+  static constexpr int REGS_CTL = F8 ? 64 : 96;
+  static constexpr int REGS_SOFTMAX = F8 ? 184 : 200;
+  static constexpr int REGS_DECODE = 80;
+  static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
+                "register split exceeds the launch allocation");
+  static constexpr int Q_BYTES = BM * HD * 2;
+  static constexpr int KV_BYTES = BN * HD * 2;
+  static constexpr int RAW_BYTES = F8 ? BN * HD : 0;
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
+  static constexpr int OFF_V = OFF_K + kStages * KV_BYTES;
+  static constexpr int OFF_RAW = OFF_V + kStages * KV_BYTES;   // raw K, raw V
+  static constexpr int OFF_BAR = OFF_RAW + 2 * RAW_BYTES;
+  static constexpr int SMEM = OFF_BAR + 640 + 1024;
+  static_assert(SMEM <= 232448, "shared memory of a CTA");
+};
+
+struct TilesKArgs {
+  cast_cache_batch batch;
+  int n_pages, page_size, page_shift, H, H_q, group, tile_tokens;   // tile_tokens = 128 / group
+  int causal, window, sinks, o_f32;
+  int64_t row_stride;
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  void* o;
+  float* lse;
+  float scale_log2;
+  unsigned* error;
+  int pairs;         // pairs of tiles that the grid has room for, a head
+  int n_split;
+  float4* part_o;    // [unit][part][HD / 4][256]
+  float2* part_ml;   // [unit][part][256]
+  unsigned long long wait_ns;
+};
+
+// One unit: tokens i0 .. of sequence b, KV head h
+struct Unit {
+  int b, h, t0, i0, n_new, p0;
+  int lo, hi, sinks;        // positions that some row sees: below sinks, or lo .. hi-1
+  int lo_all, hi_all;       // ... that every row sees: lo_all .. hi_all-1 (or below sinks)
+  int n_sink, first, tiles; // tiles of 128 positions: 0 .. n_sink-1, then first ..
+  int valid;
+};
+// position of the first key of tile j of the unit's list
+__device__ __forceinline__ int tile_pos(const Unit& u, int j) {
+  return (j < u.n_sink ? j : u.first + (j - u.n_sink)) * BN;
+}
+__device__ __forceinline__ bool all_see(const Unit& u, int pos) {
+  return pos + BN <= u.hi_all && (pos >= u.lo_all || pos + BN <= u.sinks);
+}
+__device__ __forceinline__ bool some_see(const Unit& u, int p) { return p < u.hi && (p >= u.lo || p < u.sinks); }
+
+// The unit at place `x` of the grid (one warp; the answer is every lane's): pairs of tiles run over
+// the sequences, for each head; with a causal mask a head's longest units come first.
+__device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
+  Unit u{};
+  u.h = x / a.pairs;
+  int pair = x - u.h * a.pairs;
+  const int per = 2 * a.tile_tokens;
+  int before = 0, total = 0;
+  if (a.causal) {
+    // count from the end
+    for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
+      const int b = b0 + lane;
+      int n = 0;
+      if (b < a.batch.B) n = (min(sequence_of(a.batch, b).n_new, a.batch.max_new) + per - 1) / per;
+      total += __reduce_add_sync(0xffffffffu, n);
+    }
+    pair = total - 1 - pair;
+    if (pair < 0) return u;
+  }
+  for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
+    const int b = b0 + lane;
+    int n = 0;
+    if (b < a.batch.B) {
+      const Sequence s = sequence_of(a.batch, b);
+      if (s.n_new > a.batch.max_new) atomicExch(a.error, kCacheBadInput);
+      n = (min(s.n_new, a.batch.max_new) + per - 1) / per;
+    }
+    int sum = n;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > pair);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      u.b = b0 + l;
+      u.i0 = (pair - before - __shfl_sync(0xffffffffu, sum - n, l)) * per;
+      u.valid = 1;
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (!u.valid) return u;
+  const Sequence s = sequence_of(a.batch, u.b);
+  u.t0 = s.t0;
+  u.n_new = min(s.n_new, a.batch.max_new);
+  u.p0 = s.len - s.n_new;
+  const int64_t room = (int64_t)a.batch.max_pages * a.page_size;
+  if (s.len > room) atomicExch(a.error, kCacheBadInput);
+  const int len = (int)min((int64_t)s.len, room);
+  const int i1 = min(u.i0 + per, u.n_new) - 1;
+  u.hi = a.causal ? min(len, max(u.p0 + i1 + 1, 0)) : len;
+  u.hi_all = a.causal ? min(len, max(u.p0 + u.i0 + 1, 0)) : len;
+  if (a.window > 0) {
+    u.lo = min(max(u.p0 + u.i0 - a.window + 1, 0), u.hi);
+    u.lo_all = max(u.p0 + i1 - a.window + 1, 0);
+    u.sinks = min(min(a.sinks, u.lo), u.hi);
+  }
+  u.first = u.lo / BN;
+  u.n_sink = min((u.sinks + BN - 1) / BN, u.first);
+  u.tiles = u.n_sink + max((u.hi + BN - 1) / BN - u.first, 0);
+  return u;
+}
+
+struct Bars {
+  uint64_t q_full;
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t s_full[2], p_full[2];
+  // bf16 pages: V of a stage's tile that not all rows see is ready.  One phase for each such tile of
+  // the stage; the next cannot begin before the products, and so the softmax threads, are past this one.
+  uint64_t v_fixed[kStages];
+  uint64_t raw_full[2], raw_empty[2];  // 8-bit pages: raw K, raw V
+  uint64_t fin;
+  uint32_t tmem_base;
+  int abort;
+  uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
+  float scale[2][8];                   // raw K, raw V: scales of the tile's pages
+  Unit unit;
+};
+static_assert(sizeof(Bars) <= 640, "barriers and the unit");
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+template <int N>
+__device__ __forceinline__ void end_barrier() {
+  asm volatile("barrier.sync 1, %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ bool aborted(const Bars* b) {
+  return *reinterpret_cast<const volatile int*>(&b->abort) != 0;
+}
+__device__ __forceinline__ void set_abort(Bars* b) {
+  atomicExch(&b->abort, 1);
+  atomicExch(&g_tiles_error, 1u);
+}
+__device__ __forceinline__ uint32_t tmem_ld_1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(r) : "r"(taddr) : "memory");
+  return r;
+}
+
+// Fetches the pages of K or V tile at `pos` (one warp; lane i < 128 / page_size has page i).  For
+// 8-bit pages lane i also leaves the page's scale.
+template <int HD, bool F8>
+__device__ __forceinline__ void fetch_pages(const TilesKArgs& a, const Unit& u, const CUtensorMap* map, uint8_t* dst,
+                                            uint64_t* full, float* scale, const float* scales, int pos, int lane) {
+  const int n = BN >> a.page_shift;
+  int page = a.n_pages;   // beyond the last page: reads as zeros
+  if (lane < n) {
+    const int p = pos + (lane << a.page_shift), e = p + a.page_size;
+    if (p < u.hi && (p < u.sinks || e > u.lo)) {
+      page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (p >> a.page_shift));
+      if (page < 0 || page >= a.n_pages) {
+        atomicExch(a.error, kCacheBadInput);
+        page = a.n_pages;
+      }
+    }
+    if (F8) scale[lane] = page < a.n_pages ? __ldg(scales + (int64_t)page * a.H + u.h) : 1.f;
+  }
+  __syncwarp();
+  if (lane == 0) mbar_arrive_expect_tx(full, F8 ? BN * HD : BN * HD * 2);
+  __syncwarp();
+  if (lane < n) {
+    if (F8) {
+      tma_load_3d(dst + (lane << a.page_shift) * HD, map, full, u.h * HD, 0, page);
+    } else {
+#pragma unroll
+      for (int b = 0; b < HD / 64; ++b)
+        tma_load_3d(dst + b * BN * 128 + (lane << a.page_shift) * 128, map, full, u.h * HD + b * 64, 0, page);
+    }
+  }
+}
+
+template <int HD, bool F8>
+__global__ void __launch_bounds__(F8 ? 512 : 384, 1)
+    k_cache_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                  const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ TilesKArgs a) {
+  using C = Cfg<HD, F8>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint8_t* sQ = smem + C::OFF_Q;
+  uint8_t* sK = smem + C::OFF_K;
+  uint8_t* sV = smem + C::OFF_V;
+  uint8_t* sRaw = smem + C::OFF_RAW;
+  Bars* bars = reinterpret_cast<Bars*>(smem + C::OFF_BAR);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int place = blockIdx.x / a.n_split, part = blockIdx.x - place * a.n_split;
+
+  if (warp == 0) {
+    const Unit u = unit_of(a, place, lane);
+    if (lane == 0) bars->unit = u;
+  }
+  if (threadIdx.x == 32) {
+    mbar_init(&bars->q_full, 1);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&bars->k_full[s], F8 ? 128 : 1);
+      mbar_init(&bars->k_empty[s], 1);
+      mbar_init(&bars->v_full[s], F8 ? 128 : 1);
+      mbar_init(&bars->v_empty[s], F8 ? 1 : 2);   // the products, and warp 3 that saw the tile
+      mbar_init(&bars->v_fixed[s], 32);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&bars->s_full[t], 1);
+      mbar_init(&bars->p_full[t], 128);
+      mbar_init(&bars->raw_full[t], 1);
+      mbar_init(&bars->raw_empty[t], 128);
+    }
+    mbar_init(&bars->fin, 1);
+    bars->abort = 0;
+    fence_barrier_init();
+  }
+  __syncthreads();
+  const Unit u = bars->unit;
+  if (!u.valid) return;
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, kTmemCols);
+    tmem_relinquish();
+    tc_fence_before();
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  const uint64_t lim = a.wait_ns;
+  const int k0 = (int)((int64_t)u.tiles * part / a.n_split);
+  const int n_tiles = (int)((int64_t)u.tiles * (part + 1) / a.n_split) - k0;
+  const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;
+
+  if (warp < 4) {
+    setmaxnreg_dec<C::REGS_CTL>();
+    if (warp == 0 || warp == 2) {
+      // ------------------------------------------------------------ Q and K pages / V pages
+      const bool is_k = warp == 0;
+      const CUtensorMap* map = is_k ? &tm_k : &tm_v;
+      if (lane == 0) {
+        tma_prefetch_desc(map);
+        if (is_k && n_tiles > 0) {
+          const uint32_t bytes = (uint32_t)a.tile_tokens * a.group * HD * 2;
+          mbar_arrive_expect_tx(&bars->q_full, (has_q1 ? 2 : 1) * bytes);
+          for (int t = 0; t < (has_q1 ? 2 : 1); ++t)
+#pragma unroll
+            for (int b = 0; b < HD / 64; ++b)
+              tma_load_3d(sQ + t * C::Q_BYTES + b * BM * 128, &tm_q, &bars->q_full, b * 64, u.h * a.group,
+                          u.t0 + u.i0 + t * a.tile_tokens);
+        }
+      }
+      __syncwarp();
+      uint64_t* full = is_k ? bars->k_full : bars->v_full;
+      uint64_t* empty = is_k ? bars->k_empty : bars->v_empty;
+      uint8_t* dst = is_k ? sK : sV;
+      for (int j = 0; j < n_tiles; ++j) {
+        bool ok;
+        if (F8) {
+          const int r = is_k ? 0 : 1;
+          ok = mbar_wait(&bars->raw_empty[r], ((uint32_t)j & 1u) ^ 1u, lim);
+          ok = !aborted(bars) && ok;
+          if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
+          fetch_pages<HD, true>(a, u, map, sRaw + r * C::RAW_BYTES, &bars->raw_full[r], bars->scale[r],
+                                is_k ? a.k_scale : a.v_scale, tile_pos(u, k0 + j), lane);
+        } else {
+          const int s = j % kStages;
+          ok = mbar_wait(&empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+          ok = !aborted(bars) && ok;
+          if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
+          fetch_pages<HD, false>(a, u, map, dst + s * C::KV_BYTES, &full[s], nullptr, nullptr, tile_pos(u, k0 + j), lane);
+        }
+      }
+    } else if (warp == 3 && !F8) {
+      // ------------------------------------------------------------ V of tiles that not all rows see
+      // It waits for every tile in turn and gives every stage back, so that it can be neither ahead
+      // of a phase nor overtaken.
+      for (int j = 0; j < n_tiles; ++j) {
+        const int pos = tile_pos(u, k0 + j), s = j % kStages;
+        bool ok = mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim);
+        ok = !aborted(bars) && ok;
+        if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
+        if (!all_see(u, pos)) {
+          uint8_t* tile = sV + s * C::KV_BYTES;
+          for (int i = 0; i < 4; ++i) {
+            // lane: row 32 i + lane
+            const int r = 32 * i + lane;
+            const bool some = some_see(u, pos + r);
+            bool bad = false;
+            if (some) {
+#pragma unroll 4
+              for (int c = 0; c < HD / 8; ++c) {
+                const uint4 w = *reinterpret_cast<const uint4*>(tile + (c / 8) * BN * 128 + r * 128 + ((c ^ r) & 7) * 16);
+                bad |= not_finite<false>(w);
+              }
+            }
+            const uint32_t apart = __ballot_sync(0xffffffffu, bad);
+            if (lane == 0) bars->apart[s][i] = apart;
+            if (bad || !some)
+#pragma unroll 4
+              for (int c = 0; c < HD / 8; ++c)
+                *reinterpret_cast<uint4*>(tile + (c / 8) * BN * 128 + r * 128 + ((c ^ r) & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(&bars->v_fixed[s]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->v_empty[s]);
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ------------------------------------------------------------ products
+      constexpr uint32_t idesc_qk = idesc_bf16_f32(BM, BN, false, false);
+      constexpr uint32_t idesc_pv = idesc_bf16_f32(BM, HD, false, true);
+      const int nq = has_q1 ? 2 : 1;
+      // a k-slice, query tile or stage further on adds its byte offset / 16 to the start address
+      static_assert(C::SMEM + 1024 <= 256 * 1024, "descriptor start-address field would carry");
+      const uint64_t dq = sdesc_sw128(smem_u32(sQ), 16, 1024);
+      const uint64_t dk = sdesc_sw128(smem_u32(sK), 16, 1024);
+      const uint64_t dv = sdesc_sw128(smem_u32(sV), BN * 128, 1024);
+      auto qk = [&](int t, int j) {
+        const uint64_t aq = dq + (uint64_t)((t * C::Q_BYTES) >> 4);
+        const uint64_t bk = dk + (uint64_t)(((j % kStages) * C::KV_BYTES) >> 4);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint64_t off = (uint64_t)(((kk >> 2) * (BM * 128) + (kk & 3) * 32) >> 4);
+          umma_bf16_ss(tmem + t * BN, aq + off, bk + off, idesc_qk, kk > 0 ? 1u : 0u);
+        }
+        umma_commit(&bars->s_full[t]);
+      };
+      // o is zeroed by the softmax threads before the first P, so it always accumulates
+      auto pv = [&](int t, int j) {
+        const uint64_t bv = dv + (uint64_t)(((j % kStages) * C::KV_BYTES) >> 4);
+#pragma unroll
+        for (int kk = 0; kk < BN / 16; ++kk)
+          umma_bf16_ts(tmem + 256 + t * 128, tmem + t * BN + kk * 8, bv + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, 1u);
+      };
+      bool ok = true;
+      uint32_t fixed = 0;   // bit s: parity of the next phase of v_fixed[s]
+      if (n_tiles > 0) {
+        ok = mbar_wait(&bars->q_full, 0, lim) && mbar_wait(&bars->k_full[0], 0, lim);
+        tc_fence_after();
+        if (ok) {
+          for (int t = 0; t < nq; ++t) qk(t, 0);
+          umma_commit(&bars->k_empty[0]);
+        }
+      }
+      for (int j = 0; ok && j < n_tiles; ++j) {
+        const int s = j % kStages;
+        const uint32_t ph = (uint32_t)j & 1u;
+        const bool more = j + 1 < n_tiles;
+        ok = !aborted(bars) && mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim);
+        if (ok && !F8 && !all_see(u, tile_pos(u, k0 + j))) {
+          ok = mbar_wait(&bars->v_fixed[s], (fixed >> s) & 1u, lim);
+          fixed ^= 1u << s;
+        }
+        if (ok && more) ok = mbar_wait(&bars->k_full[(j + 1) % kStages], (uint32_t)((j + 1) / kStages) & 1u, lim);
+        ok = ok && mbar_wait(&bars->p_full[0], ph, lim);
+        if (!ok) break;
+        tc_fence_after();
+        pv(0, j);
+        if (more) qk(0, j + 1);
+        if (nq == 2) {
+          if (aborted(bars) || !mbar_wait(&bars->p_full[1], ph, lim)) { ok = false; break; }
+          tc_fence_after();
+          pv(1, j);
+        }
+        umma_commit(&bars->v_empty[s]);
+        if (more) {
+          if (nq == 2) qk(1, j + 1);
+          umma_commit(&bars->k_empty[(j + 1) % kStages]);
+        }
+      }
+      if (!ok) set_abort(bars);
+      umma_commit(&bars->fin);
+      mbar_wait(&bars->fin, 0, lim);
+    }
+    __syncwarp();
+    tc_fence_before();
+    end_barrier<C::THREADS>();
+    if (warp == 1) {
+      tc_fence_after();
+      tmem_dealloc(tmem, kTmemCols);
+    }
+  } else if (warp < 12) {
+    setmaxnreg_inc<C::REGS_SOFTMAX>();
+    if (warp < 8 || has_q1) {
+      // ------------------------------------------------------------ softmax and result
+      const int t = warp < 8 ? 0 : 1;
+      const int q4 = warp & 3;
+      const int row = q4 * 32 + lane;
+      const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
+      const uint32_t colS = t * BN, colO = 256 + t * 128;
+      // the row's token and query head, and what it sees: below hi, and below sinks or from lo on
+      const int tok = row / a.group, i = u.i0 + t * a.tile_tokens + tok;
+      const bool live = tok < a.tile_tokens && i < u.n_new;
+      const int p = u.p0 + i;
+      const int hi = !live ? 0 : a.causal ? min(u.hi, max(p + 1, 0)) : u.hi;
+      const int lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
+      const int sinks = a.window > 0 ? a.sinks : 0;
+      float m_ref = -INFINITY, l = 0.f;
+      {
+        uint32_t zero[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) zero[c] = 0u;
+#pragma unroll
+        for (int c = 0; c < HD; c += 32) tmem_st_x32(tl + colO + c, zero);
+      }
+      bool ok = true;
+      uint32_t fixed = 0;
+      for (int j = 0; j < n_tiles; ++j) {
+        bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)j & 1u, lim);
+        if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
+        tc_fence_after();
+        uint32_t sr[BN];
+        tmem_ld_x64(tl + colS, sr);
+        tmem_ld_x64(tl + colS + 64, sr + 64);
+        const int pos = tile_pos(u, k0 + j);
+        const bool whole = all_see(u, pos);
+        if (!whole) {
+          // columns below hi - pos and (from lo - pos on, or below sinks - pos)
+          const int ch = hi - pos, cl = lo - pos, cs = sinks - pos;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            auto below = [&](int c) {   // bits of columns 32b .. 32b+31 that are below c
+              const int k = c - 32 * b;
+              return k <= 0 ? 0u : k >= 32 ? 0xffffffffu : (1u << k) - 1u;
+            };
+            const uint32_t see = below(ch) & (~below(cl) | below(cs));
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if (!((see >> c) & 1u)) sr[32 * b + c] = __float_as_uint(-INFINITY);
+          }
+        }
+        float m8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m8[e] = fmaxf(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1]));
+#pragma unroll
+        for (int c = 16; c < BN; c += 16)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            m8[e] = max3(m8[e], __uint_as_float(sr[c + 2 * e]), __uint_as_float(sr[c + 2 * e + 1]));
+        const float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * a.scale_log2;
+        const bool need = mx > m_ref + 8.f;
+        float corr = 1.f;
+        if (need) {
+          corr = exp2_fast(m_ref - mx);   // 0 where the row has seen nothing yet
+          m_ref = mx;
+          l *= corr;
+        }
+        // a row that has seen nothing: 2^(-inf - 0) = 0
+        const float ref = m_ref == -INFINITY ? 0.f : m_ref;
+        const float2 sc2 = make_float2(a.scale_log2, a.scale_log2);
+        const float2 nm2 = make_float2(-ref, -ref);
+        float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int c = 0; c < BN; c += 2) {
+          const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), sc2, nm2);
+          const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+          s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], e);
+          const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
+          sr[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+        }
+        const float2 s2 = __fadd2_rn(__fadd2_rn(s4[0], s4[1]), __fadd2_rn(s4[2], s4[3]));
+        l += s2.x + s2.y;
+        tmem_st_x64(tl + colS, sr);
+        if (j > 0 && __any_sync(0xffffffffu, need)) {
+#pragma unroll
+          for (int half = 0; half < HD / 64; ++half) {
+            uint32_t orr[64];
+            tmem_ld_x64(tl + colO + half * 64, orr);
+#pragma unroll
+            for (int c = 0; c < 64; ++c) orr[c] = __float_as_uint(__uint_as_float(orr[c]) * corr);
+            tmem_st_x64(tl + colO + half * 64, orr);
+          }
+        }
+        if (!whole) {
+          const int s = j % kStages;
+          w = F8 ? mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim)
+                 : mbar_wait(&bars->v_fixed[s], (fixed >> s) & 1u, lim);
+          fixed ^= 1u << s;
+          if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
+          for (int b = 0; b < 4; ++b) {
+            for (uint32_t bits = bars->apart[s][b]; bits; bits &= bits - 1) {
+              // V row r holds a value that is not finite: its token by itself, where it is seen
+              const int r = 32 * b + __ffs(bits) - 1, key = pos + r;
+              const uint32_t pp = tmem_ld_1(tl + colS + r / 2);
+              const float prob = __uint_as_float(r & 1 ? pp & 0xffff0000u : pp << 16);
+              const bool see = key < hi && (key >= lo || key < sinks);
+              const int page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (key >> a.page_shift));
+              const int64_t at = ((int64_t)page * a.page_size + (key & (a.page_size - 1))) * a.row_stride + (int64_t)u.h * HD;
+              const float f = F8 ? __ldg(a.v_scale + (int64_t)page * a.H + u.h) : 1.f;
+#pragma unroll 1
+              for (int c = 0; c < HD; c += 32) {
+                uint32_t orr[32];
+                tmem_ld_x32(tl + colO + c, orr);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  float x;
+                  if (F8) {
+                    const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + e), __NV_E4M3));
+                    x = __half2float(h) * f;
+                  } else {
+                    x = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v) + at + c + e) << 16);
+                  }
+                  if (see) orr[e] = __float_as_uint(__uint_as_float(orr[e]) + prob * x);
+                }
+                tmem_st_x32(tl + colO + c, orr);
+              }
+            }
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(&bars->p_full[t]);
+      }
+      if (ok) {
+        bool w = !aborted(bars) && mbar_wait(&bars->fin, 0, lim);
+        ok = __all_sync(0xffffffffu, w);
+      }
+      if (!ok) set_abort(bars);
+      tc_fence_after();
+      if (ok && a.n_split == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
+#pragma unroll
+        for (int half = 0; half < HD / 64; ++half) {
+          uint32_t orr[64];
+          tmem_ld_x64(tl + colO + half * 64, orr);
+          const float* v = reinterpret_cast<const float*>(orr);
+          if (live && a.o_f32) {
+            float* dst = static_cast<float*>(a.o) + out * HD + half * 64;
+#pragma unroll
+            for (int c = 0; c < 64; c += 4)
+              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[c + 1] * inv, v[c + 2] * inv, v[c + 3] * inv);
+          } else if (live) {
+            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.o) + out * HD + half * 64;
+#pragma unroll
+            for (int c = 0; c < 64; c += 8) {
+              float y[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = v[c + e] * inv;
+              *reinterpret_cast<uint4*>(dst + c) = pack8(y);
+            }
+          }
+          __syncwarp();
+        }
+        if (a.lse && live) a.lse[out] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.69314718055994531f;
+      } else if (ok) {
+        const int64_t slot = (int64_t)place * a.n_split + part;
+#pragma unroll
+        for (int half = 0; half < HD / 64; ++half) {
+          uint32_t orr[64];
+          tmem_ld_x64(tl + colO + half * 64, orr);
+          const float* v = reinterpret_cast<const float*>(orr);
+#pragma unroll
+          for (int c = 0; c < 64; c += 4)
+            __stcg(a.part_o + (slot * (HD / 4) + half * 16 + c / 4) * 256 + t * 128 + row,
+                   make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]));
+        }
+        __stcg(a.part_ml + slot * 256 + t * 128 + row, make_float2(m_ref, l));
+      }
+    }
+    tc_fence_before();
+    end_barrier<C::THREADS>();
+  } else if constexpr (F8) {
+    // -------------------------------------------------------------- decoding of raw tiles
+    setmaxnreg_dec<C::REGS_DECODE>();
+    const int tid = threadIdx.x - 384;
+    constexpr int CH = HD / 16;   // 16-code chunks of a row
+    bool ok = true;
+    for (int j = 0; ok && j < n_tiles; ++j) {
+      const int s = j % kStages, pos = tile_pos(u, k0 + j);
+      const bool whole = all_see(u, pos);
+#pragma unroll 1
+      for (int kv = 0; kv < 2; ++kv) {
+        bool w = !aborted(bars) && mbar_wait(&bars->raw_full[kv], (uint32_t)j & 1u, lim) &&
+                 mbar_wait(kv ? &bars->v_empty[s] : &bars->k_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+        // the four warps leave together: they meet at barriers below
+        if (bar_sync_or(2, 128, !w)) { ok = false; break; }
+        const uint8_t* src = sRaw + kv * C::RAW_BYTES;
+        uint8_t* dst = (kv ? sV : sK) + s * C::KV_BYTES;
+        if (kv && !whole) {
+          // V rows that hold NaN, of a tile that the rows do not all see alike (one row a thread)
+          bool bad = false;
+          if (some_see(u, pos + tid))
+            for (int c = 0; c < CH; ++c) bad |= not_finite<true>(*reinterpret_cast<const uint4*>(src + tid * HD + c * 16));
+          const uint32_t apart = __ballot_sync(0xffffffffu, bad);
+          if (lane == 0) bars->apart[s][tid >> 5] = apart;
+          asm volatile("bar.sync 2, 128;" ::: "memory");
+        }
+#pragma unroll 2
+        for (int i = 0; i < CH; ++i) {
+          const int x = tid + 128 * i, r = x / CH, cc = x % CH;
+          const uint4 q = *reinterpret_cast<const uint4*>(src + x * 16);
+          const Factor f = factor_of(bars->scale[kv][r >> a.page_shift]);
+          const uint32_t in[4] = {q.x, q.y, q.z, q.w};
+          uint32_t out[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t even, odd;
+            decode4(in[e], f, even, odd);
+            out[2 * e] = __byte_perm(even, odd, 0x5410);
+            out[2 * e + 1] = __byte_perm(even, odd, 0x7632);
+          }
+          if (kv && !whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[e] = 0u;
+          // two 16-byte chunks of the bf16 row; the second 64-channel box's lanes write theirs in
+          // the other order, so that eight lanes take eight bank groups
+          uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
+          const int c0 = 2 * (cc & 3), swap = (cc >> 2) & 1;
+          const uint4 lo4 = make_uint4(out[0], out[1], out[2], out[3]), hi4 = make_uint4(out[4], out[5], out[6], out[7]);
+          *reinterpret_cast<uint4*>(base + (((c0 + swap) ^ r) & 7) * 16) = swap ? hi4 : lo4;
+          *reinterpret_cast<uint4*>(base + (((c0 + 1 - swap) ^ r) & 7) * 16) = swap ? lo4 : hi4;
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(kv ? &bars->v_full[s] : &bars->k_full[s]);
+        mbar_arrive(&bars->raw_empty[kv]);
+      }
+    }
+    if (!ok) set_abort(bars);
+    end_barrier<C::THREADS>();
+  }
+}
+
+// Joins the parts of the units: one CTA for 32 rows of a unit.
+template <int HD>
+__global__ void __launch_bounds__(256) k_tiles_merge(const __grid_constant__ TilesKArgs a) {
+  __shared__ Unit su;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (threadIdx.x < 32) {
+    const Unit u = unit_of(a, blockIdx.x, threadIdx.x);
+    if (threadIdx.x == 0) su = u;
+  }
+  __syncthreads();
+  const Unit u = su;
+  if (!u.valid) return;
+  const int row = blockIdx.y * 32 + (threadIdx.x & 31);   // of the unit's 256
+  const int t = row >> 7, tok = (row & 127) / a.group, i = u.i0 + t * a.tile_tokens + tok;
+  if (tok >= a.tile_tokens || i >= u.n_new) return;
+  const int64_t slot = (int64_t)blockIdx.x * a.n_split;
+  float top = -INFINITY;
+  for (int p = 0; p < a.n_split; ++p) top = fmaxf(top, a.part_ml[(slot + p) * 256 + row].x);
+  float l = 0.f;
+  for (int p = 0; p < a.n_split; ++p) {
+    const float2 v = a.part_ml[(slot + p) * 256 + row];
+    l += v.x == -INFINITY ? 0.f : exp2_fast(v.x - top) * v.y;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + ((row & 127) - tok * a.group);
+  for (int c = threadIdx.x >> 5; c < HD / 4; c += 8) {
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p = 0; p < a.n_split; ++p) {
+      const float m = a.part_ml[(slot + p) * 256 + row].x;
+      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+      const float4 y = a.part_o[((slot + p) * (HD / 4) + c) * 256 + row];
+      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+    }
+    if (a.o_f32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(a.o) + out * HD + c * 4) =
+          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + out * HD + c * 4) =
+          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    }
+  }
+  if (a.lse && threadIdx.x < 32) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------- host side
+bool encode(CUtensorMap* m, bool bytes, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+            const cuuint32_t (&box)[3]) {
+  EncodeTiledFn fn = tensor_map_encoder();
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn && fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
+                  strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD, bool F8>
+cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const TilesPlan& p, cudaStream_t st) {
+  using C = Cfg<HD, F8>;
+  const cast_kv_cache& c = a.cache;
+  CUtensorMap mq, mk, mv;
+  const cuuint64_t elt = F8 ? 1 : 2;
+  const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
+  const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
+  const cuuint64_t kd[3] = {(cuuint64_t)c.H * HD, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
+  const cuuint64_t ks[2] = {(cuuint64_t)c.row_stride * elt, (cuuint64_t)c.row_stride * elt * c.page_size};
+  const cuuint32_t kb[3] = {F8 ? HD : 64, (cuuint32_t)c.page_size, 1};
+  if (!encode(&mq, false, a.q, qd, qs, qb) || !encode(&mk, F8, c.k, kd, ks, kb) || !encode(&mv, F8, c.v, kd, ks, kb))
+    return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
+  static std::atomic<uint64_t> attr_done{0};
+  cast_status setup = CAST_OK;
+  if (!once_per_device(attr_done, [&] {
+        cudaFuncAttributes fa{};
+        if (cudaFuncGetAttributes(&fa, k_cache_tiles<HD, F8>) != cudaSuccess) return false;
+        if (fa.numRegs != C::LAUNCH) {
+          // the register hand-over counts on exactly this many
+          setup = fail(CAST_ERR_UNSUPPORTED, "cache attention kernel built with %d registers per thread, expected %d", fa.numRegs,
+                       C::LAUNCH);
+          return false;
+        }
+        return cudaFuncSetAttribute(k_cache_tiles<HD, F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
+      }))
+    return setup != CAST_OK ? setup : check_launch("cache attention kernel attributes");
+  const int64_t units = (int64_t)p.pairs * c.H;
+  k_cache_tiles<HD, F8><<<(unsigned)(units * p.n_split), C::THREADS, C::SMEM, st>>>(mq, mk, mv, k);
+  cast_status s = check_launch("cache attention");
+  if (s || p.n_split == 1) return s;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)units, 8, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, k_tiles_merge<HD>, k) != cudaSuccess) return check_launch("cache attention merge");
+  return check_launch("cache attention merge");
+}
+
+}  // namespace
+
+TilesPlan tiles_plan(const cast_cache_attn_args& a) {
+  TilesPlan p{};
+  const int group = a.H_q / a.cache.H, d = a.cache.d;
+  p.tile_tokens = BM / group;
+  const int per = 2 * p.tile_tokens;
+  const int64_t T = a.batch.T, B = a.batch.B;
+  // exactly, without cu_new; with it at most one ragged pair a sequence more than the whole ones
+  const int64_t max_new = a.batch.max_new < T ? a.batch.max_new : T;
+  int64_t pairs = a.batch.cu_new ? T / per + B : B * ((T / B + per - 1) / per);
+  const int64_t bound = B * ((max_new + per - 1) / per);
+  if (pairs > bound) pairs = bound;
+  p.pairs = (int)(pairs > 0x7fffff ? 0x7fffff : pairs);
+  const int64_t units = (int64_t)p.pairs * a.cache.H;
+  const int64_t room = (int64_t)a.batch.max_pages * a.cache.page_size;
+  int64_t seen = room;
+  if (a.window > 0 && a.window + per + (int64_t)a.sinks + 3 * BN < room) seen = a.window + per + (int64_t)a.sinks + 3 * BN;
+  const int64_t tiles = (seen + BN - 1) / BN;
+  int dev = 0, nsm = 152;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
+  if (nsm < 1) nsm = 1;
+  // The split with the least estimated time: rounds of one CTA an SM, each as long as its part's tiles
+  // (about 1.7 us each) and a fixed 4 us, and for a split the parts written and read again and the
+  // second launch.
+  double best = 0;
+  p.n_split = 1;
+  for (int n = 1; n <= 16 && (n == 1 || tiles / n >= 2); ++n) {
+    const double rounds = (double)((units * n + nsm - 1) / nsm);
+    double us = rounds * ((double)((tiles + n - 1) / n) * 1.7 + 4.0);
+    if (n > 1) us += 4.0 + (double)(units * n) * 256 * d * 4 * 2 / 4e6;
+    if (n == 1 || us < best) {
+      best = us;
+      p.n_split = n;
+    }
+  }
+  if (p.n_split > 1) {
+    p.part_o_bytes = align_up((size_t)units * p.n_split * 256 * d * sizeof(float));
+    p.total_bytes = p.part_o_bytes + align_up((size_t)units * p.n_split * 256 * sizeof(float2));
+  }
+  return p;
+}
+
+cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void* ws, cudaStream_t st) {
+  const cast_kv_cache& c = a.cache;
+  if ((int64_t)p.pairs * c.H * p.n_split > 0x7fffffff)
+    return fail(CAST_ERR_UNSUPPORTED, "cast_cache_attention: too many units");
+  TilesKArgs k{};
+  k.batch = a.batch;
+  k.n_pages = c.n_pages;
+  k.page_size = c.page_size;
+  while ((1 << k.page_shift) < c.page_size) ++k.page_shift;
+  k.H = c.H;
+  k.H_q = a.H_q;
+  k.group = a.H_q / c.H;
+  k.tile_tokens = p.tile_tokens;
+  k.causal = a.causal ? 1 : 0;
+  k.window = a.window < (int64_t)a.batch.max_pages * c.page_size ? a.window : 0;
+  k.sinks = k.window > 0 ? a.sinks : 0;
+  k.o_f32 = a.o_dtype == CAST_F32;
+  k.row_stride = c.row_stride;
+  k.k = static_cast<const uint8_t*>(c.k);
+  k.v = static_cast<const uint8_t*>(c.v);
+  k.k_scale = c.k_scale;
+  k.v_scale = c.v_scale;
+  k.o = a.o;
+  k.lse = a.lse;
+  k.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;
+  if (!(k.error = cache_error_address())) return check_launch("cache error word");
+  k.pairs = p.pairs;
+  k.n_split = p.n_split;
+  k.part_o = static_cast<float4*>(ws);
+  k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
+  k.wait_ns = 2000000000ull;
+  if (c.dtype == CAST_F8E4M3) return c.d == 128 ? launch<128, true>(a, k, p, st) : launch<64, true>(a, k, p, st);
+  return c.d == 128 ? launch<128, false>(a, k, p, st) : launch<64, false>(a, k, p, st);
+}
+
+unsigned int tiles_error_word(cudaStream_t st, bool clear) {
+  unsigned int v = 0;
+  cudaMemcpyFromSymbolAsync(&v, g_tiles_error, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
+  cudaStreamSynchronize(st);
+  if (clear && v) {
+    const unsigned int z = 0;
+    cudaMemcpyToSymbolAsync(g_tiles_error, &z, sizeof(z), 0, cudaMemcpyHostToDevice, st);
+    cudaStreamSynchronize(st);
+  }
+  return v;
+}
+
+}  // namespace cast

@@ -149,6 +149,8 @@ cast_status validate_cache(const cast_kv_cache& c, const char* who);
 cast_status validate_batch(const cast_cache_batch& b, const char* who);
 // Nonzero when a cache kernel left out a page, position or token that was out of range.
 unsigned int cache_error_word(cudaStream_t st, bool clear);
+// Nonzero when the cache attention gave up on a bounded wait.
+unsigned int tiles_error_word(cudaStream_t st, bool clear);
 
 // ------------------------------------------------------------------ residual update
 cast_status launch_residual_add(void* x, const void* r, int dtype, size_t n, cudaStream_t st);

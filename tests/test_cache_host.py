@@ -103,7 +103,7 @@ BATCH_BAD = [
     ({"page_table": None}, 1), ({"kv_len": None}, 1), ({"page_table_stride": 7}, 1), ({"B": 0}, 1), ({"T": -1}, 1),
     ({"T": 7}, 1),                       # not a multiple of B without cu_new
     ({"max_new": 2}, 1),                 # T / B tokens each
-    ({"max_pages": -1}, 1), ({"cu_new": 0x700002}, 1),
+    ({"max_pages": -1}, 1), ({"cu_new": 0x700002}, 1), ({"max_new": 0, "cu_new": 0x700000}, 1),
 ]
 
 
