@@ -15,10 +15,17 @@
 // unit sees are filled with zeros instead of being read.  S = Q K^T and o += P V are m16n8k16
 // products: at 16 rows the tensor cores wait for memory anyway.
 //
-// 8-bit rows are decoded to bf16 on the way from shared memory to the products: a code's exponent
-// and mantissa moved to bf16's fields are code * 2^-120, a subnormal code included, so that one
-// multiplication by 2^120 * scale gives the value, exactly.  The order of channels inside a 16-wide
-// step of Q K^T, and of o's columns, is that in which the codes lie in their 32-bit words.
+// 8-bit rows: codes become f16 (one conversion for two, exact) on the way from shared memory to the
+// products, and the scales stay outside: a page's K scale multiplies its logits, and o is kept in
+// units of the largest V scale so far, R, so that a page's probabilities are multiplied by its scale / R
+// (a page whose scale is below 2^-10 R is decoded to bf16 instead, whose range holds the quotient).
+// Queries are f16 too, each row times the power of two that brings its largest channel below 2^15:
+// bf16's eight bits fit, and channels 2^30 below the largest are the first to lose one.  The order of
+// channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the codes lie in
+// their 32-bit words.
+// Measured at 24 sequences of 8k to 32k tokens, 8 KV heads of 128, 4 query heads each (1.11 GB of codes):
+// decoding everything to bf16 with integer operations 438 us; f16 with two CTAs an SM 246 us, three
+// 236 us, four (and three stages a warp) 255 us.
 #include <cmath>
 
 #include "cache.cuh"
@@ -29,6 +36,9 @@ namespace cast {
 namespace {
 
 constexpr float kRescale = 8.f;   // the running maximum is renewed when a logit exceeds it by 2^8
+// Probabilities are at most 2^8 times a row's largest; as f16, 2^7 keeps them below 2^16 and the small
+// ones far above its subnormals
+constexpr float kLift = 128.f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kWarps = 4;
 
@@ -113,6 +123,22 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma16816h(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Codes in the low and the high half of a word as f16 pairs
+__device__ __forceinline__ void half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack2h(float a, float b) {
+  const __half2 x = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -124,7 +150,9 @@ struct Cfg {
   static constexpr int ROWB = D * (F8 ? 1 : 2);        // bytes of a key row
   static constexpr int CHUNKS = ROWB / 16;
   static constexpr int BLOCK = 16 * ROWB;              // K or V of a 16-token block
-  static constexpr int STAGES = (24 * 1024) / (2 * BLOCK) > 8 ? 8 : (24 * 1024) / (2 * BLOCK);
+  static constexpr int CTAS = F8 ? 3 : 2;              // of an SM
+  static constexpr int ROOM = F8 ? 16 * 1024 : 24 * 1024;   // a warp's ring at most
+  static constexpr int STAGES = ROOM / (2 * BLOCK) > 8 ? 8 : ROOM / (2 * BLOCK);
   static constexpr int RING = STAGES * 2 * BLOCK;      // of one warp
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
   static constexpr int SMEM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
@@ -151,7 +179,7 @@ __device__ __forceinline__ float value_at(const uint8_t* block, int r, int c, fl
 }
 
 template <int D, bool F8, int MT>
-__global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_constant__ RowsKArgs a) {
+__global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_rows(const __grid_constant__ RowsKArgs a) {
   using C = Cfg<D, F8, MT>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_work[kWarps], s_entry;
@@ -268,14 +296,47 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
             uint32_t x, y;
             if constexpr (F8) {
               const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + s * 16 + q4 * 4));
-              x = __byte_perm(w.x, w.y, 0x5410);
-              y = __byte_perm(w.x, w.y, 0x7632);
+              x = w.x;
+              y = w.y;
             } else {
               x = __ldg(reinterpret_cast<const uint32_t*>(src + s * 16 + q4 * 2));
               y = __ldg(reinterpret_cast<const uint32_t*>(src + s * 16 + q4 * 2 + 8));
             }
             qf[m][s][j] = in ? x : 0u;
             qf[m][s][2 + j] = in ? y : 0u;
+          }
+        }
+      float unit[MT][2];   // what a row's logits are multiplied by
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          unit[m][j] = a.scale_log2;
+          if constexpr (F8) {
+            auto low = [](uint32_t w) { return __uint_as_float(w << 16); };
+            auto high = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+            float top = 0.f;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const uint32_t w = qf[m][s][e + j];
+                top = fmaxf(top, fmaxf(fabsf(low(w)), fabsf(high(w))));
+              }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // 2^-e with the largest channel in [2^14, 2^15); subnormal, zero and infinite rows as they are
+            const int e = (int)(__float_as_uint(top) >> 23) - 127 - 14;
+            const bool plain = e < -126 || e > 112;
+            const float down = plain ? 1.f : pow2f(-e);
+            if (!plain) unit[m][j] *= pow2f(e);
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+              for (int e2 = 0; e2 < 4; e2 += 2) {
+                const uint32_t w = qf[m][s][e2 + j];
+                qf[m][s][e2 + j] = pack2h(low(w) * down, high(w) * down);
+              }
           }
         }
       // positions that every row sees: [all_lo, all_hi); the others' blocks are masked
@@ -287,6 +348,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
       }
 
       float o[MT][D / 8][4], m_ref[MT][2], l[MT][2];
+      float v_unit = 0.f;   // 8-bit pages: o is in units of this over kLift
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -357,11 +419,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[m][t][e] = 0.f;
-        Factor fk, fv;
+        float2 sc = make_float2(1.f, 1.f);   // scales of the block's page
         if constexpr (F8) {
-          const float2 sc = s_scale[warp][st];
-          fk = factor_of(sc.x);
-          fv = factor_of(sc.y);
+          sc = s_scale[warp][st];
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -371,9 +431,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 uint32_t b0, b1;
-                decode4(w[j], fk, b0, b1);
+                half4(w[j], b0, b1);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) mma16816(s[m][t], qf[m][c + j], b0, b1);
+                for (int m = 0; m < MT; ++m) mma16816h(s[m][t], qf[m][c + j], b0, b1);
               }
             }
         } else {
@@ -391,13 +451,18 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
         const int base = z.block(i0 + it * kWarps) * 16;
         const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
         bool grows = false;
+        float times[MT][2];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) times[m][j] = unit[m][j] * sc.x;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float x = s[m][t][e] * a.scale_log2;
+              float x = s[m][t][e] * times[m][e >> 1];
               if (!whole) {
                 const int p = base + t * 8 + q4 * 2 + (e & 1), r = pos[m][e >> 1];
                 const bool see = p < z.hi && (!a.causal || p <= r) &&
@@ -427,6 +492,22 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
               }
             }
         }
+        float weight = 1.f;   // of the page's V codes in o's units
+        if constexpr (F8) {
+          if (sc.y > v_unit) {
+            // a larger scale: o in units of it (o is 0 before the first)
+            const float f = v_unit / sc.y;
+            v_unit = sc.y;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int t = 0; t < D / 8; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[m][t][e] *= f;
+          }
+          weight = sc.y / v_unit * kLift;
+        }
+        const bool by_f16 = F8 && weight >= kLift * 0x1p-10f;
         uint32_t pf[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -443,10 +524,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
                 l[m][j] += p;
               }
           }
-          pf[m][0] = pack2(s[m][0][0], s[m][0][1]);
-          pf[m][1] = pack2(s[m][0][2], s[m][0][3]);
-          pf[m][2] = pack2(s[m][1][0], s[m][1][1]);
-          pf[m][3] = pack2(s[m][1][2], s[m][1][3]);
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const float x = s[m][t][2 * j], y = s[m][t][2 * j + 1];
+              pf[m][2 * t + j] = by_f16 ? pack2h(x * weight, y * weight) : pack2(x, y);
+            }
         }
         // A block that the rows do not all see, with a value that is not finite: 0 times it would
         // reach the rows that do not see it, so its tokens are added one by one where they are seen.
@@ -457,7 +541,6 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
           apart = __any_sync(0xffffffffu, apart);
         }
         if (apart) {
-          const float scale = F8 ? s_scale[warp][st].y : 1.f;
 #pragma unroll
           for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -482,24 +565,49 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
                     const int n = F8 ? (c >> 1) * 16 + 2 * (q4 * 2 + e) + (c & 1) : c * 8 + q4 * 2 + e;
-                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, scale);
+                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, weight);
                   }
               }
           }
         } else if constexpr (F8) {
+          // words of V hold tokens 2 q4 and 2 q4 + 1 of channels 2 g and 2 g + 1
+          if (by_f16) {
 #pragma unroll
-          for (int c = 0; c < D / 16; c += 2) {
-            uint32_t w[4];
-            ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
+            for (int c = 0; c < D / 16; c += 2) {
+              uint32_t w[4];
+              ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              uint32_t e0, e1, d0, d1;
-              decode4(w[2 * j], fv, e0, d0);
-              decode4(w[2 * j + 1], fv, e1, d1);
+              for (int j = 0; j < 2; ++j) {
+                uint32_t e0, e1, d0, d1;
+                half4(__byte_perm(w[2 * j], 0, 0x3120), e0, d0);
+                half4(__byte_perm(w[2 * j + 1], 0, 0x3120), e1, d1);
 #pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                mma16816(o[m][2 * (c + j)], pf[m], e0, e1);
-                mma16816(o[m][2 * (c + j) + 1], pf[m], d0, d1);
+                for (int m = 0; m < MT; ++m) {
+                  mma16816h(o[m][2 * (c + j)], pf[m], e0, e1);
+                  mma16816h(o[m][2 * (c + j) + 1], pf[m], d0, d1);
+                }
+              }
+            }
+          } else {
+            const Factor f = factor_of(weight);
+#pragma unroll 1
+            for (int c = 0; c < D / 16; c += 2) {
+              uint32_t w[4];
+              ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                uint32_t e0, e1, d0, d1;
+                decode4(w[2 * j], f, e0, d0);
+                decode4(w[2 * j + 1], f, e1, d1);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                  // o is indexed by constants only
+#pragma unroll
+                  for (int k = 0; k < D / 16; k += 2)
+                    if (k == c) {
+                      mma16816(o[m][2 * (k + j)], pf[m], e0, e1);
+                      mma16816(o[m][2 * (k + j) + 1], pf[m], d0, d1);
+                    }
               }
             }
           }
@@ -536,10 +644,12 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_cache_rows(const __grid_cons
           if (q4 == 0) ml[warp * C::ROWS + r] = make_float2(m_ref[m][j], x);
           float* dst = mo + (warp * C::ROWS + r) * D;
           if constexpr (F8) {
+            const float f = v_unit / kLift;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
               *reinterpret_cast<float4*>(dst + c * 16 + q4 * 4) =
-                  make_float4(o[m][2 * c][2 * j], o[m][2 * c + 1][2 * j], o[m][2 * c][2 * j + 1], o[m][2 * c + 1][2 * j + 1]);
+                  make_float4(o[m][2 * c][2 * j] * f, o[m][2 * c + 1][2 * j] * f, o[m][2 * c][2 * j + 1] * f,
+                              o[m][2 * c + 1][2 * j + 1] * f);
           } else {
 #pragma unroll
             for (int t = 0; t < D / 8; ++t)
@@ -674,7 +784,7 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   p.row_tiles = (int)(((int64_t)max_new * group + rows - 1) / rows);
   int dev = 0, nsm = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
-  p.grid = 2 * (nsm < 1 ? 1 : nsm);
+  p.grid = (a.cache.dtype == CAST_F8E4M3 ? Cfg<128, true, 1>::CTAS : Cfg<128, false, 1>::CTAS) * (nsm < 1 ? 1 : nsm);
   p.least = 16;
   // Blocks that a unit has at most.  Up to 64 (a thousand tokens: four blocks' latency a warp's ring)
   // a CTA takes a whole unit and nothing is joined.

@@ -592,22 +592,39 @@ def rotary_table(rot_dim, layout="half", base=10000.0, sections=None, scaling=No
         p.factor = scaling[1]
         p.original_length = scaling[2] if len(scaling) > 2 else 0
     _check(_lib.cast_rotary_table_init(C.byref(p), C.byref(t)))
+    t.pointer = C.pointer(t)
     return t
+
+
+# These calls serve single tokens, where the host's microseconds are the step's: the raw stream is
+# asked for directly and tensors are measured once.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on(stream, t):
+    """The stream's handle for a call on t's device."""
+    if not t.is_cuda:
+        raise ValueError("expected CUDA tensors")
+    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _heads_stride(t, name, dtype=torch.bfloat16):
     """Token row stride of a [T, H, d] tensor whose (H, d) are contiguous."""
-    if t.dim() != 3 or (dtype is not None and t.dtype != dtype):
+    if t.dim() != 3 or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"{name}: expected [T, H, d] of {dtype}")
     T, H, d = t.shape
+    if T < 2:
+        if not t.is_contiguous():
+            raise ValueError(f"{name}: heads and channels must be contiguous")
+        return H * d
     s0, s1, s2 = t.stride()
     if (d > 1 and s2 != 1) or (H > 1 and s1 != d):
         raise ValueError(f"{name}: heads and channels must be contiguous")
-    return s0 if T > 1 else H * d
+    return s0
 
 
 def _int32(t, name, shape=None):
-    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: expected a contiguous int32 tensor" + (f" of shape {shape}" if shape else ""))
     return t.data_ptr()
 
@@ -627,12 +644,12 @@ def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
     T, H, d = x.shape
     n = table.n_axes
     pos = _int32(positions, "positions", (T,) if n == 1 and positions.dim() == 1 else (T, n))
-    o = torch.empty((T, H, d), dtype=x.dtype, device=x.device) if out is None else out
+    o = x.new_empty((T, H, d)) if out is None else out
     if out is not None and (o.shape != x.shape or o.dtype != x.dtype):
         raise ValueError("out must have x's shape and dtype")
     a = RotaryArgs(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
-                   _dtype_code(x), pos, C.pointer(table), inverse)
-    _check(_lib.cast_rotary(C.byref(a), _stream(stream)))
+                   _dtype_code(x), pos, table.pointer, inverse)
+    _check(_lib.cast_rotary(C.byref(a), _on(stream, x)))
     if out is None:
         _on_stream(stream, o)
     return o
@@ -660,13 +677,16 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
 
 
 def _batch(page_table, kv_len, cu_new, T, max_new):
-    if page_table.dim() != 2 or page_table.dtype != torch.int32 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+    if page_table.dim() != 2 or page_table.dtype is not torch.int32:
         raise ValueError("page_table: expected int32 [B, max_pages]")
     B, P = page_table.shape
+    s0, s1 = page_table.stride()
+    if P > 1 and s1 != 1:
+        raise ValueError("page_table: a sequence's pages must be contiguous")
     cu = None if cu_new is None else _int32(cu_new, "cu_new", (B + 1,))
     if max_new is None:
         max_new = T if cu is not None else T // max(B, 1)
-    return CacheBatch(page_table.data_ptr(), max(page_table.stride(0), P), P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new)
+    return CacheBatch(page_table.data_ptr(), s0 if s0 > P else P, P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new)
 
 
 def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None, rotary=None, positions=None,
@@ -687,13 +707,13 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
         qs, Hq = _heads_stride(q, "q"), q.shape[1]
         if q.shape[0] != T or q.shape[2] != d:
             raise ValueError("q must be [T, H_q, d]")
-        o = torch.empty((T, Hq, d), dtype=q.dtype, device=q.device) if q_out is None else q_out
+        o = q.new_empty((T, Hq, d)) if q_out is None else q_out
         if o.shape != q.shape:
             raise ValueError("q_out must have q's shape")
-        qp, qo, qos = q.data_ptr(), o.data_ptr(), _heads_stride(o, "q_out")
+        qp, qo, qos = q.data_ptr(), o.data_ptr(), Hq * d if q_out is None else _heads_stride(o, "q_out")
     a = AppendArgs(cache, _batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(), _heads_stride(k, "k"),
-                   _heads_stride(v, "v"), C.pointer(rotary) if rotary is not None else None, pos, qp, qo, qs, qos, Hq)
-    _check(_lib.cast_cache_append(C.byref(a), _stream(stream)))
+                   _heads_stride(v, "v"), rotary.pointer if rotary is not None else None, pos, qp, qo, qs, qos, Hq)
+    _check(_lib.cast_cache_append(C.byref(a), _on(stream, k)))
     if q_out is None:
         _on_stream(stream, o)
     return o
@@ -714,17 +734,18 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     window > 0: a row sees the last `window` positions and the first `sinks`.  Returns
     o [T, H_q*d] (and lse [T, H_q])."""
     T, Hq, d = q.shape
-    dev = q.device
-    o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
-    if o.numel() != T * Hq * d or not o.is_contiguous():
+    o = q.new_empty((T, Hq * d), dtype=out_dtype) if out is None else out
+    if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous()):
         raise ValueError("out must be contiguous [T, H_q*d]")
-    lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
+    lse = q.new_empty((T, Hq), dtype=torch.float32) if want_lse else None
     a = cache_attention_args(q, cache, page_table, kv_len, o, cu_new, max_new, causal, window, sinks, scale, lse)
-    need = _lib.cast_cache_attention_workspace_size(C.byref(a))
-    ws = torch.empty(need, dtype=torch.uint8, device=dev) if workspace is None and need else workspace
-    _check(_lib.cast_cache_attention(C.byref(a), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
-                                     _stream(stream)))
-    _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
+    ref, ws = C.byref(a), workspace
+    if ws is None:
+        need = _lib.cast_cache_attention_workspace_size(ref)
+        ws = q.new_empty(need, dtype=torch.uint8) if need else None
+    _check(_lib.cast_cache_attention(ref, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _on(stream, q)))
+    if stream is not None:
+        _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
     return (o, lse) if want_lse else o
 
 
