@@ -23,9 +23,12 @@
 // bf16's eight bits fit, and channels 2^30 below the largest are the first to lose one.  The order of
 // channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the codes lie in
 // their 32-bit words.
-// Measured at 24 sequences of 8k to 32k tokens, 8 KV heads of 128, 4 query heads each (1.11 GB of codes):
-// decoding everything to bf16 with integer operations 438 us; f16 with two CTAs an SM 246 us, three
-// 236 us, four (and three stages a warp) 255 us.
+// Bound: memory for bf16 pages, instructions for 8-bit ones (427 a block of 16 tokens, 2.1 a clock and
+// SM, against the 360 clocks that its 4 KB take at the copy rate).  Measured, GB300: 48 sequences with
+// windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB) 141 us, 5.9 TB/s; 24 sequences
+// of 8k to 32k tokens in 8 bits (1.11 GB) 202 us, 5.5 TB/s.  The latter decoding everything to bf16 with
+// integer operations 438 us; by f16 236 us with three CTAs an SM, 246 with two, 255 with four; then
+// 202 us with copies that test a whole block at once and logits scaled inside the exponent.
 #include <cmath>
 
 #include "cache.cuh"
@@ -98,7 +101,10 @@ __device__ __forceinline__ Span span_of(const RowsKArgs& a, int b, int row_tile,
 }
 
 // ---------------------------------------------------------------- warp-level pieces
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool valid) {
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_or_zero(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
@@ -149,6 +155,8 @@ struct Cfg {
   static constexpr int ROWS = 16 * MT;
   static constexpr int ROWB = D * (F8 ? 1 : 2);        // bytes of a key row
   static constexpr int CHUNKS = ROWB / 16;
+  static constexpr int LANE_ROWS = 32 / CHUNKS;        // rows that a warp's copy takes
+  static constexpr int COPIES = 16 / LANE_ROWS;
   static constexpr int BLOCK = 16 * ROWB;              // K or V of a 16-token block
   static constexpr int CTAS = F8 ? 3 : 2;              // of an SM
   static constexpr int ROOM = F8 ? 16 * 1024 : 24 * 1024;   // a warp's ring at most
@@ -348,7 +356,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       }
 
       float o[MT][D / 8][4], m_ref[MT][2], l[MT][2];
-      float v_unit = 0.f;   // 8-bit pages: o is in units of this over kLift
+      float v_unit = 0.f, v_lift = 0.f;   // 8-bit pages: o is in units of v_unit / kLift = 1 / v_lift
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -369,21 +377,32 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
         }
         return p;
       };
-      // fetches block i of the unit into stage st
+      // fetches block i of the unit into stage st: in copy c lane l has chunk l % CHUNKS of row
+      // c * LANE_ROWS + l / CHUNKS
+      const int64_t row_bytes = a.row_stride * (F8 ? 1 : 2), step = row_bytes * C::LANE_ROWS;
+      const int64_t lane_off = (lane / C::CHUNKS) * row_bytes + lane % C::CHUNKS * 16 + (int64_t)h * C::ROWB;
       auto fetch = [&](int i, int st, int page) {
         const int base = z.block(i) * 16;
         const int64_t row0 = (int64_t)max(page, 0) * a.page_size + (base & (a.page_size - 1));
-        const uint8_t* ks = a.k + (row0 * a.row_stride + (int64_t)h * D) * (F8 ? 1 : 2);
-        const uint8_t* vs = a.v + (row0 * a.row_stride + (int64_t)h * D) * (F8 ? 1 : 2);
+        const uint8_t* ks = a.k + row0 * row_bytes + lane_off;
+        const uint8_t* vs = ks + (a.v - a.k);
         const uint32_t dst = ring_at + st * 2 * C::BLOCK;
+        if (page >= 0 && base + 16 <= z.hi && (base >= z.lo || base + 16 <= z.sinks)) {
 #pragma unroll
-        for (int c = 0; c < 16 * C::CHUNKS / 32; ++c) {
-          const int x = c * 32 + lane, r = x / C::CHUNKS, cc = x % C::CHUNKS;
-          const int p = base + r;
-          const bool in = page >= 0 && p < z.hi && (p >= z.lo || p < z.sinks);
-          const int64_t off = in ? (int64_t)r * a.row_stride * (F8 ? 1 : 2) + cc * 16 : 0;
-          copy16(dst + chunk_at<C::ROWB>(r, cc), ks + off, in);
-          copy16(dst + C::BLOCK + chunk_at<C::ROWB>(r, cc), vs + off, in);
+          for (int c = 0; c < C::COPIES; ++c) {
+            const uint32_t to = dst + chunk_at<C::ROWB>(c * C::LANE_ROWS + lane / C::CHUNKS, lane % C::CHUNKS);
+            copy16(to, ks + c * step);
+            copy16(to + C::BLOCK, vs + c * step);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < C::COPIES; ++c) {
+            const int r = c * C::LANE_ROWS + lane / C::CHUNKS, p = base + r;
+            const bool in = page >= 0 && p < z.hi && (p >= z.lo || p < z.sinks);
+            const uint32_t to = dst + chunk_at<C::ROWB>(r, lane % C::CHUNKS);
+            copy16_or_zero(to, in ? ks + c * step : a.k, in);
+            copy16_or_zero(to + C::BLOCK, in ? vs + c * step : a.v, in);
+          }
         }
         if constexpr (F8) {
           // lanes 0 and 1: the page's scales, 4 bytes behind the same group of copies
@@ -450,34 +469,42 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
         }
         const int base = z.block(i0 + it * kWarps) * 16;
         const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
-        bool grows = false;
         float times[MT][2];
+        bool grows = false;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int j = 0; j < 2; ++j) times[m][j] = unit[m][j] * sc.x;
+        if (!whole) {
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const int p = base + t * 8 + q4 * 2 + e, r = pos[m][j];
+                  const bool see = p < z.hi && (!a.causal || p <= r) && (a.window <= 0 || p > r - a.window || p < a.sinks);
+                  s[m][t][2 * j + e] = see ? s[m][t][2 * j + e] * times[m][j] : -INFINITY;
+                }
+              times[m][j] = 1.f;
+            }
+        }
+        float top[MT][2];   // this lane's largest logit of the row
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float x = s[m][t][e] * times[m][e >> 1];
-              if (!whole) {
-                const int p = base + t * 8 + q4 * 2 + (e & 1), r = pos[m][e >> 1];
-                const bool see = p < z.hi && (!a.causal || p <= r) &&
-                                 (a.window <= 0 || p > r - a.window || p < a.sinks);
-                if (!see) x = -INFINITY;
-              }
-              s[m][t][e] = x;
-              grows = grows || x > m_ref[m][e >> 1] + kRescale;
-            }
+          for (int j = 0; j < 2; ++j) {
+            top[m][j] = fmaxf(fmaxf(s[m][0][2 * j], s[m][0][2 * j + 1]), fmaxf(s[m][1][2 * j], s[m][1][2 * j + 1])) * times[m][j];
+            grows = grows || top[m][j] > m_ref[m][j] + kRescale;
+          }
         if (__any_sync(0xffffffffu, grows)) {
 #pragma unroll
           for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              float x = fmaxf(fmaxf(s[m][0][2 * j], s[m][0][2 * j + 1]), fmaxf(s[m][1][2 * j], s[m][1][2 * j + 1]));
+              float x = top[m][j];
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
               x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
               if (x > m_ref[m][j]) {
@@ -492,12 +519,15 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
               }
             }
         }
-        float weight = 1.f;   // of the page's V codes in o's units
+        // 8-bit pages: probabilities carry the page's V scale in o's units (`weight`, by the exponent)
+        float weight = 1.f, shift = 0.f, back = 1.f;
+        bool by_f16 = false;
         if constexpr (F8) {
           if (sc.y > v_unit) {
             // a larger scale: o in units of it (o is 0 before the first)
             const float f = v_unit / sc.y;
             v_unit = sc.y;
+            v_lift = kLift / sc.y;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -505,31 +535,37 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[m][t][e] *= f;
           }
-          weight = sc.y / v_unit * kLift;
+          weight = sc.y * v_lift;
+          by_f16 = weight >= kLift * 0x1p-10f;
+          if (by_f16) {
+            shift = __log2f(weight);
+            back = __frcp_rn(weight);
+          }
         }
-        const bool by_f16 = F8 && weight >= kLift * 0x1p-10f;
         uint32_t pf[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             // a row that has seen nothing yet: exp2(-inf - 0) = 0
-            const float ref = m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j];
+            const float ref = shift - (m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j]);
+            float sum = 0.f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const float p = exp2_fast(s[m][t][2 * j + e] - ref);
+                const float p = exp2_fast(fmaf(s[m][t][2 * j + e], times[m][j], ref));
                 s[m][t][2 * j + e] = p;
-                l[m][j] += p;
+                sum += p;
               }
+            l[m][j] = fmaf(sum, back, l[m][j]);
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const float x = s[m][t][2 * j], y = s[m][t][2 * j + 1];
-              pf[m][2 * t + j] = by_f16 ? pack2h(x * weight, y * weight) : pack2(x, y);
+              pf[m][2 * t + j] = by_f16 ? pack2h(x, y) : pack2(x, y);
             }
         }
         // A block that the rows do not all see, with a value that is not finite: 0 times it would
@@ -565,7 +601,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
                     const int n = F8 ? (c >> 1) * 16 + 2 * (q4 * 2 + e) + (c & 1) : c * 8 + q4 * 2 + e;
-                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, weight);
+                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, by_f16 ? 1.f : weight);
                   }
               }
           }
