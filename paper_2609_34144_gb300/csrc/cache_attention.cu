@@ -898,7 +898,7 @@ extern "C" {
 // Few rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu).
 static bool by_tiles(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
-  return (int64_t)max_new * (a.H_q / a.cache.H) > 64;
+  return (int64_t)max_new * (a.H_q / a.cache.H) > 16;
 }
 
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {

@@ -19,8 +19,16 @@
 // shared memory (warp 3), and in tiles that the rows do not all see alike a V row holding NaN or
 // infinity is zeroed too and its token added by the rows that do see it, one by one.
 //
-// 8-bit pages: the same boxes land in a raw tile, and a fourth warpgroup decodes them to the bf16
-// tiles (exactly: the scales are powers of two), with the zeroing on the way.
+// 8-bit pages: K is multiplied as it lies, in the 8-bit form of the products.  A bf16 query is the sum of
+// two e4m3 numbers, exactly: times the power of two that brings its row's largest channel to 448 at
+// most, its first four bits and the rest are one each (channels 2^10 below the largest keep 2^-19 of
+// it).  So S is the sum of two products at twice the rate, and each page's scale multiplies its columns of S.
+// V is decoded to bf16 tiles (exactly: the scales are powers of two) by a fourth warpgroup, with the
+// zeroing on the way; four channels of a word take the places 0, 2, 1, 3, which o's columns inherit.
+//
+// A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
+// warpgroup and odd ones to the other, each with its own S, o, maximum and sum, so that the products of one
+// overlap the softmax of the other; the two are joined at the end.
 #include <cmath>
 
 #include "cache.cuh"
@@ -40,20 +48,22 @@ struct Cfg {
   static constexpr int THREADS = F8 ? 512 : 384;
   // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
   static constexpr int LAUNCH = F8 ? 128 : 168;
-  static constexpr int REGS_CTL = F8 ? 64 : 96;
-  static constexpr int REGS_SOFTMAX = F8 ? 184 : 200;
-  static constexpr int REGS_DECODE = 80;
+  static constexpr int REGS_CTL = F8 ? 56 : 96;
+  static constexpr int REGS_SOFTMAX = F8 ? 192 : 200;
+  static constexpr int REGS_DECODE = 72;
   static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
                 "register split exceeds the launch allocation");
-  static constexpr int Q_BYTES = BM * HD * 2;
-  static constexpr int KV_BYTES = BN * HD * 2;
+  static constexpr int Q_BYTES = BM * HD * 2;               // 8 bits: two pieces of BM * HD
+  static constexpr int K_BYTES = BN * HD * (F8 ? 1 : 2);
+  static constexpr int V_BYTES = BN * HD * 2;
   static constexpr int RAW_BYTES = F8 ? BN * HD : 0;
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
-  static constexpr int OFF_V = OFF_K + kStages * KV_BYTES;
-  static constexpr int OFF_RAW = OFF_V + kStages * KV_BYTES;   // raw K, raw V
-  static constexpr int OFF_BAR = OFF_RAW + 2 * RAW_BYTES;
-  static constexpr int SMEM = OFF_BAR + 640 + 1024;
+  static constexpr int OFF_V = OFF_K + kStages * K_BYTES;
+  static constexpr int OFF_RAW = OFF_V + kStages * V_BYTES;   // V codes
+  static constexpr int OFF_BAR = OFF_RAW + kStages * RAW_BYTES;
+  static_assert(kStages * V_BYTES >= BM * HD * 4, "o of one warpgroup passes through the V tiles");
+  static constexpr int SMEM = OFF_BAR + 1664 + 1024;
   static_assert(SMEM <= 232448, "shared memory of a CTA");
 };
 
@@ -62,8 +72,10 @@ struct TilesKArgs {
   int n_pages, page_size, page_shift, H, H_q, group, tile_tokens;   // tile_tokens = 128 / group
   int causal, window, sinks, o_f32;
   int64_t row_stride;
-  const uint8_t *k, *v;
+  const uint8_t* v;
   const float *k_scale, *v_scale;
+  const __nv_bfloat16* q;
+  int64_t q_stride;
   void* o;
   float* lse;
   float scale_log2;
@@ -163,15 +175,16 @@ struct Bars {
   // bf16 pages: V of a stage's tile that not all rows see is ready.  One phase for each such tile of
   // the stage; the next cannot begin before the products, and so the softmax threads, are past this one.
   uint64_t v_fixed[kStages];
-  uint64_t raw_full[2], raw_empty[2];  // 8-bit pages: raw K, raw V
+  uint64_t raw_full[kStages], raw_empty[kStages];   // 8-bit pages: V codes
   uint64_t fin;
   uint32_t tmem_base;
   int abort;
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
-  float scale[2][8];                   // raw K, raw V: scales of the tile's pages
+  float scale[kStages][8];             // V codes: scales of the tile's pages
+  float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
   Unit unit;
 };
-static_assert(sizeof(Bars) <= 640, "barriers and the unit");
+static_assert(sizeof(Bars) <= 1664, "barriers and the unit");
 
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
@@ -182,6 +195,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+// The channel that place c of o's columns holds (8-bit pages: see above)
+template <bool F8>
+__host__ __device__ constexpr int channel(int c) {
+  return F8 ? (c & ~3) | ((c & 1) << 1) | ((c >> 1) & 1) : c;
 }
 template <int N>
 __device__ __forceinline__ void end_barrier() {
@@ -201,34 +219,37 @@ __device__ __forceinline__ uint32_t tmem_ld_1(uint32_t taddr) {
   return r;
 }
 
-// Fetches the pages of K or V tile at `pos` (one warp; lane i < 128 / page_size has page i).  For
-// 8-bit pages lane i also leaves the page's scale.
-template <int HD, bool F8>
+// The page that holds position `p` of the unit's sequence, or n_pages (which reads as zeros) where no
+// row of the unit sees any of it or it is out of range.
+__device__ __forceinline__ int page_at(const TilesKArgs& a, const Unit& u, int p) {
+  if (!(p < u.hi && (p < u.sinks || p + a.page_size > u.lo))) return a.n_pages;
+  const int page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (p >> a.page_shift));
+  if (page >= 0 && page < a.n_pages) return page;
+  atomicExch(a.error, kCacheBadInput);
+  return a.n_pages;
+}
+
+// Fetches the pages of a K or V tile at `pos` (one warp; lane i < 128 / page_size has page i).  ROWB: bytes
+// of a row; CODES: the tile is 8-bit.  With `scale` lane i also leaves the page's scale there.
+template <int ROWB, bool CODES>
 __device__ __forceinline__ void fetch_pages(const TilesKArgs& a, const Unit& u, const CUtensorMap* map, uint8_t* dst,
                                             uint64_t* full, float* scale, const float* scales, int pos, int lane) {
   const int n = BN >> a.page_shift;
-  int page = a.n_pages;   // beyond the last page: reads as zeros
+  int page = a.n_pages;
   if (lane < n) {
-    const int p = pos + (lane << a.page_shift), e = p + a.page_size;
-    if (p < u.hi && (p < u.sinks || e > u.lo)) {
-      page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (p >> a.page_shift));
-      if (page < 0 || page >= a.n_pages) {
-        atomicExch(a.error, kCacheBadInput);
-        page = a.n_pages;
-      }
-    }
-    if (F8) scale[lane] = page < a.n_pages ? __ldg(scales + (int64_t)page * a.H + u.h) : 1.f;
+    page = page_at(a, u, pos + (lane << a.page_shift));
+    if (scale) scale[lane] = page < a.n_pages ? __ldg(scales + (int64_t)page * a.H + u.h) : 1.f;
   }
   __syncwarp();
-  if (lane == 0) mbar_arrive_expect_tx(full, F8 ? BN * HD : BN * HD * 2);
+  if (lane == 0) mbar_arrive_expect_tx(full, BN * ROWB);
   __syncwarp();
   if (lane < n) {
-    if (F8) {
-      tma_load_3d(dst + (lane << a.page_shift) * HD, map, full, u.h * HD, 0, page);
+    if (CODES) {
+      tma_load_3d(dst + (lane << a.page_shift) * ROWB, map, full, u.h * ROWB, 0, page);
     } else {
 #pragma unroll
-      for (int b = 0; b < HD / 64; ++b)
-        tma_load_3d(dst + b * BN * 128 + (lane << a.page_shift) * 128, map, full, u.h * HD + b * 64, 0, page);
+      for (int b = 0; b < ROWB / 128; ++b)
+        tma_load_3d(dst + b * BN * 128 + (lane << a.page_shift) * 128, map, full, u.h * (ROWB / 2) + b * 64, 0, page);
     }
   }
 }
@@ -254,9 +275,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     if (lane == 0) bars->unit = u;
   }
   if (threadIdx.x == 32) {
-    mbar_init(&bars->q_full, 1);
+    mbar_init(&bars->q_full, F8 ? 256 : 1);
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&bars->k_full[s], F8 ? 128 : 1);
+      mbar_init(&bars->k_full[s], 1);
       mbar_init(&bars->k_empty[s], 1);
       mbar_init(&bars->v_full[s], F8 ? 128 : 1);
       mbar_init(&bars->v_empty[s], F8 ? 1 : 2);   // the products, and warp 3 that saw the tile
@@ -265,8 +286,10 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     for (int t = 0; t < 2; ++t) {
       mbar_init(&bars->s_full[t], 1);
       mbar_init(&bars->p_full[t], 128);
-      mbar_init(&bars->raw_full[t], 1);
-      mbar_init(&bars->raw_empty[t], 128);
+    }
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&bars->raw_full[s], 1);
+      mbar_init(&bars->raw_empty[s], 128);
     }
     mbar_init(&bars->fin, 1);
     bars->abort = 0;
@@ -286,7 +309,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   const uint64_t lim = a.wait_ns;
   const int k0 = (int)((int64_t)u.tiles * part / a.n_split);
   const int n_tiles = (int)((int64_t)u.tiles * (part + 1) / a.n_split) - k0;
-  const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;
+  const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;   // else the warpgroups share the key tiles
 
   if (warp < 4) {
     setmaxnreg_dec<C::REGS_CTL>();
@@ -296,7 +319,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       const CUtensorMap* map = is_k ? &tm_k : &tm_v;
       if (lane == 0) {
         tma_prefetch_desc(map);
-        if (is_k && n_tiles > 0) {
+        if (!F8 && is_k && n_tiles > 0) {
           const uint32_t bytes = (uint32_t)a.tile_tokens * a.group * HD * 2;
           mbar_arrive_expect_tx(&bars->q_full, (has_q1 ? 2 : 1) * bytes);
           for (int t = 0; t < (has_q1 ? 2 : 1); ++t)
@@ -307,25 +330,18 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
       }
       __syncwarp();
-      uint64_t* full = is_k ? bars->k_full : bars->v_full;
-      uint64_t* empty = is_k ? bars->k_empty : bars->v_empty;
-      uint8_t* dst = is_k ? sK : sV;
+      const bool codes = F8 && !is_k;   // V codes go to the raw ring
+      uint64_t* full = is_k ? bars->k_full : codes ? bars->raw_full : bars->v_full;
+      uint64_t* empty = is_k ? bars->k_empty : codes ? bars->raw_empty : bars->v_empty;
+      uint8_t* dst = is_k ? sK : codes ? sRaw : sV;
+      const int bytes = is_k ? C::K_BYTES : codes ? C::RAW_BYTES : C::V_BYTES;
       for (int j = 0; j < n_tiles; ++j) {
-        bool ok;
-        if (F8) {
-          const int r = is_k ? 0 : 1;
-          ok = mbar_wait(&bars->raw_empty[r], ((uint32_t)j & 1u) ^ 1u, lim);
-          ok = !aborted(bars) && ok;
-          if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
-          fetch_pages<HD, true>(a, u, map, sRaw + r * C::RAW_BYTES, &bars->raw_full[r], bars->scale[r],
-                                is_k ? a.k_scale : a.v_scale, tile_pos(u, k0 + j), lane);
-        } else {
-          const int s = j % kStages;
-          ok = mbar_wait(&empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
-          ok = !aborted(bars) && ok;
-          if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
-          fetch_pages<HD, false>(a, u, map, dst + s * C::KV_BYTES, &full[s], nullptr, nullptr, tile_pos(u, k0 + j), lane);
-        }
+        const int s = j % kStages;
+        bool ok = mbar_wait(&empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+        ok = !aborted(bars) && ok;
+        if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
+        fetch_pages<HD * (F8 ? 1 : 2), F8>(a, u, map, dst + s * bytes, &full[s], codes ? bars->scale[s] : nullptr, a.v_scale,
+                                           tile_pos(u, k0 + j), lane);
       }
     } else if (warp == 3 && !F8) {
       // ------------------------------------------------------------ V of tiles that not all rows see
@@ -337,7 +353,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         ok = !aborted(bars) && ok;
         if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
         if (!all_see(u, pos)) {
-          uint8_t* tile = sV + s * C::KV_BYTES;
+          uint8_t* tile = sV + s * C::V_BYTES;
           for (int i = 0; i < 4; ++i) {
             // lane: row 32 i + lane
             const int r = 32 * i + lane;
@@ -365,65 +381,104 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
     } else if (warp == 1 && lane == 0) {
       // ------------------------------------------------------------ products
-      constexpr uint32_t idesc_qk = idesc_bf16_f32(BM, BN, false, false);
+      constexpr uint32_t idesc_qk = F8 ? idesc_e4m3_f32(BM, BN) : idesc_bf16_f32(BM, BN, false, false);
       constexpr uint32_t idesc_pv = idesc_bf16_f32(BM, HD, false, true);
-      const int nq = has_q1 ? 2 : 1;
       // a k-slice, query tile or stage further on adds its byte offset / 16 to the start address
       static_assert(C::SMEM + 1024 <= 256 * 1024, "descriptor start-address field would carry");
-      const uint64_t dq = sdesc_sw128(smem_u32(sQ), 16, 1024);
-      const uint64_t dk = sdesc_sw128(smem_u32(sK), 16, 1024);
+      constexpr bool kNarrow = F8 && HD == 64;   // 64-byte rows
+      const uint64_t dq = kNarrow ? sdesc_sw64(smem_u32(sQ), 16, 512) : sdesc_sw128(smem_u32(sQ), 16, 1024);
+      const uint64_t dk = kNarrow ? sdesc_sw64(smem_u32(sK), 16, 512) : sdesc_sw128(smem_u32(sK), 16, 1024);
       const uint64_t dv = sdesc_sw128(smem_u32(sV), BN * 128, 1024);
-      auto qk = [&](int t, int j) {
-        const uint64_t aq = dq + (uint64_t)((t * C::Q_BYTES) >> 4);
-        const uint64_t bk = dk + (uint64_t)(((j % kStages) * C::KV_BYTES) >> 4);
+      // S_t = Q_q K_j^T
+      auto qk = [&](int t, int q, int j) {
+        const uint64_t aq = dq + (uint64_t)((q * C::Q_BYTES) >> 4);
+        const uint64_t bk = dk + (uint64_t)(((j % kStages) * C::K_BYTES) >> 4);
+        if constexpr (F8) {
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint64_t off = (uint64_t)(((kk >> 2) * (BM * 128) + (kk & 3) * 32) >> 4);
-          umma_bf16_ss(tmem + t * BN, aq + off, bk + off, idesc_qk, kk > 0 ? 1u : 0u);
+          for (int piece = 0; piece < 2; ++piece)
+#pragma unroll
+            for (int kk = 0; kk < HD / 32; ++kk)
+              umma_f8_ss(tmem + t * BN, aq + (uint64_t)((piece * BM * HD + kk * 32) >> 4), bk + (uint64_t)((kk * 32) >> 4),
+                         idesc_qk, piece + kk > 0 ? 1u : 0u);
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            const uint64_t off = (uint64_t)(((kk >> 2) * (BM * 128) + (kk & 3) * 32) >> 4);
+            umma_bf16_ss(tmem + t * BN, aq + off, bk + off, idesc_qk, kk > 0 ? 1u : 0u);
+          }
         }
         umma_commit(&bars->s_full[t]);
       };
       // o is zeroed by the softmax threads before the first P, so it always accumulates
       auto pv = [&](int t, int j) {
-        const uint64_t bv = dv + (uint64_t)(((j % kStages) * C::KV_BYTES) >> 4);
+        const uint64_t bv = dv + (uint64_t)(((j % kStages) * C::V_BYTES) >> 4);
 #pragma unroll
         for (int kk = 0; kk < BN / 16; ++kk)
           umma_bf16_ts(tmem + 256 + t * 128, tmem + t * BN + kk * 8, bv + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, 1u);
       };
-      bool ok = true;
       uint32_t fixed = 0;   // bit s: parity of the next phase of v_fixed[s]
-      if (n_tiles > 0) {
-        ok = mbar_wait(&bars->q_full, 0, lim) && mbar_wait(&bars->k_full[0], 0, lim);
-        tc_fence_after();
-        if (ok) {
-          for (int t = 0; t < nq; ++t) qk(t, 0);
-          umma_commit(&bars->k_empty[0]);
-        }
-      }
-      for (int j = 0; ok && j < n_tiles; ++j) {
+      auto k_ready = [&](int j) { return mbar_wait(&bars->k_full[j % kStages], (uint32_t)(j / kStages) & 1u, lim); };
+      auto v_ready = [&](int j) {
         const int s = j % kStages;
-        const uint32_t ph = (uint32_t)j & 1u;
-        const bool more = j + 1 < n_tiles;
-        ok = !aborted(bars) && mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim);
+        bool ok = !aborted(bars) && mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim);
         if (ok && !F8 && !all_see(u, tile_pos(u, k0 + j))) {
           ok = mbar_wait(&bars->v_fixed[s], (fixed >> s) & 1u, lim);
           fixed ^= 1u << s;
         }
-        if (ok && more) ok = mbar_wait(&bars->k_full[(j + 1) % kStages], (uint32_t)((j + 1) / kStages) & 1u, lim);
-        ok = ok && mbar_wait(&bars->p_full[0], ph, lim);
-        if (!ok) break;
-        tc_fence_after();
-        pv(0, j);
-        if (more) qk(0, j + 1);
-        if (nq == 2) {
-          if (aborted(bars) || !mbar_wait(&bars->p_full[1], ph, lim)) { ok = false; break; }
+        return ok;
+      };
+      bool ok = n_tiles == 0 || mbar_wait(&bars->q_full, 0, lim);
+      if (has_q1) {
+        if (ok && n_tiles > 0) {
+          ok = k_ready(0);
+          tc_fence_after();
+          if (ok) {
+            qk(0, 0, 0);
+            qk(1, 1, 0);
+            umma_commit(&bars->k_empty[0]);
+          }
+        }
+        for (int j = 0; ok && j < n_tiles; ++j) {
+          const uint32_t ph = (uint32_t)j & 1u;
+          const bool more = j + 1 < n_tiles;
+          // K of the next tile is awaited with V, while P0 is still being formed
+          ok = v_ready(j) && (!more || k_ready(j + 1)) && mbar_wait(&bars->p_full[0], ph, lim);
+          if (!ok) break;
+          tc_fence_after();
+          pv(0, j);
+          if (more) qk(0, 0, j + 1);
+          ok = !aborted(bars) && mbar_wait(&bars->p_full[1], ph, lim);
+          if (!ok) break;
           tc_fence_after();
           pv(1, j);
+          umma_commit(&bars->v_empty[j % kStages]);
+          if (more) {
+            qk(1, 1, j + 1);
+            umma_commit(&bars->k_empty[(j + 1) % kStages]);
+          }
         }
-        umma_commit(&bars->v_empty[s]);
-        if (more) {
-          if (nq == 2) qk(1, j + 1);
-          umma_commit(&bars->k_empty[(j + 1) % kStages]);
+      } else {
+        // one query tile: warpgroup t has the key tiles t, t + 2, ...
+        static_assert(kStages == 2, "tile j's stage is its warpgroup's");
+        for (int j = 0; ok && j < min(2, n_tiles); ++j) {
+          ok = k_ready(j);
+          if (!ok) break;
+          tc_fence_after();
+          qk(j, 0, j);
+          umma_commit(&bars->k_empty[j]);
+        }
+        for (int j = 0; ok && j < n_tiles; ++j) {
+          const int t = j & 1;
+          const bool more = j + 2 < n_tiles;
+          ok = v_ready(j) && (!more || k_ready(j + 2)) && mbar_wait(&bars->p_full[t], (uint32_t)(j >> 1) & 1u, lim);
+          if (!ok) break;
+          tc_fence_after();
+          pv(t, j);
+          umma_commit(&bars->v_empty[t]);
+          if (more) {
+            qk(t, 0, j + 2);
+            umma_commit(&bars->k_empty[t]);
+          }
         }
       }
       if (!ok) set_abort(bars);
@@ -439,21 +494,75 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     }
   } else if (warp < 12) {
     setmaxnreg_inc<C::REGS_SOFTMAX>();
-    if (warp < 8 || has_q1) {
+    {
       // ------------------------------------------------------------ softmax and result
       const int t = warp < 8 ? 0 : 1;
+      const int qt = has_q1 ? t : 0;         // the query tile of this warpgroup
+      const int every = has_q1 ? 1 : 2;      // its key tiles: t (or 0), and every so many on
       const int q4 = warp & 3;
       const int row = q4 * 32 + lane;
       const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
       const uint32_t colS = t * BN, colO = 256 + t * 128;
       // the row's token and query head, and what it sees: below hi, and below sinks or from lo on
-      const int tok = row / a.group, i = u.i0 + t * a.tile_tokens + tok;
+      const int tok = row / a.group, i = u.i0 + qt * a.tile_tokens + tok;
       const bool live = tok < a.tile_tokens && i < u.n_new;
+      const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
       const int p = u.p0 + i;
       const int hi = !live ? 0 : a.causal ? min(u.hi, max(p + 1, 0)) : u.hi;
       const int lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
       const int sinks = a.window > 0 ? a.sinks : 0;
       float m_ref = -INFINITY, l = 0.f;
+      float unit = a.scale_log2;   // what the row's S is multiplied by (and, with 8-bit pages, by their scales)
+      if constexpr (F8) {
+        // the row as two e4m3 pieces of row * 2^-ex; without a second tile both warpgroups have the row
+        const __nv_bfloat16* src =
+            a.q + (int64_t)(u.t0 + (live ? i : 0)) * a.q_stride + (u.h * a.group + (live ? row - tok * a.group : 0)) * HD;
+        float top = -1.f;
+#pragma unroll 4
+        for (int c = 0; c < HD; c += 8) {
+          float x[8];
+          unpack8(__ldg(reinterpret_cast<const uint4*>(src + c)), x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (fabsf(x[e]) < INFINITY) top = fmaxf(top, fabsf(x[e]));
+        }
+        const int ex = scale_exponent(top);
+        unit *= pow2f(ex);
+        if (qt == t) {
+          const float down = live ? pow2f(-ex) : 0.f;
+          uint8_t* piece = sQ + t * C::Q_BYTES;
+#pragma unroll 2
+          for (int c = 0; c < HD; c += 8) {
+            float x[8], y[8];
+            unpack8(live ? __ldg(reinterpret_cast<const uint4*>(src + c)) : make_uint4(0, 0, 0, 0), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= down;
+            const uint2 w = encode8(x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t two = (e < 2 ? w.x : w.y) >> (16 * (e & 1));
+              const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3));
+              y[2 * e] = x[2 * e] - __low2float(h);
+              y[2 * e + 1] = x[2 * e + 1] - __high2float(h);
+            }
+            const int chunk = c / 16;
+            const int at = (HD == 128 ? row * 128 + ((chunk ^ row) & 7) * 16 : row * 64 + ((chunk ^ (row >> 1)) & 3) * 16) + c % 16;
+            *reinterpret_cast<uint2*>(piece + at) = w;
+            *reinterpret_cast<uint2*>(piece + BM * HD + at) = encode8(y);
+          }
+          fence_proxy_async_smem();
+        }
+        mbar_arrive(&bars->q_full);
+      }
+      // 8-bit pages: lane i has the K scale of page i of a key tile, fetched one tile ahead
+      auto k_scale_of = [&](int j) {
+        if (lane >= BN >> a.page_shift) return 1.f;
+        const int page = page_at(a, u, tile_pos(u, k0 + j) + (lane << a.page_shift));
+        return page < a.n_pages ? __ldg(a.k_scale + (int64_t)page * a.H + u.h) : 1.f;
+      };
+      float ks = 1.f;
+      const int j0 = has_q1 ? 0 : t;
+      if (F8 && j0 < n_tiles) ks = k_scale_of(j0);
       {
         uint32_t zero[32];
 #pragma unroll
@@ -463,8 +572,10 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       bool ok = true;
       uint32_t fixed = 0;
-      for (int j = 0; j < n_tiles; ++j) {
-        bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)j & 1u, lim);
+      for (int j = j0; j < n_tiles; j += every) {
+        const float scales = ks;
+        if (F8 && j + every < n_tiles) ks = k_scale_of(j + every);
+        bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)(has_q1 ? j : j >> 1) & 1u, lim);
         if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
         tc_fence_after();
         uint32_t sr[BN];
@@ -472,6 +583,20 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         tmem_ld_x64(tl + colS + 64, sr + 64);
         const int pos = tile_pos(u, k0 + j);
         const bool whole = all_see(u, pos);
+        float times = unit;
+        if constexpr (F8) {
+          const float f = __shfl_sync(0xffffffffu, scales, 0);
+          if (__all_sync(0xffffffffu, lane >= BN >> a.page_shift || scales == f)) {
+            times *= f;
+          } else {
+#pragma unroll
+            for (int c = 0; c < BN; c += 16) {
+              const float g = __shfl_sync(0xffffffffu, scales, c >> a.page_shift);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) sr[c + e] = __float_as_uint(__uint_as_float(sr[c + e]) * g);
+            }
+          }
+        }
         if (!whole) {
           // columns below hi - pos and (from lo - pos on, or below sinks - pos)
           const int ch = hi - pos, cl = lo - pos, cs = sinks - pos;
@@ -495,7 +620,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             m8[e] = max3(m8[e], __uint_as_float(sr[c + 2 * e]), __uint_as_float(sr[c + 2 * e + 1]));
-        const float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * a.scale_log2;
+        const float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * times;
         const bool need = mx > m_ref + 8.f;
         float corr = 1.f;
         if (need) {
@@ -505,7 +630,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         // a row that has seen nothing: 2^(-inf - 0) = 0
         const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-        const float2 sc2 = make_float2(a.scale_log2, a.scale_log2);
+        const float2 sc2 = make_float2(times, times);
         const float2 nm2 = make_float2(-ref, -ref);
         float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -553,7 +678,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
                 for (int e = 0; e < 32; ++e) {
                   float x;
                   if (F8) {
-                    const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + e), __NV_E4M3));
+                    const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + channel<F8>(e)), __NV_E4M3));
                     x = __half2float(h) * f;
                   } else {
                     x = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v) + at + c + e) << 16);
@@ -574,104 +699,128 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       if (!ok) set_abort(bars);
       tc_fence_after();
-      if (ok && a.n_split == 1) {
+      float* other = reinterpret_cast<float*>(sV);   // [HD][128]: o of the second warpgroup (every product is done)
+      const bool join = a.n_split == 1 && !has_q1;
+      if (join) {
+        if (t == 1 && ok) {
+#pragma unroll
+          for (int half = 0; half < HD / 64; ++half) {
+            uint32_t orr[64];
+            tmem_ld_x64(tl + colO + half * 64, orr);
+#pragma unroll
+            for (int c = 0; c < 64; ++c) other[(half * 64 + c) * 128 + row] = __uint_as_float(orr[c]);
+          }
+          bars->ml[row] = make_float2(m_ref, l);
+        }
+        ok = !bar_sync_or(3, 256, !ok);
+      }
+      if (ok && a.n_split == 1 && qt == t) {
+        float f0 = 1.f, f1 = 0.f;
+        if (join) {
+          const float2 v = bars->ml[row];
+          const float top = fmaxf(m_ref, v.x);
+          f0 = m_ref == -INFINITY ? 0.f : exp2_fast(m_ref - top);
+          f1 = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+          l = f0 * l + f1 * v.y;
+          m_ref = top;
+        }
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
 #pragma unroll
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
-          const float* v = reinterpret_cast<const float*>(orr);
+          float* v = reinterpret_cast<float*>(orr);
+          if (join) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c) v[c] = f0 * v[c] + f1 * other[(half * 64 + c) * 128 + row];
+          }
           if (live && a.o_f32) {
             float* dst = static_cast<float*>(a.o) + out * HD + half * 64;
 #pragma unroll
             for (int c = 0; c < 64; c += 4)
-              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[c + 1] * inv, v[c + 2] * inv, v[c + 3] * inv);
+              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[channel<F8>(c + 1)] * inv,
+                                                                v[channel<F8>(c + 2)] * inv, v[c + 3] * inv);
           } else if (live) {
             __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.o) + out * HD + half * 64;
 #pragma unroll
             for (int c = 0; c < 64; c += 8) {
               float y[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = v[c + e] * inv;
+              for (int e = 0; e < 8; ++e) y[e] = v[channel<F8>(c + e)] * inv;
               *reinterpret_cast<uint4*>(dst + c) = pack8(y);
             }
           }
           __syncwarp();
         }
         if (a.lse && live) a.lse[out] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.69314718055994531f;
-      } else if (ok) {
+      } else if (ok && a.n_split > 1) {
         const int64_t slot = (int64_t)place * a.n_split + part;
 #pragma unroll
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
           const float* v = reinterpret_cast<const float*>(orr);
+          if (live) {
 #pragma unroll
-          for (int c = 0; c < 64; c += 4)
-            __stcg(a.part_o + (slot * (HD / 4) + half * 16 + c / 4) * 256 + t * 128 + row,
-                   make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]));
+            for (int c = 0; c < 64; c += 4)
+              __stcg(a.part_o + (slot * (HD / 4) + half * 16 + c / 4) * 256 + t * 128 + row,
+                     make_float4(v[c], v[channel<F8>(c + 1)], v[channel<F8>(c + 2)], v[c + 3]));
+          }
+          __syncwarp();
         }
-        __stcg(a.part_ml + slot * 256 + t * 128 + row, make_float2(m_ref, l));
+        if (live) __stcg(a.part_ml + slot * 256 + t * 128 + row, make_float2(m_ref, l));
       }
     }
     tc_fence_before();
     end_barrier<C::THREADS>();
   } else if constexpr (F8) {
-    // -------------------------------------------------------------- decoding of raw tiles
+    // -------------------------------------------------------------- V codes to bf16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
     const int tid = threadIdx.x - 384;
     constexpr int CH = HD / 16;   // 16-code chunks of a row
     bool ok = true;
-    for (int j = 0; ok && j < n_tiles; ++j) {
+    for (int j = 0; j < n_tiles; ++j) {
       const int s = j % kStages, pos = tile_pos(u, k0 + j);
       const bool whole = all_see(u, pos);
-#pragma unroll 1
-      for (int kv = 0; kv < 2; ++kv) {
-        bool w = !aborted(bars) && mbar_wait(&bars->raw_full[kv], (uint32_t)j & 1u, lim) &&
-                 mbar_wait(kv ? &bars->v_empty[s] : &bars->k_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
-        // the four warps leave together: they meet at barriers below
-        if (bar_sync_or(2, 128, !w)) { ok = false; break; }
-        const uint8_t* src = sRaw + kv * C::RAW_BYTES;
-        uint8_t* dst = (kv ? sV : sK) + s * C::KV_BYTES;
-        if (kv && !whole) {
-          // V rows that hold NaN, of a tile that the rows do not all see alike (one row a thread)
-          bool bad = false;
-          if (some_see(u, pos + tid))
-            for (int c = 0; c < CH; ++c) bad |= not_finite<true>(*reinterpret_cast<const uint4*>(src + tid * HD + c * 16));
-          const uint32_t apart = __ballot_sync(0xffffffffu, bad);
-          if (lane == 0) bars->apart[s][tid >> 5] = apart;
-          asm volatile("bar.sync 2, 128;" ::: "memory");
-        }
-#pragma unroll 2
-        for (int i = 0; i < CH; ++i) {
-          const int x = tid + 128 * i, r = x / CH, cc = x % CH;
-          const uint4 q = *reinterpret_cast<const uint4*>(src + x * 16);
-          const Factor f = factor_of(bars->scale[kv][r >> a.page_shift]);
-          const uint32_t in[4] = {q.x, q.y, q.z, q.w};
-          uint32_t out[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t even, odd;
-            decode4(in[e], f, even, odd);
-            out[2 * e] = __byte_perm(even, odd, 0x5410);
-            out[2 * e + 1] = __byte_perm(even, odd, 0x7632);
-          }
-          if (kv && !whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[e] = 0u;
-          // two 16-byte chunks of the bf16 row; the second 64-channel box's lanes write theirs in
-          // the other order, so that eight lanes take eight bank groups
-          uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
-          const int c0 = 2 * (cc & 3), swap = (cc >> 2) & 1;
-          const uint4 lo4 = make_uint4(out[0], out[1], out[2], out[3]), hi4 = make_uint4(out[4], out[5], out[6], out[7]);
-          *reinterpret_cast<uint4*>(base + (((c0 + swap) ^ r) & 7) * 16) = swap ? hi4 : lo4;
-          *reinterpret_cast<uint4*>(base + (((c0 + 1 - swap) ^ r) & 7) * 16) = swap ? lo4 : hi4;
-        }
-        fence_proxy_async_smem();
-        mbar_arrive(kv ? &bars->v_full[s] : &bars->k_full[s]);
-        mbar_arrive(&bars->raw_empty[kv]);
+      const uint32_t ph = (uint32_t)(j / kStages) & 1u;
+      const bool w = !aborted(bars) && mbar_wait(&bars->raw_full[s], ph, lim) && mbar_wait(&bars->v_empty[s], ph ^ 1u, lim);
+      // the four warps leave together: they meet at barriers below
+      if (bar_sync_or(2, 128, !w)) { ok = false; break; }
+      const uint8_t* src = sRaw + s * C::RAW_BYTES;
+      uint8_t* dst = sV + s * C::V_BYTES;
+      if (!whole) {
+        // rows that hold NaN, of a tile that the unit's rows do not all see alike (one row a thread)
+        bool bad = false;
+        if (some_see(u, pos + tid))
+          for (int c = 0; c < CH; ++c) bad |= not_finite<true>(*reinterpret_cast<const uint4*>(src + tid * HD + c * 16));
+        const uint32_t apart = __ballot_sync(0xffffffffu, bad);
+        if (lane == 0) bars->apart[s][tid >> 5] = apart;
+        asm volatile("bar.sync 2, 128;" ::: "memory");
       }
+#pragma unroll 4
+      for (int i = 0; i < CH; ++i) {
+        const int x = tid + 128 * i, r = x / CH, cc = x % CH;
+        const uint4 q = *reinterpret_cast<const uint4*>(src + x * 16);
+        const Factor f = factor_of(bars->scale[s][r >> a.page_shift]);
+        uint32_t o[8];
+        decode4(q.x, f, o[0], o[1]);
+        decode4(q.y, f, o[2], o[3]);
+        decode4(q.z, f, o[4], o[5]);
+        decode4(q.w, f, o[6], o[7]);
+        if (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = 0u;
+        // two 16-byte chunks of the bf16 row; the lanes of the second 64 channels write theirs in the
+        // other order, so that eight lanes take eight bank groups
+        uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
+        const int c0 = 2 * (cc & 3), swap = (cc >> 2) & 1;
+        const uint4 lo4 = make_uint4(o[0], o[1], o[2], o[3]), hi4 = make_uint4(o[4], o[5], o[6], o[7]);
+        *reinterpret_cast<uint4*>(base + (((c0 + swap) ^ r) & 7) * 16) = swap ? hi4 : lo4;
+        *reinterpret_cast<uint4*>(base + (((c0 + 1 - swap) ^ r) & 7) * 16) = swap ? lo4 : hi4;
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(&bars->v_full[s]);
+      mbar_arrive(&bars->raw_empty[s]);
     }
     if (!ok) set_abort(bars);
     end_barrier<C::THREADS>();
@@ -693,22 +842,28 @@ __global__ void __launch_bounds__(256) k_tiles_merge(const __grid_constant__ Til
   const int row = blockIdx.y * 32 + (threadIdx.x & 31);   // of the unit's 256
   const int t = row >> 7, tok = (row & 127) / a.group, i = u.i0 + t * a.tile_tokens + tok;
   if (tok >= a.tile_tokens || i >= u.n_new) return;
-  const int64_t slot = (int64_t)blockIdx.x * a.n_split;
+  // a unit of one tile has two places of each row in a part
+  const bool pair = u.i0 + a.tile_tokens < u.n_new;
+  const int n = pair ? a.n_split : 2 * a.n_split;
+  const int64_t slot0 = (int64_t)blockIdx.x * a.n_split;
+  auto slot = [&](int p) { return pair ? slot0 + p : slot0 + (p >> 1); };
+  auto place = [&](int p) { return pair ? row : row + (p & 1) * 128; };
   float top = -INFINITY;
-  for (int p = 0; p < a.n_split; ++p) top = fmaxf(top, a.part_ml[(slot + p) * 256 + row].x);
+  for (int p = 0; p < n; ++p) top = fmaxf(top, a.part_ml[slot(p) * 256 + place(p)].x);
   float l = 0.f;
-  for (int p = 0; p < a.n_split; ++p) {
-    const float2 v = a.part_ml[(slot + p) * 256 + row];
+  for (int p = 0; p < n; ++p) {
+    const float2 v = a.part_ml[slot(p) * 256 + place(p)];
     l += v.x == -INFINITY ? 0.f : exp2_fast(v.x - top) * v.y;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + ((row & 127) - tok * a.group);
   for (int c = threadIdx.x >> 5; c < HD / 4; c += 8) {
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p = 0; p < a.n_split; ++p) {
-      const float m = a.part_ml[(slot + p) * 256 + row].x;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float m = a.part_ml[slot(p) * 256 + place(p)].x;
       const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
-      const float4 y = a.part_o[((slot + p) * (HD / 4) + c) * 256 + row];
+      const float4 y = a.part_o[(slot(p) * (HD / 4) + c) * 256 + place(p)];
       acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
     }
     if (a.o_f32) {
@@ -723,13 +878,12 @@ __global__ void __launch_bounds__(256) k_tiles_merge(const __grid_constant__ Til
 }
 
 // ---------------------------------------------------------------- host side
-bool encode(CUtensorMap* m, bool bytes, const void* base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
-            const cuuint32_t (&box)[3]) {
+bool encode(CUtensorMap* m, int elt, CUtensorMapSwizzle swizzle, const void* base, const cuuint64_t (&dims)[3],
+            const cuuint64_t (&strides)[2], const cuuint32_t (&box)[3]) {
   EncodeTiledFn fn = tensor_map_encoder();
   const cuuint32_t es[3] = {1, 1, 1};
-  return fn && fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
-                  strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  bytes ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  return fn && fn(m, elt == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base),
+                  dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -738,14 +892,21 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   using C = Cfg<HD, F8>;
   const cast_kv_cache& c = a.cache;
   CUtensorMap mq, mk, mv;
-  const cuuint64_t elt = F8 ? 1 : 2;
-  const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
-  const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
+  constexpr int elt = F8 ? 1 : 2;
   const cuuint64_t kd[3] = {(cuuint64_t)c.H * HD, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
   const cuuint64_t ks[2] = {(cuuint64_t)c.row_stride * elt, (cuuint64_t)c.row_stride * elt * c.page_size};
   const cuuint32_t kb[3] = {F8 ? HD : 64, (cuuint32_t)c.page_size, 1};
-  if (!encode(&mq, false, a.q, qd, qs, qb) || !encode(&mk, F8, c.k, kd, ks, kb) || !encode(&mv, F8, c.v, kd, ks, kb))
-    return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
+  // operand tiles are swizzled by their rows' 128 (or 64) bytes; V codes pass through registers
+  const CUtensorMapSwizzle operand = F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+  bool ok = encode(&mk, elt, operand, c.k, kd, ks, kb) && encode(&mv, elt, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : operand, c.v, kd, ks, kb);
+  if (F8) {
+    mq = mk;   // queries are read and split by the kernel
+  } else if (ok) {
+    const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
+    const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
+    ok = encode(&mq, 2, CU_TENSOR_MAP_SWIZZLE_128B, a.q, qd, qs, qb);
+  }
+  if (!ok) return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
   static std::atomic<uint64_t> attr_done{0};
   cast_status setup = CAST_OK;
   if (!once_per_device(attr_done, [&] {
@@ -800,13 +961,14 @@ TilesPlan tiles_plan(const cast_cache_attn_args& a) {
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
   if (nsm < 1) nsm = 1;
   // The split with the least estimated time: rounds of one CTA an SM, each as long as its part's tiles
-  // (about 1.7 us each) and a fixed 4 us, and for a split the parts written and read again and the
-  // second launch.
+  // (about 1.7 us each, 0.9 for units of one tile) and a fixed 4 us, and for a split the parts written
+  // and read again and the second launch.
+  const double tile_us = max_new <= p.tile_tokens ? 0.9 : 1.7;
   double best = 0;
   p.n_split = 1;
-  for (int n = 1; n <= 16 && (n == 1 || tiles / n >= 2); ++n) {
+  for (int n = 1; n <= 64 && (n == 1 || tiles / n >= 2); ++n) {
     const double rounds = (double)((units * n + nsm - 1) / nsm);
-    double us = rounds * ((double)((tiles + n - 1) / n) * 1.7 + 4.0);
+    double us = rounds * ((double)((tiles + n - 1) / n) * tile_us + 4.0);
     if (n > 1) us += 4.0 + (double)(units * n) * 256 * d * 4 * 2 / 4e6;
     if (n == 1 || us < best) {
       best = us;
@@ -838,7 +1000,8 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.sinks = k.window > 0 ? a.sinks : 0;
   k.o_f32 = a.o_dtype == CAST_F32;
   k.row_stride = c.row_stride;
-  k.k = static_cast<const uint8_t*>(c.k);
+  k.q = static_cast<const __nv_bfloat16*>(a.q);
+  k.q_stride = a.q_row_stride;
   k.v = static_cast<const uint8_t*>(c.v);
   k.k_scale = c.k_scale;
   k.v_scale = c.v_scale;
