@@ -635,6 +635,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
                 uint32_t e0, e1, d0, d1;
                 decode4(w[2 * j], f, e0, d0);
                 decode4(w[2 * j + 1], f, e1, d1);
+                fix_nan(w[2 * j], e0, d0);
+                fix_nan(w[2 * j + 1], e1, d1);
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                   // o is indexed by constants only

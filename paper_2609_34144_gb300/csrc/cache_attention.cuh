@@ -36,7 +36,9 @@ __device__ __forceinline__ Factor factor_of(float scale) {
   f.twice = pack2(scale, scale);
   return f;
 }
-// Codes 0, 2 (even) and 1, 3 (odd) of a word as bf16 pairs
+// Codes 0, 2 (even) and 1, 3 (odd) of a word as bf16 pairs: a code's exponent and mantissa moved to
+// bf16's fields are code * 2^-120, a subnormal code included.  The format's NaN (seven bits set) comes
+// out as 480: see fix_nan.
 __device__ __forceinline__ void decode4(uint32_t w, const Factor& f, uint32_t& even, uint32_t& odd) {
   even = ((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u);
   odd = ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
@@ -46,15 +48,27 @@ __device__ __forceinline__ void decode4(uint32_t w, const Factor& f, uint32_t& e
     even = mul2(even, f.twice);
     odd = mul2(odd, f.twice);
   }
-  // the format's NaN (all seven bits set): the fields above make 480 of it
-  if ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u) {
-    if ((w & 0x0000007fu) == 0x0000007fu) even |= 0x00007fffu;
-    if ((w & 0x00007f00u) == 0x00007f00u) odd |= 0x00007fffu;
-    if ((w & 0x007f0000u) == 0x007f0000u) even |= 0x7fff0000u;
-    if ((w & 0x7f000000u) == 0x7f000000u) odd |= 0x7fff0000u;
+}
+__device__ __forceinline__ uint32_t nan_bits(uint32_t w) { return (w & 0x7f7f7f7fu) + 0x01010101u; }
+__device__ __forceinline__ void fix_nan(uint32_t w, uint32_t& even, uint32_t& odd) {
+  if ((w & 0x0000007fu) == 0x0000007fu) even |= 0x00007fffu;
+  if ((w & 0x00007f00u) == 0x00007f00u) odd |= 0x00007fffu;
+  if ((w & 0x007f0000u) == 0x007f0000u) even |= 0x7fff0000u;
+  if ((w & 0x7f000000u) == 0x7f000000u) odd |= 0x7fff0000u;
+}
+// 16 codes, NaN included, with four consecutive ones in the order 0, 2, 1, 3
+__device__ __forceinline__ void decode16(uint2 a, uint2 b, const Factor& f, uint4& oa, uint4& ob) {
+  decode4(a.x, f, oa.x, oa.y);
+  decode4(a.y, f, oa.z, oa.w);
+  decode4(b.x, f, ob.x, ob.y);
+  decode4(b.y, f, ob.z, ob.w);
+  if (((nan_bits(a.x) | nan_bits(a.y) | nan_bits(b.x) | nan_bits(b.y)) & 0x80808080u) != 0u) {
+    fix_nan(a.x, oa.x, oa.y);
+    fix_nan(a.y, oa.z, oa.w);
+    fix_nan(b.x, ob.x, ob.y);
+    fix_nan(b.y, ob.z, ob.w);
   }
 }
-
 // Whether a 16-byte chunk of V holds a value that is not finite
 template <bool F8>
 __device__ __forceinline__ bool not_finite(const uint4& x) {

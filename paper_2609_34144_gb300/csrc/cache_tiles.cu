@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     fence_barrier_init();
   }
   __syncthreads();
-  const Unit u = bars->unit;
+  const Unit& u = bars->unit;   // read from shared memory where it is needed: registers are short
   if (!u.valid) return;
   if (warp == 1) {
     tmem_alloc(&bars->tmem_base, kTmemCols);
@@ -506,7 +506,6 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       // the row's token and query head, and what it sees: below hi, and below sinks or from lo on
       const int tok = row / a.group, i = u.i0 + qt * a.tile_tokens + tok;
       const bool live = tok < a.tile_tokens && i < u.n_new;
-      const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
       const int p = u.p0 + i;
       const int hi = !live ? 0 : a.causal ? min(u.hi, max(p + 1, 0)) : u.hi;
       const int lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
@@ -583,20 +582,6 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         tmem_ld_x64(tl + colS + 64, sr + 64);
         const int pos = tile_pos(u, k0 + j);
         const bool whole = all_see(u, pos);
-        float times = unit;
-        if constexpr (F8) {
-          const float f = __shfl_sync(0xffffffffu, scales, 0);
-          if (__all_sync(0xffffffffu, lane >= BN >> a.page_shift || scales == f)) {
-            times *= f;
-          } else {
-#pragma unroll
-            for (int c = 0; c < BN; c += 16) {
-              const float g = __shfl_sync(0xffffffffu, scales, c >> a.page_shift);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) sr[c + e] = __float_as_uint(__uint_as_float(sr[c + e]) * g);
-            }
-          }
-        }
         if (!whole) {
           // columns below hi - pos and (from lo - pos on, or below sinks - pos)
           const int ch = hi - pos, cl = lo - pos, cs = sinks - pos;
@@ -612,15 +597,30 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
               if (!((see >> c) & 1u)) sr[32 * b + c] = __float_as_uint(-INFINITY);
           }
         }
-        float m8[8];
+        // logits are S times `by` (16 columns at a time: no page is smaller); their maximum, four chains
+        float by[BN / 16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m8[e] = fmaxf(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1]));
+        for (int c = 0; c < BN / 16; ++c) by[c] = F8 ? unit * __shfl_sync(0xffffffffu, scales, (16 * c) >> a.page_shift) : unit;
+        float mx = -INFINITY;
+        if constexpr (F8) {
 #pragma unroll
-        for (int c = 16; c < BN; c += 16)
+          for (int c = 0; c < BN; c += 16) {
+            auto x = [&](int e) { return __uint_as_float(sr[c + e]); };
+            const float m0 = max3(max3(x(0), x(1), x(2)), x(3), x(4)), m1 = max3(max3(x(5), x(6), x(7)), x(8), x(9));
+            const float m2 = max3(max3(x(10), x(11), x(12)), x(13), x(14));
+            mx = fmaxf(mx, max3(m0, m1, fmaxf(m2, x(15))) * by[c / 16]);
+          }
+        } else {
+          float m8[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            m8[e] = max3(m8[e], __uint_as_float(sr[c + 2 * e]), __uint_as_float(sr[c + 2 * e + 1]));
-        const float mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * times;
+          for (int e = 0; e < 8; ++e) m8[e] = fmaxf(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1]));
+#pragma unroll
+          for (int c = 16; c < BN; c += 16)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              m8[e] = max3(m8[e], __uint_as_float(sr[c + 2 * e]), __uint_as_float(sr[c + 2 * e + 1]));
+          mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * unit;
+        }
         const bool need = mx > m_ref + 8.f;
         float corr = 1.f;
         if (need) {
@@ -630,11 +630,11 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         // a row that has seen nothing: 2^(-inf - 0) = 0
         const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-        const float2 sc2 = make_float2(times, times);
         const float2 nm2 = make_float2(-ref, -ref);
         float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int c = 0; c < BN; c += 2) {
+          const float2 sc2 = make_float2(by[c / 16], by[c / 16]);
           const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), sc2, nm2);
           const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
           s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], e);
@@ -715,6 +715,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         ok = !bar_sync_or(3, 256, !ok);
       }
       if (ok && a.n_split == 1 && qt == t) {
+        const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
         float f0 = 1.f, f1 = 0.f;
         if (join) {
           const float2 v = bars->ml[row];
@@ -800,23 +801,20 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll 4
       for (int i = 0; i < CH; ++i) {
         const int x = tid + 128 * i, r = x / CH, cc = x % CH;
-        const uint4 q = *reinterpret_cast<const uint4*>(src + x * 16);
+        // 16 codes are two 16-byte chunks of the bf16 row; the lanes of the second 64 channels take
+        // theirs in the other order, so that eight lanes store to eight bank groups
+        const int swap = (cc >> 2) & 1;
+        const uint2 w0 = *reinterpret_cast<const uint2*>(src + x * 16 + swap * 8);
+        const uint2 w1 = *reinterpret_cast<const uint2*>(src + x * 16 + (swap ^ 1) * 8);
         const Factor f = factor_of(bars->scale[s][r >> a.page_shift]);
-        uint32_t o[8];
-        decode4(q.x, f, o[0], o[1]);
-        decode4(q.y, f, o[2], o[3]);
-        decode4(q.z, f, o[4], o[5]);
-        decode4(q.w, f, o[6], o[7]);
+        uint4 o0, o1;
+        decode16(w0, w1, f, o0, o1);
         if (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = 0u;
-        // two 16-byte chunks of the bf16 row; the lanes of the second 64 channels write theirs in the
-        // other order, so that eight lanes take eight bank groups
+          o0 = o1 = make_uint4(0, 0, 0, 0);
         uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
-        const int c0 = 2 * (cc & 3), swap = (cc >> 2) & 1;
-        const uint4 lo4 = make_uint4(o[0], o[1], o[2], o[3]), hi4 = make_uint4(o[4], o[5], o[6], o[7]);
-        *reinterpret_cast<uint4*>(base + (((c0 + swap) ^ r) & 7) * 16) = swap ? hi4 : lo4;
-        *reinterpret_cast<uint4*>(base + (((c0 + 1 - swap) ^ r) & 7) * 16) = swap ? lo4 : hi4;
+        const int c0 = 2 * (cc & 3) + swap;
+        *reinterpret_cast<uint4*>(base + ((c0 ^ r) & 7) * 16) = o0;
+        *reinterpret_cast<uint4*>(base + ((c0 ^ 1 ^ r) & 7) * 16) = o1;
       }
       fence_proxy_async_smem();
       mbar_arrive(&bars->v_full[s]);
