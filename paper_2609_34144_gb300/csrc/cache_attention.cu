@@ -17,12 +17,11 @@
 //
 // 8-bit rows: codes become f16 (one conversion for two, exact) on the way from shared memory to the
 // products, and the scales stay outside: a page's K scale multiplies its logits, and o is kept in
-// units of the largest V scale so far, R, so that a page's probabilities are multiplied by its scale / R
-// (a page whose scale is below 2^-10 R is decoded to bf16 instead, whose range holds the quotient).
-// Queries are f16 too, each row times the power of two that brings its largest channel below 2^15:
-// bf16's eight bits fit, and channels 2^30 below the largest are the first to lose one.  The order of
-// channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the codes lie in
-// their 32-bit words.
+// units of the largest V scale so far over 2^7, a page's probabilities (f16) carrying its scale in those
+// units in their exponent.  Queries are f16 too, each row times the power of two that brings its largest
+// channel below 2^15: bf16's eight bits fit, and channels 2^30 below the largest are the first to lose
+// one.  The order of channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the
+// codes lie in their 32-bit words.
 // Bound: memory for bf16 pages, instructions for 8-bit ones (427 a block of 16 tokens, 2.1 a clock and
 // SM, against the 360 clocks that its 4 KB take at the copy rate).  Measured, GB300: 48 sequences with
 // windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB) 141 us, 5.9 TB/s; 24 sequences
@@ -39,9 +38,8 @@ namespace cast {
 namespace {
 
 constexpr float kRescale = 8.f;   // the running maximum is renewed when a logit exceeds it by 2^8
-// Probabilities are at most 2^8 times a row's largest; as f16, 2^7 keeps them below 2^16 and the small
-// ones far above its subnormals
-constexpr float kLift = 128.f;
+// 8-bit pages: probabilities, at most 2^8 times a row's largest, are lifted by 2^7 to use f16's range
+constexpr float kLift = 7.f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kWarps = 4;
 
@@ -135,12 +133,6 @@ __device__ __forceinline__ void mma16816h(float* c, const uint32_t* a, uint32_t 
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Codes in the low and the high half of a word as f16 pairs
-__device__ __forceinline__ void half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\t"
-      "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
-      : "=r"(lo), "=r"(hi) : "r"(w));
-}
 __device__ __forceinline__ uint32_t pack2h(float a, float b) {
   const __half2 x = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&x);
@@ -175,13 +167,13 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
   return r * ROWB + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
-// Channel c of row r of a V block
+// Channel c of row r of a V block (8 bits: the code's value)
 template <bool F8, int ROWB>
-__device__ __forceinline__ float value_at(const uint8_t* block, int r, int c, float scale) {
+__device__ __forceinline__ float value_at(const uint8_t* block, int r, int c) {
   const uint8_t* p = block + chunk_at<ROWB>(r, c * (F8 ? 1 : 2) / 16) + c * (F8 ? 1 : 2) % 16;
   if constexpr (F8) {
     const __half h(__nv_cvt_fp8_to_halfraw(*p, __NV_E4M3));
-    return __half2float(h) * scale;
+    return __half2float(h);
   }
   return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
 }
@@ -356,7 +348,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       }
 
       float o[MT][D / 8][4], m_ref[MT][2], l[MT][2];
-      float v_unit = 0.f, v_lift = 0.f;   // 8-bit pages: o is in units of v_unit / kLift = 1 / v_lift
+      float e_ref = -INFINITY;   // 8-bit pages: o is in units of 2^(e_ref - kLift)
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -519,28 +511,23 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
               }
             }
         }
-        // 8-bit pages: probabilities carry the page's V scale in o's units (`weight`, by the exponent)
-        float weight = 1.f, shift = 0.f, back = 1.f;
-        bool by_f16 = false;
+        // 8-bit pages: probabilities carry the page's V scale in o's units; a scale 2^60 below the largest
+        // adds nothing to o, and everything to the sum
+        float weight = 0.f, back = 1.f;   // log2, and its inverse for the sum
         if constexpr (F8) {
-          if (sc.y > v_unit) {
-            // a larger scale: o in units of it (o is 0 before the first)
-            const float f = v_unit / sc.y;
-            v_unit = sc.y;
-            v_lift = kLift / sc.y;
+          const float e = __log2f(sc.y);
+          if (e > e_ref) {
+            const float f = exp2_fast(e_ref - e);
+            e_ref = e;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
               for (int t = 0; t < D / 8; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[m][t][e] *= f;
+                for (int k = 0; k < 4; ++k) o[m][t][k] *= f;
           }
-          weight = sc.y * v_lift;
-          by_f16 = weight >= kLift * 0x1p-10f;
-          if (by_f16) {
-            shift = __log2f(weight);
-            back = __frcp_rn(weight);
-          }
+          weight = kLift + fmaxf(e - e_ref, -60.f);
+          back = exp2_fast(-weight);
         }
         uint32_t pf[MT][4];
 #pragma unroll
@@ -548,7 +535,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             // a row that has seen nothing yet: exp2(-inf - 0) = 0
-            const float ref = shift - (m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j]);
+            const float ref = weight - (m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j]);
             float sum = 0.f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -565,7 +552,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const float x = s[m][t][2 * j], y = s[m][t][2 * j + 1];
-              pf[m][2 * t + j] = by_f16 ? pack2h(x, y) : pack2(x, y);
+              pf[m][2 * t + j] = F8 ? pack2h(x, y) : pack2(x, y);
             }
         }
         // A block that the rows do not all see, with a value that is not finite: 0 times it would
@@ -601,51 +588,25 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
                     const int n = F8 ? (c >> 1) * 16 + 2 * (q4 * 2 + e) + (c & 1) : c * 8 + q4 * 2 + e;
-                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n, by_f16 ? 1.f : weight);
+                    o[m][c][2 * j + e] += w * value_at<F8, C::ROWB>(ring + st * 2 * C::BLOCK + C::BLOCK, t, n);
                   }
               }
           }
         } else if constexpr (F8) {
           // words of V hold tokens 2 q4 and 2 q4 + 1 of channels 2 g and 2 g + 1
-          if (by_f16) {
 #pragma unroll
-            for (int c = 0; c < D / 16; c += 2) {
-              uint32_t w[4];
-              ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
+          for (int c = 0; c < D / 16; c += 2) {
+            uint32_t w[4];
+            ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                uint32_t e0, e1, d0, d1;
-                half4(__byte_perm(w[2 * j], 0, 0x3120), e0, d0);
-                half4(__byte_perm(w[2 * j + 1], 0, 0x3120), e1, d1);
+            for (int j = 0; j < 2; ++j) {
+              uint32_t e0, e1, d0, d1;
+              half4(__byte_perm(w[2 * j], 0, 0x3120), e0, d0);
+              half4(__byte_perm(w[2 * j + 1], 0, 0x3120), e1, d1);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                  mma16816h(o[m][2 * (c + j)], pf[m], e0, e1);
-                  mma16816h(o[m][2 * (c + j) + 1], pf[m], d0, d1);
-                }
-              }
-            }
-          } else {
-            const Factor f = factor_of(weight);
-#pragma unroll 1
-            for (int c = 0; c < D / 16; c += 2) {
-              uint32_t w[4];
-              ldsm4t(vt + chunk_at<C::ROWB>(((lane >> 3) & 1) * 8 + (lane & 7), c + (lane >> 4)), w);
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                uint32_t e0, e1, d0, d1;
-                decode4(w[2 * j], f, e0, d0);
-                decode4(w[2 * j + 1], f, e1, d1);
-                fix_nan(w[2 * j], e0, d0);
-                fix_nan(w[2 * j + 1], e1, d1);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-                  // o is indexed by constants only
-#pragma unroll
-                  for (int k = 0; k < D / 16; k += 2)
-                    if (k == c) {
-                      mma16816(o[m][2 * (k + j)], pf[m], e0, e1);
-                      mma16816(o[m][2 * (k + j) + 1], pf[m], d0, d1);
-                    }
+              for (int m = 0; m < MT; ++m) {
+                mma16816h(o[m][2 * (c + j)], pf[m], e0, e1);
+                mma16816h(o[m][2 * (c + j) + 1], pf[m], d0, d1);
               }
             }
           }
@@ -682,7 +643,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
           if (q4 == 0) ml[warp * C::ROWS + r] = make_float2(m_ref[m][j], x);
           float* dst = mo + (warp * C::ROWS + r) * D;
           if constexpr (F8) {
-            const float f = v_unit / kLift;
+            const float f = exp2_fast(e_ref) * 0x1p-7f;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
               *reinterpret_cast<float4*>(dst + c * 16 + q4 * 4) =

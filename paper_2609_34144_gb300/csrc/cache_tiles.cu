@@ -22,9 +22,10 @@
 // 8-bit pages: K is multiplied as it lies, in the 8-bit form of the products.  A bf16 query is the sum of
 // two e4m3 numbers, exactly: times the power of two that brings its row's largest channel to 448 at
 // most, its first four bits and the rest are one each (channels 2^10 below the largest keep 2^-19 of
-// it).  So S is the sum of two products at twice the rate, and each page's scale multiplies its columns of S.
-// V is decoded to bf16 tiles (exactly: the scales are powers of two) by a fourth warpgroup, with the
-// zeroing on the way; four channels of a word take the places 0, 2, 1, 3, which o's columns inherit.
+// it).  So S is the sum of two products at twice the rate, and each page's scale multiplies its columns
+// of S.  V codes become f16 tiles (one conversion for two, by a fourth warpgroup, with the zeroing on the
+// way) and P is f16: o is kept in units of the largest V scale so far over 2^7, and a page's probabilities
+// carry its scale in those units in their exponent.
 //
 // A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
 // warpgroup and odd ones to the other, each with its own S, o, maximum and sum, so that the products of one
@@ -41,6 +42,8 @@ namespace {
 __device__ unsigned int g_tiles_error;
 
 constexpr int BM = 128, BN = 128, kStages = 2;
+// 8-bit pages: probabilities, at most 2^8 times a row's largest, are lifted by 2^7 to use f16's range
+constexpr float kLift = 7.f;
 constexpr int kTmemCols = 512;   // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
 
 template <int HD, bool F8>
@@ -48,9 +51,9 @@ struct Cfg {
   static constexpr int THREADS = F8 ? 512 : 384;
   // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
   static constexpr int LAUNCH = F8 ? 128 : 168;
-  static constexpr int REGS_CTL = F8 ? 56 : 96;
-  static constexpr int REGS_SOFTMAX = F8 ? 192 : 200;
-  static constexpr int REGS_DECODE = 72;
+  static constexpr int REGS_CTL = 96;
+  static constexpr int REGS_SOFTMAX = F8 ? 176 : 200;
+  static constexpr int REGS_DECODE = 64;
   static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
                 "register split exceeds the launch allocation");
   static constexpr int Q_BYTES = BM * HD * 2;               // 8 bits: two pieces of BM * HD
@@ -180,7 +183,6 @@ struct Bars {
   uint32_t tmem_base;
   int abort;
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
-  float scale[kStages][8];             // V codes: scales of the tile's pages
   float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
   Unit unit;
 };
@@ -196,11 +198,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// The channel that place c of o's columns holds (8-bit pages: see above)
-template <bool F8>
-__host__ __device__ constexpr int channel(int c) {
-  return F8 ? (c & ~3) | ((c & 1) << 1) | ((c >> 1) & 1) : c;
-}
 template <int N>
 __device__ __forceinline__ void end_barrier() {
   asm volatile("barrier.sync 1, %0;" ::"n"(N) : "memory");
@@ -211,6 +208,11 @@ __device__ __forceinline__ bool aborted(const Bars* b) {
 __device__ __forceinline__ void set_abort(Bars* b) {
   atomicExch(&b->abort, 1);
   atomicExch(&g_tiles_error, 1u);
+}
+__device__ __forceinline__ uint64_t join(uint32_t low, uint32_t high) {
+  uint64_t x;
+  asm volatile("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(low), "r"(high));
+  return x;
 }
 __device__ __forceinline__ uint32_t tmem_ld_1(uint32_t taddr) {
   uint32_t r;
@@ -230,16 +232,12 @@ __device__ __forceinline__ int page_at(const TilesKArgs& a, const Unit& u, int p
 }
 
 // Fetches the pages of a K or V tile at `pos` (one warp; lane i < 128 / page_size has page i).  ROWB: bytes
-// of a row; CODES: the tile is 8-bit.  With `scale` lane i also leaves the page's scale there.
+// of a row; CODES: the tile is 8-bit.
 template <int ROWB, bool CODES>
 __device__ __forceinline__ void fetch_pages(const TilesKArgs& a, const Unit& u, const CUtensorMap* map, uint8_t* dst,
-                                            uint64_t* full, float* scale, const float* scales, int pos, int lane) {
+                                            uint64_t* full, int pos, int lane) {
   const int n = BN >> a.page_shift;
-  int page = a.n_pages;
-  if (lane < n) {
-    page = page_at(a, u, pos + (lane << a.page_shift));
-    if (scale) scale[lane] = page < a.n_pages ? __ldg(scales + (int64_t)page * a.H + u.h) : 1.f;
-  }
+  const int page = lane < n ? page_at(a, u, pos + (lane << a.page_shift)) : 0;
   __syncwarp();
   if (lane == 0) mbar_arrive_expect_tx(full, BN * ROWB);
   __syncwarp();
@@ -340,8 +338,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         bool ok = mbar_wait(&empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
         ok = !aborted(bars) && ok;
         if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
-        fetch_pages<HD * (F8 ? 1 : 2), F8>(a, u, map, dst + s * bytes, &full[s], codes ? bars->scale[s] : nullptr, a.v_scale,
-                                           tile_pos(u, k0 + j), lane);
+        fetch_pages<HD * (F8 ? 1 : 2), F8>(a, u, map, dst + s * bytes, &full[s], tile_pos(u, k0 + j), lane);
       }
     } else if (warp == 3 && !F8) {
       // ------------------------------------------------------------ V of tiles that not all rows see
@@ -382,39 +379,44 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     } else if (warp == 1 && lane == 0) {
       // ------------------------------------------------------------ products
       constexpr uint32_t idesc_qk = F8 ? idesc_e4m3_f32(BM, BN) : idesc_bf16_f32(BM, BN, false, false);
-      constexpr uint32_t idesc_pv = idesc_bf16_f32(BM, HD, false, true);
+      constexpr uint32_t idesc_pv = F8 ? idesc_f16_f32(BM, HD, false, true) : idesc_bf16_f32(BM, HD, false, true);
       // a k-slice, query tile or stage further on adds its byte offset / 16 to the start address
       static_assert(C::SMEM + 1024 <= 256 * 1024, "descriptor start-address field would carry");
       constexpr bool kNarrow = F8 && HD == 64;   // 64-byte rows
+      // descriptors as their low words (the start address / 16 and the leading offset); the high ones are
+      // the same for a kind of operand
       const uint64_t dq = kNarrow ? sdesc_sw64(smem_u32(sQ), 16, 512) : sdesc_sw128(smem_u32(sQ), 16, 1024);
       const uint64_t dk = kNarrow ? sdesc_sw64(smem_u32(sK), 16, 512) : sdesc_sw128(smem_u32(sK), 16, 1024);
       const uint64_t dv = sdesc_sw128(smem_u32(sV), BN * 128, 1024);
+      const uint32_t ql = (uint32_t)dq, kl = (uint32_t)dk, vl = (uint32_t)dv;
+      constexpr uint32_t kHigh = kNarrow ? (uint32_t)(512 >> 4) | (1u << 14) | (4u << 29) : (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);
+      constexpr uint32_t kHighV = (uint32_t)(1024 >> 4) | (1u << 14) | (2u << 29);
       // S_t = Q_q K_j^T
       auto qk = [&](int t, int q, int j) {
-        const uint64_t aq = dq + (uint64_t)((q * C::Q_BYTES) >> 4);
-        const uint64_t bk = dk + (uint64_t)(((j % kStages) * C::K_BYTES) >> 4);
+        const uint32_t aq = ql + (uint32_t)((q * C::Q_BYTES) >> 4);
+        const uint32_t bk = kl + (uint32_t)(((j % kStages) * C::K_BYTES) >> 4);
         if constexpr (F8) {
 #pragma unroll
           for (int piece = 0; piece < 2; ++piece)
 #pragma unroll
             for (int kk = 0; kk < HD / 32; ++kk)
-              umma_f8_ss(tmem + t * BN, aq + (uint64_t)((piece * BM * HD + kk * 32) >> 4), bk + (uint64_t)((kk * 32) >> 4),
+              umma_f8_ss(tmem + t * BN, join(aq + ((piece * BM * HD + kk * 32) >> 4), kHigh), join(bk + ((kk * 32) >> 4), kHigh),
                          idesc_qk, piece + kk > 0 ? 1u : 0u);
         } else {
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk) {
-            const uint64_t off = (uint64_t)(((kk >> 2) * (BM * 128) + (kk & 3) * 32) >> 4);
-            umma_bf16_ss(tmem + t * BN, aq + off, bk + off, idesc_qk, kk > 0 ? 1u : 0u);
+            const uint32_t off = ((kk >> 2) * (BM * 128) + (kk & 3) * 32) >> 4;
+            umma_bf16_ss(tmem + t * BN, join(aq + off, kHigh), join(bk + off, kHigh), idesc_qk, kk > 0 ? 1u : 0u);
           }
         }
         umma_commit(&bars->s_full[t]);
       };
       // o is zeroed by the softmax threads before the first P, so it always accumulates
       auto pv = [&](int t, int j) {
-        const uint64_t bv = dv + (uint64_t)(((j % kStages) * C::V_BYTES) >> 4);
+        const uint32_t bv = vl + (uint32_t)(((j % kStages) * C::V_BYTES) >> 4);
 #pragma unroll
         for (int kk = 0; kk < BN / 16; ++kk)
-          umma_bf16_ts(tmem + 256 + t * 128, tmem + t * BN + kk * 8, bv + (uint64_t)((kk * 16 * 128) >> 4), idesc_pv, 1u);
+          umma_bf16_ts(tmem + 256 + t * 128, tmem + t * BN + kk * 8, join(bv + ((kk * 16 * 128) >> 4), kHighV), idesc_pv, 1u);
       };
       uint32_t fixed = 0;   // bit s: parity of the next phase of v_fixed[s]
       auto k_ready = [&](int j) { return mbar_wait(&bars->k_full[j % kStages], (uint32_t)(j / kStages) & 1u, lim); };
@@ -428,6 +430,10 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         return ok;
       };
       bool ok = n_tiles == 0 || mbar_wait(&bars->q_full, 0, lim);
+      // the warpgroups are spelled out: with a running index the addresses of a product's sixteen steps are
+      // computed between them (10 % of the kernel's time)
+      auto p_ready = [&](int t, int use) { return !aborted(bars) && mbar_wait(&bars->p_full[t], (uint32_t)use & 1u, lim); };
+      static_assert(kStages == 2, "key tile j's stage is j & 1");
       if (has_q1) {
         if (ok && n_tiles > 0) {
           ok = k_ready(0);
@@ -439,27 +445,25 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           }
         }
         for (int j = 0; ok && j < n_tiles; ++j) {
-          const uint32_t ph = (uint32_t)j & 1u;
           const bool more = j + 1 < n_tiles;
-          // K of the next tile is awaited with V, while P0 is still being formed
-          ok = v_ready(j) && (!more || k_ready(j + 1)) && mbar_wait(&bars->p_full[0], ph, lim);
+          // K of the next key tile is awaited with V, while P0 is still being formed
+          ok = v_ready(j) && (!more || k_ready(j + 1)) && p_ready(0, j);
           if (!ok) break;
           tc_fence_after();
           pv(0, j);
           if (more) qk(0, 0, j + 1);
-          ok = !aborted(bars) && mbar_wait(&bars->p_full[1], ph, lim);
+          ok = p_ready(1, j);
           if (!ok) break;
           tc_fence_after();
           pv(1, j);
-          umma_commit(&bars->v_empty[j % kStages]);
+          umma_commit(&bars->v_empty[j & 1]);
           if (more) {
             qk(1, 1, j + 1);
-            umma_commit(&bars->k_empty[(j + 1) % kStages]);
+            umma_commit(&bars->k_empty[(j + 1) & 1]);
           }
         }
       } else {
-        // one query tile: warpgroup t has the key tiles t, t + 2, ...
-        static_assert(kStages == 2, "tile j's stage is its warpgroup's");
+        // one query tile: warpgroup t has key tiles t, t + 2, ...
         for (int j = 0; ok && j < min(2, n_tiles); ++j) {
           ok = k_ready(j);
           if (!ok) break;
@@ -467,11 +471,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           qk(j, 0, j);
           umma_commit(&bars->k_empty[j]);
         }
-        for (int j = 0; ok && j < n_tiles; ++j) {
-          const int t = j & 1;
+        auto step = [&](int t, int j) {
           const bool more = j + 2 < n_tiles;
-          ok = v_ready(j) && (!more || k_ready(j + 2)) && mbar_wait(&bars->p_full[t], (uint32_t)(j >> 1) & 1u, lim);
-          if (!ok) break;
+          if (!(v_ready(j) && (!more || k_ready(j + 2)) && p_ready(t, j >> 1))) return false;
           tc_fence_after();
           pv(t, j);
           umma_commit(&bars->v_empty[t]);
@@ -479,6 +481,11 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             qk(t, 0, j + 2);
             umma_commit(&bars->k_empty[t]);
           }
+          return true;
+        };
+        for (int j = 0; ok && j < n_tiles; j += 2) {
+          ok = step(0, j);
+          if (ok && j + 1 < n_tiles) ok = step(1, j + 1);
         }
       }
       if (!ok) set_abort(bars);
@@ -553,15 +560,23 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         mbar_arrive(&bars->q_full);
       }
-      // 8-bit pages: lane i has the K scale of page i of a key tile, fetched one tile ahead
-      auto k_scale_of = [&](int j) {
-        if (lane >= BN >> a.page_shift) return 1.f;
-        const int page = page_at(a, u, tile_pos(u, k0 + j) + (lane << a.page_shift));
-        return page < a.n_pages ? __ldg(a.k_scale + (int64_t)page * a.H + u.h) : 1.f;
+      // 8-bit pages: lane c < 8 has the K scale and log2 of the V scale of columns 16c .. 16c + 15 of a key
+      // tile (one page), fetched one tile ahead
+      auto scales_of = [&](int j) {
+        float2 x = make_float2(1.f, -INFINITY);
+        if (lane < BN / 16) {
+          const int page = page_at(a, u, (tile_pos(u, k0 + j) + 16 * lane) & -a.page_size);
+          if (page < a.n_pages) {
+            x.x = __ldg(a.k_scale + (int64_t)page * a.H + u.h);
+            x.y = log2f(__ldg(a.v_scale + (int64_t)page * a.H + u.h));
+          }
+        }
+        return x;
       };
-      float ks = 1.f;
+      float2 next = make_float2(1.f, -INFINITY);
+      float e_ref = -INFINITY;   // log2 of the largest V scale so far: o is in units of 2^(e_ref - kLift)
       const int j0 = has_q1 ? 0 : t;
-      if (F8 && j0 < n_tiles) ks = k_scale_of(j0);
+      if (F8 && j0 < n_tiles) next = scales_of(j0);
       {
         uint32_t zero[32];
 #pragma unroll
@@ -572,8 +587,8 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       bool ok = true;
       uint32_t fixed = 0;
       for (int j = j0; j < n_tiles; j += every) {
-        const float scales = ks;
-        if (F8 && j + every < n_tiles) ks = k_scale_of(j + every);
+        const float2 scale = next;
+        if (F8 && j + every < n_tiles) next = scales_of(j + every);
         bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)(has_q1 ? j : j >> 1) & 1u, lim);
         if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
         tc_fence_after();
@@ -597,10 +612,6 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
               if (!((see >> c) & 1u)) sr[32 * b + c] = __float_as_uint(-INFINITY);
           }
         }
-        // logits are S times `by` (16 columns at a time: no page is smaller); their maximum, four chains
-        float by[BN / 16];
-#pragma unroll
-        for (int c = 0; c < BN / 16; ++c) by[c] = F8 ? unit * __shfl_sync(0xffffffffu, scales, (16 * c) >> a.page_shift) : unit;
         float mx = -INFINITY;
         if constexpr (F8) {
 #pragma unroll
@@ -608,7 +619,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             auto x = [&](int e) { return __uint_as_float(sr[c + e]); };
             const float m0 = max3(max3(x(0), x(1), x(2)), x(3), x(4)), m1 = max3(max3(x(5), x(6), x(7)), x(8), x(9));
             const float m2 = max3(max3(x(10), x(11), x(12)), x(13), x(14));
-            mx = fmaxf(mx, max3(m0, m1, fmaxf(m2, x(15))) * by[c / 16]);
+            mx = fmaxf(mx, max3(m0, m1, fmaxf(m2, x(15))) * __shfl_sync(0xffffffffu, scale.x, c / 16));
           }
         } else {
           float m8[8];
@@ -619,9 +630,10 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               m8[e] = max3(m8[e], __uint_as_float(sr[c + 2 * e]), __uint_as_float(sr[c + 2 * e + 1]));
-          mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])) * unit;
+          mx = max3(max3(m8[0], m8[1], m8[2]), max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7]));
         }
-        const bool need = mx > m_ref + 8.f;
+        mx *= unit;
+        bool need = mx > m_ref + 8.f;
         float corr = 1.f;
         if (need) {
           corr = exp2_fast(m_ref - mx);   // 0 where the row has seen nothing yet
@@ -630,19 +642,50 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         // a row that has seen nothing: 2^(-inf - 0) = 0
         const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-        const float2 nm2 = make_float2(-ref, -ref);
-        float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        if constexpr (F8) {
+          float e = scale.y;
 #pragma unroll
-        for (int c = 0; c < BN; c += 2) {
-          const float2 sc2 = make_float2(by[c / 16], by[c / 16]);
-          const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), sc2, nm2);
-          const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-          s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], e);
-          const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
-          sr[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+          for (int o = 4; o; o >>= 1) e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o, 8));
+          e = __shfl_sync(0xffffffffu, e, 0);
+          if (e > e_ref) {
+            corr *= exp2_fast(e_ref - e);
+            e_ref = e;
+            need = true;
+          }
+          // log2 of what this lane's columns' probabilities are multiplied by (a scale 2^60 below the largest
+          // adds nothing to o, and everything to the sum), and its inverse for the sum
+          const float w = kLift + fmaxf(scale.y - e_ref, -60.f), back = exp2_fast(-w);
+#pragma unroll
+          for (int c = 0; c < BN; c += 16) {
+            const float by = unit * __shfl_sync(0xffffffffu, scale.x, c / 16);
+            const float add = __shfl_sync(0xffffffffu, w, c / 16) - ref;
+            const float2 sc2 = make_float2(by, by), nm2 = make_float2(add, add);
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c + k]), __uint_as_float(sr[c + k + 1])), sc2, nm2);
+              const float2 p2 = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+              sum[(k >> 1) & 1] = __fadd2_rn(sum[(k >> 1) & 1], p2);
+              const __half2 h2 = __floats2half2_rn(p2.x, p2.y);
+              sr[(c + k) / 2] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            const float2 s2 = __fadd2_rn(sum[0], sum[1]);
+            l = fmaf(s2.x + s2.y, __shfl_sync(0xffffffffu, back, c / 16), l);
+          }
+        } else {
+          const float2 sc2 = make_float2(unit, unit), nm2 = make_float2(-ref, -ref);
+          float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int c = 0; c < BN; c += 2) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), sc2, nm2);
+            const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+            s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], e);
+            const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
+            sr[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+          }
+          const float2 s2 = __fadd2_rn(__fadd2_rn(s4[0], s4[1]), __fadd2_rn(s4[2], s4[3]));
+          l += s2.x + s2.y;
         }
-        const float2 s2 = __fadd2_rn(__fadd2_rn(s4[0], s4[1]), __fadd2_rn(s4[2], s4[3]));
-        l += s2.x + s2.y;
         tmem_st_x64(tl + colS, sr);
         if (j > 0 && __any_sync(0xffffffffu, need)) {
 #pragma unroll
@@ -665,11 +708,11 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
               // V row r holds a value that is not finite: its token by itself, where it is seen
               const int r = 32 * b + __ffs(bits) - 1, key = pos + r;
               const uint32_t pp = tmem_ld_1(tl + colS + r / 2);
-              const float prob = __uint_as_float(r & 1 ? pp & 0xffff0000u : pp << 16);
+              const float prob = F8 ? __half2float(__ushort_as_half((unsigned short)(r & 1 ? pp >> 16 : pp)))
+                                    : __uint_as_float(r & 1 ? pp & 0xffff0000u : pp << 16);
               const bool see = key < hi && (key >= lo || key < sinks);
               const int page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (key >> a.page_shift));
               const int64_t at = ((int64_t)page * a.page_size + (key & (a.page_size - 1))) * a.row_stride + (int64_t)u.h * HD;
-              const float f = F8 ? __ldg(a.v_scale + (int64_t)page * a.H + u.h) : 1.f;
 #pragma unroll 1
               for (int c = 0; c < HD; c += 32) {
                 uint32_t orr[32];
@@ -678,8 +721,8 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
                 for (int e = 0; e < 32; ++e) {
                   float x;
                   if (F8) {
-                    const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + channel<F8>(e)), __NV_E4M3));
-                    x = __half2float(h) * f;
+                    const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + e), __NV_E4M3));
+                    x = __half2float(h);
                   } else {
                     x = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v) + at + c + e) << 16);
                   }
@@ -699,6 +742,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       if (!ok) set_abort(bars);
       tc_fence_after();
+      const float o_unit = F8 ? exp2_fast(e_ref) * 0x1p-7f : 1.f;
       float* other = reinterpret_cast<float*>(sV);   // [HD][128]: o of the second warpgroup (every product is done)
       const bool join = a.n_split == 1 && !has_q1;
       if (join) {
@@ -708,7 +752,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             uint32_t orr[64];
             tmem_ld_x64(tl + colO + half * 64, orr);
 #pragma unroll
-            for (int c = 0; c < 64; ++c) other[(half * 64 + c) * 128 + row] = __uint_as_float(orr[c]);
+            for (int c = 0; c < 64; ++c) other[(half * 64 + c) * 128 + row] = __uint_as_float(orr[c]) * o_unit;
           }
           bars->ml[row] = make_float2(m_ref, l);
         }
@@ -716,7 +760,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       if (ok && a.n_split == 1 && qt == t) {
         const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
-        float f0 = 1.f, f1 = 0.f;
+        float f0 = o_unit, f1 = 0.f;   // of this warpgroup's o, and of the second's
         if (join) {
           const float2 v = bars->ml[row];
           const float top = fmaxf(m_ref, v.x);
@@ -724,8 +768,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           f1 = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
           l = f0 * l + f1 * v.y;
           m_ref = top;
+          f0 *= o_unit;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = l == 0.f ? 0.f : (join ? 1.f : f0) / l;
 #pragma unroll
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
@@ -739,15 +784,15 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             float* dst = static_cast<float*>(a.o) + out * HD + half * 64;
 #pragma unroll
             for (int c = 0; c < 64; c += 4)
-              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[channel<F8>(c + 1)] * inv,
-                                                                v[channel<F8>(c + 2)] * inv, v[c + 3] * inv);
+              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[c + 1] * inv,
+                                                                v[c + 2] * inv, v[c + 3] * inv);
           } else if (live) {
             __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.o) + out * HD + half * 64;
 #pragma unroll
             for (int c = 0; c < 64; c += 8) {
               float y[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = v[channel<F8>(c + e)] * inv;
+              for (int e = 0; e < 8; ++e) y[e] = v[c + e] * inv;
               *reinterpret_cast<uint4*>(dst + c) = pack8(y);
             }
           }
@@ -760,12 +805,16 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
-          const float* v = reinterpret_cast<const float*>(orr);
+          float* v = reinterpret_cast<float*>(orr);
+          if (F8) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c) v[c] *= o_unit;
+          }
           if (live) {
 #pragma unroll
             for (int c = 0; c < 64; c += 4)
               __stcg(a.part_o + (slot * (HD / 4) + half * 16 + c / 4) * 256 + t * 128 + row,
-                     make_float4(v[c], v[channel<F8>(c + 1)], v[channel<F8>(c + 2)], v[c + 3]));
+                     make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]));
           }
           __syncwarp();
         }
@@ -775,7 +824,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     tc_fence_before();
     end_barrier<C::THREADS>();
   } else if constexpr (F8) {
-    // -------------------------------------------------------------- V codes to bf16 tiles
+    // -------------------------------------------------------------- V codes to f16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
     const int tid = threadIdx.x - 384;
     constexpr int CH = HD / 16;   // 16-code chunks of a row
@@ -801,14 +850,16 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll 4
       for (int i = 0; i < CH; ++i) {
         const int x = tid + 128 * i, r = x / CH, cc = x % CH;
-        // 16 codes are two 16-byte chunks of the bf16 row; the lanes of the second 64 channels take
+        // 16 codes are two 16-byte chunks of the f16 row; the lanes of the second 64 channels take
         // theirs in the other order, so that eight lanes store to eight bank groups
         const int swap = (cc >> 2) & 1;
         const uint2 w0 = *reinterpret_cast<const uint2*>(src + x * 16 + swap * 8);
         const uint2 w1 = *reinterpret_cast<const uint2*>(src + x * 16 + (swap ^ 1) * 8);
-        const Factor f = factor_of(bars->scale[s][r >> a.page_shift]);
         uint4 o0, o1;
-        decode16(w0, w1, f, o0, o1);
+        half4(w0.x, o0.x, o0.y);
+        half4(w0.y, o0.z, o0.w);
+        half4(w1.x, o1.x, o1.y);
+        half4(w1.y, o1.z, o1.w);
         if (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
           o0 = o1 = make_uint4(0, 0, 0, 0);
         uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
