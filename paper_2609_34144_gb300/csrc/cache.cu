@@ -3,7 +3,7 @@
 //
 // Both are bound by memory: every channel is read and written once, a pair costs six flops.  What
 // is not free is the angle: 64 sines and cosines a token for heads of 128, shared by all heads, so
-// a CTA computes them once for its tokens (shared memory) and then streams heads.
+// a CTA computes them once for its tokens and several heads.
 #include <cmath>
 
 #include "cache.cuh"
@@ -41,38 +41,49 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// blockDim = (units in parallel, tokens in parallel); each thread keeps its unit (head, channels)
-// and walks over the CTA's tokens.
+// blockDim = (units in parallel, tokens in parallel): about one unit a thread, whose channels are on
+// their way while the CTA computes its tokens' angles (shared memory, pair 8u + i at 8-unit stride, so
+// that the threads of a row read without bank conflicts).
 template <class T>
 __global__ void __launch_bounds__(256) k_rotary(const __grid_constant__ RotaryKArgs a,
                                                 const __grid_constant__ cast_rotary_table tab) {
-  extern __shared__ float2 cs[];   // [tokens][pairs]
-  const int pairs = tab.rot_dim / 2, per_head = a.d / 16, units = a.H * per_head;
+  extern __shared__ float2 cs[];   // [tokens][8][pairs / 8]
+  const int pairs = tab.rot_dim / 2, turned = tab.rot_dim / 16, per_head = a.d / 16, units = a.H * per_head;
   const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.T - t0);
   const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
+  const T* x = static_cast<const T*>(a.x) + (int64_t)t0 * a.x_stride;
+  T* out = static_cast<T*>(a.out) + (int64_t)t0 * a.out_stride;
+  float v[16];
+  int c0 = 0, c1 = 0;
+  auto load = [&](int u, int t) {
+    const int h = u / per_head, c = u - h * per_head;
+    unit_channels(c, tab.layout, tab.rot_dim, c0, c1);
+    c0 += h * a.d;
+    c1 += h * a.d;
+    load8(x + t * a.x_stride + c0, v);
+    load8(x + t * a.x_stride + c1, v + 8);
+  };
+  if (threadIdx.x < units && threadIdx.y < n) load(threadIdx.x, threadIdx.y);
   for (int i = tid; i < n * pairs; i += threads) {
     const int t = i / pairs, p = i - t * pairs;
     float2 c = rotary_cs(tab, p, __ldg(a.positions + (int64_t)(t0 + t) * a.n_axes + tab.axis[p]));
     c.y *= a.sign;
-    cs[i] = c;
+    cs[t * pairs + (p & 7) * turned + (p >> 3)] = c;
   }
   __syncthreads();
-  for (int u = threadIdx.x; u < units; u += blockDim.x) {
-    const int h = u / per_head, c = u - h * per_head;
-    int c0, c1;
-    unit_channels(c, tab.layout, tab.rot_dim, c0, c1);
-    const bool turned = c < tab.rot_dim / 16;
-    const T* src = static_cast<const T*>(a.x) + (int64_t)t0 * a.x_stride + h * a.d;
-    T* dst = static_cast<T*>(a.out) + (int64_t)t0 * a.out_stride + h * a.d;
+  for (int u = threadIdx.x; u < units; u += blockDim.x)
     for (int t = threadIdx.y; t < n; t += blockDim.y) {
-      float v[16];
-      load8(src + t * a.x_stride + c0, v);
-      load8(src + t * a.x_stride + c1, v + 8);
-      if (turned) rotate_unit(v, cs + t * pairs + 8 * c, tab.layout);
-      store8(dst + t * a.out_stride + c0, v);
-      store8(dst + t * a.out_stride + c1, v + 8);
+      if (u != threadIdx.x || t != threadIdx.y) load(u, t);
+      const int c = u % per_head;
+      if (c < turned) {
+        float2 w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = cs[t * pairs + i * turned + c];
+        rotate_unit(v, w, tab.layout);
+      }
+      store8(out + t * a.out_stride + c0, v);
+      store8(out + t * a.out_stride + c1, v + 8);
     }
-  }
 }
 
 // ------------------------------------------------------------------ cast_cache_append
@@ -92,13 +103,13 @@ struct AppendKArgs {
 };
 
 // One CTA: the new tokens of one sequence in one page (a run of rows lo .. hi-1), for a group of
-// heads of K, V or the queries.  A thread holds two units (32 values) of a head's tile of
-// page_size x d, so that a page's maximum is known before the values leave the registers.
+// heads of K, V or the queries.  A thread has one unit (row, 16 channels) of every head: it computes its
+// eight angles once, and a page's maximum is known before the values leave the registers.  The next head's
+// values are fetched while this one's are turned, reduced and stored.
 template <bool F8>
-__global__ void __launch_bounds__(512) k_append(const __grid_constant__ AppendKArgs a,
-                                                const __grid_constant__ cast_rotary_table tab) {
-  extern __shared__ float2 cs[];   // [page_size][pairs]
-  __shared__ float s_max[2][16];
+__global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendKArgs a,
+                                                 const __grid_constant__ cast_rotary_table tab) {
+  __shared__ uint32_t s_max[2][32];
   const int b = blockIdx.x / a.runs, run = blockIdx.x - b * a.runs;
   const Sequence s = sequence_of(a.batch, b);
   const int p0 = s.len - s.n_new;                       // place of the first new token
@@ -112,8 +123,7 @@ __global__ void __launch_bounds__(512) k_append(const __grid_constant__ AppendKA
   int job = blockIdx.y;
   const int kind = job < a.jobs_kv ? 0 : job < 2 * a.jobs_kv ? 1 : 2;   // K, V, queries
   job -= kind == 0 ? 0 : kind == 1 ? a.jobs_kv : 2 * a.jobs_kv;
-  const int H = kind == 2 ? a.H_q : a.H;
-  const int h0 = job * a.group, h1 = min(h0 + a.group, H);
+  const int h0 = job * a.group, h1 = min(h0 + a.group, kind == 2 ? a.H_q : a.H);
   int page = 0;
   if (kind != 2) {
     page = g < a.batch.max_pages ? __ldg(a.batch.page_table + (int64_t)b * a.batch.page_table_stride + g) : -1;
@@ -122,104 +132,95 @@ __global__ void __launch_bounds__(512) k_append(const __grid_constant__ AppendKA
       return;
     }
   }
-  const int token0 = s.t0 + base - p0;   // the call's row of the page's row 0 (may lie before the run)
-  const int pairs = tab.rot_dim / 2;
-  const bool turned = a.turned && kind != 1;
-  if (turned) {
-    for (int i = threadIdx.x + lo * pairs; i < hi * pairs; i += blockDim.x) {
-      const int r = i / pairs, p = i - r * pairs;
-      const int pos = a.positions ? __ldg(a.positions + (int64_t)(token0 + r) * a.n_axes + tab.axis[p]) : base + r;
-      cs[i] = rotary_cs(tab, p, pos);
+  const int64_t token0 = (int64_t)s.t0 + base - p0;   // the call's row of the page's row 0 (may lie before the run)
+  // the thread's unit: a row and its channels
+  const int per_row = a.d / 16, row = threadIdx.x / per_row, col = threadIdx.x - row * per_row;
+  const bool in = row >= lo && row < hi;
+  const bool turned = a.turned && kind != 1 && col < tab.rot_dim / 16;
+  int c0, c1;
+  unit_channels(col, turned ? tab.layout : CAST_ROTARY_INTERLEAVED, tab.rot_dim, c0, c1);
+  float2 cs[8];
+  if (turned && in) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int p = 8 * col + i;
+      cs[i] = rotary_cs(tab, p, a.positions ? __ldg(a.positions + (token0 + row) * a.n_axes + tab.axis[p]) : base + row);
     }
-    __syncthreads();
   }
-  // unit u of a head's tile: row u / (d/16), channels by u % (d/16)
-  const int per_row = a.d / 16;
-  int row[2], c0[2], c1[2], col[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int u = threadIdx.x + j * blockDim.x;
-    row[j] = u / per_row;
-    col[j] = u - row[j] * per_row;
-    unit_channels(col[j], turned ? tab.layout : CAST_ROTARY_INTERLEAVED, turned ? tab.rot_dim : 0, c0[j], c1[j]);
+  const __nv_bfloat16* src = (kind == 0 ? a.k : kind == 1 ? a.v : a.q) +
+                             (token0 + row) * (kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride);
+  const int64_t to = kind == 2 ? (token0 + row) * a.q_out_stride : ((int64_t)page * a.page_size + row) * a.row_stride;
+  const bool codes = F8 && kind != 2;
+  uint4 n0 = make_uint4(0, 0, 0, 0), n1 = n0;
+  if (in) {
+    n0 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)h0 * a.d + c0));
+    n1 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)h0 * a.d + c1));
   }
-  const __nv_bfloat16* src = kind == 0 ? a.k : kind == 1 ? a.v : a.q;
-  const int64_t stride = kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride;
-  int phase = 0;
-  for (int h = h0; h < h1; ++h, phase ^= 1) {
-    float v[2][16];
-    float top = -1.f;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bool in = row[j] >= lo && row[j] < hi;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[j][i] = 0.f;
+  for (int h = h0; h < h1; ++h) {
+    float v[16];
+    unpack8(n0, v);
+    unpack8(n1, v + 8);
+    if (in && h + 1 < h1) {
+      n0 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(h + 1) * a.d + c0));
+      n1 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(h + 1) * a.d + c1));
+    }
+    if (turned && in) rotate_unit(v, cs, tab.layout);
+    const int64_t at = to + (int64_t)h * a.d;
+    if (!codes) {
       if (in) {
-        const __nv_bfloat16* p = src + (int64_t)(token0 + row[j]) * stride + (int64_t)h * a.d;
-        load8(p + c0[j], v[j]);
-        load8(p + c1[j], v[j] + 8);
+        __nv_bfloat16* dst = kind == 2 ? a.q_out : static_cast<__nv_bfloat16*>(kind == 0 ? a.ck : a.cv);
+        store8(dst + at + c0, v);
+        store8(dst + at + c1, v + 8);
       }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bool in = row[j] >= lo && row[j] < hi;
-      if (!in) continue;
-      if (turned && col[j] < tab.rot_dim / 16) rotate_unit(v[j], cs + row[j] * pairs + 8 * col[j], tab.layout);
-      if (F8 && kind != 2) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float m = fabsf(v[j][i]);
-          if (m < INFINITY) top = fmaxf(top, m);
-        }
-      } else {
-        __nv_bfloat16* dst = kind == 2 ? a.q_out + (int64_t)(token0 + row[j]) * a.q_out_stride
-                                       : static_cast<__nv_bfloat16*>(kind == 0 ? a.ck : a.cv) +
-                                             ((int64_t)page * a.page_size + row[j]) * a.row_stride;
-        dst += (int64_t)h * a.d;
-        store8(dst + c0[j], v[j]);
-        store8(dst + c1[j], v[j] + 8);
-      }
+      continue;
     }
     if constexpr (F8) {
-      if (kind == 2) continue;
-      // the page's scale for this head
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if ((threadIdx.x & 31) == 0) s_max[phase][threadIdx.x >> 5] = top;
+      // the page's scale for this head: magnitudes of finite values order as their bits
+      uint32_t top = 0;
+      if (in) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+          if (m < 0x7f800000u) top = max(top, m);
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if ((threadIdx.x & 31) == 0) s_max[h & 1][threadIdx.x >> 5] = top;
       float* scale = (kind == 0 ? a.k_scale : a.v_scale) + (int64_t)page * a.H + h;
       const float old = lo > 0 ? *scale : 0.f;
       __syncthreads();
-      top = s_max[phase][0];
-      for (int w = 1; w < (int)blockDim.x / 32; ++w) top = fmaxf(top, s_max[phase][w]);
-      const float now = fmaxf(pow2f(scale_exponent(top)), old);
-      uint8_t* cache = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv) + (int64_t)page * a.page_size * a.row_stride +
-                       (int64_t)h * a.d;
+      const int warps = blockDim.x / 32;
+      top = (threadIdx.x & 31) < warps ? s_max[h & 1][threadIdx.x & 31] : 0u;
+      top = __reduce_max_sync(0xffffffffu, top);
+      const float now = fmaxf(pow2f(scale_exponent(__uint_as_float(top))), old);
       const float inv = 1.f / now;   // exact: a power of two within 2^-120 .. 2^120
-  #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (row[j] < lo || row[j] >= hi) continue;
-  #pragma unroll
-        for (int i = 0; i < 16; ++i) v[j][i] *= inv;
-        uint8_t* dst = cache + row[j] * a.row_stride;
-        *reinterpret_cast<uint2*>(dst + c0[j]) = encode8(v[j]);
-        *reinterpret_cast<uint2*>(dst + c1[j]) = encode8(v[j] + 8);
-      }
-      if (lo > 0 && now > old) {
-        // the rows that were there before, rounded again at the larger scale
-        const float f = old * inv;
-        for (int i = threadIdx.x; i < lo * a.d / 8; i += blockDim.x) {
-          const int r = i / (a.d / 8);
-          uint2* p = reinterpret_cast<uint2*>(cache + r * a.row_stride + (i - r * (a.d / 8)) * 8);
-          const uint2 w = *p;
-          float x[8];
-  #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t half = (e < 2 ? w.x : w.y) >> (16 * (e & 1));
-            const __half2 y(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(half & 0xffffu), __NV_E4M3));
-            x[2 * e] = __low2float(y) * f;
-            x[2 * e + 1] = __high2float(y) * f;
-          }
-          *p = encode8(x);
+      uint8_t* cache = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv);
+      if (in) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= inv;
+        const uint2 w0 = encode8(v), w1 = encode8(v + 8);
+        if (c1 == c0 + 8) {
+          *reinterpret_cast<uint4*>(cache + at + c0) = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        } else {
+          *reinterpret_cast<uint2*>(cache + at + c0) = w0;
+          *reinterpret_cast<uint2*>(cache + at + c1) = w1;
         }
+      }
+      if (lo > 0 && now > old && row < lo) {
+        // rows that were there before, rounded again at the larger scale
+        uint4* p = reinterpret_cast<uint4*>(cache + at + 16 * col);
+        const uint4 w = *p;
+        const uint32_t in4[4] = {w.x, w.y, w.z, w.w};
+        const float f = old * inv;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t two = in4[e >> 1] >> (16 * (e & 1));
+          const __half2 y(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3));
+          v[2 * e] = __low2float(y) * f;
+          v[2 * e + 1] = __high2float(y) * f;
+        }
+        const uint2 w0 = encode8(v), w1 = encode8(v + 8);
+        *p = make_uint4(w0.x, w0.y, w1.x, w1.y);
       }
       // every thread has read `scale` before the barrier above
       if (threadIdx.x == 0) *scale = now;
@@ -396,9 +397,10 @@ cast_status cast_rotary(const cast_rotary_args* a, void* stream) {
   int tx = 1;
   while (tx < units && tx < 256) tx *= 2;
   const dim3 block(tx, 256 / tx);
-  // about two units a thread, so that a chunk of a few hundred tokens already fills the SMs; never
-  // more than 48 KB of angles
-  int tokens = (512 + units - 1) / units;
+  // about one unit a thread, and fewer tokens a CTA where the SMs would not be filled twice; never more
+  // than 48 KB of angles
+  int tokens = (256 + units - 1) / units;
+  if (tokens > (a->T + 303) / 304) tokens = (a->T + 303) / 304;
   const int cap = 48 * 1024 / (a->table->rot_dim / 2 * 8);
   if (tokens > cap) tokens = cap;
   k.tokens = tokens;
@@ -464,32 +466,24 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   k.runs = (max_new + c.page_size - 2) / c.page_size + 1;
   const int64_t gx = (int64_t)k.runs * a->batch.B;
   if (gx > 0x7fffffff) return fail(CAST_ERR_UNSUPPORTED, "%s: %lld page runs", who, (long long)gx);
-  // heads of one CTA: few enough that the grid fills the SMs, at most 8 to share the angles
+  const int threads = c.page_size * c.d / 16;
+  // heads of one CTA: eight share the angles' cost, fewer where the grid would not fill the SMs twice
   int group = 8;
-  while (group > 1 && gx * (2 * ((c.H + group - 1) / group) + (k.H_q + group - 1) / group) < 2 * 152) group /= 2;
+  while (group > 1 &&
+         gx * (2 * ((c.H + group - 1) / group) + (k.H_q + group - 1) / group) * threads < (int64_t)2 * 152 * 2048)
+    group /= 2;
   k.group = group;
   k.jobs_kv = (c.H + group - 1) / group;
   k.jobs_q = (k.H_q + group - 1) / group;
   if (2 * (int64_t)k.jobs_kv + k.jobs_q > 65535) return fail(CAST_ERR_UNSUPPORTED, "%s: too many heads", who);
   const dim3 grid((unsigned)gx, 2 * k.jobs_kv + k.jobs_q);
-  const int threads = c.page_size * c.d / 32;
-  const size_t smem = a->rotary ? (size_t)c.page_size * (a->rotary->rot_dim / 2) * sizeof(float2) : 0;
   const cast_rotary_table none{};
   const cast_rotary_table& tab = a->rotary ? *a->rotary : none;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  static std::atomic<uint64_t> attr_done{0};
-  constexpr int kMaxSmem = 128 * 64 * (int)sizeof(float2);
-  if (!once_per_device(attr_done, [&] {
-        return cudaFuncSetAttribute(k_append<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) ==
-                   cudaSuccess &&
-               cudaFuncSetAttribute(k_append<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) ==
-                   cudaSuccess;
-      }))
-    return check_launch("append smem attribute");
   if (c.dtype == CAST_F8E4M3)
-    k_append<true><<<grid, threads, smem, st>>>(k, tab);
+    k_append<true><<<grid, threads, 0, st>>>(k, tab);
   else
-    k_append<false><<<grid, threads, smem, st>>>(k, tab);
+    k_append<false><<<grid, threads, 0, st>>>(k, tab);
   return check_launch(who);
 }
 
