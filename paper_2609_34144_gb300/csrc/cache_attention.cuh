@@ -6,8 +6,10 @@
 namespace cast {
 
 struct TilesPlan {
-  int tile_tokens, pairs, n_split;
-  size_t part_o_bytes, total_bytes;
+  int tile_tokens, pairs;
+  bool whole;      // a CTA has one whole unit; else units may be cut and are joined
+  int64_t grid;
+  size_t part_o_bytes, part_ml_bytes, total_bytes;
 };
 TilesPlan tiles_plan(const cast_cache_attn_args& a);
 // Arguments must have been validated; ws holds tiles_plan(a).total_bytes.

@@ -4,8 +4,10 @@
 // Rows of one KV head are (token, query head of the group) pairs, G of them a token: a tile of 128
 // rows holds 128 / G whole tokens, a unit two consecutive tiles (Q0, Q1) of one sequence, so that each
 // K/V tile of 128 positions fetched feeds 256 rows.  The positions a unit's rows can see are a list
-// of tiles (the sinks', then the window's); a call with few units cuts the list into n_split parts,
-// whose unnormalised o, maxima and sums k_tiles_merge joins.
+// of tiles (the sinks', then the window's).  All units' lists in a row are the work of the call: one CTA
+// an SM takes an equal share of it, found from the lengths on the device, and walks through the units it
+// touches.  A unit that no CTA had whole leaves parts (unnormalised o, maxima and sums), which
+// k_tiles_merge joins.  Short lists (8 tiles) are not cut: a CTA has one unit.
 //
 // Roles (one CTA an SM): warp 0 fetches Q and the K pages, warp 2 the V pages (TMA boxes of one page x
 // 64 channels into a two-stage ring of 128-byte-swizzled tiles; a page that no row sees or that is
@@ -51,8 +53,8 @@ struct Cfg {
   static constexpr int THREADS = F8 ? 512 : 384;
   // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
   static constexpr int LAUNCH = F8 ? 128 : 168;
-  static constexpr int REGS_CTL = 96;
-  static constexpr int REGS_SOFTMAX = F8 ? 176 : 200;
+  static constexpr int REGS_CTL = F8 ? 64 : 96;
+  static constexpr int REGS_SOFTMAX = F8 ? 192 : 200;
   static constexpr int REGS_DECODE = 64;
   static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
                 "register split exceeds the launch allocation");
@@ -77,26 +79,35 @@ struct TilesKArgs {
   int64_t row_stride;
   const uint8_t* v;
   const float *k_scale, *v_scale;
-  const __nv_bfloat16* q;
-  int64_t q_stride;
   void* o;
   float* lse;
   float scale_log2;
   unsigned* error;
-  int pairs;         // pairs of tiles that the grid has room for, a head
-  int n_split;
-  float4* part_o;    // [unit][part][HD / 4][256]
-  float2* part_ml;   // [unit][part][256]
+  int pairs;         // pairs of tiles that a head may have
+  int most_pairs;    // of a sequence
+  int whole;         // a CTA has one whole unit
+  int least;         // work that a CTA takes at least
+  float4* part_o;    // [2 * grid][HD / 4][256]
+  float2* part_ml;   // [2 * grid][256]
+  struct Cut* cuts;  // [grid]
   unsigned long long wait_ns;
 };
 
-// One unit: tokens i0 .. of sequence b, KV head h
+// One unit, tokens i0 .. of sequence b, KV head h, and a CTA's part of it
 struct Unit {
   int b, h, t0, i0, n_new, p0;
+  int k0, n_tiles;          // its key tiles k0 .. k0 + n_tiles - 1
+  int work;                 // its work (see unit_work)
+  int slot;                 // where the part's result goes; -1: the part is the whole unit
   int lo, hi, sinks;        // positions that some row sees: below sinks, or lo .. hi-1
   int lo_all, hi_all;       // ... that every row sees: lo_all .. hi_all-1 (or below sinks)
   int n_sink, first, tiles; // tiles of 128 positions: 0 .. n_sink-1, then first ..
   int valid;
+};
+// What CTA c leaves for the joining: the unit that its share begins inside of, which CTAs c0 .. c1 had
+// parts of (c0 = -1: it begins with a unit)
+struct Cut {
+  int h, t0, i0, n_new, c0, c1;
 };
 // position of the first key of tile j of the unit's list
 __device__ __forceinline__ int tile_pos(const Unit& u, int j) {
@@ -107,59 +118,18 @@ __device__ __forceinline__ bool all_see(const Unit& u, int pos) {
 }
 __device__ __forceinline__ bool some_see(const Unit& u, int p) { return p < u.hi && (p >= u.lo || p < u.sinks); }
 
-// The unit at place `x` of the grid (one warp; the answer is every lane's): pairs of tiles run over
-// the sequences, for each head; with a causal mask a head's longest units come first.
-__device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
-  Unit u{};
-  u.h = x / a.pairs;
-  int pair = x - u.h * a.pairs;
-  const int per = 2 * a.tile_tokens;
-  int before = 0, total = 0;
-  if (a.causal) {
-    // count from the end
-    for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
-      const int b = b0 + lane;
-      int n = 0;
-      if (b < a.batch.B) n = (min(sequence_of(a.batch, b).n_new, a.batch.max_new) + per - 1) / per;
-      total += __reduce_add_sync(0xffffffffu, n);
-    }
-    pair = total - 1 - pair;
-    if (pair < 0) return u;
-  }
-  for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
-    const int b = b0 + lane;
-    int n = 0;
-    if (b < a.batch.B) {
-      const Sequence s = sequence_of(a.batch, b);
-      if (s.n_new > a.batch.max_new) atomicExch(a.error, kCacheBadInput);
-      n = (min(s.n_new, a.batch.max_new) + per - 1) / per;
-    }
-    int sum = n;
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += y;
-    }
-    const unsigned hit = __ballot_sync(0xffffffffu, before + sum > pair);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      u.b = b0 + l;
-      u.i0 = (pair - before - __shfl_sync(0xffffffffu, sum - n, l)) * per;
-      u.valid = 1;
-      break;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-  if (!u.valid) return u;
-  const Sequence s = sequence_of(a.batch, u.b);
+// The positions that unit u.i0 of sequence `s` sees
+__device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const Sequence& s) {
   u.t0 = s.t0;
   u.n_new = min(s.n_new, a.batch.max_new);
   u.p0 = s.len - s.n_new;
   const int64_t room = (int64_t)a.batch.max_pages * a.page_size;
-  if (s.len > room) atomicExch(a.error, kCacheBadInput);
+  if (s.len > room || s.n_new > a.batch.max_new) atomicExch(a.error, kCacheBadInput);
   const int len = (int)min((int64_t)s.len, room);
-  const int i1 = min(u.i0 + per, u.n_new) - 1;
+  const int i1 = min(u.i0 + 2 * a.tile_tokens, u.n_new) - 1;
   u.hi = a.causal ? min(len, max(u.p0 + i1 + 1, 0)) : len;
   u.hi_all = a.causal ? min(len, max(u.p0 + u.i0 + 1, 0)) : len;
+  u.lo = u.lo_all = u.sinks = 0;
   if (a.window > 0) {
     u.lo = min(max(u.p0 + u.i0 - a.window + 1, 0), u.hi);
     u.lo_all = max(u.p0 + i1 - a.window + 1, 0);
@@ -168,11 +138,168 @@ __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
   u.first = u.lo / BN;
   u.n_sink = min((u.sinks + BN - 1) / BN, u.first);
   u.tiles = u.n_sink + max((u.hi + BN - 1) / BN - u.first, 0);
+}
+// Work: a key tile of two query tiles counts 3, of one query tile 2 (1.75 and 1.2 us), a unit that sees
+// nothing 1.
+__device__ __forceinline__ int tile_work(const TilesKArgs& a, const Unit& u) {
+  return u.i0 + a.tile_tokens < u.n_new ? 3 : 2;
+}
+__device__ __forceinline__ int unit_work(const TilesKArgs& a, const Unit& u) { return max(1, u.tiles * tile_work(a, u)); }
+
+// Work of units lane, lane + 32, ... or, `serial`, of all units of sequence b
+__device__ __forceinline__ int sequence_work(const TilesKArgs& a, int b, int lane, bool serial) {
+  if (b >= a.batch.B) return 0;
+  const Sequence s = sequence_of(a.batch, b);
+  const int n = min(s.n_new, a.batch.max_new), per = 2 * a.tile_tokens;
+  Unit u{};
+  int w = 0;
+  for (u.i0 = serial ? 0 : lane * per; u.i0 < n; u.i0 += serial ? per : 32 * per) {
+    place_unit(a, u, s);
+    w += unit_work(a, u);
+  }
+  return w;
+}
+// Lane l's answer is the work of sequence b0 + l: one sequence a lane, or, where there are fewer of them
+// than units in one, one after the other by all lanes
+__device__ __forceinline__ int chunk_work(const TilesKArgs& a, int b0, int lane) {
+  if (a.batch.B >= a.most_pairs) return sequence_work(a, b0 + lane, 0, true);
+  int mine = 0;
+  for (int b = b0; b < min(b0 + 32, a.batch.B); ++b) {
+    const int w = __reduce_add_sync(0xffffffffu, sequence_work(a, b, lane, false));
+    if (b0 + lane == b) mine = w;
+  }
+  return mine;
+}
+__device__ __forceinline__ int scan(int x, int lane) {   // inclusive
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+// How the call's work is dealt out.  Units of equal work are first dealt whole, a round of one for each
+// CTA (heads slowest: what runs together reads one head's keys); what is left, or everything where units
+// differ, is a row of work items from `base` on, of which CTA c has share * c .. share * (c + 1) - 1.
+struct Deal {
+  int per_head;          // work of a head
+  int each, rounds;      // of a unit that is dealt whole, and how many a CTA has
+  int64_t base, share, total;
+};
+__device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) {   // one warp; every lane has it
+  Deal d{};
+  for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += __reduce_add_sync(0xffffffffu, chunk_work(a, b0, lane));
+  d.total = (int64_t)d.per_head * a.H;
+  if (a.batch.B == 1 && !a.causal) {
+    // one sequence without a causal mask: its units differ at most by the last one's rows and the window
+    const Sequence s = sequence_of(a.batch, 0);
+    const int n = min(s.n_new, a.batch.max_new), per = 2 * a.tile_tokens;
+    Unit u{};
+    int low = 0x7fffffff, high = 0;
+    for (u.i0 = lane * per; u.i0 < n; u.i0 += 32 * per) {
+      place_unit(a, u, s);
+      low = min(low, unit_work(a, u));
+      high = max(high, unit_work(a, u));
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    if (low == high) {
+      d.each = high;
+      d.rounds = (int)(d.total / high / ctas);
+      d.base = (int64_t)d.rounds * ctas * high;
+    }
+  }
+  d.share = max((int64_t)a.least, (d.total - d.base + ctas - 1) / ctas);
+  return d;
+}
+
+// Unit `x` of the call, whole (one warp; every lane has it), heads slowest: those that run together read
+// one head's keys.
+__device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
+  Unit u{};
+  u.h = x / a.pairs;
+  int pair = x - u.h * a.pairs;
+  const int per = 2 * a.tile_tokens;
+  for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
+    const int b = b0 + lane;
+    const int n = b < a.batch.B ? (min(sequence_of(a.batch, b).n_new, a.batch.max_new) + per - 1) / per : 0;
+    const int sum = scan(n, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, sum > pair);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      u.b = b0 + l;
+      u.i0 = (pair - __shfl_sync(0xffffffffu, sum - n, l)) * per;
+      u.valid = 1;
+      break;
+    }
+    pair -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (!u.valid) return u;
+  place_unit(a, u, sequence_of(a.batch, u.b));
+  u.n_tiles = u.tiles;
+  u.work = unit_work(a, u);
+  u.slot = -1;
+  return u;
+}
+
+// The unit that work item `at` lies in, and the part of it that items at .. stop-1 are (one warp; every
+// lane has it).  A part that begins inside the unit has the CTA's first place, else its second.
+__device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int64_t at, int64_t stop, int lane, Cut* cut) {
+  Unit u{};
+  if (cut && lane == 0) cut->c0 = -1;
+  if (at >= stop) return u;
+  const int h = (int)(at / d.per_head), per = 2 * a.tile_tokens;
+  int r = (int)(at - (int64_t)h * d.per_head), b = -1;
+  for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
+    const int w = chunk_work(a, b0, lane);
+    const int sum = scan(w, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      r -= __shfl_sync(0xffffffffu, sum - w, l);
+      b = b0 + l;
+      break;
+    }
+    r -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (b < 0) return u;
+  const Sequence s = sequence_of(a.batch, b);
+  const int n = min(s.n_new, a.batch.max_new);
+  for (int i0 = 0; i0 < n; i0 += 32 * per) {
+    u.i0 = i0 + lane * per;
+    int w = 0;
+    if (u.i0 < n) {
+      place_unit(a, u, s);
+      w = unit_work(a, u);
+    }
+    const int sum = scan(w, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      r -= __shfl_sync(0xffffffffu, sum - w, l);
+      u.i0 = i0 + l * per;
+      u.valid = 1;
+      break;
+    }
+    r -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (!u.valid) return u;
+  u.b = b;
+  u.h = h;
+  place_unit(a, u, s);
+  const int w = unit_work(a, u), each = tile_work(a, u);
+  u.work = (int)min((int64_t)(w - r), stop - at);
+  u.k0 = min((r + each - 1) / each, u.tiles);
+  u.n_tiles = min((r + u.work + each - 1) / each, u.tiles) - u.k0;
+  u.slot = u.work == w ? -1 : 2 * (int)blockIdx.x + (r > 0 ? 0 : 1);
+  if (cut && lane == 0 && r > 0) {
+    const int64_t first = at - r - d.base;
+    *cut = Cut{u.h, u.t0, u.i0, u.n_new, (int)(first / d.share), (int)((first + w - 1) / d.share)};
+  }
   return u;
 }
 
 struct Bars {
-  uint64_t q_full;
+  uint64_t q_full, q_raw;              // q_raw: 8-bit pages, the queries as they are, in the V tiles' place
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t s_full[2], p_full[2];
   // bf16 pages: V of a stage's tile that not all rows see is ready.  One phase for each such tile of
@@ -184,7 +311,7 @@ struct Bars {
   int abort;
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
   float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
-  Unit unit;
+  Unit unit, next;                     // of this segment and the next
 };
 static_assert(sizeof(Bars) <= 1664, "barriers and the unit");
 
@@ -197,6 +324,53 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+// Two floats within +-448 as e4m3 codes
+__device__ __forceinline__ uint32_t code2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool F8>
+__device__ __forceinline__ void init_barriers(Bars* bars) {
+  mbar_init(&bars->q_full, F8 ? 256 : 1);
+  mbar_init(&bars->q_raw, 1);
+  for (int s = 0; s < kStages; ++s) {
+    mbar_init(&bars->k_full[s], 1);
+    mbar_init(&bars->k_empty[s], 1);
+    mbar_init(&bars->v_full[s], F8 ? 128 : 1);
+    mbar_init(&bars->v_empty[s], F8 ? 1 : 2);   // the products, and warp 3 that saw the tile
+    mbar_init(&bars->v_fixed[s], 32);
+    mbar_init(&bars->raw_full[s], 1);
+    mbar_init(&bars->raw_empty[s], 128);
+  }
+  for (int t = 0; t < 2; ++t) {
+    mbar_init(&bars->s_full[t], 1);
+    mbar_init(&bars->p_full[t], 128);
+  }
+  mbar_init(&bars->fin, 1);
+  fence_barrier_init();
+}
+__device__ __forceinline__ void drop(uint64_t* bar) {
+  asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void drop_barriers(Bars* bars) {
+  drop(&bars->q_full);
+  drop(&bars->q_raw);
+  for (int s = 0; s < kStages; ++s) {
+    drop(&bars->k_full[s]);
+    drop(&bars->k_empty[s]);
+    drop(&bars->v_full[s]);
+    drop(&bars->v_empty[s]);
+    drop(&bars->v_fixed[s]);
+    drop(&bars->raw_full[s]);
+    drop(&bars->raw_empty[s]);
+  }
+  for (int t = 0; t < 2; ++t) {
+    drop(&bars->s_full[t]);
+    drop(&bars->p_full[t]);
+  }
+  drop(&bars->fin);
 }
 template <int N>
 __device__ __forceinline__ void end_barrier() {
@@ -266,64 +440,79 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   uint8_t* sRaw = smem + C::OFF_RAW;
   Bars* bars = reinterpret_cast<Bars*>(smem + C::OFF_BAR);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int place = blockIdx.x / a.n_split, part = blockIdx.x - place * a.n_split;
 
+  // warp 0: the CTA's share of the work, and its first unit
+  Deal d{};
+  int64_t at = 0, stop = 0;
+  int round = 0;
   if (warp == 0) {
-    const Unit u = unit_of(a, place, lane);
+    Unit u;
+    if (a.whole) {
+      u = unit_of(a, blockIdx.x, lane);
+    } else {
+      d = deal(a, gridDim.x, lane);
+      at = d.rounds > 0 ? (int64_t)blockIdx.x * d.each : blockIdx.x * d.share;
+      stop = d.rounds > 0 ? at + d.each : min(at + d.share, d.total);
+      // with the share comes what it begins inside of, for the joining
+      u = unit_at(a, d, at, stop, lane, d.rounds > 0 ? nullptr : a.cuts + blockIdx.x);
+    }
     if (lane == 0) bars->unit = u;
   }
-  if (threadIdx.x == 32) {
-    mbar_init(&bars->q_full, F8 ? 256 : 1);
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&bars->k_full[s], 1);
-      mbar_init(&bars->k_empty[s], 1);
-      mbar_init(&bars->v_full[s], F8 ? 128 : 1);
-      mbar_init(&bars->v_empty[s], F8 ? 1 : 2);   // the products, and warp 3 that saw the tile
-      mbar_init(&bars->v_fixed[s], 32);
-    }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(&bars->s_full[t], 1);
-      mbar_init(&bars->p_full[t], 128);
-    }
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&bars->raw_full[s], 1);
-      mbar_init(&bars->raw_empty[s], 128);
-    }
-    mbar_init(&bars->fin, 1);
-    bars->abort = 0;
-    fence_barrier_init();
-  }
-  __syncthreads();
-  const Unit& u = bars->unit;   // read from shared memory where it is needed: registers are short
-  if (!u.valid) return;
   if (warp == 1) {
     tmem_alloc(&bars->tmem_base, kTmemCols);
     tmem_relinquish();
     tc_fence_before();
+    if (lane == 0) {
+      init_barriers<F8>(bars);
+      bars->abort = 0;
+    }
   }
   __syncthreads();
   tc_fence_after();
+  const Unit& u = bars->unit;
   const uint32_t tmem = bars->tmem_base;
   const uint64_t lim = a.wait_ns;
-  const int k0 = (int)((int64_t)u.tiles * part / a.n_split);
-  const int n_tiles = (int)((int64_t)u.tiles * (part + 1) / a.n_split) - k0;
-  const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;   // else the warpgroups share the key tiles
+  if (!u.valid) {
+    if (warp == 1) tmem_dealloc(tmem, kTmemCols);
+    return;
+  }
+
+  // Segments: the CTA's parts of units, one after the other.  Between two of them the CTA meets twice, and
+  // its barriers begin anew in between.  Unit data is read from shared memory where it is needed.
+  auto another = [&] {
+    tc_fence_before();
+    fence_proxy_async_smem();   // what was staged in the tiles' places, before copies land there again
+    end_barrier<C::THREADS>();
+    if (threadIdx.x == 32 && !aborted(bars)) {
+      drop_barriers(bars);
+      init_barriers<F8>(bars);
+      bars->unit = bars->next;
+    }
+    end_barrier<C::THREADS>();
+    tc_fence_after();
+    return !aborted(bars) && u.valid != 0;
+  };
 
   if (warp < 4) {
     setmaxnreg_dec<C::REGS_CTL>();
+    for (;;) {
+    const int k0 = u.k0, n_tiles = u.n_tiles;
+    const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;   // else the warpgroups share the key tiles
     if (warp == 0 || warp == 2) {
       // ------------------------------------------------------------ Q and K pages / V pages
       const bool is_k = warp == 0;
       const CUtensorMap* map = is_k ? &tm_k : &tm_v;
       if (lane == 0) {
         tma_prefetch_desc(map);
-        if (!F8 && is_k && n_tiles > 0) {
+        if (is_k && n_tiles > 0) {
           const uint32_t bytes = (uint32_t)a.tile_tokens * a.group * HD * 2;
-          mbar_arrive_expect_tx(&bars->q_full, (has_q1 ? 2 : 1) * bytes);
+          uint64_t* bar = F8 ? &bars->q_raw : &bars->q_full;
+          uint8_t* to = F8 ? sV : sQ;
+          mbar_arrive_expect_tx(bar, (has_q1 ? 2 : 1) * bytes);
           for (int t = 0; t < (has_q1 ? 2 : 1); ++t)
 #pragma unroll
             for (int b = 0; b < HD / 64; ++b)
-              tma_load_3d(sQ + t * C::Q_BYTES + b * BM * 128, &tm_q, &bars->q_full, b * 64, u.h * a.group,
+              tma_load_3d(to + t * C::Q_BYTES + b * BM * 128, &tm_q, bar, b * 64, u.h * a.group,
                           u.t0 + u.i0 + t * a.tile_tokens);
         }
       }
@@ -339,6 +528,19 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         ok = !aborted(bars) && ok;
         if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
         fetch_pages<HD * (F8 ? 1 : 2), F8>(a, u, map, dst + s * bytes, &full[s], tile_pos(u, k0 + j), lane);
+      }
+      if (is_k) {
+        // all keys are under way: the next unit (none where CTAs have one unit: stop = 0)
+        at += u.work;
+        Cut* cut = nullptr;
+        if (at >= stop && round < d.rounds) {
+          if (++round == d.rounds) cut = a.cuts + blockIdx.x;
+          at = round < d.rounds ? ((int64_t)round * gridDim.x + blockIdx.x) * d.each : d.base + blockIdx.x * d.share;
+          stop = round < d.rounds ? at + d.each : min(at + d.share, d.total);
+        }
+        if (at >= stop) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        const Unit next = unit_at(a, d, at, stop, lane, cut);
+        if (lane == 0) bars->next = next;
       }
     } else if (warp == 3 && !F8) {
       // ------------------------------------------------------------ V of tiles that not all rows see
@@ -493,15 +695,14 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       mbar_wait(&bars->fin, 0, lim);
     }
     __syncwarp();
-    tc_fence_before();
-    end_barrier<C::THREADS>();
-    if (warp == 1) {
-      tc_fence_after();
-      tmem_dealloc(tmem, kTmemCols);
+    if (!another()) break;
     }
+    if (warp == 1) tmem_dealloc(tmem, kTmemCols);
   } else if (warp < 12) {
     setmaxnreg_inc<C::REGS_SOFTMAX>();
-    {
+    for (;;) {
+        const int k0 = u.k0, n_tiles = u.n_tiles;
+      const bool has_q1 = u.i0 + a.tile_tokens < u.n_new;   // else the warpgroups share the key tiles
       // ------------------------------------------------------------ softmax and result
       const int t = warp < 8 ? 0 : 1;
       const int qt = has_q1 ? t : 0;         // the query tile of this warpgroup
@@ -521,42 +722,46 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       float unit = a.scale_log2;   // what the row's S is multiplied by (and, with 8-bit pages, by their scales)
       if constexpr (F8) {
         // the row as two e4m3 pieces of row * 2^-ex; without a second tile both warpgroups have the row
-        const __nv_bfloat16* src =
-            a.q + (int64_t)(u.t0 + (live ? i : 0)) * a.q_stride + (u.h * a.group + (live ? row - tok * a.group : 0)) * HD;
-        float top = -1.f;
+        if (n_tiles > 0) {
+          bool w = !aborted(bars) && mbar_wait(&bars->q_raw, 0, lim);
+          if (!__all_sync(0xffffffffu, w)) set_abort(bars);
+          const uint8_t* src = sV + qt * C::Q_BYTES + row * 128;
+          auto eight = [&](int c) {   // channels 8 c .. 8 c + 7
+            return live ? *reinterpret_cast<const uint4*>(src + (c / 8) * BM * 128 + ((c ^ row) & 7) * 16) : make_uint4(0, 0, 0, 0);
+          };
+          uint32_t top = 0;   // magnitudes order as their bits
 #pragma unroll 4
-        for (int c = 0; c < HD; c += 8) {
-          float x[8];
-          unpack8(__ldg(reinterpret_cast<const uint4*>(src + c)), x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (fabsf(x[e]) < INFINITY) top = fmaxf(top, fabsf(x[e]));
-        }
-        const int ex = scale_exponent(top);
-        unit *= pow2f(ex);
-        if (qt == t) {
-          const float down = live ? pow2f(-ex) : 0.f;
-          uint8_t* piece = sQ + t * C::Q_BYTES;
-#pragma unroll 2
-          for (int c = 0; c < HD; c += 8) {
-            float x[8], y[8];
-            unpack8(live ? __ldg(reinterpret_cast<const uint4*>(src + c)) : make_uint4(0, 0, 0, 0), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= down;
-            const uint2 w = encode8(x);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t two = (e < 2 ? w.x : w.y) >> (16 * (e & 1));
-              const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3));
-              y[2 * e] = x[2 * e] - __low2float(h);
-              y[2 * e + 1] = x[2 * e + 1] - __high2float(h);
-            }
-            const int chunk = c / 16;
-            const int at = (HD == 128 ? row * 128 + ((chunk ^ row) & 7) * 16 : row * 64 + ((chunk ^ (row >> 1)) & 3) * 16) + c % 16;
-            *reinterpret_cast<uint2*>(piece + at) = w;
-            *reinterpret_cast<uint2*>(piece + BM * HD + at) = encode8(y);
+          for (int c = 0; c < HD / 8; ++c) {
+            const uint4 x = eight(c);
+            top = max(top, max(max(x.x & 0x7fff0000u, (x.x << 16) & 0x7fff0000u), max(x.y & 0x7fff0000u, (x.y << 16) & 0x7fff0000u)));
+            top = max(top, max(max(x.z & 0x7fff0000u, (x.z << 16) & 0x7fff0000u), max(x.w & 0x7fff0000u, (x.w << 16) & 0x7fff0000u)));
           }
-          fence_proxy_async_smem();
+          const int ex = scale_exponent(__uint_as_float(top));
+          // a row that is not finite has no finite logit
+          unit = top >= 0x7f800000u && hi > 0 ? __int_as_float(0x7fffffff) : unit * pow2f(ex);
+          if (qt == t) {
+            const float down = pow2f(-ex);
+            uint8_t* piece = sQ + t * C::Q_BYTES;
+#pragma unroll 2
+            for (int c = 0; c < HD / 8; ++c) {
+              float x[8];
+              unpack8(eight(c), x);
+              uint32_t w1[2], w2[2];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float y0 = x[2 * e] * down, y1 = x[2 * e + 1] * down;
+                const uint32_t q1 = code2(y0, y1);
+                const __half2 h(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)q1, __NV_E4M3));
+                const uint32_t q2 = code2(y0 - __low2float(h), y1 - __high2float(h));
+                w1[e >> 1] = e & 1 ? w1[e >> 1] | q1 << 16 : q1;
+                w2[e >> 1] = e & 1 ? w2[e >> 1] | q2 << 16 : q2;
+              }
+              const int at = (HD == 128 ? row * 128 + (((c >> 1) ^ row) & 7) * 16 : row * 64 + (((c >> 1) ^ (row >> 1)) & 3) * 16) + (c & 1) * 8;
+              *reinterpret_cast<uint2*>(piece + at) = make_uint2(w1[0], w1[1]);
+              *reinterpret_cast<uint2*>(piece + BM * HD + at) = make_uint2(w2[0], w2[1]);
+            }
+            fence_proxy_async_smem();
+          }
         }
         mbar_arrive(&bars->q_full);
       }
@@ -586,32 +791,43 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       bool ok = true;
       uint32_t fixed = 0;
+      const bool some_live = __any_sync(0xffffffffu, live);   // else this warp's rows are nobody's
       for (int j = j0; j < n_tiles; j += every) {
+        if (!some_live) {
+          const bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)(has_q1 ? j : j >> 1) & 1u, lim);
+          if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
+          mbar_arrive(&bars->p_full[t]);
+          continue;
+        }
         const float2 scale = next;
         if (F8 && j + every < n_tiles) next = scales_of(j + every);
         bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)(has_q1 ? j : j >> 1) & 1u, lim);
         if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
         tc_fence_after();
-        uint32_t sr[BN];
-        tmem_ld_x64(tl + colS, sr);
-        tmem_ld_x64(tl + colS + 64, sr + 64);
         const int pos = tile_pos(u, k0 + j);
         const bool whole = all_see(u, pos);
         if (!whole) {
-          // columns below hi - pos and (from lo - pos on, or below sinks - pos)
-          const int ch = hi - pos, cl = lo - pos, cs = sinks - pos;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            auto below = [&](int c) {   // bits of columns 32b .. 32b+31 that are below c
-              const int k = c - 32 * b;
+          // S of columns that the row does not see (not below hi - pos, or below lo - pos and not below
+          // sinks - pos) becomes -inf where it lies.  What few tiles need is kept in short loops: the
+          // code that every tile runs has to stay in the instruction cache, for three kinds of warps.
+#pragma unroll 1
+          for (int b = 0; b < BN; b += 32) {
+            uint32_t x[32];
+            tmem_ld_x32(tl + colS + b, x);
+            auto below = [&](int c) {   // bits of columns b .. b + 31 that are below c
+              const int k = c - b;
               return k <= 0 ? 0u : k >= 32 ? 0xffffffffu : (1u << k) - 1u;
             };
-            const uint32_t see = below(ch) & (~below(cl) | below(cs));
+            const uint32_t see = below(hi - pos) & (~below(lo - pos) | below(sinks - pos));
 #pragma unroll
             for (int c = 0; c < 32; ++c)
-              if (!((see >> c) & 1u)) sr[32 * b + c] = __float_as_uint(-INFINITY);
+              if (!((see >> c) & 1u)) x[c] = __float_as_uint(-INFINITY);
+            tmem_st_x32(tl + colS + b, x);
           }
         }
+        uint32_t sr[BN];
+        tmem_ld_x64(tl + colS, sr);
+        tmem_ld_x64(tl + colS + 64, sr + 64);
         float mx = -INFINITY;
         if constexpr (F8) {
 #pragma unroll
@@ -688,13 +904,13 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         tmem_st_x64(tl + colS, sr);
         if (j > 0 && __any_sync(0xffffffffu, need)) {
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            uint32_t x[32];
+            tmem_ld_x32(tl + colO + c, x);
 #pragma unroll
-          for (int half = 0; half < HD / 64; ++half) {
-            uint32_t orr[64];
-            tmem_ld_x64(tl + colO + half * 64, orr);
-#pragma unroll
-            for (int c = 0; c < 64; ++c) orr[c] = __float_as_uint(__uint_as_float(orr[c]) * corr);
-            tmem_st_x64(tl + colO + half * 64, orr);
+            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * corr);
+            tmem_st_x32(tl + colO + c, x);
           }
         }
         if (!whole) {
@@ -744,10 +960,10 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       tc_fence_after();
       const float o_unit = F8 ? exp2_fast(e_ref) * 0x1p-7f : 1.f;
       float* other = reinterpret_cast<float*>(sV);   // [HD][128]: o of the second warpgroup (every product is done)
-      const bool join = a.n_split == 1 && !has_q1;
+      const bool join = u.slot < 0 && !has_q1;
       if (join) {
         if (t == 1 && ok) {
-#pragma unroll
+#pragma unroll 1
           for (int half = 0; half < HD / 64; ++half) {
             uint32_t orr[64];
             tmem_ld_x64(tl + colO + half * 64, orr);
@@ -758,7 +974,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         ok = !bar_sync_or(3, 256, !ok);
       }
-      if (ok && a.n_split == 1 && qt == t) {
+      if (ok && u.slot < 0 && qt == t) {
         const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
         float f0 = o_unit, f1 = 0.f;   // of this warpgroup's o, and of the second's
         if (join) {
@@ -771,7 +987,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           f0 *= o_unit;
         }
         const float inv = l == 0.f ? 0.f : (join ? 1.f : f0) / l;
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
@@ -780,28 +996,40 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll
             for (int c = 0; c < 64; ++c) v[c] = f0 * v[c] + f1 * other[(half * 64 + c) * 128 + row];
           }
-          if (live && a.o_f32) {
-            float* dst = static_cast<float*>(a.o) + out * HD + half * 64;
+          if (a.o_f32) {
+            if (live) {
+              float* dst = static_cast<float*>(a.o) + out * HD + half * 64;
 #pragma unroll
-            for (int c = 0; c < 64; c += 4)
-              *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[c + 1] * inv,
-                                                                v[c + 2] * inv, v[c + 3] * inv);
-          } else if (live) {
-            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.o) + out * HD + half * 64;
+              for (int c = 0; c < 64; c += 4)
+                *reinterpret_cast<float4*>(dst + c) = make_float4(v[c] * inv, v[c + 1] * inv, v[c + 2] * inv, v[c + 3] * inv);
+            }
+          } else {
+            // through the queries' place (every product is done), so that eight lanes write a row's 128 bytes
+            uint8_t* stage = sQ + (warp - 4) * 4096;
 #pragma unroll
             for (int c = 0; c < 64; c += 8) {
               float y[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) y[e] = v[c + e] * inv;
-              *reinterpret_cast<uint4*>(dst + c) = pack8(y);
+              *reinterpret_cast<uint4*>(stage + lane * 128 + (((c / 8) ^ lane) & 7) * 16) = pack8(y);
+            }
+            __syncwarp();
+            const uint32_t rows = __ballot_sync(0xffffffffu, live);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int r = 4 * k + (lane >> 3);
+              const int64_t to = __shfl_sync(0xffffffffu, out, r);
+              const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 128 + ((lane ^ r) & 7) * 16);
+              if ((rows >> r) & 1u)
+                *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + to * HD + half * 64 + (lane & 7) * 8) = x;
             }
           }
           __syncwarp();
         }
         if (a.lse && live) a.lse[out] = l == 0.f ? -INFINITY : (m_ref + log2f(l)) * 0.69314718055994531f;
-      } else if (ok && a.n_split > 1) {
-        const int64_t slot = (int64_t)place * a.n_split + part;
-#pragma unroll
+      } else if (ok && u.slot >= 0) {
+        const int64_t slot = u.slot;
+#pragma unroll 1
         for (int half = 0; half < HD / 64; ++half) {
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
@@ -820,16 +1048,19 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         if (live) __stcg(a.part_ml + slot * 256 + t * 128 + row, make_float2(m_ref, l));
       }
+      if (!another()) break;
     }
-    tc_fence_before();
-    end_barrier<C::THREADS>();
   } else if constexpr (F8) {
     // -------------------------------------------------------------- V codes to f16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
     const int tid = threadIdx.x - 384;
     constexpr int CH = HD / 16;   // 16-code chunks of a row
-    bool ok = true;
-    for (int j = 0; j < n_tiles; ++j) {
+    for (;;) {
+    const int k0 = u.k0, n_tiles = u.n_tiles;
+    // the queries lie in the V tiles' place until they are split
+    bool ok = n_tiles == 0 || (!aborted(bars) && mbar_wait(&bars->q_full, 0, lim));
+    ok = !bar_sync_or(2, 128, !ok);
+    for (int j = 0; ok && j < n_tiles; ++j) {
       const int s = j % kStages, pos = tile_pos(u, k0 + j);
       const bool whole = all_see(u, pos);
       const uint32_t ph = (uint32_t)(j / kStages) & 1u;
@@ -872,47 +1103,62 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       mbar_arrive(&bars->raw_empty[s]);
     }
     if (!ok) set_abort(bars);
-    end_barrier<C::THREADS>();
+    if (!another()) break;
+    }
   }
 }
 
-// Joins the parts of the units: one CTA for 32 rows of a unit.
+// Joins the parts of the units that no CTA had whole: CTA (x, y) takes 32 rows (a lane each, four channels a
+// warp at a time) of the unit that the share of CTA x + 1 begins inside of, if that is the first such share.
+constexpr int kMergeWarps = 16;
 template <int HD>
-__global__ void __launch_bounds__(256) k_tiles_merge(const __grid_constant__ TilesKArgs a) {
-  __shared__ Unit su;
+__global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_constant__ TilesKArgs a) {
+  __shared__ float2 s_ml[kMergeWarps][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (threadIdx.x < 32) {
-    const Unit u = unit_of(a, blockIdx.x, threadIdx.x);
-    if (threadIdx.x == 0) su = u;
-  }
-  __syncthreads();
-  const Unit u = su;
-  if (!u.valid) return;
-  const int row = blockIdx.y * 32 + (threadIdx.x & 31);   // of the unit's 256
-  const int t = row >> 7, tok = (row & 127) / a.group, i = u.i0 + t * a.tile_tokens + tok;
-  if (tok >= a.tile_tokens || i >= u.n_new) return;
-  // a unit of one tile has two places of each row in a part
+  const Cut u = a.cuts[blockIdx.x + 1];
+  if (u.c0 != (int)blockIdx.x) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.y >> 2;
+  // the first CTA began the unit (its second place), the others began inside it (their first place); a
+  // unit of one tile has two places of each row in a part
+  const int c0 = u.c0;
   const bool pair = u.i0 + a.tile_tokens < u.n_new;
-  const int n = pair ? a.n_split : 2 * a.n_split;
-  const int64_t slot0 = (int64_t)blockIdx.x * a.n_split;
-  auto slot = [&](int p) { return pair ? slot0 + p : slot0 + (p >> 1); };
-  auto place = [&](int p) { return pair ? row : row + (p & 1) * 128; };
-  float top = -INFINITY;
-  for (int p = 0; p < n; ++p) top = fmaxf(top, a.part_ml[slot(p) * 256 + place(p)].x);
-  float l = 0.f;
-  for (int p = 0; p < n; ++p) {
-    const float2 v = a.part_ml[slot(p) * 256 + place(p)];
-    l += v.x == -INFINITY ? 0.f : exp2_fast(v.x - top) * v.y;
+  const int n = (u.c1 - c0 + 1) * (pair ? 1 : 2);
+  if (t == 1 && !pair) return;
+  auto slot = [&](int p) {
+    const int64_t c = c0 + (pair ? p : p >> 1);
+    return 2 * c + (c == c0 ? 1 : 0);
+  };
+  const int row = (blockIdx.y & 3) * 32 + lane, tok = row / a.group, i = u.i0 + t * a.tile_tokens + tok;
+  const bool in = tok < a.tile_tokens && i < u.n_new;
+  if (!__any_sync(0xffffffffu, in)) return;   // the same rows in every warp
+  auto place = [&](int p) { return pair ? t * 128 + row : row + (p & 1) * 128; };
+  // maximum and sum: each warp over some of the parts, then over the warps
+  float top = -INFINITY, l = 0.f;
+  if (in)
+    for (int p = warp; p < n; p += kMergeWarps) {
+      const float2 v = a.part_ml[slot(p) * 256 + place(p)];
+      const float m = fmaxf(top, v.x);
+      l = (top == -INFINITY ? 0.f : l * exp2_fast(top - m)) + (v.x == -INFINITY ? 0.f : v.y * exp2_fast(v.x - m));
+      top = m;
+    }
+  s_ml[warp][lane] = make_float2(top, l);
+  __syncthreads();
+  for (int w = 0; w < kMergeWarps; ++w) top = fmaxf(top, s_ml[w][lane].x);
+  l = 0.f;
+  for (int w = 0; w < kMergeWarps; ++w) {
+    const float2 v = s_ml[w][lane];
+    l += v.x == -INFINITY ? 0.f : v.y * exp2_fast(v.x - top);
   }
+  if (!in) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + ((row & 127) - tok * a.group);
-  for (int c = threadIdx.x >> 5; c < HD / 4; c += 8) {
+  const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
+  for (int c = warp; c < HD / 4; c += kMergeWarps) {
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
     for (int p = 0; p < n; ++p) {
       const float m = a.part_ml[slot(p) * 256 + place(p)].x;
-      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
       const float4 y = a.part_o[(slot(p) * (HD / 4) + c) * 256 + place(p)];
+      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
       acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
     }
     if (a.o_f32) {
@@ -923,7 +1169,7 @@ __global__ void __launch_bounds__(256) k_tiles_merge(const __grid_constant__ Til
           make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
     }
   }
-  if (a.lse && threadIdx.x < 32) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+  if (a.lse && warp == 0) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------- host side
@@ -947,14 +1193,11 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   const cuuint32_t kb[3] = {F8 ? HD : 64, (cuuint32_t)c.page_size, 1};
   // operand tiles are swizzled by their rows' 128 (or 64) bytes; V codes pass through registers
   const CUtensorMapSwizzle operand = F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
-  bool ok = encode(&mk, elt, operand, c.k, kd, ks, kb) && encode(&mv, elt, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : operand, c.v, kd, ks, kb);
-  if (F8) {
-    mq = mk;   // queries are read and split by the kernel
-  } else if (ok) {
-    const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
-    const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
-    ok = encode(&mq, 2, CU_TENSOR_MAP_SWIZZLE_128B, a.q, qd, qs, qb);
-  }
+  const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
+  const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
+  const bool ok = encode(&mk, elt, operand, c.k, kd, ks, kb) &&
+                  encode(&mv, elt, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : operand, c.v, kd, ks, kb) &&
+                  encode(&mq, 2, CU_TENSOR_MAP_SWIZZLE_128B, a.q, qd, qs, qb);
   if (!ok) return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
   static std::atomic<uint64_t> attr_done{0};
   cast_status setup = CAST_OK;
@@ -970,13 +1213,15 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
         return cudaFuncSetAttribute(k_cache_tiles<HD, F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
       }))
     return setup != CAST_OK ? setup : check_launch("cache attention kernel attributes");
-  const int64_t units = (int64_t)p.pairs * c.H;
-  k_cache_tiles<HD, F8><<<(unsigned)(units * p.n_split), C::THREADS, C::SMEM, st>>>(mq, mk, mv, k);
+  k_cache_tiles<HD, F8><<<(unsigned)p.grid, C::THREADS, C::SMEM, st>>>(mq, mk, mv, k);
   cast_status s = check_launch("cache attention");
-  if (s || p.n_split == 1) return s;
+  if (s || p.whole || p.grid == 1) return s;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)units, 8, 1);
-  cfg.blockDim = dim3(256, 1, 1);
+  // 32 rows of a unit a CTA, as many as a unit may have
+  const int most = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
+  const int rows = most > k.tile_tokens ? 8 : (most * k.group + 31) / 32;
+  cfg.gridDim = dim3((unsigned)(p.grid - 1), rows, 1);
+  cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1009,31 +1254,19 @@ TilesPlan tiles_plan(const cast_cache_attn_args& a) {
   int dev = 0, nsm = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
   if (nsm < 1) nsm = 1;
-  // The split with the least estimated time: rounds of one CTA an SM, each as long as its part's tiles
-  // (about 1.7 us each, 0.9 for units of one tile) and a fixed 4 us, and for a split the parts written
-  // and read again and the second launch.
-  const double tile_us = max_new <= p.tile_tokens ? 0.9 : 1.7;
-  double best = 0;
-  p.n_split = 1;
-  for (int n = 1; n <= 64 && (n == 1 || tiles / n >= 2); ++n) {
-    const double rounds = (double)((units * n + nsm - 1) / nsm);
-    double us = rounds * ((double)((tiles + n - 1) / n) * tile_us + 4.0);
-    if (n > 1) us += 4.0 + (double)(units * n) * 256 * d * 4 * 2 / 4e6;
-    if (n == 1 || us < best) {
-      best = us;
-      p.n_split = n;
-    }
-  }
-  if (p.n_split > 1) {
-    p.part_o_bytes = align_up((size_t)units * p.n_split * 256 * d * sizeof(float));
-    p.total_bytes = p.part_o_bytes + align_up((size_t)units * p.n_split * 256 * sizeof(float2));
+  p.whole = tiles <= 8;
+  p.grid = p.whole ? units : nsm;
+  if (!p.whole) {
+    p.part_o_bytes = align_up((size_t)2 * p.grid * 256 * d * sizeof(float));
+    p.part_ml_bytes = align_up((size_t)2 * p.grid * 256 * sizeof(float2));
+    p.total_bytes = p.part_o_bytes + p.part_ml_bytes + align_up((size_t)p.grid * sizeof(Cut));
   }
   return p;
 }
 
 cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void* ws, cudaStream_t st) {
   const cast_kv_cache& c = a.cache;
-  if ((int64_t)p.pairs * c.H * p.n_split > 0x7fffffff)
+  if ((int64_t)p.pairs * c.H > 0x7fffffff)
     return fail(CAST_ERR_UNSUPPORTED, "cast_cache_attention: too many units");
   TilesKArgs k{};
   k.batch = a.batch;
@@ -1049,8 +1282,6 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.sinks = k.window > 0 ? a.sinks : 0;
   k.o_f32 = a.o_dtype == CAST_F32;
   k.row_stride = c.row_stride;
-  k.q = static_cast<const __nv_bfloat16*>(a.q);
-  k.q_stride = a.q_row_stride;
   k.v = static_cast<const uint8_t*>(c.v);
   k.k_scale = c.k_scale;
   k.v_scale = c.v_scale;
@@ -1059,9 +1290,12 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;
   if (!(k.error = cache_error_address())) return check_launch("cache error word");
   k.pairs = p.pairs;
-  k.n_split = p.n_split;
+  k.most_pairs = (int)(((a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens));
+  k.whole = p.whole;
+  k.least = 12;   // four key tiles: a segment's fixed time
   k.part_o = static_cast<float4*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
+  k.cuts = reinterpret_cast<Cut*>(static_cast<char*>(ws) + p.part_o_bytes + p.part_ml_bytes);
   k.wait_ns = 2000000000ull;
   if (c.dtype == CAST_F8E4M3) return c.d == 128 ? launch<128, true>(a, k, p, st) : launch<64, true>(a, k, p, st);
   return c.d == 128 ? launch<128, false>(a, k, p, st) : launch<64, false>(a, k, p, st);

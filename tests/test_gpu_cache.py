@@ -290,6 +290,10 @@ ATTEND = [
     ([2000], [150], 1, 1, 64, 64, False, 64, 100),
     ([400, 3, 1030], [33, 3, 1], 1, 24, 64, 32, True, 0, 0),
     ([200], [3], 1, 100, 128, 16, True, 0, 0),        # a group that fills most of a tile
+    ([3000, 1500, 40], [700, 300, 40], 2, 6, 128, 64, True, 0, 0),
+    ([4000, 1, 2600], [150, 1, 513], 3, 3, 64, 16, True, 900, 200),
+    ([2900], [130], 2, 2, 128, 128, False, 0, 0),
+    ([1400] * 20, [17 + i for i in range(20)], 1, 2, 64, 32, True, 0, 0),
 ]
 
 
