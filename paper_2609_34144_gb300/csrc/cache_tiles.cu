@@ -53,9 +53,9 @@ struct Cfg {
   static constexpr int THREADS = F8 ? 512 : 384;
   // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
   static constexpr int LAUNCH = F8 ? 128 : 168;
-  static constexpr int REGS_CTL = F8 ? 64 : 96;
-  static constexpr int REGS_SOFTMAX = F8 ? 192 : 200;
-  static constexpr int REGS_DECODE = 64;
+  static constexpr int REGS_CTL = F8 ? 72 : 96;
+  static constexpr int REGS_SOFTMAX = F8 ? 184 : 200;
+  static constexpr int REGS_DECODE = 72;
   static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
                 "register split exceeds the launch allocation");
   static constexpr int Q_BYTES = BM * HD * 2;               // 8 bits: two pieces of BM * HD
