@@ -187,26 +187,30 @@ struct Deal {
 };
 __device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) {   // one warp; every lane has it
   Deal d{};
-  for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += __reduce_add_sync(0xffffffffu, chunk_work(a, b0, lane));
-  d.total = (int64_t)d.per_head * a.H;
-  if (a.batch.B == 1 && !a.causal) {
-    // one sequence without a causal mask: its units differ at most by the last one's rows and the window
+  if (a.batch.B == 1) {
     const Sequence s = sequence_of(a.batch, 0);
     const int n = min(s.n_new, a.batch.max_new), per = 2 * a.tile_tokens;
     Unit u{};
     int low = 0x7fffffff, high = 0;
     for (u.i0 = lane * per; u.i0 < n; u.i0 += 32 * per) {
       place_unit(a, u, s);
-      low = min(low, unit_work(a, u));
-      high = max(high, unit_work(a, u));
+      const int w = unit_work(a, u);
+      d.per_head += w;
+      low = min(low, w);
+      high = max(high, w);
     }
+    d.per_head = __reduce_add_sync(0xffffffffu, d.per_head);
     low = __reduce_min_sync(0xffffffffu, low);
     high = __reduce_max_sync(0xffffffffu, high);
+    d.total = (int64_t)d.per_head * a.H;
     if (low == high) {
       d.each = high;
       d.rounds = (int)(d.total / high / ctas);
       d.base = (int64_t)d.rounds * ctas * high;
     }
+  } else {
+    for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += __reduce_add_sync(0xffffffffu, chunk_work(a, b0, lane));
+    d.total = (int64_t)d.per_head * a.H;
   }
   d.share = max((int64_t)a.least, (d.total - d.base + ctas - 1) / ctas);
   return d;
@@ -248,8 +252,8 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
   if (cut && lane == 0) cut->c0 = -1;
   if (at >= stop) return u;
   const int h = (int)(at / d.per_head), per = 2 * a.tile_tokens;
-  int r = (int)(at - (int64_t)h * d.per_head), b = -1;
-  for (int b0 = 0; b0 < a.batch.B; b0 += 32) {
+  int r = (int)(at - (int64_t)h * d.per_head), b = a.batch.B == 1 ? 0 : -1;
+  for (int b0 = 0; b < 0 && b0 < a.batch.B; b0 += 32) {
     const int w = chunk_work(a, b0, lane);
     const int sum = scan(w, lane);
     const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
@@ -257,9 +261,9 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
       const int l = __ffs(hit) - 1;
       r -= __shfl_sync(0xffffffffu, sum - w, l);
       b = b0 + l;
-      break;
+    } else {
+      r -= __shfl_sync(0xffffffffu, sum, 31);
     }
-    r -= __shfl_sync(0xffffffffu, sum, 31);
   }
   if (b < 0) return u;
   const Sequence s = sequence_of(a.batch, b);
@@ -722,7 +726,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       float unit = a.scale_log2;   // what the row's S is multiplied by (and, with 8-bit pages, by their scales)
       if constexpr (F8) {
         // the row as two e4m3 pieces of row * 2^-ex; without a second tile both warpgroups have the row
-        if (n_tiles > 0) {
+        if (n_tiles > 0 && __any_sync(0xffffffffu, live)) {
           bool w = !aborted(bars) && mbar_wait(&bars->q_raw, 0, lim);
           if (!__all_sync(0xffffffffu, w)) set_abort(bars);
           const uint8_t* src = sV + qt * C::Q_BYTES + row * 128;
@@ -739,11 +743,12 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           const int ex = scale_exponent(__uint_as_float(top));
           // a row that is not finite has no finite logit
           unit = top >= 0x7f800000u && hi > 0 ? __int_as_float(0x7fffffff) : unit * pow2f(ex);
-          if (qt == t) {
+          {
             const float down = pow2f(-ex);
-            uint8_t* piece = sQ + t * C::Q_BYTES;
+            uint8_t* piece = sQ + qt * C::Q_BYTES;
+            const int c0 = has_q1 ? 0 : t * (HD / 16), c1 = has_q1 ? HD / 8 : c0 + HD / 16;   // or half of the row each
 #pragma unroll 2
-            for (int c = 0; c < HD / 8; ++c) {
+            for (int c = c0; c < c1; ++c) {
               float x[8];
               unpack8(eight(c), x);
               uint32_t w1[2], w2[2];
