@@ -1059,7 +1059,12 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     // -------------------------------------------------------------- V codes to f16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
     const int tid = threadIdx.x - 384;
-    constexpr int CH = HD / 16;   // 16-code chunks of a row
+    constexpr int CH = HD / 16;   // 16-code chunks of a row, and of a thread
+    const int quarter = lane & 3, second = (lane >> 2) & 1, w4 = warp & 3;
+    auto row_of = [&](int i) {
+      if (HD == 128) return ((i >> 1) * 4 + w4) * 8 + ((lane >> 3) ^ (second * 5));
+      return (i * 4 + w4) * 8 + (lane >> 3) * 2 + second;
+    };
     for (;;) {
     const int k0 = u.k0, n_tiles = u.n_tiles;
     // the queries lie in the V tiles' place until they are split
@@ -1083,25 +1088,28 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         if (lane == 0) bars->apart[s][tid >> 5] = apart;
         asm volatile("bar.sync 2, 128;" ::: "memory");
       }
-#pragma unroll 4
+      // A thread has chunk `quarter` of 64 channels in CH rows; all its loads come first.  Eight lanes
+      // have four chunks of two rows: of rows r and r ^ 5 the swizzled codes lie in eight bank groups, and
+      // so do the f16 chunks they become (64-channel heads: rows r and r + 1 of unswizzled codes).
+      uint4 codes[CH];
+#pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const int x = tid + 128 * i, r = x / CH, cc = x % CH;
-        // 16 codes are two 16-byte chunks of the f16 row; the lanes of the second 64 channels take
-        // theirs in the other order, so that eight lanes store to eight bank groups
-        const int swap = (cc >> 2) & 1;
-        const uint2 w0 = *reinterpret_cast<const uint2*>(src + x * 16 + swap * 8);
-        const uint2 w1 = *reinterpret_cast<const uint2*>(src + x * 16 + (swap ^ 1) * 8);
+        const int r = row_of(i), box = HD == 128 ? i & 1 : 0;
+        codes[i] = *reinterpret_cast<const uint4*>(src + r * HD + (HD == 128 ? ((box * 4 + quarter) ^ r) & 7 : quarter) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int r = row_of(i), box = HD == 128 ? i & 1 : 0;
         uint4 o0, o1;
-        half4(w0.x, o0.x, o0.y);
-        half4(w0.y, o0.z, o0.w);
-        half4(w1.x, o1.x, o1.y);
-        half4(w1.y, o1.z, o1.w);
+        half4(codes[i].x, o0.x, o0.y);
+        half4(codes[i].y, o0.z, o0.w);
+        half4(codes[i].z, o1.x, o1.y);
+        half4(codes[i].w, o1.z, o1.w);
         if (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)))
           o0 = o1 = make_uint4(0, 0, 0, 0);
-        uint8_t* base = dst + (cc / 4) * BN * 128 + r * 128;
-        const int c0 = 2 * (cc & 3) + swap;
-        *reinterpret_cast<uint4*>(base + ((c0 ^ r) & 7) * 16) = o0;
-        *reinterpret_cast<uint4*>(base + ((c0 ^ 1 ^ r) & 7) * 16) = o1;
+        uint8_t* base = dst + box * BN * 128 + r * 128;
+        *reinterpret_cast<uint4*>(base + (((2 * quarter) ^ r) & 7) * 16) = o0;
+        *reinterpret_cast<uint4*>(base + (((2 * quarter + 1) ^ r) & 7) * 16) = o1;
       }
       fence_proxy_async_smem();
       mbar_arrive(&bars->v_full[s]);
@@ -1201,7 +1209,7 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
   const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
   const bool ok = encode(&mk, elt, operand, c.k, kd, ks, kb) &&
-                  encode(&mv, elt, F8 ? CU_TENSOR_MAP_SWIZZLE_NONE : operand, c.v, kd, ks, kb) &&
+                  encode(&mv, elt, F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, c.v, kd, ks, kb) &&
                   encode(&mq, 2, CU_TENSOR_MAP_SWIZZLE_128B, a.q, qd, qs, qb);
   if (!ok) return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
   static std::atomic<uint64_t> attr_done{0};
