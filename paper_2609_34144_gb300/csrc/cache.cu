@@ -175,23 +175,31 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
       continue;
     }
     if constexpr (F8) {
-      // the page's scale for this head: magnitudes of finite values order as their bits
-      uint32_t top = 0;
-      if (in) {
+      // the page's scale for this head: the largest magnitude of the tile (magnitudes order as their
+      // bits; NaN is passed over), or, if that is infinite, the largest finite one
+      float mine = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
-          if (m < 0x7f800000u) top = max(top, m);
-        }
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
+      for (int i = 0; i < 16; ++i) mine = fmaxf(mine, fabsf(v[i]));
+      uint32_t top = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(mine) : 0u);
       if ((threadIdx.x & 31) == 0) s_max[h & 1][threadIdx.x >> 5] = top;
       float* scale = (kind == 0 ? a.k_scale : a.v_scale) + (int64_t)page * a.H + h;
       const float old = lo > 0 ? *scale : 0.f;
       __syncthreads();
       const int warps = blockDim.x / 32;
-      top = (threadIdx.x & 31) < warps ? s_max[h & 1][threadIdx.x & 31] : 0u;
-      top = __reduce_max_sync(0xffffffffu, top);
+      top = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < warps ? s_max[h & 1][threadIdx.x & 31] : 0u);
+      if (top >= 0x7f800000u) {   // every thread alike
+        mine = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (isinf(v[i])) v[i] = __int_as_float(0x7fffffff);   // the format has no infinity
+          mine = fmaxf(mine, fabsf(v[i]));
+        }
+        top = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(mine) : 0u);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s_max[h & 1][threadIdx.x >> 5] = top;
+        __syncthreads();
+        top = __reduce_max_sync(0xffffffffu, (threadIdx.x & 31) < warps ? s_max[h & 1][threadIdx.x & 31] : 0u);
+      }
       const float now = fmaxf(pow2f(scale_exponent(__uint_as_float(top))), old);
       const float inv = 1.f / now;   // exact: a power of two within 2^-120 .. 2^120
       uint8_t* cache = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv);
@@ -467,8 +475,8 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   const int64_t gx = (int64_t)k.runs * a->batch.B;
   if (gx > 0x7fffffff) return fail(CAST_ERR_UNSUPPORTED, "%s: %lld page runs", who, (long long)gx);
   const int threads = c.page_size * c.d / 16;
-  // heads of one CTA: eight share the angles' cost, fewer where the grid would not fill the SMs twice
-  int group = 8;
+  // heads of one CTA: twelve share the angles' cost, fewer where the grid would not fill the SMs twice
+  int group = 12;
   while (group > 1 &&
          gx * (2 * ((c.H + group - 1) / group) + (k.H_q + group - 1) / group) * threads < (int64_t)2 * 152 * 2048)
     group /= 2;

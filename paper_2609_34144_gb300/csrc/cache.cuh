@@ -90,26 +90,16 @@ __device__ __forceinline__ uint4 pack8(const float* v) {
 }
 
 // ------------------------------------------------------------------ 8-bit pages
-// 8 floats -> 8 e4m3 codes, to nearest even; the caller's values are within +-448 or not finite
-// (NaN and, since the format has none, infinity become NaN).
-__device__ __forceinline__ uint2 encode8(const float* v) {
-  uint32_t w[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    uint32_t r = 0;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float2 x = make_float2(v[4 * i + 2 * j], v[4 * i + 2 * j + 1]);
-      if (isinf(x.x)) x.x = __int_as_float(0x7fffffff);
-      if (isinf(x.y)) x.y = __int_as_float(0x7fffffff);
-      r |= (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) << (16 * j);
-    }
-    w[i] = r;
-  }
-  return make_uint2(w[0], w[1]);
+// Two floats within +-448 (or NaN) as e4m3 codes, to nearest even
+__device__ __forceinline__ uint32_t code2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
 }
-// Least e in [-120, 120] with amax <= 448 * 2^e (448 = 1.75 * 2^8).  A negative amax (no finite
-// value) counts as 0.
+__device__ __forceinline__ uint2 encode8(const float* v) {
+  return make_uint2(code2(v[0], v[1]) | code2(v[2], v[3]) << 16, code2(v[4], v[5]) | code2(v[6], v[7]) << 16);
+}
+// Least e in [-120, 120] with amax <= 448 * 2^e (448 = 1.75 * 2^8)
 __device__ __forceinline__ int scale_exponent(float amax) {
   if (!(amax > 0.f)) return -120;
   const uint32_t bits = __float_as_uint(amax);

@@ -329,12 +329,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Two floats within +-448 as e4m3 codes
-__device__ __forceinline__ uint32_t code2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
 template <bool F8>
 __device__ __forceinline__ void init_barriers(Bars* bars) {
   mbar_init(&bars->q_full, F8 ? 256 : 1);
