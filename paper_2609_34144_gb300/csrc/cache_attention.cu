@@ -529,7 +529,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
           weight = kLift + fmaxf(e - e_ref, -60.f);
           back = exp2_fast(-weight);
         }
-        uint32_t pf[MT][4];
+        // bf16 pages: a probability is two bf16 numbers (16 bits of it); memory leaves the time for the
+        // second product
+        uint32_t pf[MT][4], rest[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
@@ -553,6 +555,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
             for (int j = 0; j < 2; ++j) {
               const float x = s[m][t][2 * j], y = s[m][t][2 * j + 1];
               pf[m][2 * t + j] = F8 ? pack2h(x, y) : pack2(x, y);
+              if constexpr (!F8)
+                rest[m][2 * t + j] = pack2(x - __uint_as_float(pf[m][2 * t + j] << 16),
+                                           y - __uint_as_float(pf[m][2 * t + j] & 0xffff0000u));
             }
         }
         // A block that the rows do not all see, with a value that is not finite: 0 times it would
@@ -619,6 +624,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
             for (int m = 0; m < MT; ++m) {
               mma16816(o[m][2 * c], pf[m], w[0], w[1]);
               mma16816(o[m][2 * c + 1], pf[m], w[2], w[3]);
+              mma16816(o[m][2 * c], rest[m], w[0], w[1]);
+              mma16816(o[m][2 * c + 1], rest[m], w[2], w[3]);
             }
           }
         }
