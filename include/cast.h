@@ -513,10 +513,13 @@ typedef struct {
 
 /* o[t, h] = sum_j softmax_j(scale * q_t,h . k_j) v_j over the positions j that row t sees; a row that
  * sees none gives 0 (lse -inf).  The new tokens themselves are read from the cache: append first.
- * bf16 products (8-bit rows are decoded to bf16, exactly), f32 softmax and sums.  What lies at
- * positions that a row does not see never reaches it, whatever it holds.  The workspace
+ * f32 softmax and sums.  bf16 pages: bf16 products; a probability is rounded to bf16 before it meets its
+ * value (with few rows a sequence it is two bf16 numbers).  8-bit pages: the codes are multiplied as they
+ * are, queries as two numbers that keep them to 2^-19 of their row's largest channel or better,
+ * probabilities as f16 in units that keep a value to 2^-32 of the largest that the row meets or better.
+ * What lies at positions that a row does not see never reaches it, whatever it holds.  The workspace
  * (cast_cache_attention_workspace_size() bytes; NULL allowed when that is 0) holds partial results of
- * rows whose keys are split over several SMs.
+ * rows whose keys are split over several SMs.  One launch, or two where they are.
  * Errors: as cast_cache_append, and INVALID_ARG for H_q not a multiple of cache.H, a negative window
  * or sinks, a short workspace; UNSUPPORTED for H_q above 128 cache.H.  A page out of range reads as
  * zeros and positions past max_pages pages as not there; they and new tokens past max_new (whose rows

@@ -463,3 +463,105 @@ def test_attention_in_a_graph_follows_the_lengths(lib):
         k, v = P.rows(0)
         ref, _, eo, _ = R.attention(f64(q), k[:length], v[:length], 1, length)
         within(f64(out).reshape(1, 4, 64), ref, eo, f"length {length}")
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scales_far_apart_within_a_sequence(lib, new):
+    """V pages whose scales differ by up to 2^80, the largest first, last and in between: what small pages
+    weigh in the sum counts in full, and their values to the bound that the largest allows."""
+    for order in ([40, -40, 0, -3], [-40, 0, 40, -3], [-40, -3, 0, 40], [-120, -120, -120, -120], [100, 98, 100, 99]):
+        P = Pages(lib, [256], 1, 64, 64, True).fill(3)
+        for i, e in enumerate(order):
+            P.vs[int(P.table[0, i]), 0] = 2.0 ** e
+        q, o, lse = attend(lib, P, [new], 2, True, 0, 0, dtype=torch.float32)
+        check(P, q, o, lse, [new], 2, True, 0, 0)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("new", [1, 3, 30])
+def test_many_sequences(lib, f8, new):
+    """More sequences than a warp has lanes, of very different lengths."""
+    lens = [max(new, (37 * i * i) % 1700) for i in range(70)]
+    P = Pages(lib, lens, 1, 64, 16, f8, seed=2).fill(5)
+    n = [min(new, 1 + i % new) for i in range(70)]
+    q, o, lse = attend(lib, P, n, 4, True, 0, 0)
+    lib.cast_check_device()
+    check(P, q, o, lse, n, 4, True, 0, 0)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("new", [2, 60])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_not_finite_stays_its_own(lib, f8, new, bad):
+    P = Pages(lib, [500], 2, 128, 32, f8).fill(5)
+    q = randn(gen(1), new, 4, 128).to(torch.bfloat16)
+    want = lib.cast_cache_attention(q, P.cache, P.table, P.len_tensor())
+    q[1, 2, 77] = bad
+    got = lib.cast_cache_attention(q, P.cache, P.table, P.len_tensor())
+    got, want = got.view(new, 4, 128), want.view(new, 4, 128)
+    assert torch.isnan(got[1, 2]).all()
+    got[1, 2] = want[1, 2]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("new", [1, 90])
+def test_table_is_a_slice_and_longer_than_needed(lib, f8, new):
+    P = Pages(lib, [900, 333], 2, 64, 16, f8, seed=4).fill(5)
+    wide = torch.full((2, 5000), -7, dtype=torch.int32, device="cuda")
+    wide[:, 100:100 + P.table.shape[1]] = P.table
+    P.table = wide[:, 100:4100]
+    q, o, lse = attend(lib, P, [new, new], 2, True, 0, 0)
+    lib.cast_check_device()
+    check(P, q, o, lse, [new, new], 2, True, 0, 0)
+
+
+@pytest.mark.parametrize("new", [1, 90])
+def test_length_past_the_table_is_reported(lib, new):
+    P = Pages(lib, [320], 1, 64, 16, False).fill(5)
+    P.lens = [400]          # the table has room for 320
+    attend(lib, P, [new], 1, False, 0, 0)
+    with pytest.raises(lib.CastError) as e:
+        lib.cast_check_device()
+    assert e.value.status == lib.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_more_new_tokens_than_said_are_left_out(lib, f8):
+    P = Pages(lib, [300, 300], 1, 64, 16, f8).fill(5)
+    for said in (2, 60):
+        n = [said, said + 5]
+        cu = torch.tensor([0, n[0], sum(n)], dtype=torch.int32, device="cuda")
+        q = randn(gen(2), sum(n), 2, 64).to(torch.bfloat16)
+        out = torch.full((sum(n), 128), 5.0, dtype=torch.bfloat16, device="cuda")
+        lib.cast_cache_attention(q, P.cache, P.table, P.len_tensor(), cu_new=cu, max_new=said, out=out)
+        with pytest.raises(lib.CastError):
+            lib.cast_check_device()
+        assert (out[n[0] + said:] == 5).all() and not (out[:n[0] + said] == 5).all(1).any()
+
+
+@pytest.mark.parametrize("bits", [8, 16])
+def test_rollout_example(lib, bits):
+    """The example's steps (frames, a control token, a routed chunk) against 64 bits."""
+    from examples.cache_rollout import Rollout
+    r = Rollout(H=2, H_q=4, d=64, grid=(8, 8), page=64, n_pages=16, bits=bits, window=150)
+    sections = [32 - 2 * 12, 12, 12]
+    keys, values = [], []
+    for tokens, causal in ((64, False), (64, False), (1, True), (64, False), (64, False), (1, True)):
+        (q, k, v, pos), turned, o = r.step(tokens, causal)
+        for x, y in ((q, turned),):
+            ref, err = R.rotate(f64(x), pos.cpu().numpy(), 64, sections=sections)
+            within(f64(y), ref, err + R.UBF * (np.abs(ref) + err), "queries")
+        kk, vv = [], []
+        for c, s in ((r.k, r.cache._keep[2]), (r.v, r.cache._keep[3])):
+            x = f64(c) if s is None else f64(c) * f64(s)[:, None, :, None]
+            (kk if c is r.k else vv).append(x.reshape(-1, 2, 64)[:r.len])
+        ref, _ = R.rotate(f64(k), pos.cpu().numpy(), 64, sections=sections)
+        half = 2.0 ** -4 if bits == 8 else 2.0 ** -8
+        within(kk[0][r.len - tokens:], ref, half * np.abs(ref) + 2.0 ** -7, "keys")
+        want, _, eo, _ = R.attention(f64(turned), kk[0], vv[0], tokens, r.len, causal, 150, 64)
+        within(f64(o).reshape(tokens, 4, 64), want, eo, "output")
+    if bits == 16:
+        out = r.routed_chunk(n_frames=3, anchors=(0, 2), K=2)
+        assert torch.isfinite(out.float()).all()
+    lib.cast_check_device()
