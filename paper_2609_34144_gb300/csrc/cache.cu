@@ -11,8 +11,6 @@
 namespace cast {
 namespace {
 
-__device__ unsigned int g_cache_error;
-
 // ------------------------------------------------------------------ cast_rotary
 struct RotaryKArgs {
   const void* x;
@@ -96,7 +94,6 @@ struct AppendKArgs {
   void *ck, *cv;
   float *k_scale, *v_scale;
   const int* positions;
-  unsigned* error;
   int runs;               // page runs of a sequence that the grid has room for
   int group;              // heads of one CTA
   int jobs_kv, jobs_q;    // head groups of K (and of V), of the queries
@@ -115,7 +112,7 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
   const int p0 = s.len - s.n_new;                       // place of the first new token
   const int first = max(p0, 0);
   const int g = first / a.page_size + run;              // page of the sequence
-  if (run == 0 && s.n_new > a.batch.max_new && threadIdx.x == 0) atomicExch(a.error, kCacheBadInput);
+  if (run == 0 && s.n_new > a.batch.max_new && threadIdx.x == 0) left_out();
   if ((int64_t)g * a.page_size >= s.len) return;
   const int base = g * a.page_size;
   const int lo = max(first - base, 0), hi = min(s.len - base, a.page_size);
@@ -128,7 +125,7 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
   if (kind != 2) {
     page = g < a.batch.max_pages ? __ldg(a.batch.page_table + (int64_t)b * a.batch.page_table_stride + g) : -1;
     if (page < 0 || page >= a.n_pages) {
-      if (threadIdx.x == 0) atomicExch(a.error, kCacheBadInput);
+      if (threadIdx.x == 0) left_out();
       return;
     }
   }
@@ -295,22 +292,7 @@ cast_status validate_batch(const cast_cache_batch& b, const char* who) {
   return CAST_OK;
 }
 
-unsigned int* cache_error_address() {
-  void* p = nullptr;
-  return cudaGetSymbolAddress(&p, g_cache_error) == cudaSuccess ? static_cast<unsigned int*>(p) : nullptr;
-}
-
-unsigned int cache_error_word(cudaStream_t st, bool clear) {
-  unsigned int v = 0;
-  cudaMemcpyFromSymbolAsync(&v, g_cache_error, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
-  cudaStreamSynchronize(st);
-  if (clear && v) {
-    const unsigned int z = 0;
-    cudaMemcpyToSymbolAsync(g_cache_error, &z, sizeof(z), 0, cudaMemcpyHostToDevice, st);
-    cudaStreamSynchronize(st);
-  }
-  return v;
-}
+unsigned int cache_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }
 
 }  // namespace cast
 
@@ -468,7 +450,6 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   k.k_scale = c.k_scale;
   k.v_scale = c.v_scale;
   k.positions = a->positions;
-  if (!(k.error = cache_error_address())) return check_launch("cache error word");
   // a sequence's new tokens touch at most this many pages
   const int max_new = a->batch.max_new < a->batch.T ? a->batch.max_new : a->batch.T;
   k.runs = (max_new + c.page_size - 2) / c.page_size + 1;

@@ -7,10 +7,23 @@
 
 namespace cast {
 
-// Set (by any cache kernel) when a page, a position or a token was left out: cache.cu owns it.
-unsigned int* cache_error_address();
-
-constexpr int kCacheBadInput = 1;
+namespace {
+// Set when a page, a position or a token was left out: one word for each translation unit, so that its
+// kernels name it themselves.
+__device__ unsigned int g_left_out;
+__device__ __forceinline__ void left_out() { atomicExch(&g_left_out, 1u); }
+inline unsigned int read_left_out(cudaStream_t st, bool clear) {
+  unsigned int v = 0;
+  cudaMemcpyFromSymbolAsync(&v, g_left_out, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
+  cudaStreamSynchronize(st);
+  if (clear && v) {
+    const unsigned int z = 0;
+    cudaMemcpyToSymbolAsync(g_left_out, &z, sizeof(z), 0, cudaMemcpyHostToDevice, st);
+    cudaStreamSynchronize(st);
+  }
+  return v;
+}
+}  // namespace
 
 // Sequence b of a call: its new tokens are rows t0 .. t0 + n_new - 1, its cache holds `len` tokens.
 struct Sequence {

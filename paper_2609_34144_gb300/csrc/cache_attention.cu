@@ -54,7 +54,6 @@ struct RowsKArgs {
   void* o;
   float* lse;
   float scale_log2;
-  unsigned* error;
   int row_tiles;      // units of 16 * MT rows that a sequence may have
   int least;          // blocks that a CTA takes at least
   int whole;          // every CTA has one whole unit
@@ -79,10 +78,10 @@ __device__ __forceinline__ Span span_of(const RowsKArgs& a, int b, int row_tile,
   z.t0 = s.t0;
   z.p0 = s.len - s.n_new;
   const int kept = min(s.n_new, a.batch.max_new);
-  if (kept < s.n_new) atomicExch(a.error, kCacheBadInput);
+  if (kept < s.n_new) left_out();
   z.n_rows = kept * a.group;
   const int64_t room = (int64_t)a.batch.max_pages * a.page_size;
-  if (s.len > room) atomicExch(a.error, kCacheBadInput);
+  if (s.len > room) left_out();
   const int len = (int)min((int64_t)s.len, room);
   const int r0 = row_tile * rows, r1 = min(r0 + rows, z.n_rows) - 1;
   z.n_sink = z.first = z.end = z.lo = z.hi = z.sinks = 0;
@@ -364,7 +363,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
         const int g0 = (z.block(i) * 16) >> a.page_shift;
         int p = __ldg(table + g0);
         if (p < 0 || p >= a.n_pages) {
-          if (lane == 0) atomicExch(a.error, kCacheBadInput);
+          if (lane == 0) left_out();
           p = -1;
         }
         return p;
@@ -859,6 +858,9 @@ cast_status launch_rows(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) 
 }
 
 }  // namespace
+
+unsigned int cache_rows_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }
+
 }  // namespace cast
 
 using namespace cast;
@@ -917,7 +919,6 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   k.o = a->o;
   k.lse = a->lse;
   k.scale_log2 = (a->scale > 0.f ? a->scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;
-  if (!(k.error = cache_error_address())) return check_launch("cache error word");
   k.row_tiles = p.row_tiles;
   k.least = p.least;
   k.whole = p.whole;

@@ -82,7 +82,6 @@ struct TilesKArgs {
   void* o;
   float* lse;
   float scale_log2;
-  unsigned* error;
   int pairs;         // pairs of tiles that a head may have
   int most_pairs;    // of a sequence
   int whole;         // a CTA has one whole unit
@@ -124,7 +123,7 @@ __device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const S
   u.n_new = min(s.n_new, a.batch.max_new);
   u.p0 = s.len - s.n_new;
   const int64_t room = (int64_t)a.batch.max_pages * a.page_size;
-  if (s.len > room || s.n_new > a.batch.max_new) atomicExch(a.error, kCacheBadInput);
+  if (s.len > room || s.n_new > a.batch.max_new) left_out();
   const int len = (int)min((int64_t)s.len, room);
   const int i1 = min(u.i0 + 2 * a.tile_tokens, u.n_new) - 1;
   u.hi = a.causal ? min(len, max(u.p0 + i1 + 1, 0)) : len;
@@ -399,7 +398,7 @@ __device__ __forceinline__ int page_at(const TilesKArgs& a, const Unit& u, int p
   if (!(p < u.hi && (p < u.sinks || p + a.page_size > u.lo))) return a.n_pages;
   const int page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (p >> a.page_shift));
   if (page >= 0 && page < a.n_pages) return page;
-  atomicExch(a.error, kCacheBadInput);
+  left_out();
   return a.n_pages;
 }
 
@@ -1295,7 +1294,6 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.o = a.o;
   k.lse = a.lse;
   k.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;
-  if (!(k.error = cache_error_address())) return check_launch("cache error word");
   k.pairs = p.pairs;
   k.most_pairs = (int)(((a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens));
   k.whole = p.whole;
@@ -1307,6 +1305,8 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   if (c.dtype == CAST_F8E4M3) return c.d == 128 ? launch<128, true>(a, k, p, st) : launch<64, true>(a, k, p, st);
   return c.d == 128 ? launch<128, false>(a, k, p, st) : launch<64, false>(a, k, p, st);
 }
+
+unsigned int cache_tiles_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }
 
 unsigned int tiles_error_word(cudaStream_t st, bool clear) {
   unsigned int v = 0;

@@ -147,8 +147,11 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 // host checks shared by the append and the attention (cache.cu)
 cast_status validate_cache(const cast_kv_cache& c, const char* who);
 cast_status validate_batch(const cast_cache_batch& b, const char* who);
-// Nonzero when a cache kernel left out a page, position or token that was out of range.
+// Nonzero when a kernel (of the append, the attention's two forms) left out a page, position or token that
+// was out of range.
 unsigned int cache_error_word(cudaStream_t st, bool clear);
+unsigned int cache_rows_error_word(cudaStream_t st, bool clear);
+unsigned int cache_tiles_error_word(cudaStream_t st, bool clear);
 // Nonzero when the cache attention gave up on a bounded wait.
 unsigned int tiles_error_word(cudaStream_t st, bool clear);
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -139,10 +140,11 @@ class CacheAttnArgs(C.Structure):
 
 
 _lib.cast_rotary_table_init.argtypes = [C.POINTER(RotaryParams), C.POINTER(RotaryTable)]
-_lib.cast_rotary.argtypes = [C.POINTER(RotaryArgs), _vp]
-_lib.cast_cache_append.argtypes = [C.POINTER(AppendArgs), _vp]
-_lib.cast_cache_attention.argtypes = [C.POINTER(CacheAttnArgs), _vp, C.c_size_t, _vp]
-_lib.cast_cache_attention_workspace_size.argtypes = [C.POINTER(CacheAttnArgs)]
+# these take the structs by reference, or their bytes (see the packers below)
+_lib.cast_rotary.argtypes = [_vp, _vp]
+_lib.cast_cache_append.argtypes = [_vp, _vp]
+_lib.cast_cache_attention.argtypes = [_vp, _vp, C.c_size_t, _vp]
+_lib.cast_cache_attention_workspace_size.argtypes = [_vp]
 _lib.cast_cache_attention_workspace_size.restype = C.c_size_t
 _lib.cast_ffn_step.argtypes = [C.POINTER(FfnArgs), _vp, C.c_size_t, _vp]
 _lib.cast_ffn_workspace_size.argtypes = [C.POINTER(FfnArgs)]
@@ -592,13 +594,18 @@ def rotary_table(rot_dim, layout="half", base=10000.0, sections=None, scaling=No
         p.factor = scaling[1]
         p.original_length = scaling[2] if len(scaling) > 2 else 0
     _check(_lib.cast_rotary_table_init(C.byref(p), C.byref(t)))
-    t.pointer = C.pointer(t)
+    t.address = C.addressof(t)
     return t
 
 
 # These calls serve single tokens, where the host's microseconds are the step's: the raw stream is
-# asked for directly, tensors are measured once, and torch.empty is 3 us cheaper here than new_empty.
+# asked for directly, tensors are measured once, torch.empty is 3 us cheaper here than new_empty, and
+# the argument structs are packed as bytes (the same layout as the classes above).
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_BATCH = "PqiPPiii4x"
+_pack_rotary = struct.Struct("@PPqqiiiiPPi4x").pack
+_pack_append = struct.Struct("@64s" + _BATCH + "PPqqPPPPqqi4x").pack
+_pack_attention = struct.Struct("@64s" + _BATCH + "PqiiiifPiP").pack
 
 
 def _on(stream, t):
@@ -647,9 +654,9 @@ def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
     o = torch.empty((T, H, d), dtype=x.dtype, device=x.device) if out is None else out
     if out is not None and (o.shape != x.shape or o.dtype != x.dtype):
         raise ValueError("out must have x's shape and dtype")
-    a = RotaryArgs(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
-                   _dtype_code(x), pos, table.pointer, inverse)
-    _check(_lib.cast_rotary(C.byref(a), _on(stream, x)))
+    a = _pack_rotary(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
+                     _dtype_code(x), pos, table.address, inverse)
+    _check(_lib.cast_rotary(a, _on(stream, x)))
     if out is None:
         _on_stream(stream, o)
     return o
@@ -673,20 +680,23 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
     c = KvCache(F8E4M3 if f8 else BF16, n, ps, H, d, k.data_ptr(), v.data_ptr(), _row_stride(k),
                 k_scale.data_ptr() if f8 else None, v_scale.data_ptr() if f8 else None)
     c._keep = (k, v, k_scale, v_scale)
+    c.packed = bytes(c)
+    c.heads = (H, d)
     return c
 
 
 def _batch(page_table, kv_len, cu_new, T, max_new):
+    """The fields of CacheBatch."""
     if page_table.dim() != 2 or page_table.dtype is not torch.int32:
         raise ValueError("page_table: expected int32 [B, max_pages]")
     B, P = page_table.shape
     s0, s1 = page_table.stride()
     if P > 1 and s1 != 1:
         raise ValueError("page_table: a sequence's pages must be contiguous")
-    cu = None if cu_new is None else _int32(cu_new, "cu_new", (B + 1,))
+    cu = 0 if cu_new is None else _int32(cu_new, "cu_new", (B + 1,))
     if max_new is None:
-        max_new = T if cu is not None else T // max(B, 1)
-    return CacheBatch(page_table.data_ptr(), s0 if s0 > P else P, P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new)
+        max_new = T if cu else T // max(B, 1)
+    return page_table.data_ptr(), s0 if s0 > P else P, P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new
 
 
 def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None, rotary=None, positions=None,
@@ -695,37 +705,29 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
     already.  cu_new [B + 1]: ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes]
     (None: a token's place in its sequence).  With q [T, H_q, d] returns it rotated."""
     T, H, d = k.shape
-    if v.shape != k.shape or H != cache.H or d != cache.d:
+    if v.shape != k.shape or (H, d) != cache.heads:
         raise ValueError("k and v must be [T, H, d] of the cache's heads")
-    pos = None
+    pos = 0
     if positions is not None and rotary is not None:
         pos = _int32(positions, "positions", (T,) if positions.dim() == 1 and rotary.n_axes == 1 else (T, rotary.n_axes))
-    qp = qo = None
-    qs = qos = Hq = 0
+    qp = qo = qs = qos = Hq = 0
     o = None
     if q is not None:
-        qs, Hq = _heads_stride(q, "q"), q.shape[1]
-        if q.shape[0] != T or q.shape[2] != d:
+        qs = _heads_stride(q, "q")
+        Tq, Hq, dq = q.shape
+        if Tq != T or dq != d:
             raise ValueError("q must be [T, H_q, d]")
         o = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
-        if o.shape != q.shape:
+        if q_out is not None and o.shape != q.shape:
             raise ValueError("q_out must have q's shape")
         qp, qo, qos = q.data_ptr(), o.data_ptr(), Hq * d if q_out is None else _heads_stride(o, "q_out")
-    a = AppendArgs(cache, _batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(), _heads_stride(k, "k"),
-                   _heads_stride(v, "v"), rotary.pointer if rotary is not None else None, pos, qp, qo, qs, qos, Hq)
-    _check(_lib.cast_cache_append(C.byref(a), _on(stream, k)))
+    a = _pack_append(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(),
+                     _heads_stride(k, "k"), _heads_stride(v, "v"), rotary.address if rotary is not None else 0, pos, qp, qo, qs,
+                     qos, Hq)
+    _check(_lib.cast_cache_append(a, _on(stream, k)))
     if q_out is None:
         _on_stream(stream, o)
     return o
-
-
-def cache_attention_args(q, cache, page_table, kv_len, o, cu_new=None, max_new=None, causal=True, window=0, sinks=0,
-                         scale=0.0, lse=None):
-    T, Hq, d = q.shape
-    if d != cache.d:
-        raise ValueError("q must be [T, H_q, d] of the cache's head dim")
-    return CacheAttnArgs(cache, _batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
-                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), None if lse is None else lse.data_ptr())
 
 
 def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None, causal=True, window=0, sinks=0,
@@ -734,21 +736,21 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     window > 0: a row sees the last `window` positions and the first `sinks`.  Returns
     o [T, H_q*d] (and lse [T, H_q])."""
     T, Hq, d = q.shape
+    if d != cache.heads[1]:
+        raise ValueError("q must be [T, H_q, d] of the cache's head dim")
     dev = q.device
     o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
     if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous()):
         raise ValueError("out must be contiguous [T, H_q*d]")
     lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
-    a = cache_attention_args(q, cache, page_table, kv_len, o, cu_new, max_new, causal, window, sinks, scale, lse)
-    ref, ws = C.byref(a), workspace
+    a = _pack_attention(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
+                        causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), 0 if lse is None else lse.data_ptr())
+    ws = workspace
     if ws is None:
-        need = _lib.cast_cache_attention_workspace_size(ref)
+        need = _lib.cast_cache_attention_workspace_size(a)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(_lib.cast_cache_attention(ref, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _on(stream, q)))
+    _check(_lib.cast_cache_attention(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _on(stream, q)))
     if stream is not None:
         _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
     return (o, lse) if want_lse else o
 
-
-def cache_attention_workspace_size(args):
-    return _lib.cast_cache_attention_workspace_size(C.byref(args))

@@ -213,3 +213,16 @@ def test_struct_layouts_match_the_header(lib, tmp_path):
         cname, f, val = line.split()
         py = structs[cname]
         assert (C.sizeof(py) if f == "sizeof" else getattr(py, f).offset) == int(val), (cname, f)
+
+
+def test_packed_arguments_are_the_structs(lib):
+    """The bytes that the binding packs for a call lie as the ctypes classes (and so the header) do."""
+    import torch
+    k = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16)
+    cache = lib.kv_cache(k, k)
+    batch = (11, 12, 13, 14, 15, 16, 17, 18)
+    assert lib._pack_rotary(1, 2, 3, 4, 5, 6, 7, 1, 9, 0, 1) == bytes(lib.RotaryArgs(1, 2, 3, 4, 5, 6, 7, 1, 9, None, 1))
+    want = lib.AppendArgs(cache, lib.CacheBatch(*batch), 21, 22, 23, 24, None, 25, 26, 27, 28, 29, 30)
+    assert lib._pack_append(cache.packed, *batch, 21, 22, 23, 24, 0, 25, 26, 27, 28, 29, 30) == bytes(want)
+    want = lib.CacheAttnArgs(cache, lib.CacheBatch(*batch), 21, 22, 23, 1, 25, 26, 0.5, 28, 1, 30)
+    assert lib._pack_attention(cache.packed, *batch, 21, 22, 23, 1, 25, 26, 0.5, 28, 1, 30) == bytes(want)
