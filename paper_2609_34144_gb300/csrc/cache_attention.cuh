@@ -25,17 +25,13 @@ __device__ __forceinline__ void half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
       "cvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
       : "=r"(lo), "=r"(hi) : "r"(w));
 }
-// Whether a 16-byte chunk of V holds a value that is not finite
+// Whether a 16-byte chunk of V holds a value that is not finite: the carry out of an exponent (bf16) or of
+// a magnitude (codes) that is all ones
 template <bool F8>
 __device__ __forceinline__ bool not_finite(const uint4& x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (F8) bad |= (((w[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0u;
-    else bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  }
-  return bad;
+  constexpr uint32_t mask = F8 ? 0x7f7f7f7fu : 0x7f807f80u, one = F8 ? 0x01010101u : 0x00800080u;
+  const uint32_t carry = ((x.x & mask) + one) | ((x.y & mask) + one) | ((x.z & mask) + one) | ((x.w & mask) + one);
+  return (carry & (F8 ? 0x80808080u : 0x80008000u)) != 0u;
 }
 
 }  // namespace cast
