@@ -456,10 +456,11 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   const int64_t gx = (int64_t)k.runs * a->batch.B;
   if (gx > 0x7fffffff) return fail(CAST_ERR_UNSUPPORTED, "%s: %lld page runs", who, (long long)gx);
   const int threads = c.page_size * c.d / 16;
-  // heads of one CTA: twelve share the angles' cost, fewer where the grid would not fill the SMs twice
+  // heads of one CTA: twelve share the angles' cost, fewer where the grid would not fill the SMs (1024 threads
+  // each) three times
   int group = 12;
   while (group > 1 &&
-         gx * (2 * ((c.H + group - 1) / group) + (k.H_q + group - 1) / group) * threads < (int64_t)2 * 152 * 2048)
+         gx * (2 * ((c.H + group - 1) / group) + (k.H_q + group - 1) / group) * threads < (int64_t)3 * 152 * 1024)
     group /= 2;
   k.group = group;
   k.jobs_kv = (c.H + group - 1) / group;

@@ -705,29 +705,34 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
   }
 }
 
-// Joins the parts of the units that no single CTA of k_cache_rows had whole: one CTA a unit.
+// Joins the parts of the units that no single CTA of k_cache_rows had whole: one CTA a unit, one warp a
+// row and some of the parts (lanes: four channels each), then over the warps of a row.
+constexpr int kMergeWarps = 16;
 template <int D, int MT>
-__global__ void __launch_bounds__(128) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
-  constexpr int ROWS = 16 * MT;
-  __shared__ int s_sum[4], s_before[4];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+__global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
+  constexpr int ROWS = 16 * MT, LANES = D / 4, GROUPS = 32 / LANES;   // GROUPS parts at a time in a warp
+  __shared__ int s_sum[kMergeWarps], s_before[kMergeWarps];
+  __shared__ float4 s_o[kMergeWarps * GROUPS][LANES];
+  __shared__ float2 s_ml[kMergeWarps * GROUPS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int entries = a.batch.B * a.row_tiles;
   const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
   int sum = 0, before = 0;
-  for (int e = threadIdx.x; e < entries; e += 128) {
+  for (int e = threadIdx.x; e < entries; e += kMergeWarps * 32) {
     const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
     sum += n;
     before += e < entry ? n : 0;
   }
   sum = __reduce_add_sync(0xffffffffu, sum);
   before = __reduce_add_sync(0xffffffffu, before);
-  if ((threadIdx.x & 31) == 0) {
-    s_sum[threadIdx.x >> 5] = sum;
-    s_before[threadIdx.x >> 5] = before;
+  if (lane == 0) {
+    s_sum[warp] = sum;
+    s_before[warp] = before;
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
   int64_t total = 0, at = 0;
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kMergeWarps; ++w) {
     total += s_sum[w];
     at += s_before[w];
   }
@@ -740,37 +745,59 @@ __global__ void __launch_bounds__(128) k_cache_merge(const __grid_constant__ Row
   if (nb == 0) return;
   const int c0 = (int)(at / share), c1 = (int)((at + nb - 1) / share);
   if (c0 == c1) return;   // written whole
-  for (int x = threadIdx.x; x < ROWS * D / 4; x += 128) {
-    const int rr = x / (D / 4), c = x % (D / 4) * 4;
-    const int r = tile * ROWS + rr;
-    if (r >= z.n_rows) continue;
-    // CTA c0 began the unit (its second place), unless its share begins with the unit's first block,
-    // which is also k0 == 0; the others began inside it (their first place)
-    float top = -INFINITY;
-    for (int i = c0; i <= c1; ++i) {
-      const int64_t slot = 2 * i + (i == c0 ? 1 : 0);
-      top = fmaxf(top, a.part_ml[slot * ROWS + rr].x);
-    }
-    float l = 0.f;
+  // warps_per_row warps (a power of two) have every warps_per_row-th part of a row
+  const int rows = min(ROWS, z.n_rows - tile * ROWS), parts = c1 - c0 + 1;
+  int per_row = 1;
+  while (per_row * 2 * rows <= kMergeWarps && per_row * GROUPS < parts) per_row *= 2;
+  for (int r0 = 0; r0 < rows; r0 += kMergeWarps / per_row) {
+    const int rr = r0 + warp / per_row, mine = (warp % per_row) * GROUPS + lane / LANES, c = lane % LANES;
+    const bool in = rr < rows;
+    // CTA c0 began the unit (its second place), the others began inside it (their first place)
+    float top = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = c0; i <= c1; ++i) {
-      const int64_t slot = 2 * i + (i == c0 ? 1 : 0);
-      const float2 v = a.part_ml[slot * ROWS + rr];
-      const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
-      l += f * v.y;
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * ROWS + rr) * D + c);
-      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+    if (in) {
+#pragma unroll 4
+      for (int i = mine; i < parts; i += per_row * GROUPS) {
+        const int64_t slot = 2 * (int64_t)(c0 + i) + (i == 0 ? 1 : 0);
+        const float2 v = a.part_ml[slot * ROWS + rr];
+        const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * ROWS + rr) * D + c * 4);
+        const float m = fmaxf(top, v.x);
+        const float f0 = top == -INFINITY ? 0.f : exp2_fast(top - m), f1 = v.x == -INFINITY ? 0.f : exp2_fast(v.x - m);
+        l = f0 * l + f1 * v.y;
+        acc.x = f0 * acc.x + f1 * y.x; acc.y = f0 * acc.y + f1 * y.y;
+        acc.z = f0 * acc.z + f1 * y.z; acc.w = f0 * acc.w + f1 * y.w;
+        top = m;
+      }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
-    if (a.o_f32) {
-      *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c) =
-          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    } else {
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c) =
-          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    const int place = warp * GROUPS + lane / LANES;
+    s_o[place][c] = acc;
+    if (c == 0) s_ml[place] = make_float2(top, l);
+    __syncthreads();
+    if (in && mine == 0) {
+      const int n = per_row * GROUPS, first = warp * GROUPS;
+      for (int i = 0; i < n; ++i) top = fmaxf(top, s_ml[first + i].x);
+      l = 0.f;
+      acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < n; ++i) {
+        const float2 v = s_ml[first + i];
+        const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+        const float4 y = s_o[first + i][c];
+        l += f * v.y;
+        acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int r = tile * ROWS + rr;
+      const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
+      if (a.o_f32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c * 4) =
+            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      } else {
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c * 4) =
+            make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+      }
+      if (a.lse && c == 0) a.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
     }
-    if (a.lse && c == 0) a.lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    __syncthreads();
   }
 }
 
@@ -784,7 +811,7 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   RowsPlan p{};
   const int group = a.H_q / a.cache.H;
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
-  p.mt = 1;
+  p.mt = (int64_t)max_new * group > 16 ? 2 : 1;   // 16 rows of a product, or two of them for the same keys
   const int rows = 16 * p.mt;
   p.row_tiles = (int)(((int64_t)max_new * group + rows - 1) / rows);
   int dev = 0, nsm = 152;
@@ -846,7 +873,7 @@ cast_status launch_rows(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) 
   if (s || p.whole) return s;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(k.batch.B * k.row_tiles * k.H), 1, 1);
-  cfg.blockDim = dim3(128, 1, 1);
+  cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -867,10 +894,15 @@ using namespace cast;
 
 extern "C" {
 
-// Few rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu).
+// Up to 16 rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu),
+// except that heads of 64 with up to 32 rows stay where there are 32 units or more (two products of 16 rows
+// on the same keys).  Measured, tiles / rows, 32 rows, us: heads of 64, 64 units of 20k tokens 92 / 77 (8
+// bits), 92 / 79 (bf16), 108 units of 2.4k with 18 rows 34 / 28, 16 units of 60k 74 / 74, 8 units of 3k
+// 18 / 23; heads of 128, 16 units of 60k 82 / 95 (8 bits), 98 / 106 (bf16), 8 units of 3k 21 / 27.
 static bool by_tiles(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
-  return (int64_t)max_new * (a.H_q / a.cache.H) > 16;
+  const int64_t rows = (int64_t)max_new * (a.H_q / a.cache.H);
+  return rows > 32 || (rows > 16 && (a.cache.d != 64 || (int64_t)a.batch.B * a.cache.H < 32));
 }
 
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {
@@ -925,6 +957,8 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   k.part_o = static_cast<float*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p.mt == 2)   // heads of 64 only
+    return c.dtype == CAST_F8E4M3 ? launch_rows<64, true, 2>(k, p, st) : launch_rows<64, false, 2>(k, p, st);
   if (c.dtype == CAST_F8E4M3)
     return c.d == 128 ? launch_rows<128, true, 1>(k, p, st) : launch_rows<64, true, 1>(k, p, st);
   return c.d == 128 ? launch_rows<128, false, 1>(k, p, st) : launch_rows<64, false, 1>(k, p, st);

@@ -478,7 +478,7 @@ def test_scales_far_apart_within_a_sequence(lib, new):
 
 
 @pytest.mark.parametrize("f8", [False, True])
-@pytest.mark.parametrize("new", [1, 3, 30])
+@pytest.mark.parametrize("new", [1, 3, 8, 30])
 def test_many_sequences(lib, f8, new):
     """More sequences than a warp has lanes, of very different lengths."""
     lens = [max(new, (37 * i * i) % 1700) for i in range(70)]
