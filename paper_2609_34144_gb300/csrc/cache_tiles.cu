@@ -103,8 +103,8 @@ struct Unit {
   int n_sink, first, tiles; // tiles of 128 positions: 0 .. n_sink-1, then first ..
   int valid;
 };
-// What CTA c leaves for the joining: the unit that its share begins inside of, which CTAs c0 .. c1 had
-// parts of (c0 = -1: it begins with a unit)
+// What CTA c leaves for the joining: the unit that its share begins inside of, which CTAs c0 .. c1 have
+// tiles of (c0 = -1: it begins with a unit)
 struct Cut {
   int h, t0, i0, n_new, c0, c1;
 };
@@ -138,12 +138,17 @@ __device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const S
   u.n_sink = min((u.sinks + BN - 1) / BN, u.first);
   u.tiles = u.n_sink + max((u.hi + BN - 1) / BN - u.first, 0);
 }
-// Work: a key tile of two query tiles counts 3, of one query tile 2 (1.75 and 1.2 us), a unit that sees
-// nothing 1.
+// Work: a key tile of two query tiles takes 2.1 us, of one query tile 1 us, and a CTA that goes over to
+// another unit has the first key tile's softmax done ~10 us later, half of which other CTAs' memory traffic
+// gains (decode of 35 rows, 60k positions, 8 bits, with no charge 85, 8 81, 10 us 83; window of 1560 frame
+// tokens 114, 111 and 113 us; frames of 3520 tokens 925, 929 and 930 us).
+constexpr int kBegin = 16, kPair = 4, kSingle = 2;
 __device__ __forceinline__ int tile_work(const TilesKArgs& a, const Unit& u) {
-  return u.i0 + a.tile_tokens < u.n_new ? 3 : 2;
+  return u.i0 + a.tile_tokens < u.n_new ? kPair : kSingle;
 }
-__device__ __forceinline__ int unit_work(const TilesKArgs& a, const Unit& u) { return max(1, u.tiles * tile_work(a, u)); }
+__device__ __forceinline__ int unit_work(const TilesKArgs& a, const Unit& u) {
+  return u.tiles ? kBegin + u.tiles * tile_work(a, u) : 1;
+}
 
 // Work of units lane, lane + 32, ... or, `serial`, of all units of sequence b
 __device__ __forceinline__ int sequence_work(const TilesKArgs& a, int b, int lane, bool serial) {
@@ -244,59 +249,69 @@ __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
   return u;
 }
 
-// The unit that work item `at` lies in, and the part of it that items at .. stop-1 are (one warp; every
-// lane has it).  A part that begins inside the unit has the CTA's first place, else its second.
+// The first unit of which items at .. stop-1 have a tile, and that part of it (one warp; every lane has it).  A
+// unit's tile k is at item kBegin + k * tile_work.  Its first part (with tile 0) goes to the CTA's second
+// place, others to its first.
 __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int64_t at, int64_t stop, int lane, Cut* cut) {
   Unit u{};
   if (cut && lane == 0) cut->c0 = -1;
-  if (at >= stop) return u;
-  const int h = (int)(at / d.per_head), per = 2 * a.tile_tokens;
-  int r = (int)(at - (int64_t)h * d.per_head), b = a.batch.B == 1 ? 0 : -1;
-  for (int b0 = 0; b < 0 && b0 < a.batch.B; b0 += 32) {
-    const int w = chunk_work(a, b0, lane);
-    const int sum = scan(w, lane);
-    const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      r -= __shfl_sync(0xffffffffu, sum - w, l);
-      b = b0 + l;
-    } else {
+  const int64_t from = at;
+  const int per = 2 * a.tile_tokens;
+  while (at < stop) {
+    const int h = (int)(at / d.per_head);
+    int r = (int)(at - (int64_t)h * d.per_head), b = a.batch.B == 1 ? 0 : -1;
+    for (int b0 = 0; b < 0 && b0 < a.batch.B; b0 += 32) {
+      const int w = chunk_work(a, b0, lane);
+      const int sum = scan(w, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        r -= __shfl_sync(0xffffffffu, sum - w, l);
+        b = b0 + l;
+      } else {
+        r -= __shfl_sync(0xffffffffu, sum, 31);
+      }
+    }
+    if (b < 0) return u;
+    const Sequence s = sequence_of(a.batch, b);
+    const int n = min(s.n_new, a.batch.max_new);
+    bool found = false;
+    for (int i0 = 0; i0 < n; i0 += 32 * per) {
+      u.i0 = i0 + lane * per;
+      int w = 0;
+      if (u.i0 < n) {
+        place_unit(a, u, s);
+        w = unit_work(a, u);
+      }
+      const int sum = scan(w, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        r -= __shfl_sync(0xffffffffu, sum - w, l);
+        u.i0 = i0 + l * per;
+        found = true;
+        break;
+      }
       r -= __shfl_sync(0xffffffffu, sum, 31);
     }
-  }
-  if (b < 0) return u;
-  const Sequence s = sequence_of(a.batch, b);
-  const int n = min(s.n_new, a.batch.max_new);
-  for (int i0 = 0; i0 < n; i0 += 32 * per) {
-    u.i0 = i0 + lane * per;
-    int w = 0;
-    if (u.i0 < n) {
-      place_unit(a, u, s);
-      w = unit_work(a, u);
-    }
-    const int sum = scan(w, lane);
-    const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
-    if (hit) {
-      const int l = __ffs(hit) - 1;
-      r -= __shfl_sync(0xffffffffu, sum - w, l);
-      u.i0 = i0 + l * per;
+    if (!found) return u;
+    u.b = b;
+    u.h = h;
+    place_unit(a, u, s);
+    const int w = unit_work(a, u), each = tile_work(a, u), some = (int)min((int64_t)(w - r), stop - at);
+    u.k0 = (max(r - kBegin, 0) + each - 1) / each;
+    u.n_tiles = u.tiles ? (max(r + some - kBegin, 0) + each - 1) / each - u.k0 : 0;
+    if (u.n_tiles > 0 || u.tiles == 0) {
       u.valid = 1;
+      u.work = (int)(at - from) + some;
+      u.slot = u.n_tiles == u.tiles ? -1 : 2 * (int)blockIdx.x + (u.k0 > 0 ? 0 : 1);
+      if (cut && lane == 0 && u.k0 > 0) {
+        const int64_t first = at - r - d.base + kBegin;   // of tile 0
+        *cut = Cut{u.h, u.t0, u.i0, u.n_new, (int)(first / d.share), (int)((first + (u.tiles - 1) * each) / d.share)};
+      }
       break;
     }
-    r -= __shfl_sync(0xffffffffu, sum, 31);
-  }
-  if (!u.valid) return u;
-  u.b = b;
-  u.h = h;
-  place_unit(a, u, s);
-  const int w = unit_work(a, u), each = tile_work(a, u);
-  u.work = (int)min((int64_t)(w - r), stop - at);
-  u.k0 = min((r + each - 1) / each, u.tiles);
-  u.n_tiles = min((r + u.work + each - 1) / each, u.tiles) - u.k0;
-  u.slot = u.work == w ? -1 : 2 * (int)blockIdx.x + (r > 0 ? 0 : 1);
-  if (cut && lane == 0 && r > 0) {
-    const int64_t first = at - r - d.base;
-    *cut = Cut{u.h, u.t0, u.i0, u.n_new, (int)(first / d.share), (int)((first + w - 1) / d.share)};
+    at += some;
   }
   return u;
 }
@@ -1114,12 +1129,15 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   }
 }
 
-// Joins the parts of the units that no CTA had whole: CTA (x, y) takes 32 rows (a lane each, four channels a
-// warp at a time) of the unit that the share of CTA x + 1 begins inside of, if that is the first such share.
+// Joins the parts of the units that no CTA had whole: CTA (x, y, z) takes 32 rows (a lane each) and one of
+// gridDim.z shares of the channels of the unit that the share of CTA x + 1 begins inside of, if that is the
+// first such share.  A warp has four channels and every so many of the parts, so that all of a CTA's loads
+// are on their way together.
 constexpr int kMergeWarps = 16;
 template <int HD>
 __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_constant__ TilesKArgs a) {
   __shared__ float2 s_ml[kMergeWarps][32];
+  __shared__ float4 s_o[kMergeWarps][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const Cut u = a.cuts[blockIdx.x + 1];
   if (u.c0 != (int)blockIdx.x) return;
@@ -1155,18 +1173,31 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_c
     const float2 v = s_ml[w][lane];
     l += v.x == -INFINITY ? 0.f : v.y * exp2_fast(v.x - top);
   }
-  if (!in) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
-  for (int c = warp; c < HD / 4; c += kMergeWarps) {
+  // columns of four channels: `columns` of them at a time, each by `sharers` warps
+  const int mine = HD / 4 / gridDim.z, columns = min(mine, kMergeWarps), sharers = kMergeWarps / columns;
+  for (int k = 0; k < mine; k += columns) {
+    const int c = blockIdx.z * mine + k + warp % columns;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (in)
 #pragma unroll 8
-    for (int p = 0; p < n; ++p) {
-      const float m = a.part_ml[slot(p) * 256 + place(p)].x;
-      const float4 y = a.part_o[(slot(p) * (HD / 4) + c) * 256 + place(p)];
-      const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
-      acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+      for (int p = warp / columns; p < n; p += sharers) {
+        const float m = a.part_ml[slot(p) * 256 + place(p)].x;
+        const float4 y = a.part_o[(slot(p) * (HD / 4) + c) * 256 + place(p)];
+        const float f = m == -INFINITY ? 0.f : exp2_fast(m - top);
+        acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
+      }
+    if (sharers > 1) {   // (one round)
+      s_o[warp][lane] = acc;
+      __syncthreads();
+      if (warp >= columns) return;
+      for (int w = warp + columns; w < kMergeWarps; w += columns) {
+        const float4 y = s_o[w][lane];
+        acc.x += y.x; acc.y += y.y; acc.z += y.z; acc.w += y.w;
+      }
     }
+    if (!in) continue;
     if (a.o_f32) {
       *reinterpret_cast<float4*>(static_cast<float*>(a.o) + out * HD + c * 4) =
           make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
@@ -1175,7 +1206,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_c
           make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
     }
   }
-  if (a.lse && warp == 0) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+  if (a.lse && in && warp == 0 && blockIdx.z == 0) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------- host side
@@ -1226,7 +1257,8 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   // 32 rows of a unit a CTA, as many as a unit may have
   const int most = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int rows = most > k.tile_tokens ? 8 : (most * k.group + 31) / 32;
-  cfg.gridDim = dim3((unsigned)(p.grid - 1), rows, 1);
+  // and a quarter of the channels, where a unit has few rows
+  cfg.gridDim = dim3((unsigned)(p.grid - 1), rows, rows <= 2 ? 4 : 1);
   cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
