@@ -460,6 +460,11 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   // V codes: two stages, and two more in the place of a second query tile that a unit does not have
   auto raw_stage = [&](int s) { return s < 2 ? sRaw + s * C::RAW_BYTES : sQ + C::Q_BYTES + (s - 2) * C::RAW_BYTES; };
 
+  if (warp == 2 && lane == 0) {
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
   // warp 0: the CTA's share of the work, and its first unit
   Deal d{};
   int64_t at = 0, stop = 0;
@@ -522,7 +527,6 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       const bool is_k = warp == 0;
       const CUtensorMap* map = is_k ? &tm_k : &tm_v;
       if (lane == 0) {
-        tma_prefetch_desc(map);
         if (is_k && n_tiles > 0) {
           const uint32_t bytes = (uint32_t)a.tile_tokens * a.group * HD * 2;
           uint64_t* bar = F8 ? &bars->q_raw : &bars->q_full;
@@ -740,6 +744,26 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       const int lo = a.window > 0 ? max(p - a.window + 1, 0) : 0;
       const int sinks = a.window > 0 ? a.sinks : 0;
       float m_ref = -INFINITY, l = 0.f;
+      // 8-bit pages: lane c < 8 has the K and V scale of columns 16c .. 16c + 15 of a key tile (one page), fetched
+      // one tile ahead, and the page two tiles ahead, so that neither load is waited for
+      const int j0 = has_q1 ? 0 : t;
+      auto page_of = [&](int j) {
+        return lane < BN / 16 && j < n_tiles ? page_at(a, u, (tile_pos(u, k0 + j) + 16 * lane) & -a.page_size) : a.n_pages;
+      };
+      auto scales_of = [&](int page) {
+        float2 x = make_float2(1.f, 0.f);
+        if (page < a.n_pages) {
+          x.x = __ldg(a.k_scale + (int64_t)page * a.H + u.h);
+          x.y = __ldg(a.v_scale + (int64_t)page * a.H + u.h);
+        }
+        return x;
+      };
+      float2 next = make_float2(1.f, 0.f);
+      int next_page = 0;
+      if constexpr (F8) {
+        next = scales_of(page_of(j0));
+        next_page = page_of(j0 + every);
+      }
       float unit = a.scale_log2;   // what the row's S is multiplied by (and, with 8-bit pages, by their scales)
       if constexpr (F8) {
         // the row as two e4m3 pieces of row * 2^-ex; without a second tile both warpgroups have the row
@@ -787,23 +811,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         mbar_arrive(&bars->q_full);
       }
-      // 8-bit pages: lane c < 8 has the K scale and log2 of the V scale of columns 16c .. 16c + 15 of a key
-      // tile (one page), fetched one tile ahead
-      auto scales_of = [&](int j) {
-        float2 x = make_float2(1.f, -INFINITY);
-        if (lane < BN / 16) {
-          const int page = page_at(a, u, (tile_pos(u, k0 + j) + 16 * lane) & -a.page_size);
-          if (page < a.n_pages) {
-            x.x = __ldg(a.k_scale + (int64_t)page * a.H + u.h);
-            x.y = log2f(__ldg(a.v_scale + (int64_t)page * a.H + u.h));
-          }
-        }
-        return x;
-      };
-      float2 next = make_float2(1.f, -INFINITY);
       float e_ref = -INFINITY;   // log2 of the largest V scale so far: o is in units of 2^(e_ref - kLift)
-      const int j0 = has_q1 ? 0 : t;
-      if (F8 && j0 < n_tiles) next = scales_of(j0);
       {
         uint32_t zero[32];
 #pragma unroll
@@ -821,8 +829,12 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           mbar_arrive(&bars->p_full[t]);
           continue;
         }
-        const float2 scale = next;
-        if (F8 && j + every < n_tiles) next = scales_of(j + every);
+        float2 scale;
+        if constexpr (F8) {
+          scale = make_float2(next.x, log2f(next.y));
+          next = scales_of(next_page);
+          next_page = page_of(j + 2 * every);
+        }
         bool w = !aborted(bars) && mbar_wait(&bars->s_full[t], (uint32_t)(has_q1 ? j : j >> 1) & 1u, lim);
         if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
         tc_fence_after();
