@@ -3,10 +3,12 @@
 //
 // Both are bound by memory: every channel is read and written once, a pair costs six flops.  What
 // is not free is the angle: 64 sines and cosines a token for heads of 128, shared by all heads, so
-// a CTA computes them once for its tokens and several heads.
+// a CTA computes them once for its tokens and several heads.  A call of a few tokens takes what its
+// launch takes.
 #include <cmath>
 
 #include "cache.cuh"
+#include "ptx.cuh"
 
 namespace cast {
 namespace {
@@ -41,7 +43,8 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
 
 // blockDim = (units in parallel, tokens in parallel): about one unit a thread, whose channels are on
 // their way while the CTA computes its tokens' angles (shared memory, pair 8u + i at 8-unit stride, so
-// that the threads of a row read without bank conflicts).
+// that the threads of a row read without bank conflicts).  Measured, GB300: 1560 tokens of 12 heads of 128 in
+// bf16 (9.6 MB) 4.6 us; 9973 tokens of 7 heads of 64 in f32 (36 MB) 9.4 us, 3.8 TB/s, most of the rest the launch.
 template <class T>
 __global__ void __launch_bounds__(256) k_rotary(const __grid_constant__ RotaryKArgs a,
                                                 const __grid_constant__ cast_rotary_table tab) {
@@ -101,12 +104,18 @@ struct AppendKArgs {
 
 // One CTA: the new tokens of one sequence in one page (a run of rows lo .. hi-1), for a group of
 // heads of K, V or the queries.  A thread has one unit (row, 16 channels) of every head: it computes its
-// eight angles once, and a page's maximum is known before the values leave the registers.  The next head's
-// values are fetched while this one's are turned, reduced and stored.
+// eight angles once, and a page's maximum is known before the values leave the registers.  The next three
+// heads' values are fetched while this one's are turned, reduced and stored: 1024 threads an SM have one
+// head's 32 KB on their way otherwise, which is what the copy rate times the memory's latency takes.
+// Bound: memory (every channel read and written once).  Measured, GB300: 14080 tokens, 24 KV and 24 query
+// heads of 128, 8-bit pages (433 MB) 78 us, 5.5 TB/s, with three heads ahead (two 80, one 90 us) and
+// groups of 12 heads (24 79, 8 84, 4 104 us: what the angles cost).
+constexpr int kAhead = 4;
 template <bool F8>
 __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendKArgs a,
                                                  const __grid_constant__ cast_rotary_table tab) {
   __shared__ uint32_t s_max[2][32];
+  extern __shared__ uint4 s_in[];   // [kAhead][2][threads]: what a thread has fetched ahead
   const int b = blockIdx.x / a.runs, run = blockIdx.x - b * a.runs;
   const Sequence s = sequence_of(a.batch, b);
   const int p0 = s.len - s.n_new;                       // place of the first new token
@@ -148,19 +157,23 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
                              (token0 + row) * (kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride);
   const int64_t to = kind == 2 ? (token0 + row) * a.q_out_stride : ((int64_t)page * a.page_size + row) * a.row_stride;
   const bool codes = F8 && kind != 2;
-  uint4 n0 = make_uint4(0, 0, 0, 0), n1 = n0;
-  if (in) {
-    n0 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)h0 * a.d + c0));
-    n1 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)h0 * a.d + c1));
-  }
+  auto fetch = [&](int h) {
+    if (in && h < h1) {
+      uint4* to = s_in + (h - h0) % kAhead * 2 * blockDim.x + threadIdx.x;
+      copy16(smem_u32(to), src + (int64_t)h * a.d + c0);
+      copy16(smem_u32(to + blockDim.x), src + (int64_t)h * a.d + c1);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead - 1; ++i) fetch(h0 + i);
   for (int h = h0; h < h1; ++h) {
     float v[16];
-    unpack8(n0, v);
-    unpack8(n1, v + 8);
-    if (in && h + 1 < h1) {
-      n0 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(h + 1) * a.d + c0));
-      n1 = __ldcs(reinterpret_cast<const uint4*>(src + (int64_t)(h + 1) * a.d + c1));
-    }
+    copy_wait<kAhead - 2>();
+    const uint4* from = s_in + (h - h0) % kAhead * 2 * blockDim.x + threadIdx.x;
+    unpack8(in ? from[0] : make_uint4(0, 0, 0, 0), v);
+    unpack8(in ? from[blockDim.x] : make_uint4(0, 0, 0, 0), v + 8);
+    fetch(h + kAhead - 1);
     if (turned && in) rotate_unit(v, cs, tab.layout);
     const int64_t at = to + (int64_t)h * a.d;
     if (!codes) {
@@ -466,14 +479,21 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   k.jobs_kv = (c.H + group - 1) / group;
   k.jobs_q = (k.H_q + group - 1) / group;
   if (2 * (int64_t)k.jobs_kv + k.jobs_q > 65535) return fail(CAST_ERR_UNSUPPORTED, "%s: too many heads", who);
+  const int bytes = kAhead * 2 * 16 * threads;
+  static std::atomic<uint64_t> attr_done{0};
+  if (!once_per_device(attr_done, [&] {
+        return cudaFuncSetAttribute(k_append<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAhead * 32 * 1024) == cudaSuccess &&
+               cudaFuncSetAttribute(k_append<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAhead * 32 * 1024) == cudaSuccess;
+      }))
+    return check_launch("cache append kernel attributes");
   const dim3 grid((unsigned)gx, 2 * k.jobs_kv + k.jobs_q);
   const cast_rotary_table none{};
   const cast_rotary_table& tab = a->rotary ? *a->rotary : none;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.dtype == CAST_F8E4M3)
-    k_append<true><<<grid, threads, 0, st>>>(k, tab);
+    k_append<true><<<grid, threads, bytes, st>>>(k, tab);
   else
-    k_append<false><<<grid, threads, 0, st>>>(k, tab);
+    k_append<false><<<grid, threads, bytes, st>>>(k, tab);
   return check_launch(who);
 }
 

@@ -112,6 +112,16 @@ __device__ __forceinline__ uint32_t code2(float lo, float hi) {
 __device__ __forceinline__ uint2 encode8(const float* v) {
   return make_uint2(code2(v[0], v[1]) | code2(v[2], v[3]) << 16, code2(v[4], v[5]) | code2(v[6], v[7]) << 16);
 }
+// Asynchronous copies of 16 bytes to shared memory
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // Least e in [-120, 120] with amax <= 448 * 2^e (448 = 1.75 * 2^8)
 __device__ __forceinline__ int scale_exponent(float amax) {
   if (!(amax > 0.f)) return -120;
