@@ -22,12 +22,14 @@
 // channel below 2^15: bf16's eight bits fit, and channels 2^30 below the largest are the first to lose
 // one.  The order of channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the
 // codes lie in their 32-bit words.
-// Bound: memory for bf16 pages, instructions for 8-bit ones (427 a block of 16 tokens, 2.1 a clock and
-// SM, against the 360 clocks that its 4 KB take at the copy rate).  Measured, GB300: 48 sequences with
-// windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB) 141 us, 5.9 TB/s; 24 sequences
-// of 8k to 32k tokens in 8 bits (1.11 GB) 202 us, 5.5 TB/s.  The latter decoding everything to bf16 with
-// integer operations 438 us; by f16 236 us with three CTAs an SM, 246 with two, 255 with four; then
-// 202 us with copies that test a whole block at once and logits scaled inside the exponent.
+// bf16 pages: a probability is two bf16 numbers, since memory leaves the time for the second product.
+// Bound: memory for bf16 pages; for 8-bit ones memory and the latency of dependent instructions (390 a block
+// of 16 tokens, issued in half of the slots: three CTAs of 166 registers a thread are what an SM holds).
+// Measured, GB300: 48 sequences with windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB)
+// 143 us, 5.8 TB/s; 24 sequences of 8k to 32k tokens in 8 bits (1.11 GB) 188 to 208 us, 5.4 to 5.9 TB/s.  The
+// latter decoding everything to bf16 with integer operations 438 us; by f16 236 us with three CTAs an SM, 246
+// with two, 255 with four; then 202 us with copies that test a whole block at once and logits scaled inside
+// the exponent.  Units of 32 rows (MT = 2) are for 64-channel heads, which leave the registers for it.
 #include <cmath>
 
 #include "cache.cuh"

@@ -32,6 +32,14 @@
 // A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
 // warpgroup and odd ones to the other, each with its own S, o, maximum and sum, so that the products of one
 // overlap the softmax of the other; the two are joined at the end.
+//
+// Bound: products and exponentials, about 1 us each of the 1.6 us (8 bits: 1.9 us) that a key tile of two query
+// tiles takes; with one query tile of few rows the products of 128 rows (1 us a key tile, of which memory
+// needs 0.73 us).  A CTA's first key tile is done 10 us after its start.  Measured, GB300: 3520 rows of 24 heads
+// of 128 over 28160 positions, bf16 803 us, 1516 TFLOP/s, 8 bits 914 us, 1333 TFLOP/s; 1560 rows of 12 heads over
+// 12480 of 24960 positions, bf16 111 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
+// 78 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
+// 1 % slower.
 #include <cmath>
 
 #include "cache.cuh"
