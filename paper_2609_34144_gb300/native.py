@@ -610,15 +610,13 @@ _pack_attention = struct.Struct("@64s" + _BATCH + "PqiiiifPiP").pack
 
 def _on(stream, t):
     """The stream's handle for a call on t's device."""
-    if not t.is_cuda:
-        raise ValueError("expected CUDA tensors")
     return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _heads_stride(t, name, dtype=torch.bfloat16):
     """Token row stride of a [T, H, d] tensor whose (H, d) are contiguous."""
-    if t.dim() != 3 or (dtype is not None and t.dtype is not dtype):
-        raise ValueError(f"{name}: expected [T, H, d] of {dtype}")
+    if t.dim() != 3 or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
+        raise ValueError(f"{name}: expected [T, H, d] of {dtype or 'bf16 or f32'} on the GPU")
     T, H, d = t.shape
     if T < 2:
         if not t.is_contiguous():
@@ -631,8 +629,8 @@ def _heads_stride(t, name, dtype=torch.bfloat16):
 
 
 def _int32(t, name, shape=None):
-    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name}: expected a contiguous int32 tensor" + (f" of shape {shape}" if shape else ""))
+    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor on the GPU" + (f" of shape {shape}" if shape else ""))
     return t.data_ptr()
 
 
@@ -681,14 +679,15 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
                 k_scale.data_ptr() if f8 else None, v_scale.data_ptr() if f8 else None)
     c._keep = (k, v, k_scale, v_scale)
     c.packed = bytes(c)
+    c.on_gpu = all(t.is_cuda for t in (k, v, k_scale, v_scale) if t is not None)
     c.heads = (H, d)
     return c
 
 
 def _batch(page_table, kv_len, cu_new, T, max_new):
     """The fields of CacheBatch."""
-    if page_table.dim() != 2 or page_table.dtype is not torch.int32:
-        raise ValueError("page_table: expected int32 [B, max_pages]")
+    if page_table.dim() != 2 or page_table.dtype is not torch.int32 or not page_table.is_cuda:
+        raise ValueError("page_table: expected int32 [B, max_pages] on the GPU")
     B, P = page_table.shape
     s0, s1 = page_table.stride()
     if P > 1 and s1 != 1:
@@ -705,8 +704,8 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
     already.  cu_new [B + 1]: ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes]
     (None: a token's place in its sequence).  With q [T, H_q, d] returns it rotated."""
     T, H, d = k.shape
-    if v.shape != k.shape or (H, d) != cache.heads:
-        raise ValueError("k and v must be [T, H, d] of the cache's heads")
+    if v.shape != k.shape or (H, d) != cache.heads or not cache.on_gpu:
+        raise ValueError("k and v must be [T, H, d] of the cache's heads, the cache on the GPU")
     pos = 0
     if positions is not None and rotary is not None:
         pos = _int32(positions, "positions", (T,) if positions.dim() == 1 and rotary.n_axes == 1 else (T, rotary.n_axes))
@@ -736,16 +735,18 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     window > 0: a row sees the last `window` positions and the first `sinks`.  Returns
     o [T, H_q*d] (and lse [T, H_q])."""
     T, Hq, d = q.shape
-    if d != cache.heads[1]:
-        raise ValueError("q must be [T, H_q, d] of the cache's head dim")
+    if d != cache.heads[1] or not cache.on_gpu:
+        raise ValueError("q must be [T, H_q, d] of the cache's head dim, the cache on the GPU")
     dev = q.device
     o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
-    if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous()):
-        raise ValueError("out must be contiguous [T, H_q*d]")
+    if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous() or not o.is_cuda):
+        raise ValueError("out must be contiguous [T, H_q*d] on the GPU")
     lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
     a = _pack_attention(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), 0 if lse is None else lse.data_ptr())
     ws = workspace
+    if ws is not None and not ws.is_cuda:
+        raise ValueError("workspace must be on the GPU")
     if ws is None:
         need = _lib.cast_cache_attention_workspace_size(a)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None

@@ -565,3 +565,66 @@ def test_rollout_example(lib, bits):
         out = r.routed_chunk(n_frames=3, anchors=(0, 2), K=2)
         assert torch.isfinite(out.float()).all()
     lib.cast_check_device()
+
+
+def test_binding_refuses_tensors_that_are_not_on_the_gpu(lib):
+    k, q = (torch.zeros(2, h, 64, dtype=torch.bfloat16, device="cuda") for h in (1, 2))
+    pages = torch.zeros(2, 16, 1, 64, dtype=torch.bfloat16, device="cuda")
+    cache, host_cache = lib.kv_cache(pages, pages.clone()), lib.kv_cache(pages.cpu(), pages.cpu())
+    table, n = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((1, 2), (1,)))
+    n += 2
+    cu, pos, turns = torch.tensor([0, 2], dtype=torch.int32), torch.zeros(2, dtype=torch.int32), lib.rotary_table(64)
+    calls = [lambda: lib.cast_rotary(k, pos, turns), lambda: lib.cast_rotary(k, pos.cuda(), turns, out=k.cpu())]
+    for f, x in ((lambda *a, **kw: lib.cast_cache_append(a[0], a[0], *a[1:], **kw), k), (lib.cast_cache_attention, q)):
+        calls += [lambda f=f, x=x, a=a, kw=kw: f(x if a[0] else x.cpu(), *a[1:], **kw) for a, kw in (
+            ((0, cache, table, n), {}), ((1, host_cache, table, n), {}), ((1, cache, table.cpu(), n), {}),
+            ((1, cache, table, n.cpu()), {}), ((1, cache, table, n), dict(cu_new=cu)))]
+    calls += [lambda: lib.cast_cache_append(k, k.cpu(), cache, table, n), lambda: lib.cast_cache_append(k, k, cache, table, n, q=q.cpu()),
+              lambda: lib.cast_cache_append(k, k, cache, table, n, q=q, q_out=q.cpu()),
+              lambda: lib.cast_cache_append(k, k, cache, table, n, rotary=turns, positions=pos),
+              lambda: lib.cast_cache_attention(q, cache, table, n, out=q.cpu()),
+              lambda: lib.cast_cache_attention(q, cache, table, n, workspace=torch.empty(1 << 20, dtype=torch.uint8))]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+
+
+# Work that is dealt out in shares which begin and end inside units, of one query tile and of two, at their first
+# key tiles, between units and at their last
+CUT = [
+    ([20000, 131, 4100, 257], [9, 20, 40, 64], 2, 8, 64, 64, True, 0, 0),
+    ([9000] * 7, [5] * 7, 3, 15, 128, 16, True, 4000, 100),
+    ([6000, 6100, 6200], [300, 129, 17], 2, 4, 128, 32, False, 0, 0),
+    ([0, 12000, 1], [6, 40, 6], 1, 24, 128, 128, True, 0, 0),
+    ([1100 + 130 * i for i in range(9)], [70 - 7 * i for i in range(9)], 5, 5, 64, 16, True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("lens,new,H,Hq,d,page,causal,window,sinks", CUT)
+def test_units_cut_anywhere(lib, lens, new, H, Hq, d, page, causal, window, sinks, f8):
+    P = Pages(lib, lens, H, d, page, f8, seed=8).fill(9)
+    q, o, lse = attend(lib, P, new, Hq, causal, window, sinks)
+    lib.cast_check_device()
+    check(P, q, o, lse, new, Hq, causal, window, sinks)
+
+
+def test_append_of_more_heads_than_are_fetched_ahead(lib):
+    """Every number of heads from one to more than a CTA takes, into bf16 and 8-bit pages, the same rows as head by head."""
+    for f8 in (False, True):
+        for H in (1, 2, 3, 4, 5, 13, 25):
+            P, one = (Pages(lib, [300], H, 64, 64, f8, seed=1) for _ in range(2))
+            k, v = (randn(gen(s), 300, H, 64).to(torch.bfloat16) for s in (1, 2))
+            lib.cast_cache_append(k, v, P.cache, P.table, P.len_tensor())
+            for h in range(H):
+                pages = [t[:, :, h:h + 1].contiguous() for t in (one.k, one.v)]
+                scales = [t[:, h:h + 1].contiguous() for t in (one.ks, one.vs)] if f8 else []
+                lib.cast_cache_append(k[:, h:h + 1].contiguous(), v[:, h:h + 1].contiguous(), lib.kv_cache(*pages, *scales),
+                                      P.table, P.len_tensor())
+                used = P.table[0, :5].long()
+                for a, b in zip((P.k, P.v), pages):
+                    a, b = (t[used].view(torch.uint8 if f8 else torch.int16) for t in (a[:, :, h:h + 1].contiguous(), b))
+                    assert torch.equal(a.reshape(5 * 64, -1)[:300], b.reshape(5 * 64, -1)[:300]), (f8, H, h)
+                for a, b in zip((P.ks, P.vs), scales):
+                    assert torch.equal(a[used, h], b[used, 0])
+    lib.cast_check_device()
