@@ -13,7 +13,8 @@
 // lanes fetch K and V rows with 16-byte asynchronous copies into a private ring of stages, in an
 // order of 16-byte chunks that ldmatrix reads without bank conflicts, and rows that no row of the
 // unit sees are filled with zeros instead of being read.  S = Q K^T and o += P V are m16n8k16
-// products: at 16 rows the tensor cores wait for memory anyway.
+// products: at 16 rows the tensor cores wait for memory anyway.  Where a head's rows are short a unit is
+// two KV heads side by side, two warps each, which read the same memory pages at the same time.
 //
 // 8-bit rows: codes become f16 (one conversion for two, exact) on the way from shared memory to the
 // products, and the scales stay outside: a page's K scale multiplies its logits, and o is kept in
@@ -26,10 +27,11 @@
 // Bound: memory for bf16 pages; for 8-bit ones memory and the latency of dependent instructions (390 a block
 // of 16 tokens, issued in half of the slots: three CTAs of 166 registers a thread are what an SM holds).
 // Measured, GB300: 48 sequences with windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB)
-// 143 us, 5.8 TB/s; 24 sequences of 8k to 32k tokens in 8 bits (1.11 GB) 188 to 208 us, 5.4 to 5.9 TB/s.  The
-// latter decoding everything to bf16 with integer operations 438 us; by f16 236 us with three CTAs an SM, 246
-// with two, 255 with four; then 202 us with copies that test a whole block at once and logits scaled inside
-// the exponent.  Units of 32 rows (MT = 2) are for 64-channel heads, which leave the registers for it.
+// 144 us, 5.8 TB/s; 24 sequences of 8k to 32k tokens in 8 bits (1.11 GB) 190 us, 5.8 TB/s.  The latter decoding
+// everything to bf16 with integer operations 438 us; by f16 236 us with three CTAs an SM, 246 with two, 255
+// with four; then 205 us with copies that test a whole block at once and logits scaled inside the exponent,
+// and 190 us with two heads side by side.  Units of 32 rows (MT = 2) are for 64-channel heads, which leave the
+// registers for it.
 #include <cmath>
 
 #include "cache.cuh"
@@ -43,7 +45,7 @@ constexpr float kRescale = 8.f;   // the running maximum is renewed when a logit
 // 8-bit pages: probabilities, at most 2^8 times a row's largest, are lifted by 2^7 to use f16's range
 constexpr float kLift = 7.f;
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr int kWarps = 4;
+constexpr int kWarpsLog = 2, kWarps = 1 << kWarpsLog;
 
 struct RowsKArgs {
   cast_cache_batch batch;
@@ -59,8 +61,9 @@ struct RowsKArgs {
   int row_tiles;      // units of 16 * MT rows that a sequence may have
   int least;          // blocks that a CTA takes at least
   int whole;          // every CTA has one whole unit
-  float* part_o;      // [2 * grid][16 * MT][D]
-  float2* part_ml;    // [2 * grid][16 * MT]
+  int two, units;     // 1: units of two KV heads side by side, else 0; units of an entry
+  float* part_o;      // [2 * grid][1 + two][16 * MT][D]
+  float2* part_ml;    // [2 * grid][1 + two][16 * MT]
 };
 
 // What the rows of one unit see: blocks [0, n_sink) and [first, end) of 16 positions, and within
@@ -182,6 +185,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q4 = lane & 3;
   const int entries = a.batch.B * a.row_tiles;
+  // units of an entry; the warp's head in a unit, its first block and the step to its next
+  const int two = a.two, units = a.units, head = warp & two, sub = warp >> two, step = kWarps >> two;
 
   // Rows of units without any block get zeros (one CTA's threads do this)
   auto zero_rows = [&](int e, int h0, int h1) {
@@ -201,11 +206,11 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
   int entry;
   int64_t at, stop, entry_at = 0;
   if (a.whole) {
-    entry = blockIdx.x / a.H;
-    const int h = blockIdx.x - entry * a.H;
+    entry = blockIdx.x / units;
+    const int h = blockIdx.x - entry * units;
     const int nb = span_of(a, entry / a.row_tiles, entry % a.row_tiles, C::ROWS).blocks();
     if (nb == 0) {
-      zero_rows(entry, h, h + 1);
+      zero_rows(entry, h << two, (h + 1) << two);
       return;
     }
     at = (int64_t)h * nb;
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
     none = __syncthreads_or(none);
     int64_t total = 0;
     for (int w = 0; w < kWarps; ++w) total += s_work[w];
-    total *= a.H;
+    total *= units;
     const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
     at = blockIdx.x * share;
     stop = min(at + share, total);
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
           const int y = __shfl_up_sync(0xffffffffu, sum, o);
           if (lane >= o) sum += y;
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * a.H > at);
+        const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * units > at);
         if (hit) {
           if (lane == __ffs(hit) - 1) {
             s_entry = e;
@@ -254,7 +259,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
     }
     __syncthreads();
     entry = s_entry;
-    entry_at = s_before * a.H;
+    entry_at = s_before * units;
   }
 
   uint8_t* ring = smem + warp * C::RING;
@@ -265,9 +270,10 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
     const Span z = span_of(a, b, tile, C::ROWS);
     const int nb = z.blocks();
     const int* table = a.batch.page_table + (int64_t)b * a.batch.page_table_stride;
-    for (int h = nb ? (int)((at - entry_at) / nb) : a.H; h < a.H && at < stop; ++h) {
-      // blocks k0 .. k1-1 of unit (b, tile, h)
-      const int64_t unit_at = entry_at + (int64_t)h * nb;
+    for (int x = nb ? (int)((at - entry_at) / nb) : units; x < units && at < stop; ++x) {
+      // blocks k0 .. k1-1 of unit (b, tile, x)
+      const int64_t unit_at = entry_at + (int64_t)x * nb;
+      const int h = (x << two) + head;
       const int k0 = (int)(at - unit_at);
       const int k1 = (int)min((int64_t)nb, stop - unit_at);
 
@@ -364,7 +370,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       };
       // fetches block i of the unit into stage st: in copy c lane l has chunk l % CHUNKS of row
       // c * LANE_ROWS + l / CHUNKS
-      const int64_t row_bytes = a.row_stride * (F8 ? 1 : 2), step = row_bytes * C::LANE_ROWS;
+      const int64_t row_bytes = a.row_stride * (F8 ? 1 : 2), copy_step = row_bytes * C::LANE_ROWS;
       const int64_t lane_off = (lane / C::CHUNKS) * row_bytes + lane % C::CHUNKS * 16 + (int64_t)h * C::ROWB;
       auto fetch = [&](int i, int st, int page) {
         const int base = z.block(i) * 16;
@@ -376,8 +382,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
           for (int c = 0; c < C::COPIES; ++c) {
             const uint32_t to = dst + chunk_at<C::ROWB>(c * C::LANE_ROWS + lane / C::CHUNKS, lane % C::CHUNKS);
-            copy16(to, ks + c * step);
-            copy16(to + C::BLOCK, vs + c * step);
+            copy16(to, ks + c * copy_step);
+            copy16(to + C::BLOCK, vs + c * copy_step);
           }
         } else {
 #pragma unroll
@@ -385,8 +391,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
             const int r = c * C::LANE_ROWS + lane / C::CHUNKS, p = base + r;
             const bool in = page >= 0 && p < z.hi && (p >= z.lo || p < z.sinks);
             const uint32_t to = dst + chunk_at<C::ROWB>(r, lane % C::CHUNKS);
-            copy16_or_zero(to, in ? ks + c * step : a.k, in);
-            copy16_or_zero(to + C::BLOCK, in ? vs + c * step : a.v, in);
+            copy16_or_zero(to, in ? ks + c * copy_step : a.k, in);
+            copy16_or_zero(to + C::BLOCK, in ? vs + c * copy_step : a.v, in);
           }
         }
         if constexpr (F8) {
@@ -397,14 +403,14 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
           }
         }
       };
-      const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) / kWarps : 0;   // blocks of this warp
-      const int i0 = k0 + warp;
+      const int n = k1 - k0 > sub ? (k1 - k0 - sub + step - 1) >> (kWarpsLog - two) : 0;   // blocks of this warp
+      const int i0 = k0 + sub;
       __syncwarp();
       for (int st = 0; st < C::STAGES - 1; ++st) {
-        if (st < n) fetch(i0 + st * kWarps, st, page_of(i0 + st * kWarps));
+        if (st < n) fetch(i0 + st * step, st, page_of(i0 + st * step));
         copy_commit();
       }
-      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * kWarps) : -1;
+      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * step) : -1;
 
       int st = 0, into = C::STAGES - 1;
       for (int it = 0; it < n; ++it) {
@@ -412,9 +418,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
         __syncwarp();
         // the stage used one block ago takes the block STAGES - 1 ahead
         const int ahead = it + C::STAGES - 1;
-        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_page);
+        if (ahead < n) fetch(i0 + ahead * step, into, next_page);
         copy_commit();
-        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * kWarps);
+        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * step);
         const uint32_t kt = ring_at + st * 2 * C::BLOCK, vt = kt + C::BLOCK;
         float s[MT][2][4];
 #pragma unroll
@@ -452,7 +458,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
             }
           }
         }
-        const int base = z.block(i0 + it * kWarps) * 16;
+        const int base = z.block(i0 + it * step) * 16;
         const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
         float times[MT][2];
         bool grows = false;
@@ -629,7 +635,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       copy_wait<0>();
       __syncthreads();   // every warp is done with its ring: the merge takes the space
 
-      // ---- join the warps
+      // ---- join the warps of a head
       float* mo = reinterpret_cast<float*>(smem);                        // [warp][row][D]
       float2* ml = reinterpret_cast<float2*>(mo + kWarps * C::ROWS * D); // [warp][row]
 #pragma unroll
@@ -659,43 +665,49 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       const bool complete = k0 == 0 && k1 == nb;
       // a share that begins inside the unit leaves its part in the CTA's first place
       const int slot = 2 * blockIdx.x + (k0 > 0 ? 0 : 1);
-      for (int x = threadIdx.x; x < C::ROWS * D / 4; x += kWarps * 32) {
-        const int rr = x / (D / 4), c = x % (D / 4) * 4;
-        const int r = tile * C::ROWS + rr;
-        if (r >= z.n_rows) continue;
-        float top = -INFINITY;
+      for (int hw = 0; hw <= two; ++hw)
+        for (int y = threadIdx.x; y < C::ROWS * D / 4; y += kWarps * 32) {
+          const int rr = y / (D / 4), c = y % (D / 4) * 4;
+          const int r = tile * C::ROWS + rr;
+          if (r >= z.n_rows) continue;
+          float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * C::ROWS + rr].x);
-        float sum = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int w = 0; w < kWarps; ++w) top = fmaxf(top, (w & two) == hw ? ml[w * C::ROWS + rr].x : -INFINITY);
+          float sum = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float2 v = ml[w * C::ROWS + rr];
-          const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
-          sum += f * v.y;
-          const float4 y = *reinterpret_cast<const float4*>(mo + (w * C::ROWS + rr) * D + c);
-          acc.x += f * y.x; acc.y += f * y.y; acc.z += f * y.z; acc.w += f * y.w;
-        }
-        if (complete) {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
-          if (a.o_f32) {
-            *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c) =
-                make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-          } else {
-            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c) =
-                make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+          for (int w = 0; w < kWarps; ++w) {
+            // the other head's values are read and left out: no load waits for another
+            const float2 v = ml[w * C::ROWS + rr];
+            const float4 o4 = *reinterpret_cast<const float4*>(mo + (w * C::ROWS + rr) * D + c);
+            const bool its = (w & two) == hw;
+            const float f = v.x == -INFINITY ? 0.f : exp2_fast(v.x - top);
+            sum = its ? fmaf(f, v.y, sum) : sum;
+            acc.x = its ? fmaf(f, o4.x, acc.x) : acc.x;
+            acc.y = its ? fmaf(f, o4.y, acc.y) : acc.y;
+            acc.z = its ? fmaf(f, o4.z, acc.z) : acc.z;
+            acc.w = its ? fmaf(f, o4.w, acc.w) : acc.w;
           }
-          if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-        } else {
-          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * C::ROWS + rr) * D + c) = acc;
-          if (c == 0) a.part_ml[(int64_t)slot * C::ROWS + rr] = make_float2(top, sum);
+          if (complete) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + ((x << two) + hw) * a.group + r % a.group;
+            if (a.o_f32) {
+              *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c) =
+                  make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            } else {
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + row * D + c) =
+                  make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+            }
+            if (a.lse && c == 0) a.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+          } else {
+            *reinterpret_cast<float4*>(a.part_o + ((((int64_t)slot << two) + hw) * C::ROWS + rr) * D + c) = acc;
+            if (c == 0) a.part_ml[(((int64_t)slot << two) + hw) * C::ROWS + rr] = make_float2(top, sum);
+          }
         }
-      }
       __syncthreads();   // the space goes back to the rings
       at = unit_at + k1;
     }
-    entry_at += (int64_t)nb * a.H;
+    entry_at += (int64_t)nb * units;
   }
 }
 
@@ -730,12 +742,13 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
     total += s_sum[w];
     at += s_before[w];
   }
-  total *= a.H;
+  const int units = a.units;
+  total *= units;
   const int64_t share = max((int64_t)a.least, (total + ctas - 1) / ctas);
   const int tile = entry % a.row_tiles;
   const Span z = span_of(a, entry / a.row_tiles, tile, ROWS);
   const int nb = z.blocks();
-  at = at * a.H + (int64_t)h * nb;
+  at = at * units + (int64_t)(h >> a.two) * nb;
   if (nb == 0) return;
   const int c0 = (int)(at / share), c1 = (int)((at + nb - 1) / share);
   if (c0 == c1) return;   // written whole
@@ -750,11 +763,15 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
     float top = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (in) {
+      // of the CTAs' first places
+      const float2* ml = a.part_ml + (((int64_t)c0 * 2 << a.two) + (h & a.two)) * ROWS + rr;
+      const float* po = a.part_o + ((((int64_t)c0 * 2 << a.two) + (h & a.two)) * ROWS + rr) * D + c * 4;
+      const int each = ROWS << a.two;   // rows from a CTA's first place to its second
 #pragma unroll 4
       for (int i = mine; i < parts; i += per_row * GROUPS) {
-        const int64_t slot = 2 * (int64_t)(c0 + i) + (i == 0 ? 1 : 0);
-        const float2 v = a.part_ml[slot * ROWS + rr];
-        const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * ROWS + rr) * D + c * 4);
+        const int64_t rows_on = (int64_t)(2 * i + (i == 0 ? 1 : 0)) * each;
+        const float2 v = ml[rows_on];
+        const float4 y = *reinterpret_cast<const float4*>(po + rows_on * D);
         const float m = fmaxf(top, v.x);
         const float f0 = top == -INFINITY ? 0.f : exp2_fast(top - m), f1 = v.x == -INFINITY ? 0.f : exp2_fast(v.x - m);
         l = f0 * l + f1 * v.y;
@@ -797,7 +814,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
 
 // ---------------------------------------------------------------- host side
 struct RowsPlan {
-  int mt, row_tiles, grid, least;
+  int mt, row_tiles, grid, least, two;
   bool whole;            // a CTA takes a whole unit; else units may be split and are merged
   size_t part_o_bytes, total_bytes;
 };
@@ -826,8 +843,17 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
     p.grid = units > 0x7fffffff ? 0 : (int)units;
     return p;
   }
-  p.part_o_bytes = align_up((size_t)2 * p.grid * rows * a.cache.d * sizeof(float));
-  p.total_bytes = p.part_o_bytes + align_up((size_t)2 * p.grid * rows * sizeof(float2));
+  // Units of two KV heads side by side, where one head's rows are at most 128 bytes in rows of 1 KB or more:
+  // what a fetch takes of a memory page is little otherwise.  Measured, one head / two, us: 24 sequences of 8k
+  // to 32k tokens, 8 bits, 8 heads of 128 205 / 189, 8 heads of 64 165 / 127, 16 heads of 64 390 / 238; 48
+  // windows of 4096, bf16, 8 heads of 64 93 / 86, 12 heads 135 / 117, but 8 heads of 128 (256 bytes) 144 / 145;
+  // 8 bits, 4 heads of 128 (512 bytes) 184 / 185.  A unit's parts are twice as many: with 64 units 73 / 72,
+  // 32 units 44 / 46.
+  const int row = a.cache.d * (a.cache.dtype == CAST_F8E4M3 ? 1 : 2);
+  p.two = row <= 128 && a.cache.H % 2 == 0 && (int64_t)a.cache.H * row >= 1024 && (int64_t)a.batch.B * p.row_tiles * a.cache.H >= 128;
+  p.least >>= p.two;
+  p.part_o_bytes = align_up(((size_t)2 * p.grid << p.two) * rows * a.cache.d * sizeof(float));
+  p.total_bytes = p.part_o_bytes + align_up(((size_t)2 * p.grid << p.two) * rows * sizeof(float2));
   return p;
 }
 
@@ -948,6 +974,8 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   k.row_tiles = p.row_tiles;
   k.least = p.least;
   k.whole = p.whole;
+  k.two = p.two;
+  k.units = c.H >> p.two;
   k.part_o = static_cast<float*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
   cudaStream_t st = static_cast<cudaStream_t>(stream);

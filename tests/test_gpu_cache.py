@@ -628,3 +628,17 @@ def test_append_of_more_heads_than_are_fetched_ahead(lib):
                 for a, b in zip((P.ks, P.vs), scales):
                     assert torch.equal(a[used, h], b[used, 0])
     lib.cast_check_device()
+
+
+@pytest.mark.parametrize("f8,H,d", [(True, 8, 128), (True, 16, 64), (True, 18, 64), (False, 8, 64), (False, 10, 64)])
+@pytest.mark.parametrize("causal,window,sinks", [(True, 0, 0), (True, 1100, 20)])
+def test_many_heads_of_short_rows(lib, f8, H, d, causal, window, sinks):
+    """Heads whose rows are short, in sequences from nothing to over a thousand tokens."""
+    lens = [(131 * i * i) % 1500 for i in range(16)]
+    new = [1 + i % 2 for i in range(16)]
+    lens = [max(m, n) for m, n in zip(lens, new)]
+    lens[5], new[5], lens[6] = 0, 0, 1500
+    P = Pages(lib, lens, H, d, 32, f8, seed=2).fill(5)
+    q, o, lse = attend(lib, P, new, 3 * H, causal, window, sinks)
+    lib.cast_check_device()
+    check(P, q, o, lse, new, 3 * H, causal, window, sinks)
