@@ -41,6 +41,7 @@
 // 78 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
 // 1 % slower.
 #include <cmath>
+#include <type_traits>
 
 #include "cache.cuh"
 #include "cache_attention.cuh"
@@ -1160,12 +1161,13 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   }
 }
 
-// Joins the parts of the units that no CTA had whole: CTA (x, y, z) takes 32 rows (a lane each) and one of
-// gridDim.z shares of the channels of the unit that the share of CTA x + 1 begins inside of, if that is the
+// Joins the parts of the units that no CTA had whole: CTA (x, y, z) takes 32 rows (a lane each), and all
+// channels or a quarter of them, of the unit that the share of CTA x + 1 begins inside of, if that is the
 // first such share.  A warp has four channels and every so many of the parts, so that all of a CTA's loads
 // are on their way together.
 constexpr int kMergeWarps = 16;
-template <int HD>
+// SPREAD: units of few rows, of which four CTAs have a quarter of the channels each (then many CTAs had parts)
+template <int HD, bool SPREAD>
 __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_constant__ TilesKArgs a) {
   __shared__ float2 s_ml[kMergeWarps][32];
   __shared__ float4 s_o[kMergeWarps][32];
@@ -1187,6 +1189,54 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_c
   const bool in = tok < a.tile_tokens && i < u.n_new;
   if (!__any_sync(0xffffffffu, in)) return;   // the same rows in every warp
   auto place = [&](int p) { return pair ? t * 128 + row : row + (p & 1) * 128; };
+  const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
+  auto store = [&](int c, const float4& v) {
+    if (a.o_f32) *reinterpret_cast<float4*>(static_cast<float*>(a.o) + out * HD + c * 4) = v;
+    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + out * HD + c * 4) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+  };
+  // Few parts: every warp has the maxima and sums of all of them, and all of a round's loads are on their way
+  // at once: up to four parts of all of the warp's channels, or eight of four channels.
+  auto few = [&](auto most, auto at_once) {
+    constexpr int P = decltype(most)::value, Q = decltype(at_once)::value, COLUMNS = HD / 4 / kMergeWarps;
+    float2 ml[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) ml[p] = p < n ? a.part_ml[slot(p) * 256 + place(p)] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int k0 = 0; k0 < COLUMNS; k0 += Q) {
+      float4 y[Q][P];
+#pragma unroll
+      for (int k = 0; k < Q; ++k)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          y[k][p] = p < n ? a.part_o[(slot(p) * (HD / 4) + warp + (k0 + k) * kMergeWarps) * 256 + place(p)]
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+      float top = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int p = 0; p < P; ++p) top = fmaxf(top, ml[p].x);
+      float4 acc[Q];
+#pragma unroll
+      for (int k = 0; k < Q; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const float f = ml[p].x == -INFINITY ? 0.f : exp2_fast(ml[p].x - top);
+        l += f * ml[p].y;
+#pragma unroll
+        for (int k = 0; k < Q; ++k) {
+          acc[k].x += f * y[k][p].x; acc[k].y += f * y[k][p].y; acc[k].z += f * y[k][p].z; acc[k].w += f * y[k][p].w;
+        }
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int k = 0; k < Q; ++k)
+        store(warp + (k0 + k) * kMergeWarps, make_float4(acc[k].x * inv, acc[k].y * inv, acc[k].z * inv, acc[k].w * inv));
+      if (a.lse && warp == 0 && k0 == 0) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+    }
+  };
+  if constexpr (!SPREAD) if (n <= 8) {
+    if (in && n <= 4) few(std::integral_constant<int, 4>{}, std::integral_constant<int, HD / 64>{});
+    else if (in) few(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+    return;
+  }
   // maximum and sum: each warp over some of the parts, then over the warps
   float top = -INFINITY, l = 0.f;
   if (in)
@@ -1205,9 +1255,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_c
     l += v.x == -INFINITY ? 0.f : v.y * exp2_fast(v.x - top);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  const int64_t out = (int64_t)(u.t0 + i) * a.H_q + u.h * a.group + (row - tok * a.group);
   // columns of four channels: `columns` of them at a time, each by `sharers` warps
-  const int mine = HD / 4 / gridDim.z, columns = min(mine, kMergeWarps), sharers = kMergeWarps / columns;
+  constexpr int mine = HD / 4 / (SPREAD ? 4 : 1), columns = mine < kMergeWarps ? mine : kMergeWarps, sharers = kMergeWarps / columns;
   for (int k = 0; k < mine; k += columns) {
     const int c = blockIdx.z * mine + k + warp % columns;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1229,13 +1278,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_tiles_merge(const __grid_c
       }
     }
     if (!in) continue;
-    if (a.o_f32) {
-      *reinterpret_cast<float4*>(static_cast<float*>(a.o) + out * HD + c * 4) =
-          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    } else {
-      *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + out * HD + c * 4) =
-          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    }
+    store(c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
   }
   if (a.lse && in && warp == 0 && blockIdx.z == 0) a.lse[out] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
 }
@@ -1288,8 +1331,8 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   // 32 rows of a unit a CTA, as many as a unit may have
   const int most = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int rows = most > k.tile_tokens ? 8 : (most * k.group + 31) / 32;
-  // and a quarter of the channels, where a unit has few rows
-  cfg.gridDim = dim3((unsigned)(p.grid - 1), rows, rows <= 2 ? 4 : 1);
+  const bool spread = rows <= 2;
+  cfg.gridDim = dim3((unsigned)(p.grid - 1), rows, spread ? 4 : 1);
   cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -1297,7 +1340,7 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, k_tiles_merge<HD>, k) != cudaSuccess) return check_launch("cache attention merge");
+  if (cudaLaunchKernelEx(&cfg, spread ? k_tiles_merge<HD, true> : k_tiles_merge<HD, false>, k) != cudaSuccess) return check_launch("cache attention merge");
   return check_launch("cache attention merge");
 }
 
