@@ -35,10 +35,10 @@
 //
 // Bound: products and exponentials, about 1 us each of the 1.6 us (8 bits: 1.9 us) that a key tile of two query
 // tiles takes; with one query tile of few rows the products of 128 rows (1 us a key tile, of which memory
-// needs 0.73 us).  A CTA's first key tile is done 10 us after its start.  Measured, GB300: 3520 rows of 24 heads
-// of 128 over 28160 positions, bf16 803 us, 1516 TFLOP/s, 8 bits 914 us, 1333 TFLOP/s; 1560 rows of 12 heads over
-// 12480 of 24960 positions, bf16 111 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
-// 78 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
+// needs 0.73 us).  A CTA's first key tile is done 7 to 10 us after its start.  Measured, GB300: 3520 rows of 24
+// heads of 128 over 28160 positions, bf16 803 us, 1516 TFLOP/s, 8 bits 912 us, 1336 TFLOP/s; 1560 rows of 12 heads
+// over 12480 of 24960 positions, bf16 106 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
+// 75 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
 // 1 % slower.
 #include <cmath>
 #include <type_traits>
@@ -1164,7 +1164,8 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 // Joins the parts of the units that no CTA had whole: CTA (x, y, z) takes 32 rows (a lane each), and all
 // channels or a quarter of them, of the unit that the share of CTA x + 1 begins inside of, if that is the
 // first such share.  A warp has four channels and every so many of the parts, so that all of a CTA's loads
-// are on their way together.
+// are on their way together.  Bound: latency (measured: with eight parts loaded at once instead of summed one
+// after the other 1000 rows of 6 heads over 9000 positions 41 -> 38 us in all).
 constexpr int kMergeWarps = 16;
 // SPREAD: units of few rows, of which four CTAs have a quarter of the channels each (then many CTAs had parts)
 template <int HD, bool SPREAD>
