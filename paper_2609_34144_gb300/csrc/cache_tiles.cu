@@ -150,8 +150,8 @@ __device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const S
 }
 // Work: a key tile of two query tiles takes 2.1 us, of one query tile 1 us, and a CTA that goes over to
 // another unit has the first key tile's softmax done ~10 us later, half of which other CTAs' memory traffic
-// gains (decode of 35 rows, 60k positions, 8 bits, with no charge 85, 8 81, 10 us 83; window of 1560 frame
-// tokens 114, 111 and 113 us; frames of 3520 tokens 925, 929 and 930 us).
+// gains (with no charge, one of 8 us and one of 12 us: decode of 35 rows, 60k positions, 8 bits, 85, 81, 83 us;
+// window of 1560 frame tokens 114, 110, 113 us; frames of 3520 tokens 925, 929, 930 us).
 constexpr int kBegin = 16, kPair = 4, kSingle = 2;
 __device__ __forceinline__ int tile_work(const TilesKArgs& a, const Unit& u) {
   return u.i0 + a.tile_tokens < u.n_new ? kPair : kSingle;
