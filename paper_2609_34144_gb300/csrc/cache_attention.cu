@@ -915,14 +915,15 @@ using namespace cast;
 extern "C" {
 
 // Up to 16 rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu),
-// except that heads of 64 with up to 32 rows stay where there are 32 units or more (two products of 16 rows
-// on the same keys).  Measured, tiles / rows, 32 rows, us: heads of 64, 64 units of 20k tokens 92 / 77 (8
-// bits), 92 / 79 (bf16), 108 units of 2.4k with 18 rows 34 / 28, 16 units of 60k 74 / 74, 8 units of 3k
-// 18 / 23; heads of 128, 16 units of 60k 82 / 95 (8 bits), 98 / 106 (bf16), 8 units of 3k 21 / 27.
+// except that heads of 64 with up to 32 rows stay where there are 64 units or more (two products of 16 rows
+// on the same keys).  Measured, tiles / rows, heads of 64, us, 8 bits and bf16: 256 units of 5k tokens with 32
+// rows 93 / 82, 96 / 82; 108 units of 2.4k with 18 rows 35 / 30, 35 / 31; 64 units of 20k with 32 rows 78 / 78,
+// 85 / 80; 32 units of 20k 48 / 54, 52 / 52; 16 units of 60k 63 / 71, 69 / 68; 8 units of 3k 19 / 22, 17 / 22.
+// Heads of 128 with 32 rows (before the last steps of the tiles): 16 units of 60k 82 / 95, 98 / 106.
 static bool by_tiles(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int64_t rows = (int64_t)max_new * (a.H_q / a.cache.H);
-  return rows > 32 || (rows > 16 && (a.cache.d != 64 || (int64_t)a.batch.B * a.cache.H < 32));
+  return rows > 32 || (rows > 16 && (a.cache.d != 64 || (int64_t)a.batch.B * a.cache.H < 64));
 }
 
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {
