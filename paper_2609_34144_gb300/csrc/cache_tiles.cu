@@ -353,6 +353,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
+// The larger, NaN where either is NaN
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 template <bool F8>
 __device__ __forceinline__ void init_barriers(Bars* bars) {
   mbar_init(&bars->q_full, F8 ? 256 : 1);
@@ -916,7 +922,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           const float w = kLift + fmaxf(scale.y - e_ref, -60.f), back = exp2_fast(-w);
 #pragma unroll
           for (int c = 0; c < BN; c += 16) {
-            const float by = unit * __shfl_sync(0xffffffffu, scale.x, c / 16);
+            // not 0: a hidden column's -inf has to stay -inf where a row of zeros (2^-123) meets a page of zero
+            // keys (2^-120).  NaN, a query that is not finite, stays NaN.
+            const float by = max_or_nan(unit * __shfl_sync(0xffffffffu, scale.x, c / 16), 0x1p-126f);
             const float add = __shfl_sync(0xffffffffu, w, c / 16) - ref;
             const float2 sc2 = make_float2(by, by), nm2 = make_float2(add, add);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
