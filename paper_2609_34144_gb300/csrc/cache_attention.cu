@@ -17,9 +17,9 @@
 // two KV heads side by side, two warps each, which read the same memory pages at the same time.
 //
 // 8-bit rows: codes become f16 (one conversion for two, exact) on the way from shared memory to the
-// products, and the scales stay outside: a page's K scale multiplies its logits, and o is kept in
-// units of the largest V scale so far over 2^7, a page's probabilities (f16) carrying its scale in those
-// units in their exponent.  Queries are f16 too, each row times the power of two that brings its largest
+// products, and the scales stay outside: a page's K scale multiplies its logits, and a row's o is kept in
+// units of the largest V scale that it has seen so far over 2^7, a page's probabilities (f16) carrying its scale
+// in those units in their exponent.  Queries are f16 too, each row times the power of two that brings its largest
 // channel below 2^15: bf16's eight bits fit, and channels 2^30 below the largest are the first to lose
 // one.  The order of channels inside a 16-wide step of Q K^T, and of o's columns, is that in which the
 // codes lie in their 32-bit words.
@@ -347,9 +347,12 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       }
 
       float o[MT][D / 8][4], m_ref[MT][2], l[MT][2];
-      float e_ref = -INFINITY;   // 8-bit pages: o is in units of 2^(e_ref - kLift)
+      // 8-bit pages: a row's o is in units of 2^(e_ref - kLift), e_ref log2 of the largest V scale that the row has
+      // seen so far (its own: a page that it does not see must not cost its values bits)
+      float e_ref[MT][2];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
+        e_ref[m][0] = e_ref[m][1] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < D / 8; ++t)
 #pragma unroll
@@ -512,22 +515,43 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
         }
         // 8-bit pages: probabilities carry the page's V scale in o's units; a scale 2^60 below the largest
         // adds nothing to o, and everything to the sum
-        float weight = 0.f, back = 1.f;   // log2, and its inverse for the sum
+        float weight[MT][2], back[MT][2];   // log2, and its inverse for the sum
+        const float e = F8 ? __log2f(sc.y) : 0.f;
         if constexpr (F8) {
-          const float e = __log2f(sc.y);
-          if (e > e_ref) {
-            const float f = exp2_fast(e_ref - e);
-            e_ref = e;
+          bool more = false;
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) more = more || e > e_ref[m][j];
+          if (more) {
+            const int last = min(base + 15, z.hi - 1);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-              for (int t = 0; t < D / 8; ++t)
+              for (int j = 0; j < 2; ++j) {
+                // whether the row sees any of the block
+                const int r = pos[m][j], up = a.causal ? min(last, r) : last;
+                const bool some = whole || (base <= up && (a.window <= 0 || up > r - a.window || base < a.sinks));
+                if (some && e > e_ref[m][j]) {
+                  const float f = exp2_fast(e_ref[m][j] - e);
+                  e_ref[m][j] = e;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) o[m][t][k] *= f;
+                  for (int t = 0; t < D / 8; ++t) {
+                    o[m][t][2 * j] *= f;
+                    o[m][t][2 * j + 1] *= f;
+                  }
+                }
+              }
           }
-          weight = kLift + fmaxf(e - e_ref, -60.f);
-          back = exp2_fast(-weight);
         }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            // (a page that the row does not see may have a larger scale)
+            weight[m][j] = F8 ? kLift + fmaxf(fminf(e - e_ref[m][j], 0.f), -60.f) : 0.f;
+            back[m][j] = F8 ? exp2_fast(-weight[m][j]) : 1.f;
+          }
         // bf16 pages: a probability is two bf16 numbers (16 bits of it); memory leaves the time for the
         // second product
         uint32_t pf[MT][4], rest[MT][4];
@@ -536,7 +560,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             // a row that has seen nothing yet: exp2(-inf - 0) = 0
-            const float ref = weight - (m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j]);
+            const float ref = weight[m][j] - (m_ref[m][j] == -INFINITY ? 0.f : m_ref[m][j]);
             float sum = 0.f;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -546,7 +570,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
                 s[m][t][2 * j + e] = p;
                 sum += p;
               }
-            l[m][j] = fmaf(sum, back, l[m][j]);
+            l[m][j] = fmaf(sum, back[m][j], l[m][j]);
           }
 #pragma unroll
           for (int t = 0; t < 2; ++t)
@@ -649,7 +673,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
           if (q4 == 0) ml[warp * C::ROWS + r] = make_float2(m_ref[m][j], x);
           float* dst = mo + (warp * C::ROWS + r) * D;
           if constexpr (F8) {
-            const float f = exp2_fast(e_ref) * 0x1p-7f;
+            const float f = exp2_fast(e_ref[m][j]) * 0x1p-7f;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c)
               *reinterpret_cast<float4*>(dst + c * 16 + q4 * 4) =

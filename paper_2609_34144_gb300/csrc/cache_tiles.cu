@@ -26,8 +26,8 @@
 // most, its first four bits and the rest are one each (channels 2^10 below the largest keep 2^-19 of
 // it).  So S is the sum of two products at twice the rate, and each page's scale multiplies its columns
 // of S.  V codes become f16 tiles (one conversion for two, by a fourth warpgroup, with the zeroing on the
-// way) and P is f16: o is kept in units of the largest V scale so far over 2^7, and a page's probabilities
-// carry its scale in those units in their exponent.
+// way) and P is f16: a row's o is kept in units of the largest V scale that it has seen so far over 2^7, and a
+// page's probabilities carry its scale in those units in their exponent.
 //
 // A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
 // warpgroup and odd ones to the other, each with its own S, o, maximum and sum, so that the products of one
@@ -351,12 +351,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-// The larger, NaN where either is NaN
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
 template <bool F8>
@@ -826,7 +820,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         }
         mbar_arrive(&bars->q_full);
       }
-      float e_ref = -INFINITY;   // log2 of the largest V scale so far: o is in units of 2^(e_ref - kLift)
+      // log2 of the largest V scale that the row has seen so far: its o is in units of 2^(e_ref - kLift).  It is
+      // the row's own, since a page that the row does not see must not cost its values bits.
+      float e_ref = -INFINITY;
       {
         uint32_t zero[32];
 #pragma unroll
@@ -834,6 +830,16 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll
         for (int c = 0; c < HD; c += 32) tmem_st_x32(tl + colO + c, zero);
       }
+      auto scale_o = [&](float f) {
+#pragma unroll 1
+        for (int c = 0; c < HD; c += 32) {
+          uint32_t x[32];
+          tmem_ld_x32(tl + colO + c, x);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+          tmem_st_x32(tl + colO + c, x);
+        }
+      };
       bool ok = true;
       uint32_t fixed = 0;
       const bool some_live = __any_sync(0xffffffffu, live);   // else this warp's rows are nobody's
@@ -859,6 +865,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           // S of columns that the row does not see (not below hi - pos, or below lo - pos and not below
           // sinks - pos) becomes -inf where it lies.  What few tiles need is kept in short loops: the
           // code that every tile runs has to stay in the instruction cache, for three kinds of warps.
+          float e = -INFINITY;   // 8-bit pages: log2 of the largest V scale that the row (if it is one) sees
 #pragma unroll 1
           for (int b = 0; b < BN; b += 32) {
             uint32_t x[32];
@@ -872,6 +879,15 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             for (int c = 0; c < 32; ++c)
               if (!((see >> c) & 1u)) x[c] = __float_as_uint(-INFINITY);
             tmem_st_x32(tl + colS + b, x);
+            if constexpr (F8) {
+              const float e0 = __shfl_sync(0xffffffffu, scale.y, b / 16), e1 = __shfl_sync(0xffffffffu, scale.y, b / 16 + 1);
+              e = fmaxf(e, fmaxf(!live || (see & 0xffffu) ? e0 : -INFINITY, !live || see >> 16 ? e1 : -INFINITY));
+            }
+          }
+          if (F8 && __any_sync(0xffffffffu, e > e_ref)) {
+            const float f = e > e_ref ? exp2_fast(e_ref - e) : 1.f;
+            e_ref = fmaxf(e, e_ref);
+            scale_o(f);
           }
         }
         uint32_t sr[BN];
@@ -908,7 +924,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         // a row that has seen nothing: 2^(-inf - 0) = 0
         const float ref = m_ref == -INFINITY ? 0.f : m_ref;
         if constexpr (F8) {
-          float e = scale.y;
+          float e = whole ? scale.y : -INFINITY;
 #pragma unroll
           for (int o = 4; o; o >>= 1) e = fmaxf(e, __shfl_xor_sync(0xffffffffu, e, o, 8));
           e = __shfl_sync(0xffffffffu, e, 0);
@@ -917,15 +933,15 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             e_ref = e;
             need = true;
           }
-          // log2 of what this lane's columns' probabilities are multiplied by (a scale 2^60 below the largest
-          // adds nothing to o, and everything to the sum), and its inverse for the sum
-          const float w = kLift + fmaxf(scale.y - e_ref, -60.f), back = exp2_fast(-w);
+          const float lift = kLift - ref;
 #pragma unroll
           for (int c = 0; c < BN; c += 16) {
-            // not 0: a hidden column's -inf has to stay -inf where a row of zeros (2^-123) meets a page of zero
-            // keys (2^-120).  NaN, a query that is not finite, stays NaN.
-            const float by = max_or_nan(unit * __shfl_sync(0xffffffffu, scale.x, c / 16), 0x1p-126f);
-            const float add = __shfl_sync(0xffffffffu, w, c / 16) - ref;
+            // never 0: a hidden column's -inf has to stay -inf where a row of zeros (2^-123) meets a page of zero
+            // keys (2^-120).  (A factor above 2^-102 is what it was; NaN, a query that is not finite, stays NaN.)
+            const float by = fmaf(unit, __shfl_sync(0xffffffffu, scale.x, c / 16), 0x1p-126f);
+            // log2 of the page's V scale in the row's units (a scale 2^60 below the largest adds nothing to o, and
+            // everything to the sum; a page that the row does not see may have a larger one)
+            const float in = fmaxf(fminf(__shfl_sync(0xffffffffu, scale.y, c / 16) - e_ref, 0.f), -60.f), add = in + lift;
             const float2 sc2 = make_float2(by, by), nm2 = make_float2(add, add);
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -937,8 +953,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
               sr[(c + k) / 2] = *reinterpret_cast<const uint32_t*>(&h2);
             }
             const float2 s2 = __fadd2_rn(sum[0], sum[1]);
-            l = fmaf(s2.x + s2.y, __shfl_sync(0xffffffffu, back, c / 16), l);
+            l = fmaf(s2.x + s2.y, exp2_fast(-in), l);   // 2^kLift times the sum
           }
+          tmem_st_x64(tl + colS, sr);
         } else {
           const float2 sc2 = make_float2(unit, unit), nm2 = make_float2(-ref, -ref);
           float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -952,18 +969,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           }
           const float2 s2 = __fadd2_rn(__fadd2_rn(s4[0], s4[1]), __fadd2_rn(s4[2], s4[3]));
           l += s2.x + s2.y;
+          tmem_st_x64(tl + colS, sr);
         }
-        tmem_st_x64(tl + colS, sr);
-        if (j > 0 && __any_sync(0xffffffffu, need)) {
-#pragma unroll 1
-          for (int c = 0; c < HD; c += 32) {
-            uint32_t x[32];
-            tmem_ld_x32(tl + colO + c, x);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * corr);
-            tmem_st_x32(tl + colO + c, x);
-          }
-        }
+        if (j > 0 && __any_sync(0xffffffffu, need)) scale_o(corr);
         if (!whole) {
           const int s = j % kStages;
           w = F8 ? mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim)
@@ -1010,6 +1018,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       if (!ok) set_abort(bars);
       tc_fence_after();
       const float o_unit = F8 ? exp2_fast(e_ref) * 0x1p-7f : 1.f;
+      if (F8) l *= 0x1p-7f;
       float* other = reinterpret_cast<float*>(sV);   // [HD][128]: o of the second warpgroup (every product is done)
       const bool join = u.slot < 0 && !has_q1;
       if (join) {

@@ -27,3 +27,31 @@ def test_zero_queries_see_no_hidden_zero_keys(lib, new, Hq, causal, window, page
                                           out_dtype=torch.float32)
         lib.cast_check_device()
         check(P, q, o, lse, [new], Hq, causal, window, 0)
+
+
+# A page's place in its sequence (which rows see it follows from the lengths), and what it is larger by
+HIDDEN = [
+    # L, new, H_q, page, window, sinks, {page of the sequence: log2 of its scale}
+    (300, 300, 2, 16, 0, 0, {i: 6 * i for i in range(19)}),                 # a prompt whose pages grow
+    (300, 300, 1, 16, 0, 0, {i: 40 * (i % 2) for i in range(19)}),
+    (132, 40, 2, 128, 0, 0, {1: 40}),                                        # the last four rows' page
+    (1000, 200, 2, 16, 50, 0, {47: 40}),                                     # positions 752 .. 767, of the first rows' windows
+    (1000, 200, 1, 32, 50, 40, {24: 60, 0: 0, 1: -20}),
+    (5000, 150, 2, 64, 2000, 0, {44: 50, 45: 30}),                           # cut into parts
+    (600, 8, 2, 16, 181, 0, {25: 40}),                                       # drafts: positions 400 .. 415, seen from 412 on by the first row
+    (516, 8, 2, 16, 0, 0, {32: 40}),                                         # drafts: the last four rows' page
+    (5016, 8, 2, 16, 3989, 0, {63: 40}),                                     # drafts, cut into parts: 1008 .. 1023, seen from 1020 on
+    (5016, 8, 4, 32, 3989, 0, {31: 50, 32: 20}),                             # two products a head
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("L,new,Hq,page,window,sinks,scales", HIDDEN)
+def test_a_hidden_page_does_not_set_the_scale(lib, L, new, Hq, page, window, sinks, scales, d):
+    """Values of pages that a row does not see cost its own no bits, however large they are."""
+    P = Pages(lib, [L], 1, d, page, True).fill(3)
+    for i, e in scales.items():
+        P.vs[int(P.table[0, i])] = 2.0 ** e
+    q, o, lse = attend(lib, P, [new], Hq, True, window, sinks, dtype=torch.float32)
+    lib.cast_check_device()
+    check(P, q, o, lse, [new], Hq, True, window, sinks)
