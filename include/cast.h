@@ -461,7 +461,7 @@ typedef struct {
  * counted; position p lies in row p % page_size of page page_table[b, p / page_size]. */
 typedef struct {
   const int32_t* page_table;      /* device [B, max_pages]; entries no row of the call needs are not read */
-  int64_t page_table_stride;      /* elements between sequences, >= max_pages */
+  int64_t page_table_stride;      /* elements between sequences, >= max_pages, or 0: one table for all */
   int32_t max_pages;
   const int32_t* kv_len;          /* device [B], >= 0 */
   const int32_t* cu_new;          /* device [B + 1], ascending from 0 to T: sequence b's new tokens are

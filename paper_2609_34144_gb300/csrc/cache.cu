@@ -296,8 +296,8 @@ cast_status validate_batch(const cast_cache_batch& b, const char* who) {
                 b.max_pages, b.max_new);
   if (!b.page_table || !b.kv_len || !aligned4(b.page_table) || !aligned4(b.kv_len) || !aligned4(b.cu_new))
     return fail(CAST_ERR_INVALID_ARG, "%s: page_table / kv_len NULL or misaligned", who);
-  if (b.page_table_stride < b.max_pages)
-    return fail(CAST_ERR_INVALID_ARG, "%s: page_table stride %lld below max_pages %d", who,
+  if (b.page_table_stride < b.max_pages && b.page_table_stride != 0)
+    return fail(CAST_ERR_INVALID_ARG, "%s: page_table stride %lld below max_pages %d (and not 0)", who,
                 (long long)b.page_table_stride, b.max_pages);
   if (!b.cu_new && (b.T % b.B || b.T / b.B > b.max_new))
     return fail(CAST_ERR_INVALID_ARG, "%s: without cu_new every sequence has T / B = %d / %d <= max_new = %d tokens", who,

@@ -692,10 +692,14 @@ def _batch(page_table, kv_len, cu_new, T, max_new):
     s0, s1 = page_table.stride()
     if P > 1 and s1 != 1:
         raise ValueError("page_table: a sequence's pages must be contiguous")
+    if B < 2:
+        s0 = P
+    elif s0 < P and s0 != 0:   # 0: one table for all sequences (expanded)
+        raise ValueError("page_table: the sequences' rows overlap")
     cu = 0 if cu_new is None else _int32(cu_new, "cu_new", (B + 1,))
     if max_new is None:
         max_new = T if cu else T // max(B, 1)
-    return page_table.data_ptr(), s0 if s0 > P else P, P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new
+    return page_table.data_ptr(), s0, P, _int32(kv_len, "kv_len", (B,)), cu, B, T, max_new
 
 
 def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None, rotary=None, positions=None,

@@ -55,3 +55,25 @@ def test_a_hidden_page_does_not_set_the_scale(lib, L, new, Hq, page, window, sin
     q, o, lse = attend(lib, P, [new], Hq, True, window, sinks, dtype=torch.float32)
     lib.cast_check_device()
     check(P, q, o, lse, [new], Hq, True, window, sinks)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("new", [1, 40])
+def test_sequences_that_share_one_table(lib, f8, new):
+    """A table expanded over the sequences: the same bits as with a copy for each; and tokens stored through it."""
+    P = Pages(lib, [900], 2, 64, 16, f8, seed=4).fill(5)
+    lens = torch.tensor([900, 333, new, 850], dtype=torch.int32, device="cuda")
+    q = randn(gen(1), 4 * new, 4, 64).to(torch.bfloat16)
+    shared = P.table.expand(4, -1)
+    assert shared.stride(0) == 0
+    got = lib.cast_cache_attention(q, P.cache, shared, lens)
+    assert torch.equal(got, lib.cast_cache_attention(q, P.cache, shared.contiguous(), lens))
+    # each sequence ends a page of its own: tokens 16 b .. 16 b + 15
+    k = randn(gen(2), 64, 2, 64).to(torch.bfloat16)
+    ends = torch.tensor([16, 32, 48, 64], dtype=torch.int32, device="cuda")
+    lib.cast_cache_append(k, k, P.cache, shared, ends)
+    one = Pages(lib, [900], 2, 64, 16, f8, seed=4).fill(5)
+    lib.cast_cache_append(k, k, one.cache, one.table, ends[3:])
+    lib.cast_check_device()
+    bits = torch.uint8 if f8 else torch.int16
+    assert torch.equal(P.k.view(bits), one.k.view(bits)) and torch.equal(P.v.view(bits), one.v.view(bits))
