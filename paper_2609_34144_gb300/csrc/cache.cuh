@@ -43,6 +43,13 @@ __device__ __forceinline__ Sequence sequence_of(const cast_cache_batch& a, int b
   return s;
 }
 
+// Sum over a warp of numbers from 0 to 2^52 (the work of a call passes 32 bits)
+__device__ __forceinline__ int64_t warp_sum(int64_t x) {
+  const uint32_t low = __reduce_add_sync(0xffffffffu, (uint32_t)x & 0x3ffffffu);
+  const uint32_t high = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 26));
+  return ((int64_t)high << 26) + low;
+}
+
 // ------------------------------------------------------------------ rotation
 // (cos, sin) * amplitude of the angle that pair i turns by at `pos`.  The table holds turns a
 // position in units of 2^-64: the product modulo 2^64 is the turn's fraction, exactly, at any

@@ -178,8 +178,8 @@ template <int D, bool F8, int MT>
 __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_rows(const __grid_constant__ RowsKArgs a) {
   using C = Cfg<D, F8, MT>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int s_work[kWarps], s_entry;
-  __shared__ int64_t s_before;
+  __shared__ int s_entry;
+  __shared__ int64_t s_work[kWarps], s_before;
   __shared__ float2 s_scale[kWarps][C::STAGES];   // K and V scale of a stage's page
   __shared__ float s_prob[kWarps][C::ROWS][17];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -216,13 +216,14 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
     at = (int64_t)h * nb;
     stop = at + nb;
   } else {
-    int mine = 0, none = 0;
+    int64_t mine = 0;
+    int none = 0;
     for (int e = threadIdx.x; e < entries; e += kWarps * 32) {
       const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS).blocks();
       mine += n;
       none |= n == 0;
     }
-    mine = __reduce_add_sync(0xffffffffu, mine);
+    mine = warp_sum(mine);
     if (lane == 0) s_work[warp] = mine;
     none = __syncthreads_or(none);
     int64_t total = 0;
@@ -241,9 +242,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
       for (int e0 = 0; e0 < entries; e0 += 32) {
         const int e = e0 + lane;
         const int n = e < entries ? span_of(a, e / a.row_tiles, e % a.row_tiles, C::ROWS).blocks() : 0;
-        int sum = n;
+        int64_t sum = n;
         for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
           if (lane >= o) sum += y;
         }
         const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * units > at);
@@ -741,20 +742,20 @@ constexpr int kMergeWarps = 16;
 template <int D, int MT>
 __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
   constexpr int ROWS = 16 * MT, LANES = D / 4, GROUPS = 32 / LANES;   // GROUPS parts at a time in a warp
-  __shared__ int s_sum[kMergeWarps], s_before[kMergeWarps];
+  __shared__ int64_t s_sum[kMergeWarps], s_before[kMergeWarps];
   __shared__ float4 s_o[kMergeWarps * GROUPS][LANES];
   __shared__ float2 s_ml[kMergeWarps * GROUPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int entries = a.batch.B * a.row_tiles;
   const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  int sum = 0, before = 0;
+  int64_t sum = 0, before = 0;
   for (int e = threadIdx.x; e < entries; e += kMergeWarps * 32) {
     const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
     sum += n;
     before += e < entry ? n : 0;
   }
-  sum = __reduce_add_sync(0xffffffffu, sum);
-  before = __reduce_add_sync(0xffffffffu, before);
+  sum = warp_sum(sum);
+  before = warp_sum(before);
   if (lane == 0) {
     s_sum[warp] = sum;
     s_before[warp] = before;

@@ -161,12 +161,12 @@ __device__ __forceinline__ int unit_work(const TilesKArgs& a, const Unit& u) {
 }
 
 // Work of units lane, lane + 32, ... or, `serial`, of all units of sequence b
-__device__ __forceinline__ int sequence_work(const TilesKArgs& a, int b, int lane, bool serial) {
+__device__ __forceinline__ int64_t sequence_work(const TilesKArgs& a, int b, int lane, bool serial) {
   if (b >= a.batch.B) return 0;
   const Sequence s = sequence_of(a.batch, b);
   const int n = min(s.n_new, a.batch.max_new), per = 2 * a.tile_tokens;
   Unit u{};
-  int w = 0;
+  int64_t w = 0;
   for (u.i0 = serial ? 0 : lane * per; u.i0 < n; u.i0 += serial ? per : 32 * per) {
     place_unit(a, u, s);
     w += unit_work(a, u);
@@ -175,18 +175,19 @@ __device__ __forceinline__ int sequence_work(const TilesKArgs& a, int b, int lan
 }
 // Lane l's answer is the work of sequence b0 + l: one sequence a lane, or, where there are fewer of them
 // than units in one, one after the other by all lanes
-__device__ __forceinline__ int chunk_work(const TilesKArgs& a, int b0, int lane) {
+__device__ __forceinline__ int64_t chunk_work(const TilesKArgs& a, int b0, int lane) {
   if (a.batch.B >= a.most_pairs) return sequence_work(a, b0 + lane, 0, true);
-  int mine = 0;
+  int64_t mine = 0;
   for (int b = b0; b < min(b0 + 32, a.batch.B); ++b) {
-    const int w = __reduce_add_sync(0xffffffffu, sequence_work(a, b, lane, false));
+    const int64_t w = warp_sum(sequence_work(a, b, lane, false));
     if (b0 + lane == b) mine = w;
   }
   return mine;
 }
-__device__ __forceinline__ int scan(int x, int lane) {   // inclusive
+template <class T>
+__device__ __forceinline__ T scan(T x, int lane) {   // inclusive
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    const T y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
   return x;
@@ -195,7 +196,7 @@ __device__ __forceinline__ int scan(int x, int lane) {   // inclusive
 // CTA (heads slowest: what runs together reads one head's keys); what is left, or everything where units
 // differ, is a row of work items from `base` on, of which CTA c has share * c .. share * (c + 1) - 1.
 struct Deal {
-  int per_head;          // work of a head
+  int64_t per_head;      // work of a head
   int each, rounds;      // of a unit that is dealt whole, and how many a CTA has
   int64_t base, share, total;
 };
@@ -213,18 +214,18 @@ __device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) { 
       low = min(low, w);
       high = max(high, w);
     }
-    d.per_head = __reduce_add_sync(0xffffffffu, d.per_head);
+    d.per_head = warp_sum(d.per_head);
     low = __reduce_min_sync(0xffffffffu, low);
     high = __reduce_max_sync(0xffffffffu, high);
-    d.total = (int64_t)d.per_head * a.H;
+    d.total = d.per_head * a.H;
     if (low == high) {
       d.each = high;
       d.rounds = (int)(d.total / high / ctas);
       d.base = (int64_t)d.rounds * ctas * high;
     }
   } else {
-    for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += __reduce_add_sync(0xffffffffu, chunk_work(a, b0, lane));
-    d.total = (int64_t)d.per_head * a.H;
+    for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += warp_sum(chunk_work(a, b0, lane));
+    d.total = d.per_head * a.H;
   }
   d.share = max((int64_t)a.least, (d.total - d.base + ctas - 1) / ctas);
   return d;
@@ -269,10 +270,11 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
   const int per = 2 * a.tile_tokens;
   while (at < stop) {
     const int h = (int)(at / d.per_head);
-    int r = (int)(at - (int64_t)h * d.per_head), b = a.batch.B == 1 ? 0 : -1;
+    int64_t r = at - h * d.per_head;
+    int b = a.batch.B == 1 ? 0 : -1;
     for (int b0 = 0; b < 0 && b0 < a.batch.B; b0 += 32) {
-      const int w = chunk_work(a, b0, lane);
-      const int sum = scan(w, lane);
+      const int64_t w = chunk_work(a, b0, lane);
+      const int64_t sum = scan(w, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
       if (hit) {
         const int l = __ffs(hit) - 1;
@@ -293,7 +295,7 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
         place_unit(a, u, s);
         w = unit_work(a, u);
       }
-      const int sum = scan(w, lane);
+      const int64_t sum = scan((int64_t)w, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
       if (hit) {
         const int l = __ffs(hit) - 1;
@@ -308,9 +310,10 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
     u.b = b;
     u.h = h;
     place_unit(a, u, s);
-    const int w = unit_work(a, u), each = tile_work(a, u), some = (int)min((int64_t)(w - r), stop - at);
-    u.k0 = (max(r - kBegin, 0) + each - 1) / each;
-    u.n_tiles = u.tiles ? (max(r + some - kBegin, 0) + each - 1) / each - u.k0 : 0;
+    const int in = (int)r;   // items of the unit before `at`
+    const int w = unit_work(a, u), each = tile_work(a, u), some = (int)min((int64_t)(w - in), stop - at);
+    u.k0 = (max(in - kBegin, 0) + each - 1) / each;
+    u.n_tiles = u.tiles ? (max(in + some - kBegin, 0) + each - 1) / each - u.k0 : 0;
     if (u.n_tiles > 0 || u.tiles == 0) {
       u.valid = 1;
       u.work = (int)(at - from) + some;

@@ -77,3 +77,23 @@ def test_sequences_that_share_one_table(lib, f8, new):
     lib.cast_check_device()
     bits = torch.uint8 if f8 else torch.int16
     assert torch.equal(P.k.view(bits), one.k.view(bits)) and torch.equal(P.v.view(bits), one.v.view(bits))
+
+
+def test_work_beyond_32_bits(lib):
+    """65,536 sequences of two rows of 128 query heads over 2^20 positions (one page, again and again): the tiles that
+    the call has to be dealt out by are more than 2^31."""
+    B, G, d, L = 65536, 128, 64, 1 << 20
+    g = gen(3)
+    k, v = (randn(g, 1, 128, 1, d).to(torch.bfloat16) for _ in range(2))
+    table = torch.zeros((B, L // 128), dtype=torch.int32, device="cuda")
+    q = torch.randn((2 * B, G, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    out = torch.full((2 * B, G * d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lib.cast_cache_attention(q, lib.kv_cache(k, v), table, torch.full((B,), L, dtype=torch.int32, device="cuda"), causal=False, out=out)
+    lib.cast_check_device()
+    rows = torch.arange(0, 2 * B, 997, device="cuda")
+    # every position of the page has the same weight L / 128 times over
+    ref, _, eo, _ = R.attention(f64(q[rows]), f64(k[0]), f64(v[0]), len(rows), 128, causal=False)
+    # and the sums have L terms: cache_ref's bound has 128 U32 in their place
+    part = R.attention(f64(q[rows]), f64(k[0]), np.abs(f64(v[0])), len(rows), 128, causal=False)[0]
+    within(f64(out[rows]).reshape(-1, G, d), ref, eo + L * R.U32 * part, "o")
+    assert not torch.isnan(out.view(torch.int16).view(B, -1)[:, ::1000].view(torch.bfloat16)).any()
