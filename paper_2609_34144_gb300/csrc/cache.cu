@@ -122,9 +122,10 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
   const int first = max(p0, 0);
   const int g = first / a.page_size + run;              // page of the sequence
   if (run == 0 && s.n_new > a.batch.max_new && threadIdx.x == 0) left_out();
-  if ((int64_t)g * a.page_size >= s.len) return;
+  const int end = p0 + min(s.n_new, a.batch.max_new);   // behind the last token that is stored
+  if ((int64_t)g * a.page_size >= end) return;
   const int base = g * a.page_size;
-  const int lo = max(first - base, 0), hi = min(s.len - base, a.page_size);
+  const int lo = max(first - base, 0), hi = min(end - base, a.page_size);
   if (lo >= hi) return;
   int job = blockIdx.y;
   const int kind = job < a.jobs_kv ? 0 : job < 2 * a.jobs_kv ? 1 : 2;   // K, V, queries

@@ -97,3 +97,49 @@ def test_work_beyond_32_bits(lib):
     part = R.attention(f64(q[rows]), f64(k[0]), np.abs(f64(v[0])), len(rows), 128, causal=False)[0]
     within(f64(out[rows]).reshape(-1, G, d), ref, eo + L * R.U32 * part, "o")
     assert not torch.isnan(out.view(torch.int16).view(B, -1)[:, ::1000].view(torch.bfloat16)).any()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("start,new,said", [
+    ([0, 10], [7, 7], 2),                # ends inside the page that it begins in
+    ([60, 64], [9, 200], 5),             # ends inside the next page; would fill several
+    ([3, 130], [64, 70], 64),            # one sequence at the bound
+    ([-2, -4], [5, 4], 5),               # places before the sequence's beginning
+    ([-3, -1], [40, 9], 6),              # and both
+])
+def test_append_leaves_out_what_was_not_said(lib, start, new, said, f8):
+    """Tokens past max_new and places below zero: pages, scales and rotated queries are those of a call without them."""
+    H, d, Hq, page = 2, 64, 4, 64
+    lens = [max(s + n, 1) for s, n in zip(start, new)]
+    P, want = (Pages(lib, lens, H, d, page, f8, seed=1).fill(2) for _ in range(2))
+    g = gen(7)
+    T = sum(new)
+    k, v = ((3 * randn(g, T, H, d)).to(torch.bfloat16) for _ in range(2))
+    q = randn(g, T, Hq, d).to(torch.bfloat16)
+    turns = lib.rotary_table(d)
+    got_q = torch.full_like(q, 5.0)
+    want_q = got_q.clone()
+    cu = torch.tensor([0, new[0], T], dtype=torch.int32, device="cuda")
+    n = torch.tensor([s + c for s, c in zip(start, new)], dtype=torch.int32, device="cuda")
+    lib.cast_cache_append(k, v, P.cache, P.table, n, cu_new=cu, max_new=said, rotary=turns, q=q, q_out=got_q)
+    if max(new) > said:
+        with pytest.raises(lib.CastError) as e:
+            lib.cast_check_device()
+        assert e.value.status == lib.ERR_INVALID_ARG
+    lib.cast_check_device()
+    at = 0
+    for b in range(2):
+        lo, hi = at + max(0, -start[b]), at + min(new[b], said)
+        if lo < hi:
+            rows = slice(lo, hi)
+            end = torch.tensor([start[b] + hi - at], dtype=torch.int32, device="cuda")
+            want_q[rows] = lib.cast_cache_append(k[rows], v[rows], want.cache, want.table[b:b + 1], end, rotary=turns, q=q[rows])
+        at += new[b]
+    lib.cast_check_device()
+    bits = torch.uint8 if f8 else torch.int16
+    for x, y in ((P.k, want.k), (P.v, want.v)):
+        assert torch.equal(x.view(bits), y.view(bits))
+    if f8:
+        # (NaN where no page was)
+        assert all(torch.equal(x.view(torch.int32), y.view(torch.int32)) for x, y in ((P.ks, want.ks), (P.vs, want.vs)))
+    assert torch.equal(got_q.view(torch.int16), want_q.view(torch.int16))
