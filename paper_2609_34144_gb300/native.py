@@ -602,15 +602,26 @@ def rotary_table(rot_dim, layout="half", base=10000.0, sections=None, scaling=No
 # asked for directly, tensors are measured once, torch.empty is 3 us cheaper here than new_empty, and
 # the argument structs are packed as bytes (the same layout as the classes above).
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 _BATCH = "PqiPPiii4x"
 _pack_rotary = struct.Struct("@PPqqiiiiPPi4x").pack
 _pack_append = struct.Struct("@64s" + _BATCH + "PPqqPPPPqqi4x").pack
 _pack_attention = struct.Struct("@64s" + _BATCH + "PqiiiifPiP").pack
 
 
-def _on(stream, t):
-    """The stream's handle for a call on t's device."""
-    return _raw_stream(t.get_device()) if stream is None else stream.cuda_stream
+def _on(stream, device, *tensors):
+    """The stream's handle for a call on GPU `device`, which has to be the current one (the library launches
+    there and reads its properties), the tensors' and the stream's."""
+    if device < 0 or device != _current_device():
+        raise ValueError(f"tensors on GPU {device}, which is not the current one")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors on GPU {device} and on {t.device}")
+    if stream is None:
+        return _raw_stream(device)
+    if stream.device_index != device:
+        raise ValueError(f"tensors on GPU {device}, the stream on {stream.device_index}")
+    return stream.cuda_stream
 
 
 def _heads_stride(t, name, dtype=torch.bfloat16):
@@ -652,9 +663,10 @@ def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
     o = torch.empty((T, H, d), dtype=x.dtype, device=x.device) if out is None else out
     if out is not None and (o.shape != x.shape or o.dtype != x.dtype):
         raise ValueError("out must have x's shape and dtype")
+    on = _on(stream, x.get_device(), positions, out)
     a = _pack_rotary(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
                      _dtype_code(x), pos, table.address, inverse)
-    _check(_lib.cast_rotary(a, _on(stream, x)))
+    _check(_lib.cast_rotary(a, on))
     if out is None:
         _on_stream(stream, o)
     return o
@@ -679,7 +691,8 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
                 k_scale.data_ptr() if f8 else None, v_scale.data_ptr() if f8 else None)
     c._keep = (k, v, k_scale, v_scale)
     c.packed = bytes(c)
-    c.on_gpu = all(t.is_cuda for t in (k, v, k_scale, v_scale) if t is not None)
+    gpus = {t.get_device() for t in (k, v, k_scale, v_scale) if t is not None}
+    c.device = gpus.pop() if len(gpus) == 1 else -1   # -1: not on one GPU
     c.heads = (H, d)
     return c
 
@@ -708,7 +721,7 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
     already.  cu_new [B + 1]: ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes]
     (None: a token's place in its sequence).  With q [T, H_q, d] returns it rotated."""
     T, H, d = k.shape
-    if v.shape != k.shape or (H, d) != cache.heads or not cache.on_gpu:
+    if v.shape != k.shape or (H, d) != cache.heads or cache.device < 0:
         raise ValueError("k and v must be [T, H, d] of the cache's heads, the cache on the GPU")
     pos = 0
     if positions is not None and rotary is not None:
@@ -727,7 +740,8 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
     a = _pack_append(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(),
                      _heads_stride(k, "k"), _heads_stride(v, "v"), rotary.address if rotary is not None else 0, pos, qp, qo, qs,
                      qos, Hq)
-    _check(_lib.cast_cache_append(a, _on(stream, k)))
+    on = _on(stream, cache.device, k, v, page_table, kv_len, cu_new, positions if pos else None, q, q_out)
+    _check(_lib.cast_cache_append(a, on))
     if q_out is None:
         _on_stream(stream, o)
     return o
@@ -739,7 +753,7 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     window > 0: a row sees the last `window` positions and the first `sinks`.  Returns
     o [T, H_q*d] (and lse [T, H_q])."""
     T, Hq, d = q.shape
-    if d != cache.heads[1] or not cache.on_gpu:
+    if d != cache.heads[1] or cache.device < 0:
         raise ValueError("q must be [T, H_q, d] of the cache's head dim, the cache on the GPU")
     dev = q.device
     o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
@@ -748,13 +762,14 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
     a = _pack_attention(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), 0 if lse is None else lse.data_ptr())
+    on = _on(stream, cache.device, q, page_table, kv_len, cu_new, out, workspace)
     ws = workspace
     if ws is not None and not ws.is_cuda:
         raise ValueError("workspace must be on the GPU")
     if ws is None:
         need = _lib.cast_cache_attention_workspace_size(a)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _check(_lib.cast_cache_attention(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _on(stream, q)))
+    _check(_lib.cast_cache_attention(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), on))
     if stream is not None:
         _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
     return (o, lse) if want_lse else o

@@ -45,3 +45,69 @@ def test_table_stride(lib, stride, status):  # noqa: F811
     b = _batch(lib, T=0, max_new=0, page_table_stride=stride)   # nothing to do: only the checks
     assert lib.library().cast_cache_append(C.byref(_append(lib, batch=b)), None) == status
     assert lib.library().cast_cache_attention(C.byref(_attend(lib, batch=b)), None, 0, None) == status
+
+
+def _calls(lib, on):  # noqa: F811
+    """A call of each entry point whose tensors are on the GPUs on("name"); nothing is behind their addresses."""
+    def t(name, *shape, dtype=torch.bfloat16):
+        return OnGpu(torch.zeros(shape, dtype=dtype), on(name))
+
+    pages = [t("cache", 2, 16, 1, 64), t("cache_v", 2, 16, 1, 64)]
+    ints = dict(page_table=t("page_table", 1, 2, dtype=torch.int32), kv_len=t("kv_len", 1, dtype=torch.int32),
+                cu_new=t("cu_new", 2, dtype=torch.int32))
+    pos, table = t("positions", 2, dtype=torch.int32), lib.rotary_table(64)
+    yield lambda: lib.cast_rotary(t("k", 2, 1, 64), pos, table, out=t("out", 2, 1, 64))
+    yield lambda: lib.cast_cache_append(t("k", 2, 1, 64), t("v", 2, 1, 64), lib.kv_cache(*pages), rotary=table, positions=pos,
+                                        q=t("q", 2, 2, 64), q_out=t("out", 2, 2, 64), **ints)
+    yield lambda: lib.cast_cache_attention(t("q", 2, 2, 64), lib.kv_cache(*pages), out=t("out", 2, 128), workspace=t("workspace", 1 << 20),
+                                           **ints)
+
+
+class Launched(Exception):
+    pass
+
+
+@pytest.fixture
+def no_launch(lib, monkeypatch):  # noqa: F811
+    """A process whose current GPU is 1 and whose calls end where they would enter the library."""
+    def enter(*a):
+        raise Launched
+
+    for f in ("cast_rotary", "cast_cache_append", "cast_cache_attention"):
+        monkeypatch.setattr(lib._lib, f, enter)
+    monkeypatch.setattr(lib, "_current_device", lambda: 1, raising=False)
+    monkeypatch.setattr(lib, "_raw_stream", lambda device: 0)
+
+
+def test_tensors_of_the_current_gpu_are_taken(lib, no_launch):  # noqa: F811
+    for call in _calls(lib, lambda name: 1):
+        with pytest.raises(Launched):
+            call()
+
+
+def test_tensors_of_another_gpu_are_refused(lib, no_launch):  # noqa: F811
+    """All tensors on a GPU that is not the current one, or one of them on another than the rest: refused on the host."""
+    for call in _calls(lib, lambda name: 0):
+        with pytest.raises(ValueError):
+            call()
+    names = dict(rotary=("k", "positions", "out"), append=("k", "v", "cache", "cache_v", "page_table", "kv_len", "cu_new", "positions", "q", "out"),
+                 attention=("q", "cache", "cache_v", "page_table", "kv_len", "cu_new", "out", "workspace"))
+    for i, f in enumerate(names):
+        for name in names[f]:
+            call = list(_calls(lib, lambda n: 0 if n == name else 1))[i]
+            with pytest.raises(ValueError):
+                call()
+
+
+def test_a_stream_of_another_gpu_is_refused(lib, no_launch):  # noqa: F811
+    class Stream:
+        cuda_stream = 0
+
+        def __init__(self, device):
+            self.device_index = device
+
+    x, pos, table = OnGpu(torch.zeros(2, 1, 64), 1), OnGpu(torch.zeros(2, dtype=torch.int32), 1), lib.rotary_table(64)
+    with pytest.raises(Launched):
+        lib.cast_rotary(x, pos, table, out=x, stream=Stream(1))
+    with pytest.raises(ValueError):
+        lib.cast_rotary(x, pos, table, out=x, stream=Stream(0))
