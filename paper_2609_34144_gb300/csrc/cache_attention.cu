@@ -952,7 +952,10 @@ static bool by_tiles(const cast_cache_attn_args& a) {
 }
 
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* a) {
-  if (!a || a->batch.T < 1 || a->cache.H < 1 || a->H_q < a->cache.H || (a->cache.d != 64 && a->cache.d != 128)) return 0;
+  // 0 for what the call refuses: the plans divide by the sequences, and by 128 rows over the group
+  if (!a || a->batch.T < 1 || a->batch.B < 1 || a->batch.max_new < 1 || a->batch.max_pages < 0 || a->cache.page_size < 1 || a->cache.H < 1 ||
+      a->H_q < a->cache.H || a->H_q / a->cache.H > 128 || (a->cache.d != 64 && a->cache.d != 128))
+    return 0;
   return by_tiles(*a) ? tiles_plan(*a).total_bytes : rows_plan(*a).total_bytes;
 }
 

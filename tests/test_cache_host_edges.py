@@ -1,10 +1,15 @@
 """The paged KV cache's entry points on the CPU, at the edges of what they take."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
 
 from tests.test_cache_host import _append, _attend, _batch, lib  # noqa: F401
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 class OnGpu:
@@ -111,3 +116,36 @@ def test_a_stream_of_another_gpu_is_refused(lib, no_launch):  # noqa: F811
         lib.cast_rotary(x, pos, table, out=x, stream=Stream(1))
     with pytest.raises(ValueError):
         lib.cast_rotary(x, pos, table, out=x, stream=Stream(0))
+
+
+WORKSPACE = """
+import ctypes as C
+from paper_2609_34144_gb300 import native as lib
+from tests.test_cache_host import _attend, _batch, _cache
+for kw, b, c in (({"H_q": 2 * 129}, {}, {}), ({"H_q": 1 << 20}, {}, {}), ({}, {"B": 0}, {}), ({"H_q": 64}, {"B": 0}, {}), ({"H_q": 64}, {"B": -1}, {}),
+                 ({"H_q": 3}, {}, {}), ({"H_q": 0}, {}, {}), ({}, {}, {"H": 0}), ({}, {}, {"d": 96}), ({}, {"T": -4}, {}), ({}, {"max_new": -1}, {}),
+                 ({}, {"max_pages": -1}, {}), ({}, {}, {"page_size": 0})):
+    a = _attend(lib, cache=_cache(lib, **c), batch=_batch(lib, **b), **kw)
+    print(lib.library().cast_cache_attention_workspace_size(C.byref(a)))
+print(lib.library().cast_cache_attention_workspace_size(None))
+"""
+
+
+def test_workspace_of_arguments_that_the_call_refuses_is_zero(lib):  # noqa: F811
+    """In a process of its own: a division by zero would end it."""
+    r = subprocess.run([sys.executable, "-c", WORKSPACE], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert r.stdout.split() == ["0"] * 14
+
+
+def test_binding_refuses_heads_and_batches_that_the_library_refuses(lib, monkeypatch):  # noqa: F811
+    """More than 128 query heads a KV head, and no sequences: an error, as from the library itself."""
+    monkeypatch.setattr(lib, "_current_device", lambda: 0)
+    monkeypatch.setattr(lib, "_raw_stream", lambda device: 0)
+    pages = [OnGpu(torch.zeros(2, 16, 1, 64, dtype=torch.bfloat16)) for _ in range(2)]
+    for heads, B, status in ((129, 1, lib.ERR_UNSUPPORTED), (64, 0, lib.ERR_INVALID_ARG)):
+        q, out = (OnGpu(torch.zeros(2, heads * 64, dtype=torch.bfloat16).view(s)) for s in ((2, heads, 64), (2, heads * 64)))
+        ints = [OnGpu(torch.zeros(s, dtype=torch.int32)) for s in ((B, 2), (B,))]
+        with pytest.raises(lib.CastError) as e:
+            lib.cast_cache_attention(q, lib.kv_cache(*pages), *ints, out=out)
+        assert e.value.status == status
