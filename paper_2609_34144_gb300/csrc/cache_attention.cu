@@ -898,6 +898,8 @@ cast_status validate_attention(const cast_cache_attn_args* a, const char* who) {
   if (a->batch.T == 0) return CAST_OK;
   if (!a->q || !aligned16(a->q) || !a->o || !aligned16(a->o))
     return fail(CAST_ERR_INVALID_ARG, "%s: q or o is NULL or not 16-byte aligned", who);
+  if (reinterpret_cast<uintptr_t>(a->lse) % sizeof(float))
+    return fail(CAST_ERR_INVALID_ARG, "%s: lse is not 4-byte aligned", who);
   if (a->q_row_stride < (int64_t)a->H_q * a->cache.d || a->q_row_stride % 8)
     return fail(CAST_ERR_INVALID_ARG, "%s: q row stride %lld must be >= H_q*d and a multiple of 8", who,
                 (long long)a->q_row_stride);

@@ -149,3 +149,11 @@ def test_binding_refuses_heads_and_batches_that_the_library_refuses(lib, monkeyp
         with pytest.raises(lib.CastError) as e:
             lib.cast_cache_attention(q, lib.kv_cache(*pages), *ints, out=out)
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("lse", [0xa00001, 0xa00002, 0xa00003])
+def test_lse_has_to_be_aligned(lib, lse):  # noqa: F811
+    # (without a workspace, which a call that gets past the check would miss)
+    a = _attend(lib, batch=_batch(lib, max_pages=1000, page_table_stride=1000), lse=lse)
+    assert lib.library().cast_cache_attention(C.byref(a), None, 0, None) == lib.ERR_INVALID_ARG
+    assert b"lse" in lib.library().cast_last_error_detail()
