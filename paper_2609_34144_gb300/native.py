@@ -645,12 +645,15 @@ def _int32(t, name, shape=None):
     return t.data_ptr()
 
 
-def _on_stream(stream, *tensors):
-    """Tensors allocated for a call on another stream than the current one stay alive until it is done."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+def _empty(stream, shape, dtype, device):
+    """A tensor that the call on `stream` writes.  Of another stream than the current one it takes that stream's
+    memory: what the current stream has given back it may still be reading.  Both keep it until they are done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
@@ -660,15 +663,13 @@ def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
     T, H, d = x.shape
     n = table.n_axes
     pos = _int32(positions, "positions", (T,) if n == 1 and positions.dim() == 1 else (T, n))
-    o = torch.empty((T, H, d), dtype=x.dtype, device=x.device) if out is None else out
-    if out is not None and (o.shape != x.shape or o.dtype != x.dtype):
+    if out is not None and (out.shape != x.shape or out.dtype != x.dtype):
         raise ValueError("out must have x's shape and dtype")
     on = _on(stream, x.get_device(), positions, out)
+    o = _empty(stream, (T, H, d), x.dtype, x.device) if out is None else out
     a = _pack_rotary(x.data_ptr(), o.data_ptr(), stride, H * d if out is None else _heads_stride(o, "out", None), T, H, d,
                      _dtype_code(x), pos, table.address, inverse)
     _check(_lib.cast_rotary(a, on))
-    if out is None:
-        _on_stream(stream, o)
     return o
 
 
@@ -723,6 +724,7 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
     T, H, d = k.shape
     if v.shape != k.shape or (H, d) != cache.heads or cache.device < 0:
         raise ValueError("k and v must be [T, H, d] of the cache's heads, the cache on the GPU")
+    on = _on(stream, cache.device, k, v, page_table, kv_len, cu_new, positions if rotary is not None else None, q, q_out)
     pos = 0
     if positions is not None and rotary is not None:
         pos = _int32(positions, "positions", (T,) if positions.dim() == 1 and rotary.n_axes == 1 else (T, rotary.n_axes))
@@ -733,17 +735,14 @@ def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None
         Tq, Hq, dq = q.shape
         if Tq != T or dq != d:
             raise ValueError("q must be [T, H_q, d]")
-        o = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
+        o = _empty(stream, (T, Hq, d), torch.bfloat16, q.device) if q_out is None else q_out
         if q_out is not None and o.shape != q.shape:
             raise ValueError("q_out must have q's shape")
         qp, qo, qos = q.data_ptr(), o.data_ptr(), Hq * d if q_out is None else _heads_stride(o, "q_out")
     a = _pack_append(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), k.data_ptr(), v.data_ptr(),
                      _heads_stride(k, "k"), _heads_stride(v, "v"), rotary.address if rotary is not None else 0, pos, qp, qo, qs,
                      qos, Hq)
-    on = _on(stream, cache.device, k, v, page_table, kv_len, cu_new, positions if pos else None, q, q_out)
     _check(_lib.cast_cache_append(a, on))
-    if q_out is None:
-        _on_stream(stream, o)
     return o
 
 
@@ -755,22 +754,20 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     T, Hq, d = q.shape
     if d != cache.heads[1] or cache.device < 0:
         raise ValueError("q must be [T, H_q, d] of the cache's head dim, the cache on the GPU")
+    on = _on(stream, cache.device, q, page_table, kv_len, cu_new, out, workspace)
     dev = q.device
-    o = torch.empty((T, Hq * d), dtype=out_dtype, device=dev) if out is None else out
+    o = _empty(stream, (T, Hq * d), out_dtype, dev) if out is None else out
     if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous() or not o.is_cuda):
         raise ValueError("out must be contiguous [T, H_q*d] on the GPU")
-    lse = torch.empty((T, Hq), dtype=torch.float32, device=dev) if want_lse else None
+    lse = _empty(stream, (T, Hq), torch.float32, dev) if want_lse else None
     a = _pack_attention(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), 0 if lse is None else lse.data_ptr())
-    on = _on(stream, cache.device, q, page_table, kv_len, cu_new, out, workspace)
     ws = workspace
     if ws is not None and not ws.is_cuda:
         raise ValueError("workspace must be on the GPU")
     if ws is None:
         need = _lib.cast_cache_attention_workspace_size(a)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        ws = _empty(stream, need, torch.uint8, dev) if need else None
     _check(_lib.cast_cache_attention(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), on))
-    if stream is not None:
-        _on_stream(stream, lse, o if out is None else None, ws if workspace is None else None)
     return (o, lse) if want_lse else o
 

@@ -143,3 +143,38 @@ def test_append_leaves_out_what_was_not_said(lib, start, new, said, f8):
         # (NaN where no page was)
         assert all(torch.equal(x.view(torch.int32), y.view(torch.int32)) for x, y in ((P.ks, want.ks), (P.vs, want.vs)))
     assert torch.equal(got_q.view(torch.int16), want_q.view(torch.int16))
+
+
+@pytest.mark.parametrize("which", ["rotary", "append", "rows", "tiles", "lse"])
+def test_outputs_on_another_stream_leave_memory_in_use_alone(lib, which):
+    """A tensor that the current stream still reads was given back before a call on another stream."""
+    P = Pages(lib, [3000], 2, 64, 16, False, seed=4).fill(5)
+    new = 100 if which == "tiles" else 4
+    T = 2048 if which in ("rotary", "append") else new
+    turns, n = lib.rotary_table(64), P.len_tensor()
+    q = randn(gen(1), T, 4, 64).to(torch.bfloat16)
+    k = randn(gen(2), T, 2, 64).to(torch.bfloat16)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+
+    def call():
+        if which == "rotary":
+            return lib.cast_rotary(q, pos, turns, stream=s)
+        if which == "append":
+            return lib.cast_cache_append(k, k, P.cache, P.table, n, rotary=turns, q=q, stream=s)
+        out = lib.cast_cache_attention(q, P.cache, P.table, n, want_lse=True, stream=s)
+        return out[which == "lse"]
+
+    want = call()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        held = torch.full_like(want, 7.0)
+        kept = torch.empty_like(want)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        kept.copy_(held)
+        del held
+        got = call()
+        torch.cuda.synchronize()
+        assert (kept == 7).all() and torch.equal(got, want)
+    lib.cast_check_device()
