@@ -611,12 +611,12 @@ _pack_attention = struct.Struct("@64s" + _BATCH + "PqiiiifPiP").pack
 
 def _on(stream, device, *tensors):
     """The stream's handle for a call on GPU `device`, which has to be the current one (the library launches
-    there and reads its properties), the tensors' and the stream's."""
+    there and reads its properties), the stream's, and that of every tensor (-1: the host's)."""
     if device < 0 or device != _current_device():
-        raise ValueError(f"tensors on GPU {device}, which is not the current one")
+        raise ValueError(f"tensors on GPU {device} (-1: the host), which is not the current one")
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise ValueError(f"tensors on GPU {device} and on {t.device}")
+            raise ValueError(f"tensors on GPU {device} and on GPU {t.get_device()} (-1: the host)")
     if stream is None:
         return _raw_stream(device)
     if stream.device_index != device:
@@ -626,8 +626,8 @@ def _on(stream, device, *tensors):
 
 def _heads_stride(t, name, dtype=torch.bfloat16):
     """Token row stride of a [T, H, d] tensor whose (H, d) are contiguous."""
-    if t.dim() != 3 or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
-        raise ValueError(f"{name}: expected [T, H, d] of {dtype or 'bf16 or f32'} on the GPU")
+    if t.dim() != 3 or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name}: expected [T, H, d] of {dtype or 'bf16 or f32'}")
     T, H, d = t.shape
     if T < 2:
         if not t.is_contiguous():
@@ -640,8 +640,8 @@ def _heads_stride(t, name, dtype=torch.bfloat16):
 
 
 def _int32(t, name, shape=None):
-    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name}: expected a contiguous int32 tensor on the GPU" + (f" of shape {shape}" if shape else ""))
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor" + (f" of shape {shape}" if shape else ""))
     return t.data_ptr()
 
 
@@ -700,8 +700,8 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
 
 def _batch(page_table, kv_len, cu_new, T, max_new):
     """The fields of CacheBatch."""
-    if page_table.dim() != 2 or page_table.dtype is not torch.int32 or not page_table.is_cuda:
-        raise ValueError("page_table: expected int32 [B, max_pages] on the GPU")
+    if page_table.dim() != 2 or page_table.dtype is not torch.int32:
+        raise ValueError("page_table: expected int32 [B, max_pages]")
     B, P = page_table.shape
     s0, s1 = page_table.stride()
     if P > 1 and s1 != 1:
@@ -757,14 +757,12 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     on = _on(stream, cache.device, q, page_table, kv_len, cu_new, out, workspace)
     dev = q.device
     o = _empty(stream, (T, Hq * d), out_dtype, dev) if out is None else out
-    if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous() or not o.is_cuda):
-        raise ValueError("out must be contiguous [T, H_q*d] on the GPU")
+    if out is not None and (o.numel() != T * Hq * d or not o.is_contiguous()):
+        raise ValueError("out must be contiguous [T, H_q*d]")
     lse = _empty(stream, (T, Hq), torch.float32, dev) if want_lse else None
     a = _pack_attention(cache.packed, *_batch(page_table, kv_len, cu_new, T, max_new), q.data_ptr(), _heads_stride(q, "q"), Hq,
                         causal, window, sinks, scale, o.data_ptr(), _dtype_code(o), 0 if lse is None else lse.data_ptr())
     ws = workspace
-    if ws is not None and not ws.is_cuda:
-        raise ValueError("workspace must be on the GPU")
     if ws is None:
         need = _lib.cast_cache_attention_workspace_size(a)
         ws = _empty(stream, need, torch.uint8, dev) if need else None
