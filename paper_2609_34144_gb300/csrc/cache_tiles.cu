@@ -487,6 +487,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       u = unit_of(a, blockIdx.x, lane);
     } else {
       d = deal(a, gridDim.x, lane);
+      // whole units come first: should the CTA give up before its share, the joining must find no cut that the
+      // workspace held before
+      if (d.rounds > 0 && lane == 0) a.cuts[blockIdx.x].c0 = -1;
       at = d.rounds > 0 ? (int64_t)blockIdx.x * d.each : blockIdx.x * d.share;
       stop = d.rounds > 0 ? at + d.each : min(at + d.share, d.total);
       // with the share comes what it begins inside of, for the joining

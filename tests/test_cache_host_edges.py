@@ -1,6 +1,7 @@
 """The paged KV cache's entry points on the CPU, at the edges of what they take."""
 import ctypes as C
 import os
+import re
 import subprocess
 import sys
 
@@ -157,3 +158,20 @@ def test_lse_has_to_be_aligned(lib, lse):  # noqa: F811
     a = _attend(lib, batch=_batch(lib, max_pages=1000, page_table_stride=1000), lse=lse)
     assert lib.library().cast_cache_attention(C.byref(a), None, 0, None) == lib.ERR_INVALID_ARG
     assert b"lse" in lib.library().cast_last_error_detail()
+
+
+def _tiles_kernel():
+    """The text of k_cache_tiles, without comments."""
+    text = open(os.path.join(ROOT, "paper_2609_34144_gb300", "csrc", "cache_tiles.cu")).read()
+    text = re.sub(r"//[^\n]*", "", text)
+    start = text.index("k_cache_tiles(const __grid_constant__")
+    return text[start:text.index("k_tiles_merge", start)]
+
+
+def test_every_share_of_tiles_has_a_cut_before_the_first_wait():
+    """The joining follows the cuts in the workspace also when a CTA gave up: each has to be written, or marked as
+    none, before anything is waited for (whole units first: marked; else found with the share)."""
+    text = _tiles_kernel()
+    start = text[:text.index("mbar_wait")]
+    assert "a.cuts[blockIdx.x].c0 = -1" in start
+    assert re.search(r"unit_at\(a, d, at, stop, lane, d.rounds > 0 \? nullptr : a.cuts \+ blockIdx.x\)", start)

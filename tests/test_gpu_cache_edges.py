@@ -178,3 +178,14 @@ def test_outputs_on_another_stream_leave_memory_in_use_alone(lib, which):
         torch.cuda.synchronize()
         assert (kept == 7).all() and torch.equal(got, want)
     lib.cast_check_device()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_a_workspace_of_earlier_calls(lib, f8):
+    """Calls of other shapes leave their cuts and parts behind; whole units, shares of them and single units follow."""
+    ws = torch.full((1 << 26,), 0x7f, dtype=torch.uint8, device="cuda")
+    for L, new, H in ((3000, 900, 4), (2000, 700, 40), (4000, 130, 1), (2500, 128, 152), (2500, 128, 153), (3000, 900, 4)):
+        P = Pages(lib, [L], H, 64, 64, f8).fill(3)
+        q, o, lse = attend(lib, P, [new], H, False, 0, 0, workspace=ws)
+        lib.cast_check_device()
+        check(P, q, o, lse, [new], H, False, 0, 0)
