@@ -340,6 +340,7 @@ struct Bars {
   uint64_t fin;
   uint32_t tmem_base;
   int abort;
+  int issued[2];                       // of a CTA that gave up: key tiles whose K (V) copies have begun, else many
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
   float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
   Unit unit, next;                     // of this segment and the next
@@ -504,6 +505,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     if (lane == 0) {
       init_barriers<F8>(bars);
       bars->abort = 0;
+      bars->issued[0] = bars->issued[1] = 0x7fffffff;
     }
   }
   __syncthreads();
@@ -565,7 +567,11 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         const int s = j & ((1 << log_stages) - 1);
         bool ok = mbar_wait(&empty[s], ((uint32_t)(j >> log_stages) & 1u) ^ 1u, lim);
         ok = !aborted(bars) && ok;
-        if (!__all_sync(0xffffffffu, ok)) { set_abort(bars); break; }
+        if (!__all_sync(0xffffffffu, ok)) {
+          if (lane == 0) bars->issued[is_k ? 0 : 1] = j;
+          set_abort(bars);
+          break;
+        }
         uint8_t* to = codes ? raw_stage(s) : dst + s * bytes;
         fetch_pages<HD * (F8 ? 1 : 2), F8>(a, u, map, to, &full[s], tile_pos(u, k0 + j), lane);
       }
@@ -736,6 +742,17 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     }
     __syncwarp();
     if (!another()) break;
+    }
+    if ((warp == 0 || warp == 2) && aborted(bars)) {
+      // the CTA gave up: none of its copies may land after it has left.  They are the segment's last, of which no
+      // stage has begun anew, and its queries.
+      const int issued = min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
+      uint64_t* full = warp == 0 ? bars->k_full : F8 ? bars->raw_full : bars->v_full;
+      const int log_stages = warp == 0 ? (C::K_STAGES == 4 ? 2 : 1) : F8 && u.i0 + a.tile_tokens >= u.n_new ? 2 : 1;
+#pragma unroll 1
+      for (int j = max(issued - (1 << log_stages), 0); j < issued; ++j)
+        mbar_wait(&full[j & ((1 << log_stages) - 1)], (uint32_t)(j >> log_stages) & 1u, lim);
+      if (warp == 0 && u.n_tiles > 0) mbar_wait(F8 ? &bars->q_raw : &bars->q_full, 0, lim);
     }
     if (warp == 1) tmem_dealloc(tmem, kTmemCols);
   } else if (warp < 12) {

@@ -175,3 +175,15 @@ def test_every_share_of_tiles_has_a_cut_before_the_first_wait():
     start = text[:text.index("mbar_wait")]
     assert "a.cuts[blockIdx.x].c0 = -1" in start
     assert re.search(r"unit_at\(a, d, at, stop, lane, d.rounds > 0 \? nullptr : a.cuts \+ blockIdx.x\)", start)
+
+
+def test_copies_of_a_cta_that_gave_up_are_awaited():
+    """Warps 0 and 2 begin the copies into shared memory; where the CTA gave up they wait (with a limit) for those
+    that are on their way, and for the queries, before it leaves."""
+    text = _tiles_kernel()
+    assert text.count("fetch_pages<") == 1 and text.count("tma_load_3d(") == 1
+    leave = text[text.index("tma_load_3d("):text.index("setmaxnreg_inc")]
+    leave = leave[leave.rindex("another()"):]
+    gave_up = leave[leave.index("aborted(bars)"):leave.index("tmem_dealloc")]
+    assert re.search(r"for \(int j = max\(issued - .*mbar_wait\(&full\[.*lim\)", gave_up, re.S)
+    assert re.search(r"mbar_wait\(F8 \? &bars->q_raw : &bars->q_full, 0, lim\)", gave_up)
