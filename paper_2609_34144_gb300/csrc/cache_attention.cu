@@ -868,14 +868,15 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
     p.grid = units > 0x7fffffff ? 0 : (int)units;
     return p;
   }
-  // Units of two KV heads side by side, where one head's rows are at most 128 bytes in rows of 1 KB or more:
-  // what a fetch takes of a memory page is little otherwise.  Measured, one head / two, us: 24 sequences of 8k
-  // to 32k tokens, 8 bits, 8 heads of 128 205 / 189, 8 heads of 64 165 / 127, 16 heads of 64 390 / 238; 48
-  // windows of 4096, bf16, 8 heads of 64 93 / 86, 12 heads 135 / 117, but 8 heads of 128 (256 bytes) 144 / 145;
-  // 8 bits, 4 heads of 128 (512 bytes) 184 / 185.  A unit's parts are twice as many: with 64 units 73 / 72,
-  // 32 units 44 / 46.
+  // Units of two KV heads side by side, where one head's rows are at most 128 bytes in rows of 512 or more: what
+  // a fetch takes of a memory page is little otherwise.  Measured, one head / two, us: 24 sequences of 8k to 32k
+  // tokens, 8 bits, 8 heads of 128 205 / 191 (on another box 192 / 191), 8 heads of 64 165 / 127, 10 of 64
+  // 237 / 155, 16 of 64 358 to 400 / 240; bf16, 8 heads of 64 207 / 185; 32 sequences, 6 heads of 128 in 8 bits
+  // 190 / 181, of 64 in bf16 197 / 178; 48 sequences, rows of 512 bytes: 8 bits, 4 heads of 128 189 / 188, windows
+  // of 4096 53.5 / 53.9, 8 heads of 64 69 / 64; bf16, 4 of 64 178 / 175, windows 8 of 64 87.5 / 82.5, 12 of 64
+  // 128 / 113, but 8 of 128 (256 bytes each) 144 / 145.  A unit's parts are twice as many: with 64 units 73 / 72, 32 units 44 / 46.
   const int row = a.cache.d * (a.cache.dtype == CAST_F8E4M3 ? 1 : 2);
-  p.two = row <= 128 && a.cache.H % 2 == 0 && (int64_t)a.cache.H * row >= 1024 && (int64_t)a.batch.B * p.row_tiles * a.cache.H >= 128;
+  p.two = row <= 128 && a.cache.H % 2 == 0 && (int64_t)a.cache.H * row >= 512 && (int64_t)a.batch.B * p.row_tiles * a.cache.H >= 128;
   p.least >>= p.two;
   p.part_o_bytes = align_up(((size_t)2 * p.grid << p.two) * rows * a.cache.d * sizeof(float));
   p.total_bytes = p.part_o_bytes + align_up(((size_t)2 * p.grid << p.two) * rows * sizeof(float2));

@@ -8,7 +8,7 @@ import sys
 import pytest
 import torch
 
-from tests.test_cache_host import _append, _attend, _batch, lib  # noqa: F401
+from tests.test_cache_host import _append, _attend, _batch, _cache, lib  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -187,3 +187,15 @@ def test_copies_of_a_cta_that_gave_up_are_awaited():
     gave_up = leave[leave.index("aborted(bars)"):leave.index("tmem_dealloc")]
     assert re.search(r"for \(int j = max\(issued - .*mbar_wait\(&full\[.*lim\)", gave_up, re.S)
     assert re.search(r"mbar_wait\(F8 \? &bars->q_raw : &bars->q_full, 0, lim\)", gave_up)
+
+
+@pytest.mark.parametrize("dtype,d,H,two", [("f8", 64, 8, True), ("f8", 64, 10, True), ("f8", 128, 4, True), ("bf16", 64, 4, True), ("bf16", 64, 8, True),
+                                           ("f8", 64, 6, False), ("bf16", 128, 8, False)])
+def test_two_heads_side_by_side_where_rows_are_short(lib, dtype, d, H, two):  # noqa: F811
+    """Which calls take units of two KV heads shows in the workspace: twice the parts of an odd number of heads."""
+    def need(heads):
+        cache = _cache(lib, dtype=lib.F8E4M3 if dtype == "f8" else lib.BF16, H=heads, d=d, row_stride=heads * d)
+        batch = _batch(lib, B=64, T=64, max_new=1, max_pages=1000, page_table_stride=1000)
+        return lib.library().cast_cache_attention_workspace_size(C.byref(_attend(lib, cache=cache, batch=batch, H_q=heads)))
+
+    assert need(H) == (2 if two else 1) * need(H + 1)

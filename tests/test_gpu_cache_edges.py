@@ -189,3 +189,16 @@ def test_a_workspace_of_earlier_calls(lib, f8):
         q, o, lse = attend(lib, P, [new], H, False, 0, 0, workspace=ws)
         lib.cast_check_device()
         check(P, q, o, lse, [new], H, False, 0, 0)
+
+
+@pytest.mark.parametrize("f8,H,d", [(True, 8, 64), (True, 10, 64), (True, 4, 128), (True, 6, 128), (False, 4, 64), (False, 6, 64)])
+@pytest.mark.parametrize("causal,window,sinks", [(True, 0, 0), (False, 1100, 20)])
+def test_heads_whose_rows_are_short_side_by_side(lib, f8, H, d, causal, window, sinks):
+    """Rows of 512 to 1024 bytes, in sequences from nothing to over a thousand tokens."""
+    lens = [max((131 * i * i) % 1500, 1 + i % 3) for i in range(34)]
+    new = [1 + i % 3 for i in range(34)]
+    lens[5], new[5], lens[6] = 0, 0, 1500
+    P = Pages(lib, lens, H, d, 32, f8, seed=2).fill(5)
+    q, o, lse = attend(lib, P, new, 2 * H, causal, window, sinks)
+    lib.cast_check_device()
+    check(P, q, o, lse, new, 2 * H, causal, window, sinks)
