@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           if (F8 && __any_sync(0xffffffffu, e > e_ref)) {
             const float f = e > e_ref ? exp2_fast(e_ref - e) : 1.f;
             e_ref = fmaxf(e, e_ref);
-            scale_o(f);
+            if (j > 0) scale_o(f);   // (o is 0 before the first tile)
           }
         }
         uint32_t sr[BN];
