@@ -4,9 +4,9 @@ tokens attend to the first frame and a window of recent ones.
     python examples/cache_rollout.py [--bits 8] [--steps 12]
 
 Frames of Hg x Wg tokens have (frame, row, column) positions and see all of their own frame; every third
-step a single control token follows its frame, which is the same two calls with one row.  Pages of bf16 are
-history blocks as cast_block_step takes them: at the end the anchors of one more chunk are routed over all
-pages that are full.  Random data of a small model's shape.
+step a single control token follows its frame, which is the same two calls with one row.  cast_block_step takes
+history blocks in the order in which they lie and knows no page table, so the one session's pages are handed
+out in order: at the end the anchors of one more chunk are routed over all bf16 pages that are full.  Random data of a small model's shape.
 """
 from __future__ import annotations
 

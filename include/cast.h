@@ -450,7 +450,8 @@ typedef struct {
   int32_t n_pages, page_size;     /* page_size 16, 32, 64 or 128 tokens */
   int32_t H, d;                   /* KV heads; d in {64, 128} */
   void* k;                        /* device [n_pages, page_size, H, d].  With CAST_BF16 this is the */
-  void* v;                        /* layout of history blocks [M, B_v, H, d] (cast_route_args) */
+  void* v;                        /* layout of history blocks [M, B_v, H, d] (cast_route_args), which
+                                     are taken in the order in which they lie */
   int64_t row_stride;             /* elements between token rows: >= H*d, a multiple of 16; a page
                                      is page_size consecutive rows */
   float* k_scale;                 /* CAST_F8E4M3: device [n_pages, H], powers of two: a row holds */
@@ -476,7 +477,8 @@ typedef struct {
   const void* v;
   int64_t k_row_stride, v_row_stride;    /* >= H*d, multiples of 8 */
   const cast_rotary_table* rotary;       /* HOST; NULL: keys are stored as they are */
-  const int32_t* positions;       /* device [T, n_axes]; NULL: a token's place in its sequence (one axis) */
+  const int32_t* positions;       /* device [T, n_axes]; NULL: a token's place in its sequence (one axis);
+                                     not read without `rotary` */
   const void* q;                  /* optional device bf16 [T, H_q, d]: rotated into q_out in this launch */
   void* q_out;                    /* device bf16 [T, H_q, d]; may be q */
   int64_t q_row_stride, q_out_row_stride;
@@ -516,7 +518,8 @@ typedef struct {
  * f32 softmax and sums.  bf16 pages: bf16 products; a probability is rounded to bf16 before it meets its
  * value (with few rows a sequence it is two bf16 numbers).  8-bit pages: the codes are multiplied as they
  * are, queries as two numbers that keep them to 2^-19 of their row's largest channel or better,
- * probabilities as f16 in units that keep a value to 2^-32 of the largest that the row meets or better.
+ * probabilities as f16 that carry their page's V scale, which loses of a token at most 2^-32 of what its
+ * codes would be at the largest V scale that the row sees.
  * What lies at positions that a row does not see never reaches it, whatever it holds.  The workspace
  * (cast_cache_attention_workspace_size() bytes; NULL allowed when that is 0) holds partial results of
  * rows whose keys are split over several SMs.  One launch, or two where they are.

@@ -25,12 +25,12 @@
 // codes lie in their 32-bit words.
 // bf16 pages: a probability is two bf16 numbers, since memory leaves the time for the second product.
 // Bound: memory for bf16 pages; for 8-bit ones memory and the latency of dependent instructions (390 a block
-// of 16 tokens, issued in half of the slots: three CTAs of 166 registers a thread are what an SM holds).
+// of 16 tokens, issued in half of the slots: three CTAs of 165 registers a thread are what an SM holds).
 // Measured, GB300: 48 sequences with windows of 4096, 8 KV heads of 128, 4 query heads each, bf16 (830 MB)
-// 144 us, 5.8 TB/s; 24 sequences of 8k to 32k tokens in 8 bits (1.11 GB) 190 us, 5.8 TB/s.  The latter decoding
-// everything to bf16 with integer operations 438 us; by f16 236 us with three CTAs an SM, 246 with two, 255
-// with four; then 205 us with copies that test a whole block at once and logits scaled inside the exponent,
-// and 190 us with two heads side by side.  Units of 32 rows (MT = 2) are for 64-channel heads, which leave the
+// 138 to 144 us, 5.9 TB/s; 24 sequences of 8k to 32k tokens in 8 bits (1.11 GB) 191 us, 5.8 TB/s.  The latter
+// decoding everything to bf16 with integer operations 438 us; by f16 236 us with three CTAs an SM, 246 with two,
+// 255 with four; then 205 us with copies that test a whole block at once and logits scaled inside the exponent,
+// 190 us with two heads side by side, and 191 us with V units of a row's own.  Units of 32 rows (MT = 2) are for 64-channel heads, which leave the
 // registers for it.
 #include <cmath>
 
@@ -945,9 +945,10 @@ extern "C" {
 // Up to 16 rows a sequence and KV head go to k_cache_rows, more to the tiles of 128 (cache_tiles.cu),
 // except that heads of 64 with up to 32 rows stay where there are 64 units or more (two products of 16 rows
 // on the same keys).  Measured, tiles / rows, heads of 64, us, 8 bits and bf16: 256 units of 5k tokens with 32
-// rows 93 / 82, 96 / 82; 108 units of 2.4k with 18 rows 35 / 30, 35 / 31; 64 units of 20k with 32 rows 78 / 78,
-// 85 / 80; 32 units of 20k 48 / 54, 52 / 52; 16 units of 60k 63 / 71, 69 / 68; 8 units of 3k 19 / 22, 17 / 22.
-// Heads of 128 with 32 rows (before the last steps of the tiles): 16 units of 60k 82 / 95, 98 / 106.
+// rows 101 / 82, 95 / 81; 108 units of 2.4k with 18 rows 36 / 30, 35 / 31; 64 units of 20k with 32 rows 80 / 79,
+// 84 / 79; 32 units of 20k 49 / 54, 51 / 52; 16 units of 60k 64 / 72, 68 / 68; 8 units of 3k 19 / 22, 17 / 21.
+// Heads of 128 have not the registers for two products (8 bits spill 650 bytes; bf16 takes 255): 32 rows, 16 units
+// of 60k 71 / 188, 90 / 108; 256 units of 5k 112 / 240, 123 / 129.
 static bool by_tiles(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int64_t rows = (int64_t)max_new * (a.H_q / a.cache.H);

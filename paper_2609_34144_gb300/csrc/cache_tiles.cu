@@ -14,7 +14,9 @@
 // out of range is fetched from beyond the cache's end, which reads as zeros), warp 1 issues the
 // products in the order S0 S1 | PV0 S0' PV1 S1' | ..., and two warpgroups hold one query row a thread:
 // S from TMEM, mask, running maximum (renewed when a logit exceeds it by 2^8) and sum, P as bf16 back
-// to TMEM, where the P V product reads it.  The products of one thread complete in order, so a
+// to TMEM, where the P V product reads it (bf16 as V is: the two operands of a product have one type, and P in
+// two pieces would be a second product where products bound; the sum is of the unrounded P.  The error is 1.4
+// times that of the output's rounding alone).  The products of one thread complete in order, so a
 // thread that has S of tile j may change o, which holds tiles 0 .. j-1, before it hands over P.
 //
 // 0 times a value that is not finite is not 0: rows of V that no row of the unit sees are zeroed in
@@ -27,7 +29,8 @@
 // it).  So S is the sum of two products at twice the rate, and each page's scale multiplies its columns
 // of S.  V codes become f16 tiles (one conversion for two, by a fourth warpgroup, with the zeroing on the
 // way) and P is f16: a row's o is kept in units of the largest V scale that it has seen so far over 2^7, and a
-// page's probabilities carry its scale in those units in their exponent.
+// page's probabilities carry its scale in those units in their exponent.  f16 ends at 2^-25: of a token that
+// loses 2^-32 of what its codes would be at that scale, at most.
 //
 // A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
 // warpgroup and odd ones to the other, each with its own S, o, maximum and sum, so that the products of one
@@ -36,9 +39,9 @@
 // Bound: products and exponentials, about 1 us each of the 1.6 us (8 bits: 1.9 us) that a key tile of two query
 // tiles takes; with one query tile of few rows the products of 128 rows (1 us a key tile, of which memory
 // needs 0.73 us).  A CTA's first key tile is done 7 to 10 us after its start.  Measured, GB300: 3520 rows of 24
-// heads of 128 over 28160 positions, bf16 803 us, 1516 TFLOP/s, 8 bits 912 us, 1336 TFLOP/s; 1560 rows of 12 heads
-// over 12480 of 24960 positions, bf16 106 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
-// 75 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
+// heads of 128 over 28160 positions, bf16 807 us, 1508 TFLOP/s, 8 bits 912 us, 1335 TFLOP/s; 1560 rows of 12 heads
+// over 12480 of 24960 positions, bf16 108 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
+// 76 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
 // 1 % slower.
 #include <cmath>
 #include <type_traits>
@@ -148,10 +151,11 @@ __device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const S
   u.n_sink = min((u.sinks + BN - 1) / BN, u.first);
   u.tiles = u.n_sink + max((u.hi + BN - 1) / BN - u.first, 0);
 }
-// Work: a key tile of two query tiles takes 2.1 us, of one query tile 1 us, and a CTA that goes over to
-// another unit has the first key tile's softmax done ~10 us later, half of which other CTAs' memory traffic
-// gains (with no charge, one of 8 us and one of 12 us: decode of 35 rows, 60k positions, 8 bits, 85, 81, 83 us;
-// window of 1560 frame tokens 114, 110, 113 us; frames of 3520 tokens 925, 929, 930 us).
+// Work, in items of about half a microsecond: a key tile of two query tiles takes 1.6 to 1.9 us, of one query
+// tile 1 us, and a CTA that goes over to another unit has the first key tile's softmax done ~10 us later, half of
+// which other CTAs' memory traffic gains (kBegin 0, 16 and 24 when it was chosen: decode of 35 rows, 60k
+// positions, 8 bits, 85, 81, 83 us; window of 1560 frame tokens 114, 110, 113 us; frames of 3520 tokens 925, 929,
+// 930 us).
 constexpr int kBegin = 16, kPair = 4, kSingle = 2;
 __device__ __forceinline__ int tile_work(const TilesKArgs& a, const Unit& u) {
   return u.i0 + a.tile_tokens < u.n_new ? kPair : kSingle;
@@ -1444,7 +1448,7 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.pairs = p.pairs;
   k.most_pairs = (int)(((a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens));
   k.whole = p.whole;
-  k.least = 12;   // four key tiles: a segment's fixed time
+  k.least = 12;   // three key tiles of two query tiles, six of one: fewer are not worth a part
   k.part_o = static_cast<float4*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
   k.cuts = reinterpret_cast<Cut*>(static_cast<char*>(ws) + p.part_o_bytes + p.part_ml_bytes);

@@ -719,8 +719,9 @@ def _batch(page_table, kv_len, cu_new, T, max_new):
 def cast_cache_append(k, v, cache, page_table, kv_len, cu_new=None, max_new=None, rotary=None, positions=None,
                       q=None, q_out=None, stream=None):
     """Stores new tokens' keys (rotated) and values [T, H, d] in the cache; kv_len [B] counts them
-    already.  cu_new [B + 1]: ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes]
-    (None: a token's place in its sequence).  With q [T, H_q, d] returns it rotated."""
+    already.  page_table [B, max_pages] may be one table expanded over the sequences.  cu_new [B + 1]:
+    ragged rows (None: T / B each); positions: int32 [T] or [T, n_axes] (None: a token's place in its
+    sequence; not read without a rotary table).  With q [T, H_q, d] returns it rotated."""
     T, H, d = k.shape
     if v.shape != k.shape or (H, d) != cache.heads or cache.device < 0:
         raise ValueError("k and v must be [T, H, d] of the cache's heads, the cache on the GPU")
