@@ -133,11 +133,6 @@ __device__ __forceinline__ uint32_t pack2h(float a, float b) {
   const __half2 x = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&x);
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 template <int D, bool F8, int MT>
 struct Cfg {
   static constexpr int ROWS = 16 * MT;
@@ -855,7 +850,9 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   p.grid = (a.cache.dtype == CAST_F8E4M3 ? Cfg<128, true, 1>::CTAS : Cfg<128, false, 1>::CTAS) * (nsm < 1 ? 1 : nsm);
   p.least = 16;
   // Blocks that a unit has at most.  Up to 64 (a thousand tokens: four blocks' latency a warp's ring)
-  // a CTA takes a whole unit and nothing is joined.
+  // a CTA takes a whole unit and nothing is joined.  Measured, shares / whole units, us: one sequence of 301
+  // tokens 12.5 / 6.9; 1000 tokens, 32 units 15.9 / 16.1, 384 units 48 / 46, ragged 38 / 34; but 4000 tokens (250
+  // blocks), 32 units 23 / 57, 384 units 131 / 147.
   const int64_t room = (int64_t)a.batch.max_pages * a.cache.page_size;
   int64_t most = room / 16;
   if (a.window > 0) {

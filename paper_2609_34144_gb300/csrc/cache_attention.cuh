@@ -15,6 +15,11 @@ TilesPlan tiles_plan(const cast_cache_attn_args& a);
 // Arguments must have been validated; ws holds tiles_plan(a).total_bytes.
 cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void* ws, cudaStream_t st);
 
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&x);

@@ -351,11 +351,6 @@ struct Bars {
 };
 static_assert(sizeof(Bars) <= 1664, "barriers and the unit");
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -1411,6 +1406,9 @@ TilesPlan tiles_plan(const cast_cache_attn_args& a) {
   int dev = 0, nsm = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
   if (nsm < 1) nsm = 1;
+  // Measured, shares / whole units, us: 6 prompts of up to 1201 with a window of 500 33 / 21.5, 16 chunks of 700 of
+  // 1000 positions 46 / 37, 4 of 256 19.6 / 19.1; but of 3000 positions (24 tiles) 2 chunks of 512 23 / 41, 6 of up to
+  // 1201 38 / 41, 16 of 700 88 / 80.
   p.whole = tiles <= 8;
   p.grid = p.whole ? units : nsm;
   if (!p.whole) {
