@@ -18,7 +18,7 @@
  *   cast_block_step        the three in order at one attention residual site
  *
  * and the history as a serving loop keeps it, a paged KV cache: cast_rotary,
- * cast_cache_append, cast_cache_attention.
+ * cast_cache_append, cast_cache_attention, cast_cache_read.
  *
  * Conventions shared by every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller; `anchors` and
@@ -394,6 +394,8 @@ size_t cast_select_workspace_size(const cast_select_args* args);
 /* ------------------------------------------------------------------------ */
 #define CAST_F8E4M3 2             /* cache pages only: 8-bit floats (4 exponent, 3 mantissa bits,
                                      no infinity), one scale for each (page, KV head) */
+#define CAST_F4E2M1 3             /* cache pages only: 4-bit floats (sign, 2 exponent bits, 1 mantissa bit: 0,
+                                     1/2, 1, 3/2, 2, 3, 4, 6), one scale for 16 channels of a token and head */
 
 #define CAST_ROTARY_HALF 0        /* pair i = channels (i, i + rot_dim / 2) */
 #define CAST_ROTARY_INTERLEAVED 1 /* pair i = channels (2 i, 2 i + 1) */
@@ -446,16 +448,22 @@ typedef struct {
 cast_status cast_rotary(const cast_rotary_args* args, void* stream);
 
 typedef struct {
-  int32_t dtype;                  /* CAST_BF16 or CAST_F8E4M3 */
+  int32_t dtype;                  /* CAST_BF16, CAST_F8E4M3 or CAST_F4E2M1 */
   int32_t n_pages, page_size;     /* page_size 16, 32, 64 or 128 tokens */
   int32_t H, d;                   /* KV heads; d in {64, 128} */
   void* k;                        /* device [n_pages, page_size, H, d].  With CAST_BF16 this is the */
   void* v;                        /* layout of history blocks [M, B_v, H, d] (cast_route_args), which
-                                     are taken in the order in which they lie */
+                                     are taken in the order in which they lie.  CAST_F4E2M1: device
+                                     [n_pages, H, page_size, d / 2] bytes, channel 2i in the low half */
   int64_t row_stride;             /* elements between token rows: >= H*d, a multiple of 16; a page
-                                     is page_size consecutive rows */
-  float* k_scale;                 /* CAST_F8E4M3: device [n_pages, H], powers of two: a row holds */
-  float* v_scale;                 /* code * scale */
+                                     is page_size consecutive rows.  CAST_F4E2M1: a page begins
+                                     page_size * row_stride elements (two a byte) behind the one before */
+  void* k_scale;                  /* CAST_F8E4M3: device f32 [n_pages, H], powers of two: a row holds */
+  void* v_scale;                  /* code * scale.  CAST_F4E2M1: device [n_pages, H, page_size, d / 16] bytes, 16-byte
+                                     aligned, each a scale of 5 exponent and 3 mantissa bits: an f16 number's bits
+                                     without sign, shifted right by 7 (0xf8 and above: not finite).  Appended ones are
+                                     at most 10240, so that every value is exact in f16 and in bf16; the kernels form
+                                     values in f16, where those above 65504 are infinite */
 } cast_kv_cache;
 
 /* The sequences of a call.  Sequence b has kv_len[b] tokens in the cache once its new ones are
@@ -491,7 +499,9 @@ typedef struct {
  * [-120, 120]; a page that the sequence only continues (its first new row is not row 0) keeps the
  * larger of its scale and 2^e, and its earlier rows are rounded again at a scale that grew (a power
  * of two: nothing but subnormal codes changes).  Codes are x / scale to nearest even; NaN and
- * infinity become NaN.  The pages written by one call are distinct.
+ * infinity become NaN.  CAST_F4E2M1: channels 16 i .. 16 i + 15 of a token and head share a scale, max |x| / 6 to
+ * nearest even (at most 10240), and codes are x / scale to nearest even (at most 6); a group with NaN or infinity is
+ * all NaN.  Nothing but the new tokens' rows is written.  The pages written by one call are distinct.
  * One launch.  Errors: INVALID_ARG for NULL or misaligned pointers, bad shapes, strides or tables;
  * UNSUPPORTED for d not 64/128, page_size not 16/32/64/128.  A page outside [0, n_pages), a position
  * past max_pages pages or a new token past max_new is left out, recorded, and reported by
@@ -519,7 +529,9 @@ typedef struct {
  * value (with few rows a sequence it is two bf16 numbers).  8-bit pages: the codes are multiplied as they
  * are, queries as two numbers that keep them to 2^-19 of their row's largest channel or better,
  * probabilities as f16 that carry their page's V scale, which loses of a token at most 2^-32 of what its
- * codes would be at the largest V scale that the row sees.
+ * codes would be at the largest V scale that the row sees.  4-bit pages: f16 products of the values as they are, of
+ * queries as f16 numbers that keep their bits down to 2^-29 of their row's largest channel, and of probabilities as
+ * f16, which loses 2^-12 of one, or 2^-32 of the row's largest.
  * What lies at positions that a row does not see never reaches it, whatever it holds.  The workspace
  * (cast_cache_attention_workspace_size() bytes; NULL allowed when that is 0) holds partial results of
  * rows whose keys are split over several SMs.  One launch, or two where they are.
@@ -530,6 +542,24 @@ typedef struct {
 cast_status cast_cache_attention(const cast_cache_attn_args* args, void* workspace,
                                  size_t workspace_bytes, void* stream);
 size_t cast_cache_attention_workspace_size(const cast_cache_attn_args* args);
+
+typedef struct {
+  cast_kv_cache cache;            /* pages of any dtype */
+  cast_cache_batch batch;         /* its rows: the last cu_new[b + 1] - cu_new[b] (or T / B) of a sequence's kv_len[b]
+                                     tokens; any other run of tokens is the end of a smaller kv_len */
+  void* k_out;                    /* device [T, H, d] of out_dtype; NULL: not wanted (not both) */
+  void* v_out;
+  int64_t k_row_stride, v_row_stride;    /* elements: >= H*d, multiples of 8 */
+  int32_t out_dtype;              /* CAST_BF16 or CAST_F32 */
+} cast_cache_read_args;
+
+/* Row i of sequence b becomes what the cache holds of its token at position p = kv_len[b] - new_b + i, in the
+ * sequence's order: bf16 rows are history blocks [M, B_v, H, d] for the routing whatever their pages' type and order.
+ * Appended values of 8 or 4 bits are exact in bf16.  Positions p < 0, past max_pages pages, or in a page outside
+ * [0, n_pages) read as zeros; the latter two and new tokens past max_new (whose rows are not written) are recorded
+ * and reported by cast_check_device() as INVALID_ARG.  One launch.  Errors: as cast_cache_append, and INVALID_ARG
+ * for both outputs NULL or a bad out_dtype. */
+cast_status cast_cache_read(const cast_cache_read_args* args, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Status                                                                    */

@@ -1,5 +1,5 @@
 // The paged KV cache's writers: rotary positions (cast_rotary) and the append of new tokens to the
-// pages with the rotation and the 8-bit quantisation on the way (cast_cache_append).
+// pages with the rotation and the quantisation to 8 or 4 bits on the way (cast_cache_append).
 //
 // Both are bound by memory: every channel is read and written once, a pair costs six flops.  What
 // is not free is the angle: 64 sines and cosines a token for heads of 128, shared by all heads, so
@@ -95,7 +95,7 @@ struct AppendKArgs {
   const __nv_bfloat16 *k, *v, *q;
   __nv_bfloat16* q_out;
   void *ck, *cv;
-  float *k_scale, *v_scale;
+  float *k_scale, *v_scale;       // 4-bit pages: bytes
   const int* positions;
   int runs;               // page runs of a sequence that the grid has room for
   int group;              // heads of one CTA
@@ -111,7 +111,7 @@ struct AppendKArgs {
 // heads of 128, 8-bit pages (433 MB) 78 us, 5.5 TB/s, with three heads ahead (two 80, one 90 us) and
 // groups of 12 heads (24 79, 8 84, 4 104 us: what the angles cost).
 constexpr int kAhead = 4;
-template <bool F8>
+template <int KIND>   // the pages' type
 __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendKArgs a,
                                                  const __grid_constant__ cast_rotary_table tab) {
   __shared__ uint32_t s_max[2][32];
@@ -157,7 +157,8 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
   const __nv_bfloat16* src = (kind == 0 ? a.k : kind == 1 ? a.v : a.q) +
                              (token0 + row) * (kind == 0 ? a.k_stride : kind == 1 ? a.v_stride : a.q_stride);
   const int64_t to = kind == 2 ? (token0 + row) * a.q_out_stride : ((int64_t)page * a.page_size + row) * a.row_stride;
-  const bool codes = F8 && kind != 2;
+  constexpr bool F8 = KIND == CAST_F8E4M3, F4 = KIND == CAST_F4E2M1;
+  const bool codes = (F8 || F4) && kind != 2;
   auto fetch = [&](int h) {
     if (in && h < h1) {
       uint4* to = s_in + (h - h0) % kAhead * 2 * blockDim.x + threadIdx.x;
@@ -244,6 +245,56 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
       // every thread has read `scale` before the barrier above
       if (threadIdx.x == 0) *scale = now;
     }
+    if constexpr (F4) {
+      // A scale's 16 channels are two runs of 8: both of this thread's unit or, where the half layout parts them,
+      // one of this unit and one of another of the row, whose threads are neighbours in the warp
+      uint32_t top[2] = {0, 0};   // magnitudes order as their bits, NaN and infinity above all others
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top[i >> 3] = max(top[i >> 3], __float_as_uint(fabsf(v[i])));
+      const bool parted = c1 != c0 + 8;
+      uint32_t both[2] = {max(top[0], top[1]), 0};
+      both[1] = both[0];
+      if (__any_sync(0xffffffffu, parted)) {
+        // run r = channel / 8 belongs to unit r (its first run), r - turned units (its second), or r / 2
+        const int turned_units = tab.rot_dim / 16, row0 = (threadIdx.x & 31) & -per_row;
+        uint32_t mate[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int run = ((i ? c1 : c0) >> 3) ^ 1;
+          const int owner = run < turned_units ? run : run < 2 * turned_units ? run - turned_units : run >> 1;
+          const bool second = run < turned_units ? false : run < 2 * turned_units ? true : run & 1;
+          const uint32_t a0 = __shfl_sync(0xffffffffu, top[0], row0 + owner), a1 = __shfl_sync(0xffffffffu, top[1], row0 + owner);
+          mate[i] = second ? a1 : a0;
+        }
+        if (parted) {
+          both[0] = max(top[0], mate[0]);
+          both[1] = max(top[1], mate[1]);
+        }
+      }
+      if (in) {
+        const int64_t first_row = ((int64_t)page * a.H + h) * a.page_size + row;   // of the scales
+        uint8_t* cache = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv) + (int64_t)page * a.page_size * a.row_stride / 2 +
+                         ((int64_t)h * a.page_size + row) * (a.d / 2);
+        uint8_t* scales = reinterpret_cast<uint8_t*>(kind == 0 ? a.k_scale : a.v_scale) + first_row * (a.d / 16);
+        uint32_t word[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t code = scale4_code(both[i]);
+          const float s = scale4_value(code), r = code ? 1.f / s : 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[8 * i + e] = code == kScaleNan ? 0.f : over_scale(v[8 * i + e], s, r);
+          word[i] = encode4(v + 8 * i);
+          const int run = (i ? c1 : c0) >> 3;
+          if (!(run & 1)) scales[run >> 1] = (uint8_t)code;
+        }
+        if (parted) {
+          *reinterpret_cast<uint32_t*>(cache + c0 / 2) = word[0];
+          *reinterpret_cast<uint32_t*>(cache + c1 / 2) = word[1];
+        } else {
+          *reinterpret_cast<uint2*>(cache + c0 / 2) = make_uint2(word[0], word[1]);
+        }
+      }
+    }
   }
 }
 
@@ -261,6 +312,8 @@ cast_status check_table(const cast_rotary_table* t, int d, const char* who) {
   return CAST_OK;
 }
 
+}  // namespace
+
 cast_status check_rows(const void* p, int64_t stride, int64_t least, const char* name, const char* who) {
   if (!p || !aligned16(p)) return fail(CAST_ERR_INVALID_ARG, "%s: %s is NULL or not 16-byte aligned", who, name);
   if (stride < least || stride % 8)
@@ -269,12 +322,10 @@ cast_status check_rows(const void* p, int64_t stride, int64_t least, const char*
   return CAST_OK;
 }
 
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-
-}  // namespace
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 cast_status validate_cache(const cast_kv_cache& c, const char* who) {
-  if (c.dtype != CAST_BF16 && c.dtype != CAST_F8E4M3)
+  if (c.dtype != CAST_BF16 && c.dtype != CAST_F8E4M3 && c.dtype != CAST_F4E2M1)
     return fail(CAST_ERR_INVALID_ARG, "%s: cache dtype %d", who, c.dtype);
   if (c.d != 64 && c.d != 128) return fail(CAST_ERR_UNSUPPORTED, "%s: head dim %d (64 or 128)", who, c.d);
   if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128)
@@ -288,6 +339,8 @@ cast_status validate_cache(const cast_kv_cache& c, const char* who) {
                 (long long)c.row_stride);
   if (c.dtype == CAST_F8E4M3 && (!c.k_scale || !c.v_scale || !aligned4(c.k_scale) || !aligned4(c.v_scale)))
     return fail(CAST_ERR_INVALID_ARG, "%s: 8-bit pages need k_scale and v_scale", who);
+  if (c.dtype == CAST_F4E2M1 && (!c.k_scale || !c.v_scale || !aligned16(c.k_scale) || !aligned16(c.v_scale)))
+    return fail(CAST_ERR_INVALID_ARG, "%s: 4-bit pages need k_scale and v_scale, 16-byte aligned", who);
   return CAST_OK;
 }
 
@@ -461,8 +514,8 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   k.q_out = static_cast<__nv_bfloat16*>(a->q_out);
   k.ck = c.k;
   k.cv = c.v;
-  k.k_scale = c.k_scale;
-  k.v_scale = c.v_scale;
+  k.k_scale = static_cast<float*>(c.k_scale);
+  k.v_scale = static_cast<float*>(c.v_scale);
   k.positions = a->positions;
   // a sequence's new tokens touch at most this many pages
   const int max_new = a->batch.max_new < a->batch.T ? a->batch.max_new : a->batch.T;
@@ -483,8 +536,9 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   const int bytes = kAhead * 2 * 16 * threads;
   static std::atomic<uint64_t> attr_done{0};
   if (!once_per_device(attr_done, [&] {
-        return cudaFuncSetAttribute(k_append<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAhead * 32 * 1024) == cudaSuccess &&
-               cudaFuncSetAttribute(k_append<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAhead * 32 * 1024) == cudaSuccess;
+        for (auto* f : {k_append<CAST_F8E4M3>, k_append<CAST_F4E2M1>, k_append<CAST_BF16>})
+          if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kAhead * 32 * 1024) != cudaSuccess) return false;
+        return true;
       }))
     return check_launch("cache append kernel attributes");
   const dim3 grid((unsigned)gx, 2 * k.jobs_kv + k.jobs_q);
@@ -492,9 +546,11 @@ cast_status cast_cache_append(const cast_append_args* a, void* stream) {
   const cast_rotary_table& tab = a->rotary ? *a->rotary : none;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.dtype == CAST_F8E4M3)
-    k_append<true><<<grid, threads, bytes, st>>>(k, tab);
+    k_append<CAST_F8E4M3><<<grid, threads, bytes, st>>>(k, tab);
+  else if (c.dtype == CAST_F4E2M1)
+    k_append<CAST_F4E2M1><<<grid, threads, bytes, st>>>(k, tab);
   else
-    k_append<false><<<grid, threads, bytes, st>>>(k, tab);
+    k_append<CAST_BF16><<<grid, threads, bytes, st>>>(k, tab);
   return check_launch(who);
 }
 

@@ -1,4 +1,4 @@
-// What the paged-cache kernels share: sequences and pages of a call, 8-bit pages, the rotation.
+// What the paged-cache kernels share: sequences and pages of a call, 8- and 4-bit pages, the rotation.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -137,5 +137,59 @@ __device__ __forceinline__ int scale_exponent(float amax) {
   return min(max(e, -120), 120);
 }
 __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }
+
+// ------------------------------------------------------------------ 4-bit pages
+// A page is [H][page_size][d / 2] bytes of codes (channel 2i in the low half of byte i), so that a head's rows
+// lie together: 64-byte rows a KV head apart would cost memory half of its rate.  Its scales, [H][page_size][d / 16]
+// bytes, are the upper eight bits of f16 numbers without sign (5 exponent, 3 mantissa bits): the range of a scale in
+// f16 makes one for the page superfluous, a shift by 7 decodes it, and its four significant bits times a code's two
+// are exact in f16 and in bf16.
+constexpr uint32_t kScaleTop = 0xe2;    // 10240: six times it is the largest value within f16
+constexpr uint32_t kScaleNan = 0xff;
+
+// The scale of 16 channels whose largest magnitude has these bits, as its byte: max / 6 to nearest even
+__device__ __forceinline__ uint32_t scale4_code(uint32_t top) {
+  if (top >= 0x7f800000u) return kScaleNan;
+  const float a = __fdiv_rn(__uint_as_float(top), 6.f);
+  if (a < 0x1p-14f) return (uint32_t)__float2int_rn(a * 0x1p17f);   // multiples of 2^-17
+  uint32_t u = __float_as_uint(a);
+  u += 0x7ffffu + ((u >> 20) & 1u);
+  return min((u >> 20) - (uint32_t)((127 - 15) << 3), kScaleTop);
+}
+__device__ __forceinline__ float scale4_value(uint32_t code) {
+  return __half2float(__ushort_as_half((unsigned short)(code << 7)));
+}
+// x / s for a scale s and r = 1 / s rounded: x r corrected once by its remainder, which is exact (Markstein's
+// correction).  Where the quotient is half way between two codes it comes out exactly: it differs from x r by 2^-23
+// of itself at most, the correction is good to 2^-47, and the halfway points have three bits.
+__device__ __forceinline__ float over_scale(float x, float s, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, s, x), r, q);
+}
+// Eight floats as codes, to nearest even (6 at most), the first in the lowest four bits
+__device__ __forceinline__ uint32_t encode4(const float* v) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+// The four bytes of a word as f16 pairs (low half, high half of a byte)
+__device__ __forceinline__ void half8(uint32_t w, uint32_t* h) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// A scale's byte (the lowest of w) as an f16 pair of it twice, and of two scales
+__device__ __forceinline__ uint32_t scale4_pair(uint32_t w) { return __byte_perm(w, 0, 0x4040) << 7; }
+__device__ __forceinline__ uint32_t scale4_pair(uint32_t low, uint32_t high) { return (low << 7) | (high << 23); }
+__device__ __forceinline__ uint32_t times2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 
 }  // namespace cast

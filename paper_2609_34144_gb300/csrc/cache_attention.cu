@@ -885,6 +885,7 @@ cast_status validate_attention(const cast_cache_attn_args* a, const char* who) {
   cast_status s = validate_cache(a->cache, who);
   if (s) return s;
   if ((s = validate_batch(a->batch, who))) return s;
+  if (a->cache.dtype == CAST_F4E2M1) return fail(CAST_ERR_UNSUPPORTED, "%s: 4-bit pages", who);
   if (a->H_q < 1 || a->H_q % a->cache.H)
     return fail(CAST_ERR_INVALID_ARG, "%s: H_q %d is not a multiple of the cache's %d heads", who, a->H_q, a->cache.H);
   if (a->H_q / a->cache.H > 128) return fail(CAST_ERR_UNSUPPORTED, "%s: %d query heads a KV head", who, a->H_q / a->cache.H);
@@ -995,8 +996,8 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   k.q_stride = a->q_row_stride;
   k.k = static_cast<const uint8_t*>(c.k);
   k.v = static_cast<const uint8_t*>(c.v);
-  k.k_scale = c.k_scale;
-  k.v_scale = c.v_scale;
+  k.k_scale = static_cast<const float*>(c.k_scale);
+  k.v_scale = static_cast<const float*>(c.v_scale);
   k.q = static_cast<const __nv_bfloat16*>(a->q);
   k.o = a->o;
   k.lse = a->lse;

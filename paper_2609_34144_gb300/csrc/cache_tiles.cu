@@ -1438,8 +1438,8 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.o_f32 = a.o_dtype == CAST_F32;
   k.row_stride = c.row_stride;
   k.v = static_cast<const uint8_t*>(c.v);
-  k.k_scale = c.k_scale;
-  k.v_scale = c.v_scale;
+  k.k_scale = static_cast<const float*>(c.k_scale);
+  k.v_scale = static_cast<const float*>(c.v_scale);
   k.o = a.o;
   k.lse = a.lse;
   k.scale_log2 = (a.scale > 0.f ? a.scale : 1.f / sqrtf((float)c.d)) * 1.4426950408889634f;

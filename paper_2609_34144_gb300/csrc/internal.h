@@ -144,12 +144,14 @@ unsigned int dense_error_word(cudaStream_t st, bool clear);
 
 // ------------------------------------------------------------------ paged KV cache
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-// host checks shared by the append and the attention (cache.cu)
+// host checks shared by the append, the reading and the attention (cache.cu)
 cast_status validate_cache(const cast_kv_cache& c, const char* who);
 cast_status validate_batch(const cast_cache_batch& b, const char* who);
-// Nonzero when a kernel (of the append, the attention's two forms) left out a page, position or token that
+cast_status check_rows(const void* p, int64_t stride, int64_t least, const char* name, const char* who);
+// Nonzero when a kernel (of the append, the reading, the attention's two forms) left out a page, position or token that
 // was out of range.
 unsigned int cache_error_word(cudaStream_t st, bool clear);
+unsigned int cache_read_error_word(cudaStream_t st, bool clear);
 unsigned int cache_rows_error_word(cudaStream_t st, bool clear);
 unsigned int cache_tiles_error_word(cudaStream_t st, bool clear);
 // Nonzero when the cache attention gave up on a bounded wait.

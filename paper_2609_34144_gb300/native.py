@@ -21,7 +21,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_TIMEOUT = 0, 1, 2, 3, 4
-F32, BF16, F8E4M3 = 0, 1, 2
+F32, BF16, F8E4M3, F4E2M1 = 0, 1, 2, 3
 ROUTE_OMISSION, ROUTE_SIMILARITY = 0, 1
 HIST_BLOCKS, HIST_FRAMES = 0, 1
 GATE_PAPER, GATE_ZERO, GATE_ONE = 0, 1, 2
@@ -139,10 +139,16 @@ class CacheAttnArgs(C.Structure):
                 ("o_dtype", _i32), ("lse", _vp)]
 
 
+class CacheReadArgs(C.Structure):
+    _fields_ = [("cache", KvCache), ("batch", CacheBatch), ("k_out", _vp), ("v_out", _vp), ("k_row_stride", _i64),
+                ("v_row_stride", _i64), ("out_dtype", _i32)]
+
+
 _lib.cast_rotary_table_init.argtypes = [C.POINTER(RotaryParams), C.POINTER(RotaryTable)]
 # these take the structs by reference, or their bytes (see the packers below)
 _lib.cast_rotary.argtypes = [_vp, _vp]
 _lib.cast_cache_append.argtypes = [_vp, _vp]
+_lib.cast_cache_read.argtypes = [_vp, _vp]
 _lib.cast_cache_attention.argtypes = [_vp, _vp, C.c_size_t, _vp]
 _lib.cast_cache_attention_workspace_size.argtypes = [_vp]
 _lib.cast_cache_attention_workspace_size.restype = C.c_size_t
@@ -178,7 +184,7 @@ for _f in ("cast_route_topk", "cast_route_topk_noalloc", "cast_anchor_attention"
     getattr(_lib, _f).restype = C.c_int
 
 EXPORTED = ["cast_rotary_table_init", "cast_rotary", "cast_cache_append", "cast_cache_attention",
-            "cast_cache_attention_workspace_size",
+            "cast_cache_attention_workspace_size", "cast_cache_read",
             "cast_select_frames", "cast_select_workspace_size", "cast_ffn_step",
             "cast_ffn_workspace_size",
             "cast_route_topk", "cast_route_workspace_size", "cast_route_topk_noalloc",
@@ -576,6 +582,9 @@ def ffn_workspace_size(x, anchors, w1, b1, w2, b2, grid, r_out):
 
 
 # --------------------------------------------------------------------------- paged KV cache
+_F4X2 = getattr(torch, "float4_e2m1fn_x2", None)
+
+
 def rotary_table(rot_dim, layout="half", base=10000.0, sections=None, scaling=None):
     """The table cast_rotary and cast_cache_append rotate by (host data, made once).  layout:
     "half" (pairs i, i + rot_dim/2) or "interleaved" (2i, 2i+1); sections: pairs of each position
@@ -607,6 +616,7 @@ _BATCH = "PqiPPiii4x"
 _pack_rotary = struct.Struct("@PPqqiiiiPPi4x").pack
 _pack_append = struct.Struct("@64s" + _BATCH + "PPqqPPPPqqi4x").pack
 _pack_attention = struct.Struct("@64s" + _BATCH + "PqiiiifPiP").pack
+_pack_read = struct.Struct("@64s" + _BATCH + "PPqqi4x").pack
 
 
 def _on(stream, device, *tensors):
@@ -675,27 +685,51 @@ def cast_rotary(x, positions, table, inverse=False, out=None, stream=None):
 
 def kv_cache(k, v, k_scale=None, v_scale=None):
     """Handle of a paged cache: k, v [n_pages, page_size, H, d], bf16 or float8_e4m3fn (or its bits
-    as uint8) with f32 scales [n_pages, H].  It keeps the tensors it describes."""
+    as uint8) with f32 scales [n_pages, H]; 4-bit pages: uint8 (or float4_e2m1fn_x2) [n_pages, H, page_size, d/2],
+    two channels a byte, with uint8 scales [n_pages, H, page_size, d/16].  It keeps the tensors it describes."""
     if k.shape != v.shape or k.dim() != 4 or k.dtype != v.dtype:
-        raise ValueError("k and v: [n_pages, page_size, H, d] of one shape and dtype")
-    n, ps, H, d = k.shape
-    if _row_stride(k) != _row_stride(v):
-        raise ValueError("k and v must have the same row stride")
-    f8 = k.dtype in (torch.float8_e4m3fn, torch.uint8)
-    if not f8 and k.dtype != torch.bfloat16:
-        raise TypeError(f"unsupported cache dtype {k.dtype}")
-    if f8:
+        raise ValueError("k and v: [n_pages, page_size, H, d] (4 bits: [n_pages, H, page_size, d/2]) of one shape and dtype")
+    f4 = k.dtype is _F4X2 or (k.dtype is torch.uint8 and k_scale is not None and k_scale.dtype is torch.uint8)
+    f8 = not f4 and k.dtype in (torch.float8_e4m3fn, torch.uint8)
+    if f4:
+        n, H, ps, d = k.shape
+        d *= 2
+        stride = _page_stride(k)
+        if stride != _page_stride(v):
+            raise ValueError("k and v must have the same page stride")
+        shape, what = (n, H, ps, d // 16), "4-bit pages need contiguous uint8 scales [n_pages, H, page_size, d/16]"
+    else:
+        n, ps, H, d = k.shape
+        stride = _row_stride(k)
+        if stride != _row_stride(v):
+            raise ValueError("k and v must have the same row stride")
+        if not f8 and k.dtype != torch.bfloat16:
+            raise TypeError(f"unsupported cache dtype {k.dtype}")
+        shape, what = (n, H), "8-bit pages need contiguous f32 scales [n_pages, H]"
+    if f8 or f4:
         for s in (k_scale, v_scale):
-            if s is None or s.dtype != torch.float32 or tuple(s.shape) != (n, H) or not s.is_contiguous():
-                raise ValueError("8-bit pages need contiguous f32 scales [n_pages, H]")
-    c = KvCache(F8E4M3 if f8 else BF16, n, ps, H, d, k.data_ptr(), v.data_ptr(), _row_stride(k),
-                k_scale.data_ptr() if f8 else None, v_scale.data_ptr() if f8 else None)
+            if s is None or s.dtype != (torch.uint8 if f4 else torch.float32) or tuple(s.shape) != shape or not s.is_contiguous():
+                raise ValueError(what)
+    c = KvCache(F4E2M1 if f4 else F8E4M3 if f8 else BF16, n, ps, H, d, k.data_ptr(), v.data_ptr(), stride,
+                k_scale.data_ptr() if f8 or f4 else None, v_scale.data_ptr() if f8 or f4 else None)
     c._keep = (k, v, k_scale, v_scale)
     c.packed = bytes(c)
     gpus = {t.get_device() for t in (k, v, k_scale, v_scale) if t is not None}
     c.device = gpus.pop() if len(gpus) == 1 else -1   # -1: not on one GPU
     c.heads = (H, d)
     return c
+
+
+def _page_stride(t):
+    """Elements (two a byte) a token row that lie between the pages of 4-bit pages [n_pages, H, page_size, d/2]."""
+    n, H, ps, half = t.shape
+    if t.numel() == 0 or not t[0].is_contiguous():
+        raise ValueError("4-bit pages: heads, rows and channels of a page must be contiguous")
+    if n < 2:
+        return H * half * 2
+    if t.stride(0) * 2 % ps:
+        raise ValueError("4-bit pages: the page stride must be a multiple of page_size / 2 bytes")
+    return t.stride(0) * 2 // ps
 
 
 def _batch(page_table, kv_len, cu_new, T, max_new):
@@ -770,3 +804,26 @@ def cast_cache_attention(q, cache, page_table, kv_len, cu_new=None, max_new=None
     _check(_lib.cast_cache_attention(a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), on))
     return (o, lse) if want_lse else o
 
+
+def cast_cache_read(cache, page_table, kv_len, rows, cu_new=None, max_new=None, keys=True, values=True,
+                    dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+    """What the cache (of any type) holds of the last tokens of its sequences, in their order: `rows` of them in all,
+    rows / B each or, with cu_new [B + 1], cu_new[b + 1] - cu_new[b]; kv_len [B] says where they end.  Returns (k, v),
+    each [rows, H, d] of `dtype` (bf16 or f32), None where keys or values is False and no output is given."""
+    H, d = cache.heads
+    if cache.device < 0:
+        raise ValueError("the cache must be on the GPU")
+    for t in (k_out, v_out):
+        if t is not None and (tuple(t.shape) != (rows, H, d) or t.dtype is not dtype):
+            raise ValueError("k_out and v_out must be [rows, H, d] of dtype")
+    on = _on(stream, cache.device, page_table, kv_len, cu_new, k_out, v_out)
+    dev = page_table.device
+    k = _empty(stream, (rows, H, d), dtype, dev) if k_out is None and keys else k_out
+    v = _empty(stream, (rows, H, d), dtype, dev) if v_out is None and values else v_out
+    if k is None and v is None:
+        raise ValueError("neither keys nor values are wanted")
+    a = _pack_read(cache.packed, *_batch(page_table, kv_len, cu_new, rows, max_new), 0 if k is None else k.data_ptr(),
+                   0 if v is None else v.data_ptr(), H * d if k_out is None else _heads_stride(k, "k_out", None),
+                   H * d if v_out is None else _heads_stride(v, "v_out", None), F32 if dtype is torch.float32 else BF16 if dtype is torch.bfloat16 else -1)
+    _check(_lib.cast_cache_read(a, on))
+    return k, v

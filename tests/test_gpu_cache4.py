@@ -1,0 +1,274 @@
+"""4-bit pages on the GPU against 64 bits: the append, the reading back (of pages of every type), the attention."""
+import numpy as np
+import pytest
+import torch
+
+from tests import cache4_ref as R4
+from tests import cache_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape):
+    return torch.randn(shape, generator=g, device="cuda")
+
+
+def i32(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Pages4:
+    """A 4-bit cache of B sequences, pages in no order, NaN scales wherever nothing was stored."""
+
+    def __init__(self, lib, lens, H, d, page, seed=0, spare=2, apart=False):
+        g = gen(seed)
+        self.lib, self.lens, self.H, self.d, self.page = lib, list(lens), H, d, page
+        per = [-(-n // page) for n in lens]
+        n = sum(per) + spare
+        pool = torch.randint(0, 256, (n, 2, H, page, d // 2), generator=g, device="cuda", dtype=torch.uint8)
+        # K and V of a page side by side in one pool, or tensors of their own
+        self.k, self.v = (pool[:, 0], pool[:, 1]) if apart else (pool[:, 0].contiguous(), pool[:, 1].contiguous())
+        self.ks, self.vs = (torch.full((n, H, page, d // 16), 0xff, dtype=torch.uint8, device="cuda") for _ in range(2))
+        order = torch.randperm(n, generator=torch.Generator().manual_seed(seed))
+        self.table = torch.full((len(lens), max(max(per), 1)), -7, dtype=torch.int32)
+        at = 0
+        for b, c in enumerate(per):
+            self.table[b, :c] = order[at:at + c].int()
+            at += c
+        self.table = self.table.cuda()
+        self.kv_len = i32(*lens)
+        self.cache = lib.kv_cache(self.k, self.v, self.ks, self.vs)
+
+    def fill(self, seed=1, scale=1.0):
+        """Everything stored: codes of normal numbers, in place."""
+        g = gen(seed)
+        out = []
+        for b, n in enumerate(self.lens):
+            k, v = (randn(g, n, self.H, self.d) * scale for _ in range(2))
+            kq, ks = R4.quantise(f64(k))
+            vq, vs = R4.quantise(f64(v))
+            for page_t, scale_t, q, s in ((self.k, self.ks, kq, ks), (self.v, self.vs, vq, vs)):
+                codes = encode(q, s)
+                for i in range(0, n, self.page):
+                    p, m = int(self.table[b, i // self.page]), min(self.page, n - i)
+                    page_t[p, :, :m] = torch.from_numpy(codes[i:i + m]).cuda().transpose(0, 1)
+                    scale_t[p, :, :m] = torch.from_numpy(s[i:i + m]).cuda().transpose(0, 1)
+            out.append((kq, vq))
+        return out
+
+    def held(self, name, b):
+        """Values [len, H, d] and scale bytes of sequence b as they lie."""
+        t, s = (self.k, self.ks) if name == "k" else (self.v, self.vs)
+        n, p = self.lens[b], self.table[b, :-(-self.lens[b] // self.page)].long()
+        codes = t[p].transpose(1, 2).reshape(-1, self.H, self.d // 2)[:n].cpu().numpy()
+        scales = s[p].transpose(1, 2).reshape(-1, self.H, self.d // 16)[:n].cpu().numpy()
+        return R4.decode(codes, scales), scales
+
+
+def encode(values, scales):
+    s = np.repeat(R4.scale_value(scales), 16, -1)
+    with np.errstate(all="ignore"):
+        m = np.where((s > 0) & np.isfinite(s), np.abs(values) / np.where(s > 0, s, 1), 0)
+    c = np.searchsorted(R4.VALUES, m).astype(np.uint8) | np.where(values < 0, 8, 0).astype(np.uint8)
+    return (c[..., 0::2] | c[..., 1::2] << 4).astype(np.uint8)
+
+
+# ------------------------------------------------------------------------------------ append
+APPEND = [
+    # lens, new, H, H_q, d, page, rot, layout, sections
+    ([301], [1], 2, 8, 128, 16, 128, "half", None),
+    ([5, 17, 64, 33], [1, 1, 1, 1], 3, 3, 64, 16, 64, "half", None),
+    ([100, 7, 40], [64, 7, 1], 5, 10, 128, 32, 64, "interleaved", None),
+    ([200, 131], [131, 90], 1, 4, 64, 64, 48, "half", None),          # a scale's channels in two units
+    ([300], [290], 13, 13, 128, 128, 96, "half", [16, 16, 16]),
+    ([40, 50], [40, 50], 2, 0, 64, 16, 0, "half", None),              # keys as they are
+    ([129], [129], 4, 0, 128, 64, 16, "interleaved", None),
+]
+
+
+@pytest.mark.parametrize("lens,new,H,H_q,d,page,rot,layout,sections", APPEND)
+@pytest.mark.parametrize("apart", [False, True])
+def test_append(lib, lens, new, H, H_q, d, page, rot, layout, sections, apart):
+    c = Pages4(lib, lens, H, d, page, seed=len(lens) + d, apart=apart)
+    before = c.fill(seed=5)
+    g = gen(7)
+    T = sum(new)
+    k, v = randn(g, T, H, d).to(torch.bfloat16), (3 * randn(g, T, H, d)).to(torch.bfloat16)
+    q = randn(g, T, H_q, d).to(torch.bfloat16) if H_q else None
+    table = lib.rotary_table(rot, layout, sections=sections) if rot else None
+    axes = len(sections or [0])
+    pos = torch.randint(0, 5000, (T, axes), generator=g, device="cuda", dtype=torch.int32) if axes > 1 else None
+    cu = i32(*np.concatenate([[0], np.cumsum(new)]))
+    untouched = torch.ones(c.k.shape[0], dtype=torch.bool, device="cuda")
+    for b in range(len(lens)):
+        untouched[c.table[b, :-(-lens[b] // page)].long()] = False
+    spare = [t[untouched].clone() for t in (c.k, c.v, c.ks, c.vs)]
+    out = lib.cast_cache_append(k, v, c.cache, c.table, c.kv_len, cu_new=cu, rotary=table, positions=pos, q=q)
+    lib.cast_check_device()
+    for was, t in zip(spare, (c.k, c.v, c.ks, c.vs)):
+        assert torch.equal(was, t[untouched])
+    at = 0
+    for b, (n, m) in enumerate(zip(lens, new)):
+        rows = slice(at, at + m)
+        p = pos[rows].cpu().numpy() if pos is not None else np.arange(n - m, n)[:, None]
+        x, err = f64(k[rows]), np.zeros((m, H, d))
+        if rot:
+            x, err = R.rotate(x, p, rot, layout, sections=sections)
+        held, scales = c.held("k", b)
+        assert np.array_equal(held[:n - m], before[b][0][:n - m])
+        R4.check_quantised(held[n - m:], scales[n - m:], x, err)
+        held, scales = c.held("v", b)
+        assert np.array_equal(held[:n - m], before[b][1][:n - m])
+        want, code = R4.quantise(f64(v[rows]))       # bf16 values: no rounding before, so to the bit
+        assert np.array_equal(held[n - m:], want) and np.array_equal(scales[n - m:], code)
+        if H_q:
+            x, err = R.rotate(f64(q[rows]), p, rot, layout, sections=sections)
+            assert (np.abs(f64(out[rows]) - x) <= err + R.UBF * (np.abs(x) + err)).all()
+        at += m
+
+
+def test_append_every_scale_and_every_tie(lib):
+    """Values at and around the halfway points of codes, at every scale that a group's largest channel gives; ties of
+    the scale itself; the ends of the range; zeros."""
+    rows = []
+    for e in range(-22, 18):
+        for m in range(128, 256):
+            top = m * 2.0 ** (e - 7)
+            s = float(R4.scale_value(R4.scale_code(np.array([top / 6])))[0])
+            t = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 1.0, 6.0]) * s
+            rows.append(np.concatenate([[top], t * (1 - 2 * (np.arange(9) % 2)), [0, -0.0, -top, top / 2, top / 3, 2.0 ** -19]])[:16])
+    x = torch.tensor(np.array(rows), dtype=torch.float32, device="cuda").to(torch.bfloat16)
+    T = x.shape[0] // 4
+    x = x.reshape(T, 1, 64)
+    c = Pages4(lib, [T], 1, 64, 128)
+    lib.cast_cache_append(x, x, c.cache, c.table, c.kv_len)
+    want, code = R4.quantise(f64(x))
+    for name in "kv":
+        held, scales = c.held(name, 0)
+        assert np.array_equal(scales, code) and np.array_equal(held, want)
+
+
+def test_append_what_is_not_finite_or_too_large(lib):
+    x = torch.ones((4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    x[0, 0, 3], x[1, 0, 20], x[2, 0, 63], x[3, 0, 5] = float("nan"), float("inf"), float("-inf"), 3e38
+    c = Pages4(lib, [4], 1, 64, 16)
+    lib.cast_cache_append(x, x, c.cache, c.table, c.kv_len)
+    held, scales = c.held("k", 0)
+    assert (scales[[0, 1, 2], 0, [0, 1, 3]] == R4.NAN_SCALE).all() and scales[3, 0, 0] == 0xe2
+    want = np.ones((4, 64)) * 1.0
+    one = R4.quantise(np.ones((1, 16)))[0][0, 0]
+    want[:] = one
+    want[0, :16], want[1, 16:32], want[2, 48:] = np.nan, np.nan, np.nan
+    want[3, :16] = 0
+    want[3, 5] = 61440
+    assert np.array_equal(held[:, 0], want, equal_nan=True)
+
+
+# ------------------------------------------------------------------------------------ reading back
+READ = [
+    # lens, rows, H, d, page
+    ([301], [301], 2, 128, 16),
+    ([5, 17, 64, 33], [1, 17, 3, 30], 3, 64, 16),
+    ([700, 7, 411], [650, 0, 333], 5, 128, 32),
+    ([2000, 131], [1999, 90], 1, 64, 64),
+    ([300, 1], [290, 1], 13, 128, 128),
+]
+
+
+@pytest.mark.parametrize("lens,new,H,d,page", READ)
+@pytest.mark.parametrize("kind", ["f4", "f8", "bf16"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_read(lib, lens, new, H, d, page, kind, dtype):
+    g = gen(len(lens) * 3 + d)
+    c = Pages4(lib, lens, H, d, page, seed=3, apart=True)
+    cache = c.cache
+    if kind == "f4":
+        want = c.fill(seed=9)
+    else:
+        n = c.k.shape[0]
+        k, v = randn(g, n, page, H, d), randn(g, n, page, H, d)
+        ks = vs = None
+        if kind == "f8":
+            k, v = (100 * k).to(torch.float8_e4m3fn), (100 * v).to(torch.float8_e4m3fn)
+            ks, vs = (torch.exp2(torch.randint(-20, 8, (n, H), generator=g, device="cuda").float()) for _ in range(2))
+        else:
+            k, v = k.to(torch.bfloat16), v.to(torch.bfloat16)
+        cache = lib.kv_cache(k, v, ks, vs)
+        want = []
+        for b, m in enumerate(lens):
+            p = c.table[b, :-(-m // page)].long()
+            one = lambda x, s: ((x.view(torch.uint8)[p].view(x.dtype) if s is not None else x[p]).double() *
+                                (s[p].double()[:, None, :, None] if s is not None else 1)).reshape(-1, H, d)[:m].cpu().numpy()
+            want.append((one(k, ks), one(v, vs)))
+    cu = i32(*np.concatenate([[0], np.cumsum(new)]))
+    T = sum(new)
+    room = torch.full((T + 3, 2, H, d), 7.0, dtype=dtype, device="cuda")
+    ko, vo = lib.cast_cache_read(cache, c.table, c.kv_len, T + 3, cu_new=cu, dtype=dtype, v_out=room[:, 1])
+    lib.cast_check_device()
+    assert vo.data_ptr() == room[:, 1].data_ptr() and (room[:, 0] == 7).all() and (room[T:] == 7).all()
+    at = 0
+    for b, m in enumerate(new):
+        for got, ref in ((ko, want[b][0]), (vo, want[b][1])):
+            assert np.array_equal(f64(got[at:at + m]), ref[lens[b] - m:], equal_nan=True)   # (a code may be NaN)
+        at += m
+    only, none = lib.cast_cache_read(cache, c.table, c.kv_len, T, cu_new=cu, dtype=dtype, values=False)
+    assert none is None and torch.equal(only.nan_to_num(3.0), ko[:T].nan_to_num(3.0))
+    none, only = lib.cast_cache_read(cache, c.table, c.kv_len, T, cu_new=cu, dtype=dtype, keys=False)
+    assert none is None and torch.equal(only.nan_to_num(3.0), vo[:T].nan_to_num(3.0))
+
+
+def test_read_what_is_not_there(lib):
+    """Positions below 0 and pages out of range read as zeros; rows past max_new are left as they were."""
+    c = Pages4(lib, [40], 2, 64, 16)
+    c.fill()
+    k, v = lib.cast_cache_read(c.cache, c.table, i32(5), 9)
+    lib.cast_check_device()
+    assert (k[:4] == 0).all() and (v[:4] == 0).all() and (k[4:] != 0).any()
+    table = c.table.clone()
+    table[0, 1] = 99
+    k, v = lib.cast_cache_read(c.cache, table, c.kv_len, 40)
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+    assert (k[16:32] == 0).all() and (v[16:32] == 0).all() and (k[32:] != 0).any()
+    k, _ = lib.cast_cache_read(c.cache, c.table[:, :1], c.kv_len, 40)
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+    assert (k[16:] == 0).all() and (k[:16] != 0).any()
+    out = torch.full((40, 2, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    lib.cast_cache_read(c.cache, c.table, c.kv_len, 40, cu_new=i32(0, 40), max_new=7, k_out=out, values=False)
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+    assert (out[7:] == 5).all()
+    assert lib.cast_cache_read(c.cache, c.table, c.kv_len, 0)[0].shape == (0, 2, 64)
+
+
+def test_read_shows_nan_groups(lib):
+    c = Pages4(lib, [3], 1, 64, 16)
+    c.fill()
+    page = int(c.table[0, 0])
+    c.vs[page, 0, 1, 2] = R4.NAN_SCALE
+    k, v = lib.cast_cache_read(c.cache, c.table, c.kv_len, 3, dtype=torch.float32)
+    bad = torch.isnan(v)
+    assert not torch.isnan(k).any() and bad[1, 0, 32:48].all() and int(bad.sum()) == 16
+
+
+def test_read_gives_blocks_that_route(lib):
+    """The pages of a 4-bit history as the blocks that the routing takes: the same choice as from the values."""
+    M, Bv, H, d = 6, 64, 2, 64
+    c = Pages4(lib, [M * Bv], H, d, 16)
+    (kq, vq), = c.fill(seed=21)
+    k, v = lib.cast_cache_read(c.cache, c.table, c.kv_len, M * Bv)
+    q = randn(gen(2), 2, 64, H, d).to(torch.bfloat16)
+    want = [torch.from_numpy(x).cuda().to(torch.bfloat16).view(M, Bv, H, d) for x in (kq, vq)]
+    a = lib.cast_route_topk(q, [0, 1], k.view(M, Bv, H, d), v.view(M, Bv, H, d), 3)
+    b = lib.cast_route_topk(q, [0, 1], *want, 3)
+    first = lambda x: x[0] if isinstance(x, tuple) else x
+    assert torch.equal(first(a), first(b))
