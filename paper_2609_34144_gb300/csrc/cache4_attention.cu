@@ -1,0 +1,440 @@
+// Attention over 4-bit pages for few rows a sequence (single tokens, drafts): k_cache_rows4.  Units, shares of the
+// work and the joining are those of k_cache_rows (cache_attention.cu); inside a CTA each warp works on its own blocks
+// of 16 tokens with its own running maximum, sum and o in registers.
+//
+// The codes become f16 in registers (a conversion and a product with the scale for two, both exact), so the issue of
+// instructions is what bounds the kernel beside memory, and everything follows from it:
+// - Tokens are the products' first operand: S^T = K Q^T and o^T += V^T P^T as m16n8k16, 16 tokens (channels) by 8 rows,
+//   half of the products and of the exponentials that 16 rows would take.  P^T comes from S^T by a transposition of
+//   8x8 tiles of f16 (movmatrix).
+// - The channels' order inside S's sum is free: a lane takes a quarter of a token's row, one or two scales, as one
+//   load.  So is the order of o's channels: a lane has D / 8 of them, one scale, for all of its tokens.  The order of
+//   tokens inside the products is chosen so that these loads meet few bank conflicts (token_of).
+// - V's products want two tokens of one channel side by side: the halves of two words are exchanged while they are
+//   codes (six instructions for 16 values).
+// A query is f16 times a power of two (its largest channel below 2^15), a probability f16 lifted by 2^7.
+//
+// Hidden tokens of a block that the rows do not all see: logits become -inf; their V scales, the only thing that can
+// make a value not finite, become 0, and tokens whose scales are not finite are added one by one where they are seen.
+// A page out of range is scales of 0.
+#include <cmath>
+
+#include "cache.cuh"
+#include "cache_attention.cuh"
+#include "cache_rows.cuh"
+#include "ptx.cuh"
+
+namespace cast {
+namespace {
+
+// NT: units of 8 NT rows
+template <int D, int NT>
+struct Cfg4 {
+  static constexpr int ROWS = 8 * NT;
+  static constexpr int ROWB = D / 2, SROWB = D / 16;      // bytes of a token's codes and scales
+  static constexpr int BLOCK = 16 * ROWB, SBLOCK = 16 * SROWB;
+  static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
+  static constexpr int CTAS = D * NT <= 128 ? 4 : 3;      // of an SM
+  static constexpr int ROOM = (CTAS == 4 ? 13 : 17) * 1024;   // a warp's ring at most
+  static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
+  static constexpr int RING = STAGES * STAGE;
+  static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
+  static constexpr int SMEM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
+  static_assert(STAGES >= 4 && SMEM <= 72 * 1024, "CTAs of an SM");
+};
+
+// The block's token that lane group g's row of a product is (and token + 8 that row g + 8 is): token 4 j + (q ^ j) for
+// row 2 q + j, so that neither the eight lanes that load K together nor those of V meet more than two to a bank.
+__device__ __forceinline__ int token_of(int row) { return 4 * (row & 1) + ((row >> 1) ^ (row & 1)); }
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Whether any of four scale bytes gives values that may not be finite
+__device__ __forceinline__ bool odd_scale(uint32_t code) { return code > kScaleTop; }
+__device__ __forceinline__ float value4(uint32_t code, uint32_t scale) {
+  const uint32_t m = code & 7u;
+  const float v = m < 2 ? 0.5f * m : (float)(2u + (m & 1u)) * pow2f((int)(m >> 1) - 2);
+  return __half2float(__float2half_rn((code & 8u ? -v : v) * scale4_value(scale)));
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
+  using C = Cfg4<D, NT>;
+  constexpr int KW = D / 32;   // words of a lane's part of a K row; a V row's part has D / 64
+  constexpr int VW = D / 64;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, q4 = lane & 3;
+  const Share mine = share_of<D, C::ROWS>(a);
+  int entry = mine.entry;
+  int64_t at = mine.at, entry_at = mine.entry_at;
+  const int64_t stop = mine.stop;
+  if (at >= stop) return;
+
+  uint8_t* ring = smem + warp * C::RING;
+  const uint32_t ring_at = smem_u32(ring);
+  const int kt0 = token_of(g);                       // this lane's K tokens: kt0 and kt0 + 8
+  const int vt0 = q4, vt1 = 4 + (q4 ^ 1);            // ... and V tokens: these, and 8 further on
+  const int64_t page_bytes = (int64_t)a.page_size * a.row_stride / 2;
+  const uint8_t* kscale = reinterpret_cast<const uint8_t*>(a.k_scale);
+  const uint8_t* vscale = reinterpret_cast<const uint8_t*>(a.v_scale);
+
+  for (; at < stop; ++entry) {
+    const int b = entry / a.row_tiles, tile = entry % a.row_tiles;
+    const Span z = span_of(a, b, tile, C::ROWS);
+    const int nb = z.blocks();
+    const int* table = a.batch.page_table + (int64_t)b * a.batch.page_table_stride;
+    for (int h = nb ? (int)((at - entry_at) / nb) : a.H; h < a.H && at < stop; ++h) {
+      // blocks k0 .. k1-1 of unit (b, tile, h)
+      const int64_t unit_at = entry_at + (int64_t)h * nb;
+      const int k0 = (int)(at - unit_at);
+      const int k1 = (int)min((int64_t)nb, stop - unit_at);
+
+      // fetches block i of the unit into stage st
+      auto page_of = [&](int i) {
+        int p = __ldg(table + ((z.block(i) * 16) >> a.page_shift));
+        if (p < 0 || p >= a.n_pages) {
+          if (lane == 0) left_out();
+          p = -1;
+        }
+        return p;
+      };
+      auto fetch = [&](int i, int st, int page) {
+        const int row = (z.block(i) * 16) & (a.page_size - 1);
+        const uint32_t dst = ring_at + st * C::STAGE;
+        if (page >= 0) {
+          const int64_t from = page * page_bytes + (int64_t)(h * a.page_size + row) * C::ROWB + lane * 16;
+#pragma unroll
+          for (int c = 0; c < C::BLOCK; c += 512) {
+            copy16(dst + c + lane * 16, a.k + from + c);
+            copy16(dst + C::BLOCK + c + lane * 16, a.v + from + c);
+          }
+        }
+        if (lane < 2 * C::SBLOCK / 16) {
+          const bool is_v = lane >= C::SBLOCK / 16;
+          const int64_t from = (((int64_t)max(page, 0) * a.H + h) * a.page_size + row) * C::SROWB + (lane & (C::SBLOCK / 16 - 1)) * 16;
+          copy16_or_zero(dst + 2 * C::BLOCK + lane * 16, (is_v ? vscale : kscale) + from, page >= 0);
+        }
+      };
+      const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
+      const int i0 = k0 + warp;
+      __syncwarp();
+      for (int st = 0; st < C::STAGES - 1; ++st) {
+        if (st < n) fetch(i0 + st * kWarps, st, page_of(i0 + st * kWarps));
+        copy_commit();
+      }
+      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * kWarps) : -1;
+
+      // Q^T fragments: row g of each 8 (product s takes channels (D / 4) q4 + 4 s .. + 3 of lane group q4)
+      uint32_t qf[NT][D / 16][2];
+      float unit[NT][2];   // what the logits of rows 2 q4 and 2 q4 + 1 are multiplied by
+      int pos[NT][2];      // their positions
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int r = tile * C::ROWS + t * 8 + g;
+        const bool in = r < z.n_rows;
+        const int i = r / a.group;
+        const __nv_bfloat16* src =
+            a.q + (int64_t)(z.t0 + (in ? i : 0)) * a.q_stride + (h * a.group + (in ? r - i * a.group : 0)) * D + q4 * (D / 4);
+        uint32_t top = 0;   // magnitudes order as their bits
+#pragma unroll
+        for (int s = 0; s < D / 16; s += 2) {
+          const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + s * 4));
+          qf[t][s][0] = in ? w.x : 0u;
+          qf[t][s][1] = in ? w.y : 0u;
+          qf[t][s + 1][0] = in ? w.z : 0u;
+          qf[t][s + 1][1] = in ? w.w : 0u;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = qf[t][s + (e >> 1)][e & 1];
+            top = max(top, max(x & 0x7fff0000u, (x << 16) & 0x7fff0000u));
+          }
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^-e with the largest channel in [2^14, 2^15); subnormal, zero and infinite rows as they are
+        const int e = (int)(top >> 23) - 127 - 14;
+        const bool plain = e < -126 || e > 112;
+        const float down = plain ? 1.f : pow2f(-e), up = a.scale_log2 * (plain ? 1.f : pow2f(e));
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t w = qf[t][s][j];
+            qf[t][s][j] = pack2h(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
+          }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          unit[t][j] = __shfl_sync(0xffffffffu, up, (2 * q4 + j) * 4);
+          const int rr = tile * C::ROWS + t * 8 + 2 * q4 + j;
+          pos[t][j] = rr < z.n_rows ? z.p0 + rr / a.group : -1;
+        }
+      }
+      // positions that every row sees: [all_lo, all_hi); the others' blocks are masked
+      int all_lo = 0, all_hi = z.hi;
+      {
+        const int r1 = min(tile * C::ROWS + C::ROWS, z.n_rows) - 1;
+        if (a.causal) all_hi = min(z.hi, max(z.p0 + tile * C::ROWS / a.group + 1, 0));
+        if (a.window > 0) all_lo = max(z.p0 + r1 / a.group - a.window + 1, 0);
+      }
+      auto sees = [&](int p, int r) { return p < z.hi && (!a.causal || p <= r) && (a.window <= 0 || p > r - a.window || p < a.sinks); };
+
+      float o[NT][D / 16][4], m_ref[NT][2], l[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][i][e] = 0.f;
+        m_ref[t][0] = m_ref[t][1] = -INFINITY;
+        l[t][0] = l[t][1] = 0.f;
+      }
+
+      int st = 0, into = C::STAGES - 1;
+      for (int it = 0; it < n; ++it) {
+        copy_wait<C::STAGES - 2>();
+        __syncwarp();
+        // the stage used one block ago takes the block STAGES - 1 ahead
+        const int ahead = it + C::STAGES - 1;
+        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_page);
+        copy_commit();
+        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * kWarps);
+        const uint8_t* kt = ring + st * C::STAGE;
+        const uint8_t* vt = kt + C::BLOCK;
+        const uint8_t* ks = kt + 2 * C::BLOCK;
+        const uint8_t* vs = ks + C::SBLOCK;
+
+        // ---- S^T = K Q^T
+        float s[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+        {
+          uint32_t kw[2][KW], sc[2][2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint8_t* p = kt + (kt0 + 8 * j) * C::ROWB + q4 * (D / 8);
+            if constexpr (D == 128) {
+              const uint4 w = *reinterpret_cast<const uint4*>(p);
+              kw[j][0] = w.x; kw[j][1] = w.y; kw[j][2] = w.z; kw[j][3] = w.w;
+              const uint32_t two = *reinterpret_cast<const uint16_t*>(ks + (kt0 + 8 * j) * C::SROWB + q4 * 2);
+              sc[j][0] = scale4_pair(two);
+              sc[j][1] = __byte_perm(two, 0, 0x4141) << 7;
+            } else {
+              const uint2 w = *reinterpret_cast<const uint2*>(p);
+              kw[j][0] = w.x; kw[j][1] = w.y;
+              sc[j][0] = scale4_pair(ks[(kt0 + 8 * j) * C::SROWB + q4]);
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < KW; ++w) {
+            uint32_t x[4], y[4];
+            half8(kw[0][w], x);
+            half8(kw[1][w], y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[e] = times2(x[e], sc[0][w / 2]);
+              y[e] = times2(y[e], sc[1][w / 2]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t f[4] = {x[2 * u], y[2 * u], x[2 * u + 1], y[2 * u + 1]};
+#pragma unroll
+              for (int t = 0; t < NT; ++t) mma16816h(s[t], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
+            }
+          }
+        }
+
+        const int base = z.block(i0 + it * kWarps) * 16;
+        const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
+        // V's codes and scales, before the exponentials wait for S
+        uint32_t vw[4][VW], vc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int token = (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+          const uint8_t* p = vt + token * C::ROWB + g * (D / 16);
+          if constexpr (D == 128) {
+            const uint2 w = *reinterpret_cast<const uint2*>(p);
+            vw[j][0] = w.x;
+            vw[j][1] = w.y;
+            vc[j] = vs[token * C::SROWB + g];
+          } else {
+            vw[j][0] = *reinterpret_cast<const uint32_t*>(p);
+            vc[j] = vs[token * C::SROWB + (g >> 1)];
+          }
+        }
+        bool apart = false;
+        if (!whole) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[t][e] = sees(base + kt0 + (e & 2 ? 8 : 0), pos[t][e & 1]) ? s[t][e] * unit[t][e & 1] : -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int p = base + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+            if (!(p < z.hi && (p >= z.lo || p < z.sinks))) vc[j] = 0;   // nobody's
+            apart |= odd_scale(vc[j]);
+          }
+          apart = __any_sync(0xffffffffu, apart);
+        }
+
+        // ---- running maximum; what is left of a logit's factor
+        float times[NT][2], top[NT][2];
+        bool grows = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            times[t][j] = whole ? unit[t][j] : 1.f;
+            top[t][j] = fmaxf(s[t][j], s[t][2 + j]) * times[t][j];
+            grows = grows || top[t][j] > m_ref[t][j] + kRescale;
+          }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              float x = top[t][j];
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+              if (x > m_ref[t][j]) {
+                const float f = exp2_fast(m_ref[t][j] - x);
+                m_ref[t][j] = x;
+                l[t][j] *= f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                  o[t][i][j] *= f;
+                  o[t][i][2 + j] *= f;
+                }
+              }
+            }
+        }
+        // ---- P^T, 2^kLift times the probabilities; l is the sum of them as they are before the rounding
+        uint32_t pf[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            // a row that has seen nothing yet: exp2(-inf - 0) = 0
+            const float ref = kLift - (m_ref[t][j] == -INFINITY ? 0.f : m_ref[t][j]);
+            s[t][j] = exp2_fast(fmaf(s[t][j], times[t][j], ref));
+            s[t][2 + j] = exp2_fast(fmaf(s[t][2 + j], times[t][j], ref));
+            l[t][j] += s[t][j] + s[t][2 + j];
+          }
+          pf[t][0] = transposed(pack2h(s[t][0], s[t][1]));
+          pf[t][1] = transposed(pack2h(s[t][2], s[t][3]));
+        }
+
+        // ---- o^T += V^T P^T
+        if (apart) {
+          // tokens one by one, where they are seen: P's column of a token is in the lanes that have it as a K token
+#pragma unroll 1
+          for (int token = 0; token < 16; ++token) {
+            // the lane group whose K token this is: row 2 q + j of token 4 j + (q ^ j)
+            const int k = token & 7, from = (2 * ((k & 3) ^ (k >> 2)) + (k >> 2)) * 4 + q4;
+            const int p = base + token;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) {
+                const float w0 = __shfl_sync(0xffffffffu, s[t][j], from), w1 = __shfl_sync(0xffffffffu, s[t][2 + j], from);
+                if (!sees(p, pos[t][j])) continue;
+                const float w = token < 8 ? w0 : w1;
+                const uint32_t scale = vs[token * C::SROWB + (D == 128 ? g : g >> 1)];
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                  const uint32_t two = vt[token * C::ROWB + g * (D / 16) + i];
+                  o[t][i][j] += w * value4(two, scale);
+                  o[t][i][2 + j] += w * value4(two >> 4, scale);
+                }
+              }
+          }
+        } else {
+          const uint32_t s0 = scale4_pair(vc[0], vc[1]), s1 = scale4_pair(vc[2], vc[3]);
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            constexpr uint32_t low = 0x0f0f0f0fu;
+            // bytes of two tokens' codes of one channel: channels 0 2 4 6, and 1 3 5 7, of the word's eight
+            uint32_t x[4], y[4], u[4], v[4];
+            half8((vw[0][w] & low) | ((vw[1][w] << 4) & ~low), x);
+            half8(((vw[0][w] >> 4) & low) | (vw[1][w] & ~low), y);
+            half8((vw[2][w] & low) | ((vw[3][w] << 4) & ~low), u);
+            half8(((vw[2][w] >> 4) & low) | (vw[3][w] & ~low), v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t f[4] = {times2(x[e], s0), times2(y[e], s0), times2(u[e], s1), times2(v[e], s1)};
+#pragma unroll
+              for (int t = 0; t < NT; ++t) mma16816h(o[t][4 * w + e], f, pf[t][0], pf[t][1]);
+            }
+          }
+        }
+        __syncwarp();
+        into = st;
+        st = st + 1 == C::STAGES ? 0 : st + 1;
+      }
+      copy_wait<0>();
+      __syncthreads();   // every warp is done with its ring: the merge takes the space
+
+      float* mo = reinterpret_cast<float*>(smem);                        // [warp][row][D]
+      float2* ml = reinterpret_cast<float2*>(mo + kWarps * C::ROWS * D); // [warp][row]
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float x = l[t][j];
+          x += __shfl_xor_sync(0xffffffffu, x, 4);
+          x += __shfl_xor_sync(0xffffffffu, x, 8);
+          x += __shfl_xor_sync(0xffffffffu, x, 16);
+          const int r = t * 8 + 2 * q4 + j;
+          if (g == 0) ml[warp * C::ROWS + r] = make_float2(m_ref[t][j], x * 0x1p-7f);
+          float* dst = mo + (warp * C::ROWS + r) * D + g * (D / 8);
+#pragma unroll
+          for (int i = 0; i < D / 16; i += 2)
+            *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(o[t][i][j] * 0x1p-7f, o[t][i][2 + j] * 0x1p-7f,
+                                                                  o[t][i + 1][j] * 0x1p-7f, o[t][i + 1][2 + j] * 0x1p-7f);
+        }
+      __syncthreads();
+      // a share that begins inside the unit leaves its part in the CTA's first place
+      join_warps<D, C::ROWS>(a, z, h, tile, k0 == 0 && k1 == nb, 2 * blockIdx.x + (k0 > 0 ? 0 : 1), mo, ml);
+      __syncthreads();   // the space goes back to the rings
+      at = unit_at + k1;
+    }
+    entry_at += (int64_t)nb * a.H;
+  }
+}
+
+template <int D, int NT>
+cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
+  using C = Cfg4<D, NT>;
+  static std::atomic<uint64_t> attr_done{0};
+  if (!once_per_device(attr_done, [&] {
+        return cudaFuncSetAttribute(k_cache_rows4<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
+      }))
+    return check_launch("cache attention smem attribute");
+  k_cache_rows4<D, NT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
+  cast_status s = check_launch("cache attention");
+  if (s || p.whole) return s;
+  return launch_merge<D, C::ROWS>(k, p.grid, st);
+}
+
+}  // namespace
+
+int rows4_ctas(int d, int mt) {
+  if (d == 128) return mt == 1 ? Cfg4<128, 1>::CTAS : Cfg4<128, 2>::CTAS;
+  return mt == 1 ? Cfg4<64, 1>::CTAS : mt == 2 ? Cfg4<64, 2>::CTAS : Cfg4<64, 4>::CTAS;
+}
+
+cast_status launch_rows4(const RowsKArgs& k, const RowsPlan& p, int d, cudaStream_t st) {
+  if (d == 128) return p.mt == 1 ? launch<128, 1>(k, p, st) : launch<128, 2>(k, p, st);
+  return p.mt == 1 ? launch<64, 1>(k, p, st) : p.mt == 2 ? launch<64, 2>(k, p, st) : launch<64, 4>(k, p, st);
+}
+
+unsigned int cache_rows4_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }
+
+}  // namespace cast

@@ -635,7 +635,7 @@ cast_status cast_check_device(void* stream) {
   const unsigned int wr = route_error_word(st, true);
   const unsigned int wd = dense_error_word(st, true);
   const unsigned int wc = cache_error_word(st, true) | cache_read_error_word(st, true) | cache_rows_error_word(st, true) |
-                          cache_tiles_error_word(st, true);
+                          cache_rows4_error_word(st, true) | cache_tiles_error_word(st, true);
   const unsigned int wt = tiles_error_word(st, true);
   if (wa == 1u || wp || wd || wt || wr == 2u) return fail(CAST_ERR_DEVICE_TIMEOUT, "a kernel gave up on a bounded wait");
   if (wa == 2u) return fail(CAST_ERR_INVALID_ARG, "attention: a routed block index was outside [0, M)");

@@ -153,6 +153,7 @@ cast_status check_rows(const void* p, int64_t stride, int64_t least, const char*
 unsigned int cache_error_word(cudaStream_t st, bool clear);
 unsigned int cache_read_error_word(cudaStream_t st, bool clear);
 unsigned int cache_rows_error_word(cudaStream_t st, bool clear);
+unsigned int cache_rows4_error_word(cudaStream_t st, bool clear);
 unsigned int cache_tiles_error_word(cudaStream_t st, bool clear);
 // Nonzero when the cache attention gave up on a bounded wait.
 unsigned int tiles_error_word(cudaStream_t st, bool clear);

@@ -62,3 +62,38 @@ def check_quantised(values, scales, x, err):
     lo, hi = nearest((g - e) / d * np.where(g > e, 1 - u, 1 + u)) * s, nearest((g + e) / d * np.where(g < -e, 1 - u, 1 + u)) * s
     v = values.reshape(g.shape)
     assert (np.minimum(lo, hi) <= v).all() and (v <= np.maximum(lo, hi)).all()
+
+
+def attention(q, k, v, length, causal=True, window=0, sinks=0, scale=None):
+    """One sequence: q [n, H_q, d], k, v [length, H, d] f64 -> (o, lse, bound of o before its rounding, bound of lse)."""
+    U32 = 2.0 ** -24
+    n, Hq, d = q.shape
+    H = k.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    p, j = length - n + np.arange(n)[:, None], np.arange(length)[None, :]
+    see = np.ones((n, length), bool)
+    if causal:
+        see &= j <= p
+    if window > 0:
+        see &= (j > p - window) | (j < sinks)
+    see &= p >= 0 if causal else True
+    o, eo = np.zeros((n, Hq, d)), np.zeros((n, Hq, d))
+    lse, el = np.full((n, Hq), -np.inf), np.zeros((n, Hq))
+    seen = see.any(0)[:, None]
+    for h in range(Hq):
+        kk, vv = np.where(seen, k[:, h // (Hq // H)], 0), np.where(seen, v[:, h // (Hq // H)], 0)
+        x = np.where(see, q[:, h] @ kk.T * scale, -np.inf)
+        size = np.where(see, np.abs(q[:, h]) @ np.abs(kk).T * abs(scale), 0)
+        top = x.max(1, initial=-np.inf, keepdims=True)
+        w = np.where(see, np.exp(x - np.where(np.isfinite(top), top, 0)), 0)
+        s = w.sum(1, keepdims=True)
+        some = s[:, 0] > 0
+        prob = np.divide(w, s, out=np.zeros_like(w), where=s > 0)
+        o[:, h] = prob @ vv
+        lse[some, h] = (top + np.log(np.where(s > 0, s, 1)))[some, 0]
+        # a logit is off by at most (d + 8) u32 of its absolute sum (an f32 sum in any order) and by the scale's and the
+        # exponent's rounding; a probability is an f16 number: 2^-11 of itself, or 2^-32 of the row's largest
+        logit = (d + 8) * U32 * size.max(1, initial=0) + 4 * U32 * np.abs(np.where(see, x, 0)).max(1, initial=0)
+        eo[:, h] = (2.0 ** -11 + 2 * logit[:, None] + length * U32 + 2.0 ** -20) * (prob @ np.abs(vv)) + 2.0 ** -32 * (see @ np.abs(vv))
+        el[:, h] = logit + length * U32 + 2.0 ** -20 * (1 + np.abs(np.where(some, lse[:, h], 0)))
+    return o, lse, eo, el

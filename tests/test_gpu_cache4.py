@@ -272,3 +272,55 @@ def test_read_gives_blocks_that_route(lib):
     b = lib.cast_route_topk(q, [0, 1], *want, 3)
     first = lambda x: x[0] if isinstance(x, tuple) else x
     assert torch.equal(first(a), first(b))
+
+
+# ------------------------------------------------------------------------------------ attention
+def check_attention(lib, c, held, q, new, out, lse, only=None, **kw):
+    at = 0
+    for b, m in enumerate(new):
+        if m == 0:
+            continue
+        rows = slice(at, at + m)
+        o, want, eo, el = R4.attention(f64(q[rows]), *held[b], c.lens[b], **kw)
+        got = f64(out[rows]).reshape(o.shape)
+        tol = eo + (R.UBF * (np.abs(o) + eo) if out.dtype == torch.bfloat16 else R.U32 * np.abs(o))
+        bad = ~(np.abs(got - o) <= tol)
+        assert not bad.any(), f"sequence {b}: {bad.sum()} of {bad.size} outside, worst {np.nanmax(np.abs(got - o) / np.maximum(tol, 1e-300)):.3g} x"
+        if lse is not None:
+            x = lse[rows].cpu().numpy().astype(np.float64)
+            assert np.array_equal(np.isinf(x), np.isinf(want))
+            f = np.isfinite(want)
+            assert (np.abs(x - want)[f] <= el[f]).all()
+        at += m
+
+
+ROWS = [
+    # lens, new, H, H_q, d, page, causal, window, sinks
+    ([1], [1], 1, 1, 64, 16, True, 0, 0),
+    ([301], [1], 2, 8, 64, 16, True, 0, 0),
+    ([301, 17, 1, 1500], [1, 1, 1, 1], 3, 12, 128, 16, True, 0, 0),
+    ([3000, 2500, 777], [1, 1, 1], 8, 32, 128, 64, True, 0, 0),           # shares cut anywhere
+    ([3000, 2500, 777], [1, 1, 1], 2, 30, 64, 128, True, 0, 0),           # 15 rows
+    ([2050, 90], [4, 3], 5, 10, 128, 32, True, 0, 0),                     # drafts: 8 rows
+    ([2050, 90], [7, 1], 5, 10, 128, 32, False, 0, 0),                    # 14 rows, ragged
+    ([4000, 1500, 2], [1, 1, 1], 4, 16, 128, 16, True, 1024, 40),
+    ([4000, 1500, 31], [2, 1, 2], 3, 15, 64, 16, True, 333, 5),
+    ([900, 1000], [5, 5], 40, 120, 64, 32, True, 0, 0),                   # 15 rows
+    ([700] * 33, [1] * 33, 2, 2, 64, 16, False, 100, 0),
+    ([500, 400], [8, 8], 33, 99, 64, 16, True, 0, 0),                     # 24 rows, 66 units
+    ([1300, 400], [8, 3], 33, 132, 64, 64, True, 200, 17),                # 32 rows
+]
+
+
+@pytest.mark.parametrize("lens,new,H,H_q,d,page,causal,window,sinks", ROWS)
+def test_attention_few_rows(lib, lens, new, H, H_q, d, page, causal, window, sinks):
+    c = Pages4(lib, lens, H, d, page, seed=H, apart=d == 128)
+    held = c.fill(seed=H + d)
+    q = (1.5 * randn(gen(d), sum(new), H_q, d)).to(torch.bfloat16)
+    cu = i32(*np.concatenate([[0], np.cumsum(new)])) if len(set(new)) > 1 else None
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=cu, max_new=max(new), want_lse=True, **kw)
+    lib.cast_check_device()
+    check_attention(lib, c, held, q, new, o, lse, **kw)
+    o32 = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=cu, max_new=max(new), out_dtype=torch.float32, **kw)
+    check_attention(lib, c, held, q, new, o32, None, **kw)
