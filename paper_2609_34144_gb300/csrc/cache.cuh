@@ -159,6 +159,12 @@ __device__ __forceinline__ uint32_t scale4_code(uint32_t top) {
 __device__ __forceinline__ float scale4_value(uint32_t code) {
   return __half2float(__ushort_as_half((unsigned short)(code << 7)));
 }
+// What the lowest four bits of `code` stand for with a scale, in f16 as pairs of them are formed
+__device__ __forceinline__ float value4(uint32_t code, uint32_t scale) {
+  const uint32_t m = code & 7u;
+  const float v = m < 2 ? 0.5f * m : (float)(2u + (m & 1u)) * pow2f((int)(m >> 1) - 2);
+  return __half2float(__float2half_rn((code & 8u ? -v : v) * scale4_value(scale)));
+}
 // x / s for a scale s and r = 1 / s rounded: x r corrected once by its remainder, which is exact (Markstein's
 // correction).  Where the quotient is half way between two codes it comes out exactly: it differs from x r by 2^-23
 // of itself at most, the correction is good to 2^-47, and the halfway points have three bits.

@@ -54,12 +54,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 }
 // Whether any of four scale bytes gives values that may not be finite
 __device__ __forceinline__ bool odd_scale(uint32_t code) { return code > kScaleTop; }
-__device__ __forceinline__ float value4(uint32_t code, uint32_t scale) {
-  const uint32_t m = code & 7u;
-  const float v = m < 2 ? 0.5f * m : (float)(2u + (m & 1u)) * pow2f((int)(m >> 1) - 2);
-  return __half2float(__float2half_rn((code & 8u ? -v : v) * scale4_value(scale)));
-}
-
 template <int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
   using C = Cfg4<D, NT>;
@@ -157,7 +151,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // 2^-e with the largest channel in [2^14, 2^15); subnormal, zero and infinite rows as they are
         const int e = (int)(top >> 23) - 127 - 14;
-        const bool plain = e < -126 || e > 112;
+        const bool plain = e < -126 || e > 113;
         const float down = plain ? 1.f : pow2f(-e), up = a.scale_log2 * (plain ? 1.f : pow2f(e));
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)

@@ -654,7 +654,6 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   if (s) return s;
   if (a->batch.T == 0) return CAST_OK;
   const bool tiles = by_tiles(*a);
-  if (tiles && a->cache.dtype == CAST_F4E2M1) return fail(CAST_ERR_UNSUPPORTED, "%s: %d new tokens on 4-bit pages", who, a->batch.max_new);
   const TilesPlan tp = tiles ? tiles_plan(*a) : TilesPlan{};
   const RowsPlan p = tiles ? RowsPlan{} : rows_plan(*a);
   const size_t need = tiles ? tp.total_bytes : p.total_bytes;

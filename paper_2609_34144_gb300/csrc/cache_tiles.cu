@@ -60,26 +60,34 @@ constexpr int BM = 128, BN = 128, kStages = 2;
 constexpr float kLift = 7.f;
 constexpr int kTmemCols = 512;   // S0/P0 at 0, S1/P1 at 128, O0 at 256, O1 at 384
 
-template <int HD, bool F8>
+// KIND: the pages' type
+template <int HD, int KIND>
 struct Cfg {
-  static constexpr int THREADS = F8 ? 512 : 384;
+  static constexpr bool F8 = KIND == CAST_F8E4M3, F4 = KIND == CAST_F4E2M1, DECODED = F8 || F4;
+  static constexpr int THREADS = DECODED ? 512 : 384;
   // registers a thread at launch, and after the hand-over: control warps, softmax, decoders
-  static constexpr int LAUNCH = F8 ? 128 : 168;
-  static constexpr int REGS_CTL = F8 ? 72 : 96;
-  static constexpr int REGS_SOFTMAX = F8 ? 184 : 200;
+  static constexpr int LAUNCH = DECODED ? 128 : 168;
+  static constexpr int REGS_CTL = DECODED ? 72 : 96;
+  static constexpr int REGS_SOFTMAX = DECODED ? 184 : 200;
   static constexpr int REGS_DECODE = 72;
-  static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (F8 ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
+  static_assert(128 * REGS_CTL + 256 * REGS_SOFTMAX + (DECODED ? 128 * REGS_DECODE : 0) <= THREADS * LAUNCH,
                 "register split exceeds the launch allocation");
   static constexpr int Q_BYTES = BM * HD * 2;               // 8 bits: two pieces of BM * HD
   static constexpr int K_BYTES = BN * HD * (F8 ? 1 : 2);
   static constexpr int V_BYTES = BN * HD * 2;
-  static constexpr int RAW_BYTES = F8 ? BN * HD : 0;
+  // codes on their way: V's (8 bits), or K's and V's with their scales (4 bits).  In the place of a second query
+  // tile that a unit does not have lie as many stages again (4 bits, heads of 64: there is room for all of them)
+  static constexpr int CODE_BYTES = BN * HD / 2;   // 4 bits
+  static constexpr int RAW_BYTES = F8 ? BN * HD : F4 ? CODE_BYTES + BN * HD / 16 : 0;
+  static constexpr int RAW_STAGES = F4 ? (HD == 128 ? 3 : 6) : kStages;
+  static constexpr int RAW_MORE = F4 ? (HD == 128 ? 3 : 0) : kStages;
+  static_assert(RAW_MORE * RAW_BYTES <= Q_BYTES, "a query tile's place");
   static constexpr int K_STAGES = F8 ? 4 : 2;   // 4 against 2: 8 bits, 35 rows 82 -> 79 us, frames of 3520 tokens 929 -> 924 us
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * Q_BYTES;
   static constexpr int OFF_V = OFF_K + K_STAGES * K_BYTES;
   static constexpr int OFF_RAW = OFF_V + kStages * V_BYTES;   // V codes
-  static constexpr int OFF_BAR = OFF_RAW + kStages * RAW_BYTES;
+  static constexpr int OFF_BAR = OFF_RAW + RAW_STAGES * RAW_BYTES;
   static_assert(kStages * V_BYTES >= BM * HD * 4, "o of one warpgroup passes through the V tiles");
   static constexpr int SMEM = OFF_BAR + 1664 + 1024;
   static_assert(SMEM <= 232448, "shared memory of a CTA");
@@ -90,8 +98,8 @@ struct TilesKArgs {
   int n_pages, page_size, page_shift, H, H_q, group, tile_tokens;   // tile_tokens = 128 / group
   int causal, window, sinks, o_f32;
   int64_t row_stride;
-  const uint8_t* v;
-  const float *k_scale, *v_scale;
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;   // 4-bit pages: bytes
   void* o;
   float* lse;
   float scale_log2;
@@ -340,12 +348,13 @@ struct Bars {
   // bf16 pages: V of a stage's tile that not all rows see is ready.  One phase for each such tile of
   // the stage; the next cannot begin before the products, and so the softmax threads, are past this one.
   uint64_t v_fixed[kStages];
-  uint64_t raw_full[4], raw_empty[4];   // 8-bit pages: V codes
+  uint64_t raw_full[6], raw_empty[6];   // 8-bit pages: V codes; 4-bit pages: K and V codes and scales
   uint64_t fin;
   uint32_t tmem_base;
   int abort;
   int issued[2];                       // of a CTA that gave up: key tiles whose K (V) copies have begun, else many
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
+  uint32_t absent[6];                  // 4-bit pages: pages of a stage's codes that were not fetched
   float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
   Unit unit, next;                     // of this segment and the next
 };
@@ -356,19 +365,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-template <bool F8>
+template <class C>
 __device__ __forceinline__ void init_barriers(Bars* bars) {
-  mbar_init(&bars->q_full, F8 ? 256 : 1);
+  mbar_init(&bars->q_full, C::DECODED ? 256 : 1);
   mbar_init(&bars->q_raw, 1);
   for (int s = 0; s < 4; ++s) {
-    mbar_init(&bars->k_full[s], 1);
+    mbar_init(&bars->k_full[s], C::F4 ? 128 : 1);
     mbar_init(&bars->k_empty[s], 1);
+  }
+  for (int s = 0; s < 6; ++s) {
     mbar_init(&bars->raw_full[s], 1);
     mbar_init(&bars->raw_empty[s], 128);
   }
   for (int s = 0; s < kStages; ++s) {
-    mbar_init(&bars->v_full[s], F8 ? 128 : 1);
-    mbar_init(&bars->v_empty[s], F8 ? 1 : 2);   // the products, and warp 3 that saw the tile
+    mbar_init(&bars->v_full[s], C::DECODED ? 128 : 1);
+    mbar_init(&bars->v_empty[s], C::DECODED ? 1 : 2);   // the products, and warp 3 that saw the tile
     mbar_init(&bars->v_fixed[s], 32);
   }
   for (int t = 0; t < 2; ++t) {
@@ -387,6 +398,8 @@ __device__ __forceinline__ void drop_barriers(Bars* bars) {
   for (int s = 0; s < 4; ++s) {
     drop(&bars->k_full[s]);
     drop(&bars->k_empty[s]);
+  }
+  for (int s = 0; s < 6; ++s) {
     drop(&bars->raw_full[s]);
     drop(&bars->raw_empty[s]);
   }
@@ -455,11 +468,31 @@ __device__ __forceinline__ void fetch_pages(const TilesKArgs& a, const Unit& u, 
   }
 }
 
-template <int HD, bool F8>
-__global__ void __launch_bounds__(F8 ? 512 : 384, 1)
+// Fetches the 4-bit pages of a K or V tile at `pos` (one warp; lane i < 128 / page_size has page i, whose rows of a
+// head lie together): codes, and behind the tile's codes the scales.  What is not fetched is named in `absent`.
+template <int HD>
+__device__ __forceinline__ void fetch_codes(const TilesKArgs& a, const Unit& u, const uint8_t* cache, const float* scales,
+                                            uint8_t* dst, uint32_t* absent, uint64_t* full, int pos, int lane) {
+  const int n = BN >> a.page_shift, codes = a.page_size * (HD / 2), more = a.page_size * (HD / 16);
+  const int page = lane < n ? page_at(a, u, pos + (lane << a.page_shift)) : a.n_pages;
+  const uint32_t there = __ballot_sync(0xffffffffu, page < a.n_pages);
+  if (lane == 0) {
+    *absent = ~there;
+    mbar_arrive_expect_tx(full, __popc(there) * (codes + more));
+  }
+  __syncwarp();
+  if (page < a.n_pages) {
+    bulk_load(dst + lane * codes, cache + (int64_t)page * a.page_size * a.row_stride / 2 + (int64_t)u.h * codes, codes, full);
+    bulk_load(dst + BN * (HD / 2) + lane * more, reinterpret_cast<const uint8_t*>(scales) + ((int64_t)page * a.H + u.h) * more, more, full);
+  }
+}
+
+template <int HD, int KIND>
+__global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
     k_cache_tiles(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ TilesKArgs a) {
-  using C = Cfg<HD, F8>;
+  using C = Cfg<HD, KIND>;
+  constexpr bool F8 = C::F8, F4 = C::F4, DECODED = C::DECODED;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -469,13 +502,16 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
   uint8_t* sRaw = smem + C::OFF_RAW;
   Bars* bars = reinterpret_cast<Bars*>(smem + C::OFF_BAR);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // V codes: two stages, and two more in the place of a second query tile that a unit does not have
-  auto raw_stage = [&](int s) { return s < 2 ? sRaw + s * C::RAW_BYTES : sQ + C::Q_BYTES + (s - 2) * C::RAW_BYTES; };
+  auto raw_stage = [&](int s) {
+    return s < C::RAW_STAGES ? sRaw + s * C::RAW_BYTES : sQ + C::Q_BYTES + (s - C::RAW_STAGES) * C::RAW_BYTES;
+  };
 
   if (warp == 2 && lane == 0) {
     tma_prefetch_desc(&tm_q);
-    tma_prefetch_desc(&tm_k);
-    tma_prefetch_desc(&tm_v);
+    if (!F4) {
+      tma_prefetch_desc(&tm_k);
+      tma_prefetch_desc(&tm_v);
+    }
   }
   // warp 0: the CTA's share of the work, and its first unit
   Deal d{};
@@ -502,7 +538,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     tmem_relinquish();
     tc_fence_before();
     if (lane == 0) {
-      init_barriers<F8>(bars);
+      init_barriers<C>(bars);
       bars->abort = 0;
       bars->issued[0] = bars->issued[1] = 0x7fffffff;
     }
@@ -525,7 +561,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     end_barrier<C::THREADS>();
     if (threadIdx.x == 32 && !aborted(bars)) {
       drop_barriers(bars);
-      init_barriers<F8>(bars);
+      init_barriers<C>(bars);
       bars->unit = bars->next;
     }
     end_barrier<C::THREADS>();
@@ -545,8 +581,8 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       if (lane == 0) {
         if (is_k && n_tiles > 0) {
           const uint32_t bytes = (uint32_t)a.tile_tokens * a.group * HD * 2;
-          uint64_t* bar = F8 ? &bars->q_raw : &bars->q_full;
-          uint8_t* to = F8 ? sV : sQ;
+          uint64_t* bar = DECODED ? &bars->q_raw : &bars->q_full;
+          uint8_t* to = DECODED ? sV : sQ;
           mbar_arrive_expect_tx(bar, (has_q1 ? 2 : 1) * bytes);
           for (int t = 0; t < (has_q1 ? 2 : 1); ++t)
 #pragma unroll
@@ -562,7 +598,26 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       uint8_t* dst = is_k ? sK : sV;
       const int bytes = is_k ? C::K_BYTES : codes ? C::RAW_BYTES : C::V_BYTES;
       const int log_stages = is_k ? (C::K_STAGES == 4 ? 2 : 1) : codes && !has_q1 ? 2 : 1;
-      for (int j = 0; j < n_tiles; ++j) {
+      if constexpr (F4) {
+        // warp 0 alone, in the order in which the tiles are decoded: K0, then K of tile j + 1 and V of tile j
+        const int ring = C::RAW_STAGES + (has_q1 ? 0 : C::RAW_MORE);
+        int s = 0;
+        uint32_t phase = 0;
+        for (int c = 0; is_k && c < 2 * n_tiles; ++c) {
+          const bool ok = !aborted(bars) && mbar_wait(&bars->raw_empty[s], phase ^ 1u, lim) && !aborted(bars);
+          if (!__all_sync(0xffffffffu, ok)) {
+            if (lane == 0) bars->issued[0] = c;
+            set_abort(bars);
+            break;
+          }
+          const bool key = c == 0 || ((c & 1) && c < 2 * n_tiles - 1);
+          const int j = key ? (c + 1) / 2 : (c - 1) / 2;
+          fetch_codes<HD>(a, u, key ? a.k : a.v, key ? a.k_scale : a.v_scale, raw_stage(s), &bars->absent[s], &bars->raw_full[s],
+                          tile_pos(u, k0 + j), lane);
+          if (++s == ring) s = 0, phase ^= 1u;
+        }
+      }
+      for (int j = 0; !F4 && j < n_tiles; ++j) {
         const int s = j & ((1 << log_stages) - 1);
         bool ok = mbar_wait(&empty[s], ((uint32_t)(j >> log_stages) & 1u) ^ 1u, lim);
         ok = !aborted(bars) && ok;
@@ -587,7 +642,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         const Unit next = unit_at(a, d, at, stop, lane, cut);
         if (lane == 0) bars->next = next;
       }
-    } else if (warp == 3 && !F8) {
+    } else if (warp == 3 && !DECODED) {
       // ------------------------------------------------------------ V of tiles that not all rows see
       // It waits for every tile in turn and gives every stage back, so that it can be neither ahead
       // of a phase nor overtaken.
@@ -625,8 +680,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
     } else if (warp == 1 && lane == 0) {
       // ------------------------------------------------------------ products
-      constexpr uint32_t idesc_qk = F8 ? idesc_e4m3_f32(BM, BN) : idesc_bf16_f32(BM, BN, false, false);
-      constexpr uint32_t idesc_pv = F8 ? idesc_f16_f32(BM, HD, false, true) : idesc_bf16_f32(BM, HD, false, true);
+      constexpr uint32_t idesc_qk =
+          F8 ? idesc_e4m3_f32(BM, BN) : F4 ? idesc_f16_f32(BM, BN, false, false) : idesc_bf16_f32(BM, BN, false, false);
+      constexpr uint32_t idesc_pv = DECODED ? idesc_f16_f32(BM, HD, false, true) : idesc_bf16_f32(BM, HD, false, true);
       // a k-slice, query tile or stage further on adds its byte offset / 16 to the start address
       static_assert(C::SMEM + 1024 <= 256 * 1024, "descriptor start-address field would carry");
       constexpr bool kNarrow = F8 && HD == 64;   // 64-byte rows
@@ -670,7 +726,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       auto v_ready = [&](int j) {
         const int s = j % kStages;
         bool ok = !aborted(bars) && mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim);
-        if (ok && !F8 && !all_see(u, tile_pos(u, k0 + j))) {
+        if (ok && !DECODED && !all_see(u, tile_pos(u, k0 + j))) {
           ok = mbar_wait(&bars->v_fixed[s], (fixed >> s) & 1u, lim);
           fixed ^= 1u << s;
         }
@@ -745,13 +801,20 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
     if ((warp == 0 || warp == 2) && aborted(bars)) {
       // the CTA gave up: none of its copies may land after it has left.  They are the segment's last, of which no
       // stage has begun anew, and its queries.
-      const int issued = min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
+      if constexpr (F4) {
+        const int issued = min(bars->issued[0], 2 * u.n_tiles);
+        const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
+#pragma unroll 1
+        for (int c = max(issued - ring, 0); warp == 0 && c < issued; ++c)
+          mbar_wait(&bars->raw_full[c % ring], (uint32_t)(c / ring) & 1u, lim);
+      }
+      const int issued = F4 ? 0 : min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
       uint64_t* full = warp == 0 ? bars->k_full : F8 ? bars->raw_full : bars->v_full;
       const int log_stages = warp == 0 ? (C::K_STAGES == 4 ? 2 : 1) : F8 && u.i0 + a.tile_tokens >= u.n_new ? 2 : 1;
 #pragma unroll 1
       for (int j = max(issued - (1 << log_stages), 0); j < issued; ++j)
         mbar_wait(&full[j & ((1 << log_stages) - 1)], (uint32_t)(j >> log_stages) & 1u, lim);
-      if (warp == 0 && u.n_tiles > 0) mbar_wait(F8 ? &bars->q_raw : &bars->q_full, 0, lim);
+      if (warp == 0 && u.n_tiles > 0) mbar_wait(DECODED ? &bars->q_raw : &bars->q_full, 0, lim);
     }
     if (warp == 1) tmem_dealloc(tmem, kTmemCols);
   } else if (warp < 12) {
@@ -839,6 +902,43 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
             }
             fence_proxy_async_smem();
           }
+        }
+        mbar_arrive(&bars->q_full);
+      }
+      if constexpr (F4) {
+        // the row in f16, times the power of two that brings its largest channel below 2^15 (subnormal, zero and
+        // infinite rows as they are); without a second tile both warpgroups have the row, and write half of it each
+        if (n_tiles > 0 && __any_sync(0xffffffffu, live)) {
+          bool w = !aborted(bars) && mbar_wait(&bars->q_raw, 0, lim);
+          if (!__all_sync(0xffffffffu, w)) set_abort(bars);
+          auto place = [&](int c) { return (c / 8) * BM * 128 + row * 128 + ((c ^ row) & 7) * 16; };   // of channels 8 c ..
+          const uint8_t* src = sV + qt * C::Q_BYTES;
+          auto eight = [&](int c) { return live ? *reinterpret_cast<const uint4*>(src + place(c)) : make_uint4(0, 0, 0, 0); };
+          uint32_t top = 0;   // magnitudes order as their bits
+#pragma unroll 4
+          for (int c = 0; c < HD / 8; ++c) {
+            const uint4 x = eight(c);
+            top = max(top, max(max(x.x & 0x7fff0000u, (x.x << 16) & 0x7fff0000u), max(x.y & 0x7fff0000u, (x.y << 16) & 0x7fff0000u)));
+            top = max(top, max(max(x.z & 0x7fff0000u, (x.z << 16) & 0x7fff0000u), max(x.w & 0x7fff0000u, (x.w << 16) & 0x7fff0000u)));
+          }
+          const int ex = (int)(top >> 23) - 127 - 14;
+          const bool plain = ex < -126 || ex > 113;
+          const float down = plain ? 1.f : pow2f(-ex);
+          if (!plain) unit *= pow2f(ex);
+          const int c0 = has_q1 ? 0 : t * (HD / 16), c1 = has_q1 ? HD / 8 : c0 + HD / 16;
+#pragma unroll 2
+          for (int c = c0; c < c1; ++c) {
+            float x[8];
+            uint32_t h[4];
+            unpack8(eight(c), x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __half2 h2 = __floats2half2_rn(x[2 * e] * down, x[2 * e + 1] * down);
+              h[e] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            *reinterpret_cast<uint4*>(sQ + qt * C::Q_BYTES + place(c)) = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+          fence_proxy_async_smem();
         }
         mbar_arrive(&bars->q_full);
       }
@@ -979,15 +1079,21 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           }
           tmem_st_x64(tl + colS, sr);
         } else {
-          const float2 sc2 = make_float2(unit, unit), nm2 = make_float2(-ref, -ref);
+          const float shift = F4 ? kLift - ref : -ref;
+          const float2 sc2 = make_float2(unit, unit), nm2 = make_float2(shift, shift);
           float2 s4[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
           for (int c = 0; c < BN; c += 2) {
             const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), sc2, nm2);
             const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
             s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], e);
-            const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
-            sr[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+            if constexpr (F4) {
+              const __half2 h2 = __floats2half2_rn(e.x, e.y);
+              sr[c / 2] = *reinterpret_cast<const uint32_t*>(&h2);
+            } else {
+              const __nv_bfloat162 b2 = __floats2bfloat162_rn(e.x, e.y);
+              sr[c / 2] = *reinterpret_cast<const uint32_t*>(&b2);
+            }
           }
           const float2 s2 = __fadd2_rn(__fadd2_rn(s4[0], s4[1]), __fadd2_rn(s4[2], s4[3]));
           l += s2.x + s2.y;
@@ -996,7 +1102,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
         if (j > 0 && __any_sync(0xffffffffu, need)) scale_o(corr);
         if (!whole) {
           const int s = j % kStages;
-          w = F8 ? mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim)
+          w = DECODED ? mbar_wait(&bars->v_full[s], (uint32_t)(j / kStages) & 1u, lim)
                  : mbar_wait(&bars->v_fixed[s], (fixed >> s) & 1u, lim);
           fixed ^= 1u << s;
           if (!__all_sync(0xffffffffu, w)) { ok = false; break; }
@@ -1005,11 +1111,14 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
               // V row r holds a value that is not finite: its token by itself, where it is seen
               const int r = 32 * b + __ffs(bits) - 1, key = pos + r;
               const uint32_t pp = tmem_ld_1(tl + colS + r / 2);
-              const float prob = F8 ? __half2float(__ushort_as_half((unsigned short)(r & 1 ? pp >> 16 : pp)))
+              const float prob = DECODED ? __half2float(__ushort_as_half((unsigned short)(r & 1 ? pp >> 16 : pp)))
                                     : __uint_as_float(r & 1 ? pp & 0xffff0000u : pp << 16);
               const bool see = key < hi && (key >= lo || key < sinks);
               const int page = __ldg(a.batch.page_table + (int64_t)u.b * a.batch.page_table_stride + (key >> a.page_shift));
-              const int64_t at = ((int64_t)page * a.page_size + (key & (a.page_size - 1))) * a.row_stride + (int64_t)u.h * HD;
+              const int in_page = key & (a.page_size - 1);
+              const int64_t at = F4 ? (int64_t)page * a.page_size * a.row_stride / 2 + ((int64_t)u.h * a.page_size + in_page) * (HD / 2)
+                                    : ((int64_t)page * a.page_size + in_page) * a.row_stride + (int64_t)u.h * HD;
+              const uint8_t* scales4 = reinterpret_cast<const uint8_t*>(a.v_scale) + (((int64_t)page * a.H + u.h) * a.page_size + in_page) * (HD / 16);
 #pragma unroll 1
               for (int c = 0; c < HD; c += 32) {
                 uint32_t orr[32];
@@ -1017,7 +1126,9 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) {
                   float x;
-                  if (F8) {
+                  if constexpr (F4) {
+                    x = value4((uint32_t)__ldg(a.v + at + (c + e) / 2) >> (4 * (e & 1)), __ldg(scales4 + (c + e) / 16));
+                  } else if constexpr (F8) {
                     const __half h(__nv_cvt_fp8_to_halfraw(__ldg(a.v + at + c + e), __NV_E4M3));
                     x = __half2float(h);
                   } else {
@@ -1039,8 +1150,8 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       }
       if (!ok) set_abort(bars);
       tc_fence_after();
-      const float o_unit = F8 ? exp2_fast(e_ref) * 0x1p-7f : 1.f;
-      if (F8) l *= 0x1p-7f;
+      const float o_unit = F8 ? exp2_fast(e_ref) * 0x1p-7f : F4 ? 0x1p-7f : 1.f;
+      if (DECODED) l *= 0x1p-7f;
       float* other = reinterpret_cast<float*>(sV);   // [HD][128]: o of the second warpgroup (every product is done)
       const bool join = u.slot < 0 && !has_q1;
       if (join) {
@@ -1116,7 +1227,7 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
           uint32_t orr[64];
           tmem_ld_x64(tl + colO + half * 64, orr);
           float* v = reinterpret_cast<float*>(orr);
-          if (F8) {
+          if (DECODED) {
 #pragma unroll
             for (int c = 0; c < 64; ++c) v[c] *= o_unit;
           }
@@ -1193,6 +1304,84 @@ __global__ void __launch_bounds__(F8 ? 512 : 384, 1)
       fence_proxy_async_smem();
       mbar_arrive(&bars->v_full[s]);
       mbar_arrive(&bars->raw_empty[rs]);
+    }
+    if (!ok) set_abort(bars);
+    if (!another()) break;
+    }
+  } else if constexpr (F4) {
+    // -------------------------------------------------------------- K and V codes and scales to f16 tiles
+    setmaxnreg_dec<C::REGS_DECODE>();
+    const int tid = threadIdx.x - 384, w4 = warp & 3;
+    // A thread has 32 channels (16 bytes of codes, two scales) of a row at a time.  Eight lanes load 128 bytes in a row
+    // of codes, and the 16-byte chunks that they store lie in eight bank groups: heads of 128, rows r and r ^ 3, and the
+    // second 64 channels' chunks in another order; heads of 64, four rows.
+    constexpr int CHUNKS = HD / 32, ITEMS = CHUNKS;
+    const int chunk = lane & (CHUNKS - 1), box = HD == 128 ? chunk >> 1 : 0;
+    auto row_of = [&](int i) {
+      if (HD == 128) return i * 32 + w4 * 8 + (lane >> 4) * 4 + (((lane >> 3) & 1) ^ (((lane >> 2) & 1) * 3));
+      return i * 64 + w4 * 16 + (lane >> 1);
+    };
+    for (;;) {
+    const int k0 = u.k0, n_tiles = u.n_tiles;
+    const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
+    int rs = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int it = 0; ok && it < 2 * n_tiles; ++it) {
+      const bool key = it == 0 || ((it & 1) && it < 2 * n_tiles - 1);
+      const int j = key ? (it + 1) / 2 : (it - 1) / 2;
+      const int s = j % kStages, pos = tile_pos(u, k0 + j);
+      const bool whole = key || all_see(u, pos);
+      bool w = !aborted(bars) && mbar_wait(&bars->raw_full[rs], phase, lim) &&
+               mbar_wait(key ? &bars->k_empty[s] : &bars->v_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+      // the queries lie in the V tiles' place until they are turned into f16
+      if (w && !key && j < kStages) w = mbar_wait(&bars->q_full, 0, lim);
+      // the four warps leave together: they meet at barriers below
+      if (bar_sync_or(2, 128, !w)) { ok = false; break; }
+      const uint8_t* src = raw_stage(rs);
+      const uint8_t* scales = src + C::CODE_BYTES;
+      const uint32_t absent = bars->absent[rs];
+      uint8_t* dst = key ? sK + s * C::K_BYTES : sV + s * C::V_BYTES;
+      auto not_there = [&](int r) { return ((absent >> (r >> a.page_shift)) & 1u) != 0u; };
+      if (!whole) {
+        // V rows whose scales are not finite, of a tile that the unit's rows do not all see alike (one row a thread)
+        bool bad = false;
+        if (some_see(u, pos + tid) && !not_there(tid))
+          for (int c = 0; c < HD / 16; ++c) bad |= scales[tid * (HD / 16) + c] > kScaleTop;
+        const uint32_t apart = __ballot_sync(0xffffffffu, bad);
+        if (lane == 0) bars->apart[s][tid >> 5] = apart;
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+      }
+      uint4 codes[ITEMS];
+      uint32_t sc[ITEMS];
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int r = row_of(i);
+        codes[i] = *reinterpret_cast<const uint4*>(src + r * (HD / 2) + chunk * 16);
+        sc[i] = *reinterpret_cast<const uint16_t*>(scales + r * (HD / 16) + chunk * 2);
+      }
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        const int r = row_of(i);
+        const bool none = not_there(r) || (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)));
+        const uint32_t x[4] = {box ? codes[i].y : codes[i].x, box ? codes[i].x : codes[i].y, box ? codes[i].w : codes[i].z,
+                               box ? codes[i].z : codes[i].w};
+        const uint32_t pair[2] = {scale4_pair(sc[i]), __byte_perm(sc[i], 0, 0x4141) << 7};
+        uint8_t* to = dst + box * BN * 128 + r * 128;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t h[4];
+          half8(x[e], h);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = none ? 0u : times2(h[k], pair[e >> 1]);
+          const int idx = (HD == 128 ? (chunk & 1) : chunk) * 4 + (e ^ box);
+          *reinterpret_cast<uint4*>(to + ((idx ^ r) & 7) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(key ? &bars->k_full[s] : &bars->v_full[s]);
+      mbar_arrive(&bars->raw_empty[rs]);
+      if (++rs == ring) rs = 0, phase ^= 1u;
     }
     if (!ok) set_abort(bars);
     if (!another()) break;
@@ -1333,11 +1522,12 @@ bool encode(CUtensorMap* m, int elt, CUtensorMapSwizzle swizzle, const void* bas
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int HD, bool F8>
+template <int HD, int KIND>
 cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const TilesPlan& p, cudaStream_t st) {
-  using C = Cfg<HD, F8>;
+  using C = Cfg<HD, KIND>;
+  constexpr bool F8 = C::F8;
   const cast_kv_cache& c = a.cache;
-  CUtensorMap mq, mk, mv;
+  CUtensorMap mq, mk{}, mv{};   // (4-bit pages are fetched without K's and V's)
   constexpr int elt = F8 ? 1 : 2;
   const cuuint64_t kd[3] = {(cuuint64_t)c.H * HD, (cuuint64_t)c.page_size, (cuuint64_t)c.n_pages};
   const cuuint64_t ks[2] = {(cuuint64_t)c.row_stride * elt, (cuuint64_t)c.row_stride * elt * c.page_size};
@@ -1346,25 +1536,25 @@ cast_status launch(const cast_cache_attn_args& a, const TilesKArgs& k, const Til
   const CUtensorMapSwizzle operand = F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
   const cuuint64_t qd[3] = {HD, (cuuint64_t)a.H_q, (cuuint64_t)a.batch.T}, qs[2] = {HD * 2, (cuuint64_t)a.q_row_stride * 2};
   const cuuint32_t qb[3] = {64, (cuuint32_t)k.group, (cuuint32_t)k.tile_tokens};
-  const bool ok = encode(&mk, elt, operand, c.k, kd, ks, kb) &&
-                  encode(&mv, elt, F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, c.v, kd, ks, kb) &&
+  const bool ok = (C::F4 || (encode(&mk, elt, operand, c.k, kd, ks, kb) &&
+                  encode(&mv, elt, F8 && HD == 64 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, c.v, kd, ks, kb))) &&
                   encode(&mq, 2, CU_TENSOR_MAP_SWIZZLE_128B, a.q, qd, qs, qb);
   if (!ok) return fail(CAST_ERR_CUDA, "cache attention: cuTensorMapEncodeTiled failed");
   static std::atomic<uint64_t> attr_done{0};
   cast_status setup = CAST_OK;
   if (!once_per_device(attr_done, [&] {
         cudaFuncAttributes fa{};
-        if (cudaFuncGetAttributes(&fa, k_cache_tiles<HD, F8>) != cudaSuccess) return false;
+        if (cudaFuncGetAttributes(&fa, k_cache_tiles<HD, KIND>) != cudaSuccess) return false;
         if (fa.numRegs != C::LAUNCH) {
           // the register hand-over counts on exactly this many
           setup = fail(CAST_ERR_UNSUPPORTED, "cache attention kernel built with %d registers per thread, expected %d", fa.numRegs,
                        C::LAUNCH);
           return false;
         }
-        return cudaFuncSetAttribute(k_cache_tiles<HD, F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
+        return cudaFuncSetAttribute(k_cache_tiles<HD, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
       }))
     return setup != CAST_OK ? setup : check_launch("cache attention kernel attributes");
-  k_cache_tiles<HD, F8><<<(unsigned)p.grid, C::THREADS, C::SMEM, st>>>(mq, mk, mv, k);
+  k_cache_tiles<HD, KIND><<<(unsigned)p.grid, C::THREADS, C::SMEM, st>>>(mq, mk, mv, k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole || p.grid == 1) return s;
   cudaLaunchConfig_t cfg{};
@@ -1437,6 +1627,7 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.sinks = k.window > 0 ? a.sinks : 0;
   k.o_f32 = a.o_dtype == CAST_F32;
   k.row_stride = c.row_stride;
+  k.k = static_cast<const uint8_t*>(c.k);
   k.v = static_cast<const uint8_t*>(c.v);
   k.k_scale = static_cast<const float*>(c.k_scale);
   k.v_scale = static_cast<const float*>(c.v_scale);
@@ -1451,8 +1642,9 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
   k.cuts = reinterpret_cast<Cut*>(static_cast<char*>(ws) + p.part_o_bytes + p.part_ml_bytes);
   k.wait_ns = 2000000000ull;
-  if (c.dtype == CAST_F8E4M3) return c.d == 128 ? launch<128, true>(a, k, p, st) : launch<64, true>(a, k, p, st);
-  return c.d == 128 ? launch<128, false>(a, k, p, st) : launch<64, false>(a, k, p, st);
+  if (c.dtype == CAST_F8E4M3) return c.d == 128 ? launch<128, CAST_F8E4M3>(a, k, p, st) : launch<64, CAST_F8E4M3>(a, k, p, st);
+  if (c.dtype == CAST_F4E2M1) return c.d == 128 ? launch<128, CAST_F4E2M1>(a, k, p, st) : launch<64, CAST_F4E2M1>(a, k, p, st);
+  return c.d == 128 ? launch<128, CAST_BF16>(a, k, p, st) : launch<64, CAST_BF16>(a, k, p, st);
 }
 
 unsigned int cache_tiles_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }

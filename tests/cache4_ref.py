@@ -33,7 +33,7 @@ def nearest(x):
 
 def decode(codes, scales):
     """Values [..., d] of codes [..., d / 2] with scales [..., d / 16], in f16 as the kernels form them."""
-    c = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], -1).astype(np.int64)
+    c = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], 2 * codes.shape[-1]).astype(np.int64)
     with np.errstate(all="ignore"):
         v = VALUES[c & 7] * np.where(c & 8, -1.0, 1.0) * np.repeat(scale_value(scales), 16, -1)
         return v.astype(np.float16).astype(np.float64)
@@ -41,7 +41,7 @@ def decode(codes, scales):
 
 def quantise(x):
     """(values, scale codes) of x [..., d]; a group that is not all finite is NaN."""
-    g = x.reshape(*x.shape[:-1], -1, 16)
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // 16, 16)
     fine = np.isfinite(g).all(-1)
     g = np.where(fine[..., None], g, 0)
     code = scale_code(np.abs(g).max(-1) / 6)

@@ -324,3 +324,125 @@ def test_attention_few_rows(lib, lens, new, H, H_q, d, page, causal, window, sin
     check_attention(lib, c, held, q, new, o, lse, **kw)
     o32 = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=cu, max_new=max(new), out_dtype=torch.float32, **kw)
     check_attention(lib, c, held, q, new, o32, None, **kw)
+
+
+TILES = [
+    # lens, new, H, H_q, d, page, causal, window, sinks
+    ([17], [17], 1, 1, 128, 16, True, 0, 0),
+    ([301], [40], 2, 8, 64, 16, True, 0, 0),
+    ([200, 500], [129, 77], 1, 3, 64, 16, True, 0, 0),
+    ([300, 17, 1000], [130, 5, 64], 3, 3, 128, 32, True, 0, 0),
+    ([2000], [300], 2, 2, 128, 64, False, 0, 0),                    # parts joined over CTAs
+    ([3000, 1500, 100], [9, 9, 9], 2, 10, 128, 128, True, 0, 0),    # one tile of few rows
+    ([2600, 700], [200, 130], 2, 6, 64, 64, True, 500, 4),
+    ([2600, 700], [260, 130], 1, 2, 128, 16, False, 700, 130),
+    ([1500] * 3, [128] * 3, 5, 5, 128, 64, False, 0, 0),
+    ([900, 1], [300, 1], 1, 128, 64, 32, True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("lens,new,H,H_q,d,page,causal,window,sinks", TILES)
+def test_attention_many_rows(lib, lens, new, H, H_q, d, page, causal, window, sinks):
+    test_attention_few_rows(lib, lens, new, H, H_q, d, page, causal, window, sinks)
+
+
+HIDDEN = [
+    # lens, new, H, H_q, d, page, causal, window, sinks
+    ([333], [1], 2, 4, 128, 16, True, 100, 5),
+    ([333], [3], 1, 4, 64, 32, True, 0, 0),
+    ([333, 200], [40, 12], 2, 4, 128, 16, True, 0, 0),
+    ([700], [300], 1, 2, 64, 64, True, 130, 9),
+]
+
+
+@pytest.mark.parametrize("lens,new,H,H_q,d,page,causal,window,sinks", HIDDEN)
+def test_attention_never_reads_what_is_hidden(lib, lens, new, H, H_q, d, page, causal, window, sinks):
+    """NaN and infinite scales: at positions that no row sees they change nothing; at a position that some rows see,
+    those rows alone."""
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    c = Pages4(lib, lens, H, d, page, seed=2)
+    held = c.fill(seed=3)
+    T = sum(new)
+    q = randn(gen(4), T, H_q, d).to(torch.bfloat16)
+    cu = i32(*np.concatenate([[0], np.cumsum(new)]))
+    call = lambda: lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=cu, max_new=max(new), out_dtype=torch.float32, **kw)
+    clean = call()
+    at = 0
+    for b, (n, m) in enumerate(zip(lens, new)):
+        p, j = n - m + np.arange(m)[:, None], np.arange(n)[None, :]
+        see = np.ones((m, n), bool)
+        if causal:
+            see &= j <= p
+        if window:
+            see &= (j > p - window) | (j < sinks)
+        ref, _, eo, _ = R4.attention(f64(q[at:at + m]), *held[b], n, **kw)
+        ref, eo = ref.reshape(m, -1), (eo + R.U32 * np.abs(ref)).reshape(m, -1)
+
+        def unchanged(got, rows):
+            """Of rows that do not see the token: to the bit where nobody sees it, else within the bound (the tokens of
+            its block are added one by one, in another order and by other roundings)."""
+            if not rows.any():
+                assert torch.equal(got, clean), (b, key)
+            assert (np.abs(f64(got[mine]) - ref) <= eo)[~rows.cpu().numpy()].all(), (b, key)
+
+        for bad in (0xff, 0xf8):
+            for key in sorted({0, n - 1, n - m, max(0, n - m - window), n // 3}):
+                page_of, row = int(c.table[b, key // page]), key % page
+                keep = c.vs[page_of, :, row].clone()
+                c.vs[page_of, :, row] = bad
+                got = call()
+                rows = torch.from_numpy(see[:, key]).cuda()
+                mine = slice(at, at + m)
+                unchanged(got, rows)
+                # every channel: a value that is not finite, or infinity times a code of 0
+                assert not torch.isfinite(got[mine][rows]).any(), (b, key)
+                others = torch.ones(T, dtype=torch.bool, device="cuda")
+                others[mine] = False
+                assert torch.equal(got[others], clean[others])
+                c.vs[page_of, :, row] = keep
+                keep = c.ks[page_of, :, row].clone()
+                c.ks[page_of, :, row] = bad
+                got = call()
+                unchanged(got, rows)
+                if bad == 0xff:
+                    assert torch.isnan(got[mine][rows]).all(), (b, key)
+                c.ks[page_of, :, row] = keep
+        at += m
+    lib.cast_check_device()
+    check_attention(lib, c, held, q, new, clean, None, **kw)
+
+
+@pytest.mark.parametrize("new,d", [(1, 128), (8, 64), (40, 128), (300, 64)])
+def test_attention_of_pages_and_rows_that_are_not_there(lib, new, d):
+    """A page out of range reads as zeros; a sequence of no tokens gives zeros; rows behind the last are left."""
+    c = Pages4(lib, [600, 0], 2, d, 16, seed=8)
+    (k, v), _ = c.fill(seed=9)
+    table = c.table.clone()
+    table[0, 5], table[0, 30] = -1, 10 ** 6
+    q = randn(gen(1), 2 * new, 4, d).to(torch.bfloat16)
+    out = torch.full((2 * new + 2, 4 * d), 7.0, device="cuda")
+    cu = i32(0, new, 2 * new)
+    qq = torch.cat([q, q[:2]])
+    lib.cast_cache_attention(qq, c.cache, table, c.kv_len, cu_new=cu, max_new=new, causal=False, out=out, out_dtype=torch.float32)
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+    assert (out[2 * new:] == 7).all() and (out[new:2 * new] == 0).all()
+    for x in (k, v):
+        x[80:96] = 0
+        x[480:496] = 0
+    check_attention(lib, c, [(k, v), None], q[:new], [new], out[:new], None, causal=False)
+
+
+@pytest.mark.parametrize("new,H_q,d", [(1, 4, 128), (1, 12, 64), (60, 4, 128), (200, 2, 64)])
+def test_attention_of_large_and_small_values(lib, new, H_q, d):
+    """Values at the ends of what 4 bits hold; queries at the ends of bf16, rows of zeros."""
+    c = Pages4(lib, [700], 2, d, 32, seed=8)
+    (k, v), = c.fill(seed=9, scale=9000.0)
+    q = randn(gen(1), new, H_q, d).to(torch.bfloat16) * 1e-4
+    q[new // 2] = 0
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, want_lse=True, out_dtype=torch.float32)
+    check_attention(lib, c, [(k, v)], q, [new], o, lse)
+    (k, v), = c.fill(seed=10, scale=2e-4)
+    q = randn(gen(2), new, H_q, d).to(torch.bfloat16) * 2e4
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, want_lse=True, out_dtype=torch.float32)
+    check_attention(lib, c, [(k, v)], q, [new], o, lse)
