@@ -1,6 +1,6 @@
 // Attention over 4-bit pages for few rows a sequence (single tokens, drafts): k_cache_rows4.  Units, shares of the
 // work and the joining are those of k_cache_rows (cache_attention.cu); inside a CTA each warp works on its own blocks
-// of 16 tokens with its own running maximum, sum and o in registers.
+// of 32 tokens with its own running maximum, sum and o in registers.
 //
 // The codes become f16 in registers (a conversion and a product with the scale for two, both exact), so the issue of
 // instructions is what bounds the kernel beside memory, and everything follows from it:
@@ -27,20 +27,22 @@
 namespace cast {
 namespace {
 
+constexpr int BT = 32;   // tokens of a block: two products' sixteen
+
 // NT: units of 8 NT rows
 template <int D, int NT>
 struct Cfg4 {
   static constexpr int ROWS = 8 * NT;
   static constexpr int ROWB = D / 2, SROWB = D / 16;      // bytes of a token's codes and scales
-  static constexpr int BLOCK = 16 * ROWB, SBLOCK = 16 * SROWB;
+  static constexpr int BLOCK = BT * ROWB, SBLOCK = BT * SROWB;
   static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
   static constexpr int CTAS = D * NT <= 128 ? 4 : 3;      // of an SM
-  static constexpr int ROOM = (CTAS == 4 ? 13 : 17) * 1024;   // a warp's ring at most
+  static constexpr int ROOM = (CTAS == 4 ? 13 * 1024 + 512 : 18 * 1024);   // a warp's ring at most
   static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
   static constexpr int RING = STAGES * STAGE;
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
   static constexpr int SMEM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
-  static_assert(STAGES >= 4 && SMEM <= 72 * 1024, "CTAs of an SM");
+  static_assert(STAGES >= 3 && (SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
 };
 
 // The block's token that lane group g's row of a product is (and token + 8 that row g + 8 is): token 4 j + (q ^ j) for
@@ -52,8 +54,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// Whether any of four scale bytes gives values that may not be finite
-__device__ __forceinline__ bool odd_scale(uint32_t code) { return code > kScaleTop; }
 template <int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
   using C = Cfg4<D, NT>;
@@ -62,11 +62,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q4 = lane & 3;
-  const Share mine = share_of<D, C::ROWS>(a);
-  int entry = mine.entry;
-  int64_t at = mine.at, entry_at = mine.entry_at;
-  const int64_t stop = mine.stop;
-  if (at >= stop) return;
+  int entry;
+  int64_t at, stop, entry_at;
+  if (!share_of<D, C::ROWS, BT>(a, entry, at, stop, entry_at)) return;
 
   uint8_t* ring = smem + warp * C::RING;
   const uint32_t ring_at = smem_u32(ring);
@@ -78,7 +76,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
 
   for (; at < stop; ++entry) {
     const int b = entry / a.row_tiles, tile = entry % a.row_tiles;
-    const Span z = span_of(a, b, tile, C::ROWS);
+    const Span z = span_of<BT>(a, b, tile, C::ROWS);
     const int nb = z.blocks();
     const int* table = a.batch.page_table + (int64_t)b * a.batch.page_table_stride;
     for (int h = nb ? (int)((at - entry_at) / nb) : a.H; h < a.H && at < stop; ++h) {
@@ -87,40 +85,60 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const int k0 = (int)(at - unit_at);
       const int k1 = (int)min((int64_t)nb, stop - unit_at);
 
-      // fetches block i of the unit into stage st
-      auto page_of = [&](int i) {
-        int p = __ldg(table + ((z.block(i) * 16) >> a.page_shift));
-        if (p < 0 || p >= a.n_pages) {
-          if (lane == 0) left_out();
-          p = -1;
+      // The pages of block i's halves (-1: out of range, reads as zeros; or, of pages of 16, seen by no row)
+      auto pages_of = [&](int i) {
+        const int base = z.block(i) * BT;
+        auto page_at = [&](int p) {
+          int page = __ldg(table + (p >> a.page_shift));
+          if (page < 0 || page >= a.n_pages) {
+            if (lane == 0) left_out();
+            page = -1;
+          }
+          return page;
+        };
+        auto some = [&](int p) { return p < z.hi && (p + 16 > z.lo || p < z.sinks); };
+        int2 pages;
+        if (a.page_shift > 4) {
+          pages.x = pages.y = page_at(base);
+        } else {
+          pages.x = some(base) ? page_at(base) : -1;
+          pages.y = some(base + 16) ? page_at(base + 16) : -1;
         }
-        return p;
+        return pages;
       };
-      auto fetch = [&](int i, int st, int page) {
-        const int row = (z.block(i) * 16) & (a.page_size - 1);
-        const uint32_t dst = ring_at + st * C::STAGE;
-        if (page >= 0) {
-          const int64_t from = page * page_bytes + (int64_t)(h * a.page_size + row) * C::ROWB + lane * 16;
+      // fetches block i of the unit into stage st
+      auto fetch = [&](int i, int st, int2 pages) {
+        const int base = z.block(i) * BT;
+        const uint32_t dst = ring_at + st * C::STAGE + lane * 16;
 #pragma unroll
-          for (int c = 0; c < C::BLOCK; c += 512) {
-            copy16(dst + c + lane * 16, a.k + from + c);
-            copy16(dst + C::BLOCK + c + lane * 16, a.v + from + c);
+        for (int half = 0; half < 2; ++half) {
+          const int page = half ? pages.y : pages.x, row = (base + 16 * half) & (a.page_size - 1);
+          if (page >= 0) {
+            const int64_t from = page * page_bytes + (h * a.page_size + row) * C::ROWB + lane * 16;
+#pragma unroll
+            for (int c = 0; c < C::BLOCK / 2; c += 512) {
+              copy16(dst + half * (C::BLOCK / 2) + c, a.k + from + c);
+              copy16(dst + C::BLOCK + half * (C::BLOCK / 2) + c, a.v + from + c);
+            }
           }
         }
-        if (lane < 2 * C::SBLOCK / 16) {
-          const bool is_v = lane >= C::SBLOCK / 16;
-          const int64_t from = (((int64_t)max(page, 0) * a.H + h) * a.page_size + row) * C::SROWB + (lane & (C::SBLOCK / 16 - 1)) * 16;
-          copy16_or_zero(dst + 2 * C::BLOCK + lane * 16, (is_v ? vscale : kscale) + from, page >= 0);
+        // scales: K's first half, its second, V's first, V's second
+        constexpr int CH = C::SBLOCK / 32;   // chunks of a half
+        if (lane < 4 * CH) {
+          const bool is_v = lane >= 2 * CH, second = (lane / CH) & 1;
+          const int page = second ? pages.y : pages.x, row = (base + (second ? 16 : 0)) & (a.page_size - 1);
+          const int64_t from = (((int64_t)max(page, 0) * a.H + h) * a.page_size + row) * C::SROWB + (lane & (CH - 1)) * 16;
+          copy16_or_zero(dst + 2 * C::BLOCK, (is_v ? vscale : kscale) + from, page >= 0);
         }
       };
       const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
       const int i0 = k0 + warp;
       __syncwarp();
       for (int st = 0; st < C::STAGES - 1; ++st) {
-        if (st < n) fetch(i0 + st * kWarps, st, page_of(i0 + st * kWarps));
+        if (st < n) fetch(i0 + st * kWarps, st, pages_of(i0 + st * kWarps));
         copy_commit();
       }
-      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * kWarps) : -1;
+      int2 next_pages = C::STAGES - 1 < n ? pages_of(i0 + (C::STAGES - 1) * kWarps) : make_int2(-1, -1);
 
       // Q^T fragments: row g of each 8 (product s takes channels (D / 4) q4 + 4 s .. + 3 of lane group q4)
       uint32_t qf[NT][D / 16][2];
@@ -193,35 +211,37 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         __syncwarp();
         // the stage used one block ago takes the block STAGES - 1 ahead
         const int ahead = it + C::STAGES - 1;
-        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_page);
+        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_pages);
         copy_commit();
-        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * kWarps);
+        if (ahead + 1 < n) next_pages = pages_of(i0 + (ahead + 1) * kWarps);
         const uint8_t* kt = ring + st * C::STAGE;
         const uint8_t* vt = kt + C::BLOCK;
         const uint8_t* ks = kt + 2 * C::BLOCK;
         const uint8_t* vs = ks + C::SBLOCK;
 
-        // ---- S^T = K Q^T
-        float s[NT][4];
+        // ---- S^T = K Q^T, of 16 tokens and of the other 16
+        float s[NT][2][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int half = 0; half < 2; ++half) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
-        {
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][half][e] = 0.f;
           uint32_t kw[2][KW], sc[2][2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const uint8_t* p = kt + (kt0 + 8 * j) * C::ROWB + q4 * (D / 8);
+            const int token = 16 * half + kt0 + 8 * j;
+            const uint8_t* p = kt + token * C::ROWB + q4 * (D / 8);
             if constexpr (D == 128) {
               const uint4 w = *reinterpret_cast<const uint4*>(p);
               kw[j][0] = w.x; kw[j][1] = w.y; kw[j][2] = w.z; kw[j][3] = w.w;
-              const uint32_t two = *reinterpret_cast<const uint16_t*>(ks + (kt0 + 8 * j) * C::SROWB + q4 * 2);
+              const uint32_t two = *reinterpret_cast<const uint16_t*>(ks + token * C::SROWB + q4 * 2);
               sc[j][0] = scale4_pair(two);
               sc[j][1] = __byte_perm(two, 0, 0x4141) << 7;
             } else {
               const uint2 w = *reinterpret_cast<const uint2*>(p);
               kw[j][0] = w.x; kw[j][1] = w.y;
-              sc[j][0] = scale4_pair(ks[(kt0 + 8 * j) * C::SROWB + q4]);
+              sc[j][0] = scale4_pair(ks[token * C::SROWB + q4]);
             }
           }
 #pragma unroll
@@ -238,43 +258,21 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             for (int u = 0; u < 2; ++u) {
               const uint32_t f[4] = {x[2 * u], y[2 * u], x[2 * u + 1], y[2 * u + 1]};
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma16816h(s[t], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
+              for (int t = 0; t < NT; ++t) mma16816h(s[t][half], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
             }
           }
         }
 
-        const int base = z.block(i0 + it * kWarps) * 16;
-        const bool whole = base + 16 <= all_hi && (base >= all_lo || base + 16 <= z.sinks);
-        // V's codes and scales, before the exponentials wait for S
-        uint32_t vw[4][VW], vc[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int token = (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
-          const uint8_t* p = vt + token * C::ROWB + g * (D / 16);
-          if constexpr (D == 128) {
-            const uint2 w = *reinterpret_cast<const uint2*>(p);
-            vw[j][0] = w.x;
-            vw[j][1] = w.y;
-            vc[j] = vs[token * C::SROWB + g];
-          } else {
-            vw[j][0] = *reinterpret_cast<const uint32_t*>(p);
-            vc[j] = vs[token * C::SROWB + (g >> 1)];
-          }
-        }
-        bool apart = false;
+        const int base = z.block(i0 + it * kWarps) * BT;
+        const bool whole = base + BT <= all_hi && (base >= all_lo || base + BT <= z.sinks);
         if (!whole) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              s[t][e] = sees(base + kt0 + (e & 2 ? 8 : 0), pos[t][e & 1]) ? s[t][e] * unit[t][e & 1] : -INFINITY;
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int p = base + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
-            if (!(p < z.hi && (p >= z.lo || p < z.sinks))) vc[j] = 0;   // nobody's
-            apart |= odd_scale(vc[j]);
-          }
-          apart = __any_sync(0xffffffffu, apart);
+              for (int e = 0; e < 4; ++e)
+                s[t][half][e] = sees(base + 16 * half + kt0 + (e & 2 ? 8 : 0), pos[t][e & 1]) ? s[t][half][e] * unit[t][e & 1] : -INFINITY;
         }
 
         // ---- running maximum; what is left of a logit's factor
@@ -285,7 +283,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             times[t][j] = whole ? unit[t][j] : 1.f;
-            top[t][j] = fmaxf(s[t][j], s[t][2 + j]) * times[t][j];
+            top[t][j] = fmaxf(fmaxf(s[t][0][j], s[t][0][2 + j]), fmaxf(s[t][1][j], s[t][1][2 + j])) * times[t][j];
             grows = grows || top[t][j] > m_ref[t][j] + kRescale;
           }
         if (__any_sync(0xffffffffu, grows)) {
@@ -310,61 +308,95 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             }
         }
         // ---- P^T, 2^kLift times the probabilities; l is the sum of them as they are before the rounding
-        uint32_t pf[NT][2];
+        uint32_t pf[NT][2][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             // a row that has seen nothing yet: exp2(-inf - 0) = 0
             const float ref = kLift - (m_ref[t][j] == -INFINITY ? 0.f : m_ref[t][j]);
-            s[t][j] = exp2_fast(fmaf(s[t][j], times[t][j], ref));
-            s[t][2 + j] = exp2_fast(fmaf(s[t][2 + j], times[t][j], ref));
-            l[t][j] += s[t][j] + s[t][2 + j];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              s[t][half][j] = exp2_fast(fmaf(s[t][half][j], times[t][j], ref));
+              s[t][half][2 + j] = exp2_fast(fmaf(s[t][half][2 + j], times[t][j], ref));
+            }
+            l[t][j] += (s[t][0][j] + s[t][0][2 + j]) + (s[t][1][j] + s[t][1][2 + j]);
           }
-          pf[t][0] = transposed(pack2h(s[t][0], s[t][1]));
-          pf[t][1] = transposed(pack2h(s[t][2], s[t][3]));
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            pf[t][half][0] = transposed(pack2h(s[t][half][0], s[t][half][1]));
+            pf[t][half][1] = transposed(pack2h(s[t][half][2], s[t][half][3]));
+          }
         }
 
         // ---- o^T += V^T P^T
-        if (apart) {
-          // tokens one by one, where they are seen: P's column of a token is in the lanes that have it as a K token
-#pragma unroll 1
-          for (int token = 0; token < 16; ++token) {
-            // the lane group whose K token this is: row 2 q + j of token 4 j + (q ^ j)
-            const int k = token & 7, from = (2 * ((k & 3) ^ (k >> 2)) + (k >> 2)) * 4 + q4;
-            const int p = base + token;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+        for (int half = 0; half < 2; ++half) {
+          uint32_t vw[4][VW], vc[4];
 #pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const float w0 = __shfl_sync(0xffffffffu, s[t][j], from), w1 = __shfl_sync(0xffffffffu, s[t][2 + j], from);
-                if (!sees(p, pos[t][j])) continue;
-                const float w = token < 8 ? w0 : w1;
-                const uint32_t scale = vs[token * C::SROWB + (D == 128 ? g : g >> 1)];
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                  const uint32_t two = vt[token * C::ROWB + g * (D / 16) + i];
-                  o[t][i][j] += w * value4(two, scale);
-                  o[t][i][2 + j] += w * value4(two >> 4, scale);
-                }
-              }
+          for (int j = 0; j < 4; ++j) {
+            const int token = 16 * half + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+            const uint8_t* p = vt + token * C::ROWB + g * (D / 16);
+            if constexpr (D == 128) {
+              const uint2 w = *reinterpret_cast<const uint2*>(p);
+              vw[j][0] = w.x;
+              vw[j][1] = w.y;
+              vc[j] = vs[token * C::SROWB + g];
+            } else {
+              vw[j][0] = *reinterpret_cast<const uint32_t*>(p);
+              vc[j] = vs[token * C::SROWB + (g >> 1)];
+            }
           }
-        } else {
-          const uint32_t s0 = scale4_pair(vc[0], vc[1]), s1 = scale4_pair(vc[2], vc[3]);
+          bool apart = false;
+          if (!whole) {
 #pragma unroll
-          for (int w = 0; w < VW; ++w) {
-            constexpr uint32_t low = 0x0f0f0f0fu;
-            // bytes of two tokens' codes of one channel: channels 0 2 4 6, and 1 3 5 7, of the word's eight
-            uint32_t x[4], y[4], u[4], v[4];
-            half8((vw[0][w] & low) | ((vw[1][w] << 4) & ~low), x);
-            half8(((vw[0][w] >> 4) & low) | (vw[1][w] & ~low), y);
-            half8((vw[2][w] & low) | ((vw[3][w] << 4) & ~low), u);
-            half8(((vw[2][w] >> 4) & low) | (vw[3][w] & ~low), v);
+            for (int j = 0; j < 4; ++j) {
+              const int p = base + 16 * half + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+              if (!(p < z.hi && (p >= z.lo || p < z.sinks))) vc[j] = 0;   // nobody's
+              apart |= vc[j] > kScaleTop;
+            }
+            apart = __any_sync(0xffffffffu, apart);
+          }
+          if (apart) {
+            // tokens one by one, where they are seen: P's column of a token is in the lanes that have it as a K token
+#pragma unroll 1
+            for (int token = 0; token < 16; ++token) {
+              // the lane group whose K token this is: row 2 q + j of token 4 j + (q ^ j)
+              const int k = token & 7, from = (2 * ((k & 3) ^ (k >> 2)) + (k >> 2)) * 4 + q4;
+              const int p = base + 16 * half + token;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t f[4] = {times2(x[e], s0), times2(y[e], s0), times2(u[e], s1), times2(v[e], s1)};
+              for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma16816h(o[t][4 * w + e], f, pf[t][0], pf[t][1]);
+                for (int j = 0; j < 2; ++j) {
+                  const float w0 = __shfl_sync(0xffffffffu, s[t][half][j], from), w1 = __shfl_sync(0xffffffffu, s[t][half][2 + j], from);
+                  if (!sees(p, pos[t][j])) continue;
+                  const float w = token < 8 ? w0 : w1;
+                  const uint32_t scale = vs[(16 * half + token) * C::SROWB + (D == 128 ? g : g >> 1)];
+#pragma unroll
+                  for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t two = vt[(16 * half + token) * C::ROWB + g * (D / 16) + i];
+                    o[t][i][j] += w * value4(two, scale);
+                    o[t][i][2 + j] += w * value4(two >> 4, scale);
+                  }
+                }
+            }
+          } else {
+            const uint32_t s0 = scale4_pair(vc[0], vc[1]), s1 = scale4_pair(vc[2], vc[3]);
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              constexpr uint32_t low = 0x0f0f0f0fu;
+              // bytes of two tokens' codes of one channel: channels 0 2 4 6, and 1 3 5 7, of the word's eight
+              uint32_t x[4], y[4], u[4], v[4];
+              half8((vw[0][w] & low) | ((vw[1][w] << 4) & ~low), x);
+              half8(((vw[0][w] >> 4) & low) | (vw[1][w] & ~low), y);
+              half8((vw[2][w] & low) | ((vw[3][w] << 4) & ~low), u);
+              half8(((vw[2][w] >> 4) & low) | (vw[3][w] & ~low), v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t f[4] = {times2(x[e], s0), times2(y[e], s0), times2(u[e], s1), times2(v[e], s1)};
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma16816h(o[t][4 * w + e], f, pf[t][half][0], pf[t][half][1]);
+              }
             }
           }
         }
@@ -414,7 +446,7 @@ cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
   k_cache_rows4<D, NT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
-  return launch_merge<D, C::ROWS>(k, p.grid, st);
+  return launch_merge<D, C::ROWS, BT>(k, p.grid, st);
 }
 
 }  // namespace

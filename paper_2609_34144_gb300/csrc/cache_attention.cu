@@ -90,11 +90,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg<D, F8, MT>::CTAS) k_cache_row
   const int two = a.two, units = a.units, head = warp & two, sub = warp >> two, step = kWarps >> two;
 
   // ---- this CTA's share of the call's blocks
-  const Share mine = share_of<D, C::ROWS>(a);
-  int entry = mine.entry;
-  int64_t at = mine.at, entry_at = mine.entry_at;
-  const int64_t stop = mine.stop;
-  if (at >= stop) return;
+  int entry;
+  int64_t at, stop, entry_at;
+  if (!share_of<D, C::ROWS>(a, entry, at, stop, entry_at)) return;
 
   uint8_t* ring = smem + warp * C::RING;
   const uint32_t ring_at = smem_u32(ring);
@@ -545,7 +543,7 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   int dev = 0, nsm = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
   p.grid = (f4 ? rows4_ctas(a.cache.d, p.mt) : a.cache.dtype == CAST_F8E4M3 ? Cfg<128, true, 1>::CTAS : Cfg<128, false, 1>::CTAS) * (nsm < 1 ? 1 : nsm);
-  p.least = 16;
+  p.least = f4 ? 8 : 16;   // blocks of 32 tokens, or of 16
   // Blocks that a unit has at most.  Up to 64 (a thousand tokens: four blocks' latency a warp's ring)
   // a CTA takes a whole unit and nothing is joined.  Measured, shares / whole units, us: one sequence of 301
   // tokens 12.5 / 6.9; 1000 tokens, 32 units 15.9 / 16.1, 384 units 48 / 46, ragged 38 / 34; but 4000 tokens (250

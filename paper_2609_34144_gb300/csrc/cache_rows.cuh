@@ -33,7 +33,7 @@ constexpr float kLift = 7.f;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kWarpsLog = 2, kWarps = 1 << kWarpsLog;
 
-// What the rows of one unit see: blocks [0, n_sink) and [first, end) of 16 positions, and within
+// What the rows of one unit see: blocks [0, n_sink) and [first, end) of BT positions, and within
 // them the positions below `sinks` or from lo on, below hi.
 struct Span {
   int n_sink, first, end;
@@ -44,6 +44,7 @@ struct Span {
   __device__ __forceinline__ int blocks() const { return n_sink + max(end - first, 0); }
   __device__ __forceinline__ int block(int i) const { return i < n_sink ? i : first + (i - n_sink); }
 };
+template <int BT = 16>
 __device__ __forceinline__ Span span_of(const RowsKArgs& a, int b, int row_tile, int rows) {
   const Sequence s = sequence_of(a.batch, b);
   Span z;
@@ -63,9 +64,9 @@ __device__ __forceinline__ Span span_of(const RowsKArgs& a, int b, int row_tile,
     z.lo = min(max(z.p0 + r0 / a.group - a.window + 1, 0), z.hi);
     z.sinks = min(min(a.sinks, z.lo), z.hi);
   }
-  z.first = z.lo / 16;
-  z.end = (z.hi + 15) / 16;
-  z.n_sink = min((z.sinks + 15) / 16, z.first);
+  z.first = z.lo / BT;
+  z.end = (z.hi + BT - 1) / BT;
+  z.n_sink = min((z.sinks + BT - 1) / BT, z.first);
   return z;
 }
 
@@ -115,34 +116,30 @@ __device__ __forceinline__ void zero_rows(const RowsKArgs& a, int e, int h0, int
 }
 
 // A CTA's share of the call's blocks: [at, stop), and the entry (sequence, row tile) it begins in, whose blocks
-// begin at entry_at.  Empty (at >= stop) for a CTA without one.
-struct Share {
-  int entry;
-  int64_t at, stop, entry_at;
-};
-template <int D, int ROWS>
-__device__ __forceinline__ Share share_of(const RowsKArgs& a) {
+// begin at entry_at.  False for a CTA without one.
+template <int D, int ROWS, int BT = 16>
+__device__ __forceinline__ bool share_of(const RowsKArgs& a, int& entry, int64_t& at, int64_t& stop, int64_t& entry_at) {
   __shared__ int s_entry;
   __shared__ int64_t s_work[kWarps], s_before;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int entries = a.batch.B * a.row_tiles, units = a.units;
-  Share x{};
+  entry_at = 0;
   if (a.whole) {
-    x.entry = blockIdx.x / units;
-    const int h = blockIdx.x - x.entry * units;
-    const int nb = span_of(a, x.entry / a.row_tiles, x.entry % a.row_tiles, ROWS).blocks();
+    entry = blockIdx.x / units;
+    const int h = blockIdx.x - entry * units;
+    const int nb = span_of<BT>(a, entry / a.row_tiles, entry % a.row_tiles, ROWS).blocks();
     if (nb == 0) {
-      zero_rows<D, ROWS>(a, x.entry, h << a.two, (h + 1) << a.two);
-      return x;
+      zero_rows<D, ROWS>(a, entry, h << a.two, (h + 1) << a.two);
+      return false;
     }
-    x.at = (int64_t)h * nb;
-    x.stop = x.at + nb;
-    return x;
+    at = (int64_t)h * nb;
+    stop = at + nb;
+    return true;
   }
   int64_t mine = 0;
   int none = 0;
   for (int e = threadIdx.x; e < entries; e += kWarps * 32) {
-    const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
+    const int n = span_of<BT>(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
     mine += n;
     none |= n == 0;
   }
@@ -153,24 +150,24 @@ __device__ __forceinline__ Share share_of(const RowsKArgs& a) {
   for (int w = 0; w < kWarps; ++w) total += s_work[w];
   total *= units;
   const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
-  x.at = blockIdx.x * share;
-  x.stop = min(x.at + share, total);
+  at = blockIdx.x * share;
+  stop = min(at + share, total);
   if (none && blockIdx.x == 0) {
     for (int e = 0; e < entries; ++e)
-      if (span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks() == 0) zero_rows<D, ROWS>(a, e, 0, a.H);
+      if (span_of<BT>(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks() == 0) zero_rows<D, ROWS>(a, e, 0, a.H);
   }
-  if (x.at >= x.stop) return x;
+  if (at >= stop) return false;
   if (warp == 0) {
     int64_t before = 0;
     for (int e0 = 0; e0 < entries; e0 += 32) {
       const int e = e0 + lane;
-      const int n = e < entries ? span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks() : 0;
+      const int n = e < entries ? span_of<BT>(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks() : 0;
       int64_t sum = n;
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t y = __shfl_up_sync(0xffffffffu, sum, o);
         if (lane >= o) sum += y;
       }
-      const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * units > x.at);
+      const unsigned hit = __ballot_sync(0xffffffffu, (before + sum) * units > at);
       if (hit) {
         if (lane == __ffs(hit) - 1) {
           s_entry = e;
@@ -182,9 +179,9 @@ __device__ __forceinline__ Share share_of(const RowsKArgs& a) {
     }
   }
   __syncthreads();
-  x.entry = s_entry;
-  x.entry_at = s_before * units;
-  return x;
+  entry = s_entry;
+  entry_at = s_before * units;
+  return true;
 }
 
 // Joins the warps of a unit (their unnormalised o [warp][row][D], maxima and sums [warp][row] in shared memory) into
@@ -237,7 +234,7 @@ __device__ __forceinline__ void join_warps(const RowsKArgs& a, const Span& z, in
 // Joins the parts of the units that no single CTA of k_cache_rows or k_cache_rows4 had whole: one CTA a unit, one warp a
 // row and some of the parts (lanes: four channels each), then over the warps of a row.
 constexpr int kMergeWarps = 16;
-template <int D, int ROWS>
+template <int D, int ROWS, int BT>
 __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
   constexpr int LANES = D / 4, GROUPS = 32 / LANES;   // GROUPS parts at a time in a warp
   __shared__ int64_t s_sum[kMergeWarps], s_before[kMergeWarps];
@@ -248,7 +245,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
   const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
   int64_t sum = 0, before = 0;
   for (int e = threadIdx.x; e < entries; e += kMergeWarps * 32) {
-    const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
+    const int n = span_of<BT>(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
     sum += n;
     before += e < entry ? n : 0;
   }
@@ -269,7 +266,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
   total *= units;
   const int64_t share = max((int64_t)a.least, (total + ctas - 1) / ctas);
   const int tile = entry % a.row_tiles;
-  const Span z = span_of(a, entry / a.row_tiles, tile, ROWS);
+  const Span z = span_of<BT>(a, entry / a.row_tiles, tile, ROWS);
   const int nb = z.blocks();
   at = at * units + (int64_t)(h >> a.two) * nb;
   if (nb == 0) return;
@@ -336,7 +333,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
 }
 
 // The joining's launch behind the kernel that left the parts
-template <int D, int ROWS>
+template <int D, int ROWS, int BT = 16>
 cast_status launch_merge(const RowsKArgs& k, int ctas, cudaStream_t st) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(k.batch.B * k.row_tiles * k.H), 1, 1);
@@ -347,7 +344,7 @@ cast_status launch_merge(const RowsKArgs& k, int ctas, cudaStream_t st) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, k_cache_merge<D, ROWS>, k, ctas) != cudaSuccess) return check_launch("cache attention merge");
+  if (cudaLaunchKernelEx(&cfg, k_cache_merge<D, ROWS, BT>, k, ctas) != cudaSuccess) return check_launch("cache attention merge");
   return check_launch("cache attention merge");
 }
 

@@ -373,7 +373,7 @@ __device__ __forceinline__ void init_barriers(Bars* bars) {
     mbar_init(&bars->k_full[s], C::F4 ? 128 : 1);
     mbar_init(&bars->k_empty[s], 1);
   }
-  for (int s = 0; s < 6; ++s) {
+  for (int s = 0; s < C::RAW_STAGES + C::RAW_MORE; ++s) {
     mbar_init(&bars->raw_full[s], 1);
     mbar_init(&bars->raw_empty[s], 128);
   }
@@ -392,6 +392,7 @@ __device__ __forceinline__ void init_barriers(Bars* bars) {
 __device__ __forceinline__ void drop(uint64_t* bar) {
   asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+template <class C>
 __device__ __forceinline__ void drop_barriers(Bars* bars) {
   drop(&bars->q_full);
   drop(&bars->q_raw);
@@ -399,7 +400,7 @@ __device__ __forceinline__ void drop_barriers(Bars* bars) {
     drop(&bars->k_full[s]);
     drop(&bars->k_empty[s]);
   }
-  for (int s = 0; s < 6; ++s) {
+  for (int s = 0; s < C::RAW_STAGES + C::RAW_MORE; ++s) {
     drop(&bars->raw_full[s]);
     drop(&bars->raw_empty[s]);
   }
@@ -560,7 +561,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
     fence_proxy_async_smem();   // what was staged in the tiles' places, before copies land there again
     end_barrier<C::THREADS>();
     if (threadIdx.x == 32 && !aborted(bars)) {
-      drop_barriers(bars);
+      drop_barriers<C>(bars);
       init_barriers<C>(bars);
       bars->unit = bars->next;
     }
