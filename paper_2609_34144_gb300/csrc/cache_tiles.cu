@@ -469,13 +469,16 @@ __device__ __forceinline__ void fetch_pages(const TilesKArgs& a, const Unit& u, 
   }
 }
 
-// Fetches the 4-bit pages of a K or V tile at `pos` (one warp; lane i < 128 / page_size has page i, whose rows of a
-// head lie together): codes, and behind the tile's codes the scales.  What is not fetched is named in `absent`.
+// The page of a 4-bit K or V tile at `pos` that lane i < 128 / page_size fetches (n_pages: none)
+__device__ __forceinline__ int code_page(const TilesKArgs& a, const Unit& u, int pos, int lane) {
+  return lane < (BN >> a.page_shift) ? page_at(a, u, pos + (lane << a.page_shift)) : a.n_pages;
+}
+// Fetches a lane's page (one warp), whose rows of a head lie together: codes, and behind the tile's codes the scales.
+// What is not fetched is named in `absent`.
 template <int HD>
 __device__ __forceinline__ void fetch_codes(const TilesKArgs& a, const Unit& u, const uint8_t* cache, const float* scales,
-                                            uint8_t* dst, uint32_t* absent, uint64_t* full, int pos, int lane) {
-  const int n = BN >> a.page_shift, codes = a.page_size * (HD / 2), more = a.page_size * (HD / 16);
-  const int page = lane < n ? page_at(a, u, pos + (lane << a.page_shift)) : a.n_pages;
+                                            uint8_t* dst, uint32_t* absent, uint64_t* full, int page, int lane) {
+  const int codes = a.page_size * (HD / 2), more = a.page_size * (HD / 16);
   const uint32_t there = __ballot_sync(0xffffffffu, page < a.n_pages);
   if (lane == 0) {
     *absent = ~there;
@@ -487,6 +490,9 @@ __device__ __forceinline__ void fetch_codes(const TilesKArgs& a, const Unit& u, 
     bulk_load(dst + BN * (HD / 2) + lane * more, reinterpret_cast<const uint8_t*>(scales) + ((int64_t)page * a.H + u.h) * more, more, full);
   }
 }
+// 4-bit tiles are fetched and decoded in the order K0, then K of tile j + 1 and V of tile j: the places in it
+__device__ __forceinline__ int key_place(int j) { return j ? 2 * j - 1 : 0; }
+__device__ __forceinline__ int value_place(int j, int n_tiles) { return min(2 * j + 2, 2 * n_tiles - 1); }
 
 template <int HD, int KIND>
 __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
@@ -600,22 +606,19 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
       const int bytes = is_k ? C::K_BYTES : codes ? C::RAW_BYTES : C::V_BYTES;
       const int log_stages = is_k ? (C::K_STAGES == 4 ? 2 : 1) : codes && !has_q1 ? 2 : 1;
       if constexpr (F4) {
-        // warp 0 alone, in the order in which the tiles are decoded: K0, then K of tile j + 1 and V of tile j
+        // one ring for K (this is warp 0) and V; the page is looked up a tile ahead, so that nothing waits for it
         const int ring = C::RAW_STAGES + (has_q1 ? 0 : C::RAW_MORE);
-        int s = 0;
-        uint32_t phase = 0;
-        for (int c = 0; is_k && c < 2 * n_tiles; ++c) {
-          const bool ok = !aborted(bars) && mbar_wait(&bars->raw_empty[s], phase ^ 1u, lim) && !aborted(bars);
+        int page = n_tiles > 0 ? code_page(a, u, tile_pos(u, k0), lane) : 0;
+        for (int j = 0; j < n_tiles; ++j) {
+          const int c = is_k ? key_place(j) : value_place(j, n_tiles), s = c % ring;
+          const bool ok = !aborted(bars) && mbar_wait(&bars->raw_empty[s], ((uint32_t)(c / ring) & 1u) ^ 1u, lim) && !aborted(bars);
           if (!__all_sync(0xffffffffu, ok)) {
-            if (lane == 0) bars->issued[0] = c;
+            if (lane == 0) bars->issued[is_k ? 0 : 1] = j;
             set_abort(bars);
             break;
           }
-          const bool key = c == 0 || ((c & 1) && c < 2 * n_tiles - 1);
-          const int j = key ? (c + 1) / 2 : (c - 1) / 2;
-          fetch_codes<HD>(a, u, key ? a.k : a.v, key ? a.k_scale : a.v_scale, raw_stage(s), &bars->absent[s], &bars->raw_full[s],
-                          tile_pos(u, k0 + j), lane);
-          if (++s == ring) s = 0, phase ^= 1u;
+          fetch_codes<HD>(a, u, is_k ? a.k : a.v, is_k ? a.k_scale : a.v_scale, raw_stage(s), &bars->absent[s], &bars->raw_full[s], page, lane);
+          if (j + 1 < n_tiles) page = code_page(a, u, tile_pos(u, k0 + j + 1), lane);
         }
       }
       for (int j = 0; !F4 && j < n_tiles; ++j) {
@@ -803,11 +806,13 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
       // the CTA gave up: none of its copies may land after it has left.  They are the segment's last, of which no
       // stage has begun anew, and its queries.
       if constexpr (F4) {
-        const int issued = min(bars->issued[0], 2 * u.n_tiles);
+        const int issued = min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
         const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
 #pragma unroll 1
-        for (int c = max(issued - ring, 0); warp == 0 && c < issued; ++c)
+        for (int j = max(issued - ring, 0); j < issued; ++j) {
+          const int c = warp == 0 ? key_place(j) : value_place(j, u.n_tiles);
           mbar_wait(&bars->raw_full[c % ring], (uint32_t)(c / ring) & 1u, lim);
+        }
       }
       const int issued = F4 ? 0 : min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
       uint64_t* full = warp == 0 ? bars->k_full : F8 ? bars->raw_full : bars->v_full;
@@ -1312,10 +1317,10 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
   } else if constexpr (F4) {
     // -------------------------------------------------------------- K and V codes and scales to f16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
-    const int tid = threadIdx.x - 384, w4 = warp & 3;
+    const int w4 = warp & 3;
     // A thread has 32 channels (16 bytes of codes, two scales) of a row at a time.  Eight lanes load 128 bytes in a row
     // of codes, and the 16-byte chunks that they store lie in eight bank groups: heads of 128, rows r and r ^ 3, and the
-    // second 64 channels' chunks in another order; heads of 64, four rows.
+    // second 64 channels' chunks in another order; heads of 64, four rows.  A warp has 8 (16) rows of each 32 (64).
     constexpr int CHUNKS = HD / 32, ITEMS = CHUNKS;
     const int chunk = lane & (CHUNKS - 1), box = HD == 128 ? chunk >> 1 : 0;
     auto row_of = [&](int i) {
@@ -1327,62 +1332,89 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
     const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
     int rs = 0;
     uint32_t phase = 0;
-    bool ok = true;
-    for (int it = 0; ok && it < 2 * n_tiles; ++it) {
-      const bool key = it == 0 || ((it & 1) && it < 2 * n_tiles - 1);
-      const int j = key ? (it + 1) / 2 : (it - 1) / 2;
-      const int s = j % kStages, pos = tile_pos(u, k0 + j);
-      const bool whole = key || all_see(u, pos);
-      bool w = !aborted(bars) && mbar_wait(&bars->raw_full[rs], phase, lim) &&
-               mbar_wait(key ? &bars->k_empty[s] : &bars->v_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
-      // the queries lie in the V tiles' place until they are turned into f16
-      if (w && !key && j < kStages) w = mbar_wait(&bars->q_full, 0, lim);
-      // the four warps leave together: they meet at barriers below
-      if (bar_sync_or(2, 128, !w)) { ok = false; break; }
+    uint4 codes[ITEMS];
+    uint32_t sc[ITEMS], absent = 0;
+    // the next tile's codes to registers, and their place given back
+    auto load = [&] {
+      if (!__all_sync(0xffffffffu, !aborted(bars) && mbar_wait(&bars->raw_full[rs], phase, lim))) return false;
       const uint8_t* src = raw_stage(rs);
-      const uint8_t* scales = src + C::CODE_BYTES;
-      const uint32_t absent = bars->absent[rs];
-      uint8_t* dst = key ? sK + s * C::K_BYTES : sV + s * C::V_BYTES;
-      auto not_there = [&](int r) { return ((absent >> (r >> a.page_shift)) & 1u) != 0u; };
-      if (!whole) {
-        // V rows whose scales are not finite, of a tile that the unit's rows do not all see alike (one row a thread)
-        bool bad = false;
-        if (some_see(u, pos + tid) && !not_there(tid))
-          for (int c = 0; c < HD / 16; ++c) bad |= scales[tid * (HD / 16) + c] > kScaleTop;
-        const uint32_t apart = __ballot_sync(0xffffffffu, bad);
-        if (lane == 0) bars->apart[s][tid >> 5] = apart;
-        asm volatile("bar.sync 2, 128;" ::: "memory");
-      }
-      uint4 codes[ITEMS];
-      uint32_t sc[ITEMS];
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int r = row_of(i);
         codes[i] = *reinterpret_cast<const uint4*>(src + r * (HD / 2) + chunk * 16);
-        sc[i] = *reinterpret_cast<const uint16_t*>(scales + r * (HD / 16) + chunk * 2);
+        sc[i] = *reinterpret_cast<const uint16_t*>(src + C::CODE_BYTES + r * (HD / 16) + chunk * 2);
+      }
+      absent = bars->absent[rs];
+      mbar_arrive(&bars->raw_empty[rs]);
+      if (++rs == ring) rs = 0, phase ^= 1u;
+      return true;
+    };
+    bool ok = n_tiles == 0 || load();
+    for (int it = 0; ok && it < 2 * n_tiles; ++it) {
+      const bool key = it == 0 || ((it & 1) && it < 2 * n_tiles - 1);
+      const int j = key ? (it + 1) / 2 : (it - 1) / 2;
+      const int s = j % kStages, pos = tile_pos(u, k0 + j);
+      const bool whole = (key || all_see(u, pos)) && (absent << (32 - (BN >> a.page_shift))) == 0u;
+      uint4 now[ITEMS];
+      uint32_t now_sc[ITEMS];
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i) {
+        now[i] = codes[i];
+        now_sc[i] = sc[i];
+      }
+      const uint32_t gone = absent;
+      // the next tile's loads are on their way while this one's codes are turned
+      if (it + 1 < 2 * n_tiles) ok = load();
+      ok = ok && !aborted(bars) && mbar_wait(key ? &bars->k_empty[s] : &bars->v_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+      // the queries lie in the V tiles' place until they are turned into f16
+      if (ok && !key && j < kStages) ok = mbar_wait(&bars->q_full, 0, lim);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      uint8_t* dst = key ? sK + s * C::K_BYTES : sV + s * C::V_BYTES;
+      if (!whole) {
+        // rows of pages that are not there; V rows that no row of the unit sees, and those whose scales are not finite,
+        // whose tokens are added one by one
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          const int r = row_of(i);
+          bool none = ((gone >> (r >> a.page_shift)) & 1u) != 0u;
+          if (!key) {
+            none = none || !some_see(u, pos + r);
+            const bool bad = !none && !all_see(u, pos) && ((now_sc[i] & 0xffu) > kScaleTop || now_sc[i] >> 8 > kScaleTop);
+            // bit l of `odd`: lane l's chunk of its row; the row's bits, of 32 rows (HD 128: 8 of each i are this warp's)
+            const uint32_t odd = __ballot_sync(0xffffffffu, bad);
+            uint32_t mine = 0;
+            for (int l = 0; l < 32; l += CHUNKS) {
+              const int row = HD == 128 ? (l >> 4) * 4 + (((l >> 3) & 1) ^ (((l >> 2) & 1) * 3)) : l >> 1;
+              if ((odd >> l) & ((1u << CHUNKS) - 1u)) mine |= 1u << row;
+            }
+            none = none || ((mine >> (r & (HD == 128 ? 7 : 15))) & 1u);
+            if (lane == 0) {
+              if (HD == 128) reinterpret_cast<uint8_t*>(bars->apart[s])[4 * i + w4] = (uint8_t)mine;
+              else reinterpret_cast<uint16_t*>(bars->apart[s])[4 * i + w4] = (uint16_t)mine;
+            }
+          }
+          if (none) now_sc[i] = 0;
+        }
       }
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int r = row_of(i);
-        const bool none = not_there(r) || (!whole && (!some_see(u, pos + r) || ((bars->apart[s][r >> 5] >> (r & 31)) & 1u)));
-        const uint32_t x[4] = {box ? codes[i].y : codes[i].x, box ? codes[i].x : codes[i].y, box ? codes[i].w : codes[i].z,
-                               box ? codes[i].z : codes[i].w};
-        const uint32_t pair[2] = {scale4_pair(sc[i]), __byte_perm(sc[i], 0, 0x4141) << 7};
+        const uint32_t x[4] = {box ? now[i].y : now[i].x, box ? now[i].x : now[i].y, box ? now[i].w : now[i].z, box ? now[i].z : now[i].w};
+        const uint32_t pair[2] = {scale4_pair(now_sc[i]), __byte_perm(now_sc[i], 0, 0x4141) << 7};
         uint8_t* to = dst + box * BN * 128 + r * 128;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t h[4];
           half8(x[e], h);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) h[k] = none ? 0u : times2(h[k], pair[e >> 1]);
+          for (int k = 0; k < 4; ++k) h[k] = times2(h[k], pair[e >> 1]);
           const int idx = (HD == 128 ? (chunk & 1) : chunk) * 4 + (e ^ box);
           *reinterpret_cast<uint4*>(to + ((idx ^ r) & 7) * 16) = make_uint4(h[0], h[1], h[2], h[3]);
         }
       }
       fence_proxy_async_smem();
       mbar_arrive(key ? &bars->k_full[s] : &bars->v_full[s]);
-      mbar_arrive(&bars->raw_empty[rs]);
-      if (++rs == ring) rs = 0, phase ^= 1u;
     }
     if (!ok) set_abort(bars);
     if (!another()) break;
