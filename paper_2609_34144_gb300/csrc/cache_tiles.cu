@@ -106,7 +106,6 @@ struct TilesKArgs {
   int pairs;         // pairs of tiles that a head may have
   int most_pairs;    // of a sequence
   int whole;         // a CTA has one whole unit
-  int least;         // work that a CTA takes at least
   float4* part_o;    // [2 * grid][HD / 4][256]
   float2* part_ml;   // [2 * grid][256]
   struct Cut* cuts;  // [grid]
@@ -164,15 +163,26 @@ __device__ __forceinline__ void place_unit(const TilesKArgs& a, Unit& u, const S
 // which other CTAs' memory traffic gains (kBegin 0, 16 and 24 when it was chosen: decode of 35 rows, 60k
 // positions, 8 bits, 85, 81, 83 us; window of 1560 frame tokens 114, 110, 113 us; frames of 3520 tokens 925, 929,
 // 930 us).
-constexpr int kBegin = 16, kPair = 4, kSingle = 2;
+// 4-bit pages: in halves of that, since a key tile of one query tile takes 1.1 to 1.3 us (the decoding), of two 1.75 us.
+template <int KIND>
+struct Work {
+  static constexpr int kBegin = 16, kPair = 4, kSingle = 2, kLeast = 12;
+};
+template <>
+struct Work<CAST_F4E2M1> {
+  static constexpr int kBegin = 32, kPair = 8, kSingle = 5, kLeast = 24;
+};
+template <int KIND>
 __device__ __forceinline__ int tile_work(const TilesKArgs& a, const Unit& u) {
-  return u.i0 + a.tile_tokens < u.n_new ? kPair : kSingle;
+  return u.i0 + a.tile_tokens < u.n_new ? Work<KIND>::kPair : Work<KIND>::kSingle;
 }
+template <int KIND>
 __device__ __forceinline__ int unit_work(const TilesKArgs& a, const Unit& u) {
-  return u.tiles ? kBegin + u.tiles * tile_work(a, u) : 1;
+  return u.tiles ? Work<KIND>::kBegin + u.tiles * tile_work<KIND>(a, u) : 1;
 }
 
 // Work of units lane, lane + 32, ... or, `serial`, of all units of sequence b
+template <int KIND>
 __device__ __forceinline__ int64_t sequence_work(const TilesKArgs& a, int b, int lane, bool serial) {
   if (b >= a.batch.B) return 0;
   const Sequence s = sequence_of(a.batch, b);
@@ -181,17 +191,18 @@ __device__ __forceinline__ int64_t sequence_work(const TilesKArgs& a, int b, int
   int64_t w = 0;
   for (u.i0 = serial ? 0 : lane * per; u.i0 < n; u.i0 += serial ? per : 32 * per) {
     place_unit(a, u, s);
-    w += unit_work(a, u);
+    w += unit_work<KIND>(a, u);
   }
   return w;
 }
 // Lane l's answer is the work of sequence b0 + l: one sequence a lane, or, where there are fewer of them
 // than units in one, one after the other by all lanes
+template <int KIND>
 __device__ __forceinline__ int64_t chunk_work(const TilesKArgs& a, int b0, int lane) {
-  if (a.batch.B >= a.most_pairs) return sequence_work(a, b0 + lane, 0, true);
+  if (a.batch.B >= a.most_pairs) return sequence_work<KIND>(a, b0 + lane, 0, true);
   int64_t mine = 0;
   for (int b = b0; b < min(b0 + 32, a.batch.B); ++b) {
-    const int64_t w = warp_sum(sequence_work(a, b, lane, false));
+    const int64_t w = warp_sum(sequence_work<KIND>(a, b, lane, false));
     if (b0 + lane == b) mine = w;
   }
   return mine;
@@ -212,6 +223,7 @@ struct Deal {
   int each, rounds;      // of a unit that is dealt whole, and how many a CTA has
   int64_t base, share, total;
 };
+template <int KIND>
 __device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) {   // one warp; every lane has it
   Deal d{};
   if (a.batch.B == 1) {
@@ -221,7 +233,7 @@ __device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) { 
     int low = 0x7fffffff, high = 0;
     for (u.i0 = lane * per; u.i0 < n; u.i0 += 32 * per) {
       place_unit(a, u, s);
-      const int w = unit_work(a, u);
+      const int w = unit_work<KIND>(a, u);
       d.per_head += w;
       low = min(low, w);
       high = max(high, w);
@@ -236,15 +248,17 @@ __device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) { 
       d.base = (int64_t)d.rounds * ctas * high;
     }
   } else {
-    for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += warp_sum(chunk_work(a, b0, lane));
+    for (int b0 = 0; b0 < a.batch.B; b0 += 32) d.per_head += warp_sum(chunk_work<KIND>(a, b0, lane));
     d.total = d.per_head * a.H;
   }
-  d.share = max((int64_t)a.least, (d.total - d.base + ctas - 1) / ctas);
+  // kLeast: three key tiles of two query tiles, six of one: fewer are not worth a part
+  d.share = max((int64_t)Work<KIND>::kLeast, (d.total - d.base + ctas - 1) / ctas);
   return d;
 }
 
 // Unit `x` of the call, whole (one warp; every lane has it), heads slowest: those that run together read
 // one head's keys.
+template <int KIND>
 __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
   Unit u{};
   u.h = x / a.pairs;
@@ -267,7 +281,7 @@ __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
   if (!u.valid) return u;
   place_unit(a, u, sequence_of(a.batch, u.b));
   u.n_tiles = u.tiles;
-  u.work = unit_work(a, u);
+  u.work = unit_work<KIND>(a, u);
   u.slot = -1;
   return u;
 }
@@ -275,6 +289,7 @@ __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
 // The first unit of which items at .. stop-1 have a tile, and that part of it (one warp; every lane has it).  A
 // unit's tile k is at item kBegin + k * tile_work.  Its first part (with tile 0) goes to the CTA's second
 // place, others to its first.
+template <int KIND>
 __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int64_t at, int64_t stop, int lane, Cut* cut) {
   Unit u{};
   if (cut && lane == 0) cut->c0 = -1;
@@ -285,7 +300,7 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
     int64_t r = at - h * d.per_head;
     int b = a.batch.B == 1 ? 0 : -1;
     for (int b0 = 0; b < 0 && b0 < a.batch.B; b0 += 32) {
-      const int64_t w = chunk_work(a, b0, lane);
+      const int64_t w = chunk_work<KIND>(a, b0, lane);
       const int64_t sum = scan(w, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
       if (hit) {
@@ -305,7 +320,7 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
       int w = 0;
       if (u.i0 < n) {
         place_unit(a, u, s);
-        w = unit_work(a, u);
+        w = unit_work<KIND>(a, u);
       }
       const int64_t sum = scan((int64_t)w, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, sum > r);
@@ -323,15 +338,15 @@ __device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int6
     u.h = h;
     place_unit(a, u, s);
     const int in = (int)r;   // items of the unit before `at`
-    const int w = unit_work(a, u), each = tile_work(a, u), some = (int)min((int64_t)(w - in), stop - at);
-    u.k0 = (max(in - kBegin, 0) + each - 1) / each;
-    u.n_tiles = u.tiles ? (max(in + some - kBegin, 0) + each - 1) / each - u.k0 : 0;
+    const int w = unit_work<KIND>(a, u), each = tile_work<KIND>(a, u), some = (int)min((int64_t)(w - in), stop - at);
+    u.k0 = (max(in - Work<KIND>::kBegin, 0) + each - 1) / each;
+    u.n_tiles = u.tiles ? (max(in + some - Work<KIND>::kBegin, 0) + each - 1) / each - u.k0 : 0;
     if (u.n_tiles > 0 || u.tiles == 0) {
       u.valid = 1;
       u.work = (int)(at - from) + some;
       u.slot = u.n_tiles == u.tiles ? -1 : 2 * (int)blockIdx.x + (u.k0 > 0 ? 0 : 1);
       if (cut && lane == 0 && u.k0 > 0) {
-        const int64_t first = at - r - d.base + kBegin;   // of tile 0
+        const int64_t first = at - r - d.base + Work<KIND>::kBegin;   // of tile 0
         *cut = Cut{u.h, u.t0, u.i0, u.n_new, (int)(first / d.share), (int)((first + (u.tiles - 1) * each) / d.share)};
       }
       break;
@@ -370,15 +385,15 @@ __device__ __forceinline__ void init_barriers(Bars* bars) {
   mbar_init(&bars->q_full, C::DECODED ? 256 : 1);
   mbar_init(&bars->q_raw, 1);
   for (int s = 0; s < 4; ++s) {
-    mbar_init(&bars->k_full[s], C::F4 ? 128 : 1);
+    mbar_init(&bars->k_full[s], C::F4 ? 64 : 1);
     mbar_init(&bars->k_empty[s], 1);
   }
   for (int s = 0; s < C::RAW_STAGES + C::RAW_MORE; ++s) {
     mbar_init(&bars->raw_full[s], 1);
-    mbar_init(&bars->raw_empty[s], 128);
+    mbar_init(&bars->raw_empty[s], C::F4 ? 64 : 128);
   }
   for (int s = 0; s < kStages; ++s) {
-    mbar_init(&bars->v_full[s], C::DECODED ? 128 : 1);
+    mbar_init(&bars->v_full[s], C::F4 ? 64 : C::F8 ? 128 : 1);
     mbar_init(&bars->v_empty[s], C::DECODED ? 1 : 2);   // the products, and warp 3 that saw the tile
     mbar_init(&bars->v_fixed[s], 32);
   }
@@ -490,9 +505,17 @@ __device__ __forceinline__ void fetch_codes(const TilesKArgs& a, const Unit& u, 
     bulk_load(dst + BN * (HD / 2) + lane * more, reinterpret_cast<const uint8_t*>(scales) + ((int64_t)page * a.H + u.h) * more, more, full);
   }
 }
-// 4-bit tiles are fetched and decoded in the order K0, then K of tile j + 1 and V of tile j: the places in it
-__device__ __forceinline__ int key_place(int j) { return j ? 2 * j - 1 : 0; }
-__device__ __forceinline__ int value_place(int j, int n_tiles) { return min(2 * j + 2, 2 * n_tiles - 1); }
+// 4-bit tiles: K and V have a ring of code stages each, in order of fetching and of decoding (in one ring the faster of
+// the two would meet a stage two rounds behind, which a barrier's one bit does not tell from a free one).  Heads of 128
+// with a second query tile: one stage for K (its codes go to registers as soon as they are there) and two for V; with
+// its place free, and heads of 64: three each.
+template <int HD>
+__device__ __forceinline__ int code_ring(bool key, bool has_q1) { return HD == 128 && has_q1 ? (key ? 1 : 2) : 3; }
+template <int HD>
+__device__ __forceinline__ int code_stage(bool key, int i) {
+  if (HD == 64) return key ? i : i + 3;
+  return key ? (i ? i + 2 : 0) : (i < 2 ? i + 1 : 5);
+}
 
 template <int HD, int KIND>
 __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
@@ -527,16 +550,16 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
   if (warp == 0) {
     Unit u;
     if (a.whole) {
-      u = unit_of(a, blockIdx.x, lane);
+      u = unit_of<KIND>(a, blockIdx.x, lane);
     } else {
-      d = deal(a, gridDim.x, lane);
+      d = deal<KIND>(a, gridDim.x, lane);
       // whole units come first: should the CTA give up before its share, the joining must find no cut that the
       // workspace held before
       if (d.rounds > 0 && lane == 0) a.cuts[blockIdx.x].c0 = -1;
       at = d.rounds > 0 ? (int64_t)blockIdx.x * d.each : blockIdx.x * d.share;
       stop = d.rounds > 0 ? at + d.each : min(at + d.share, d.total);
       // with the share comes what it begins inside of, for the joining
-      u = unit_at(a, d, at, stop, lane, d.rounds > 0 ? nullptr : a.cuts + blockIdx.x);
+      u = unit_at<KIND>(a, d, at, stop, lane, d.rounds > 0 ? nullptr : a.cuts + blockIdx.x);
     }
     if (lane == 0) bars->unit = u;
   }
@@ -606,12 +629,13 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
       const int bytes = is_k ? C::K_BYTES : codes ? C::RAW_BYTES : C::V_BYTES;
       const int log_stages = is_k ? (C::K_STAGES == 4 ? 2 : 1) : codes && !has_q1 ? 2 : 1;
       if constexpr (F4) {
-        // one ring for K (this is warp 0) and V; the page is looked up a tile ahead, so that nothing waits for it
-        const int ring = C::RAW_STAGES + (has_q1 ? 0 : C::RAW_MORE);
+        // the page is looked up a tile ahead, so that nothing waits for it
+        const int ring = code_ring<HD>(is_k, has_q1);
+        int i = 0, around = 0;   // place in the ring, and rounds of it
         int page = n_tiles > 0 ? code_page(a, u, tile_pos(u, k0), lane) : 0;
         for (int j = 0; j < n_tiles; ++j) {
-          const int c = is_k ? key_place(j) : value_place(j, n_tiles), s = c % ring;
-          const bool ok = !aborted(bars) && mbar_wait(&bars->raw_empty[s], ((uint32_t)(c / ring) & 1u) ^ 1u, lim) && !aborted(bars);
+          const int s = code_stage<HD>(is_k, i);
+          const bool ok = !aborted(bars) && mbar_wait(&bars->raw_empty[s], ((uint32_t)around & 1u) ^ 1u, lim) && !aborted(bars);
           if (!__all_sync(0xffffffffu, ok)) {
             if (lane == 0) bars->issued[is_k ? 0 : 1] = j;
             set_abort(bars);
@@ -619,6 +643,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
           }
           fetch_codes<HD>(a, u, is_k ? a.k : a.v, is_k ? a.k_scale : a.v_scale, raw_stage(s), &bars->absent[s], &bars->raw_full[s], page, lane);
           if (j + 1 < n_tiles) page = code_page(a, u, tile_pos(u, k0 + j + 1), lane);
+          if (++i == ring) i = 0, ++around;
         }
       }
       for (int j = 0; !F4 && j < n_tiles; ++j) {
@@ -643,7 +668,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
           stop = round < d.rounds ? at + d.each : min(at + d.share, d.total);
         }
         if (at >= stop) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        const Unit next = unit_at(a, d, at, stop, lane, cut);
+        const Unit next = unit_at<KIND>(a, d, at, stop, lane, cut);
         if (lane == 0) bars->next = next;
       }
     } else if (warp == 3 && !DECODED) {
@@ -807,12 +832,10 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
       // stage has begun anew, and its queries.
       if constexpr (F4) {
         const int issued = min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
-        const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
+        const int ring = code_ring<HD>(warp == 0, u.i0 + a.tile_tokens < u.n_new);
 #pragma unroll 1
-        for (int j = max(issued - ring, 0); j < issued; ++j) {
-          const int c = warp == 0 ? key_place(j) : value_place(j, u.n_tiles);
-          mbar_wait(&bars->raw_full[c % ring], (uint32_t)(c / ring) & 1u, lim);
-        }
+        for (int j = max(issued - ring, 0); j < issued; ++j)
+          mbar_wait(&bars->raw_full[code_stage<HD>(warp == 0, j % ring)], (uint32_t)(j / ring) & 1u, lim);
       }
       const int issued = F4 ? 0 : min(bars->issued[warp == 0 ? 0 : 1], u.n_tiles);
       uint64_t* full = warp == 0 ? bars->k_full : F8 ? bars->raw_full : bars->v_full;
@@ -1317,91 +1340,83 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
   } else if constexpr (F4) {
     // -------------------------------------------------------------- K and V codes and scales to f16 tiles
     setmaxnreg_dec<C::REGS_DECODE>();
-    const int w4 = warp & 3;
+    // Two warps have the K tiles and two the V tiles, so that neither waits for what the other waits for.
+    const bool key = warp < 14;
+    const int half = warp & 1;
     // A thread has 32 channels (16 bytes of codes, two scales) of a row at a time.  Eight lanes load 128 bytes in a row
     // of codes, and the 16-byte chunks that they store lie in eight bank groups: heads of 128, rows r and r ^ 3, and the
-    // second 64 channels' chunks in another order; heads of 64, four rows.  A warp has 8 (16) rows of each 32 (64).
-    constexpr int CHUNKS = HD / 32, ITEMS = CHUNKS;
+    // second 64 channels' chunks in another order; heads of 64, four rows.  A warp has 8 (16) rows of each 16 (32).
+    constexpr int CHUNKS = HD / 32, ROWS = 32 / CHUNKS, ITEMS = BN / ROWS / 2;
     const int chunk = lane & (CHUNKS - 1), box = HD == 128 ? chunk >> 1 : 0;
-    auto row_of = [&](int i) {
-      if (HD == 128) return i * 32 + w4 * 8 + (lane >> 4) * 4 + (((lane >> 3) & 1) ^ (((lane >> 2) & 1) * 3));
-      return i * 64 + w4 * 16 + (lane >> 1);
-    };
+    auto row_in = [](int l) { return HD == 128 ? (l >> 4) * 4 + (((l >> 3) & 1) ^ (((l >> 2) & 1) * 3)) : l >> 1; };   // of ROWS
+    auto row_of = [&](int i) { return (2 * i + half) * ROWS + row_in(lane); };
     for (;;) {
     const int k0 = u.k0, n_tiles = u.n_tiles;
-    const int ring = C::RAW_STAGES + (u.i0 + a.tile_tokens < u.n_new ? 0 : C::RAW_MORE);
-    int rs = 0;
-    uint32_t phase = 0;
-    uint4 codes[ITEMS];
-    uint32_t sc[ITEMS], absent = 0;
-    // the next tile's codes to registers, and their place given back
-    auto load = [&] {
-      if (!__all_sync(0xffffffffu, !aborted(bars) && mbar_wait(&bars->raw_full[rs], phase, lim))) return false;
+    const int ring = code_ring<HD>(key, u.i0 + a.tile_tokens < u.n_new);
+    int place = 0, around = 0;   // in the ring, and rounds of it
+    bool ok = true;
+    for (int j = 0; j < n_tiles; ++j) {
+      const int rs = code_stage<HD>(key, place);
+      const int s = j % kStages, pos = tile_pos(u, k0 + j);
+      // the codes to registers, and their place given back
+      ok = __all_sync(0xffffffffu, !aborted(bars) && mbar_wait(&bars->raw_full[rs], (uint32_t)around & 1u, lim));
+      if (!ok) break;
       const uint8_t* src = raw_stage(rs);
+      uint4 codes[ITEMS];
+      uint32_t sc[ITEMS];
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int r = row_of(i);
         codes[i] = *reinterpret_cast<const uint4*>(src + r * (HD / 2) + chunk * 16);
         sc[i] = *reinterpret_cast<const uint16_t*>(src + C::CODE_BYTES + r * (HD / 16) + chunk * 2);
       }
-      absent = bars->absent[rs];
+      const uint32_t absent = bars->absent[rs];
       mbar_arrive(&bars->raw_empty[rs]);
-      if (++rs == ring) rs = 0, phase ^= 1u;
-      return true;
-    };
-    bool ok = n_tiles == 0 || load();
-    for (int it = 0; ok && it < 2 * n_tiles; ++it) {
-      const bool key = it == 0 || ((it & 1) && it < 2 * n_tiles - 1);
-      const int j = key ? (it + 1) / 2 : (it - 1) / 2;
-      const int s = j % kStages, pos = tile_pos(u, k0 + j);
-      const bool whole = (key || all_see(u, pos)) && (absent << (32 - (BN >> a.page_shift))) == 0u;
-      uint4 now[ITEMS];
-      uint32_t now_sc[ITEMS];
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) {
-        now[i] = codes[i];
-        now_sc[i] = sc[i];
-      }
-      const uint32_t gone = absent;
-      // the next tile's loads are on their way while this one's codes are turned
-      if (it + 1 < 2 * n_tiles) ok = load();
-      ok = ok && !aborted(bars) && mbar_wait(key ? &bars->k_empty[s] : &bars->v_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
+      if (++place == ring) place = 0, ++around;
+      ok = !aborted(bars) && mbar_wait(key ? &bars->k_empty[s] : &bars->v_empty[s], ((uint32_t)(j / kStages) & 1u) ^ 1u, lim);
       // the queries lie in the V tiles' place until they are turned into f16
       if (ok && !key && j < kStages) ok = mbar_wait(&bars->q_full, 0, lim);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       uint8_t* dst = key ? sK + s * C::K_BYTES : sV + s * C::V_BYTES;
-      if (!whole) {
-        // rows of pages that are not there; V rows that no row of the unit sees, and those whose scales are not finite,
-        // whose tokens are added one by one
+      const bool alike = key || all_see(u, pos);
+      if (!alike || (absent << (32 - (BN >> a.page_shift))) != 0u) {
+        // rows of pages that are not there, and V rows that no row of the unit sees
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
           const int r = row_of(i);
-          bool none = ((gone >> (r >> a.page_shift)) & 1u) != 0u;
-          if (!key) {
-            none = none || !some_see(u, pos + r);
-            const bool bad = !none && !all_see(u, pos) && ((now_sc[i] & 0xffu) > kScaleTop || now_sc[i] >> 8 > kScaleTop);
-            // bit l of `odd`: lane l's chunk of its row; the row's bits, of 32 rows (HD 128: 8 of each i are this warp's)
-            const uint32_t odd = __ballot_sync(0xffffffffu, bad);
-            uint32_t mine = 0;
-            for (int l = 0; l < 32; l += CHUNKS) {
-              const int row = HD == 128 ? (l >> 4) * 4 + (((l >> 3) & 1) ^ (((l >> 2) & 1) * 3)) : l >> 1;
-              if ((odd >> l) & ((1u << CHUNKS) - 1u)) mine |= 1u << row;
-            }
-            none = none || ((mine >> (r & (HD == 128 ? 7 : 15))) & 1u);
-            if (lane == 0) {
-              if (HD == 128) reinterpret_cast<uint8_t*>(bars->apart[s])[4 * i + w4] = (uint8_t)mine;
-              else reinterpret_cast<uint16_t*>(bars->apart[s])[4 * i + w4] = (uint16_t)mine;
+          if (((absent >> (r >> a.page_shift)) & 1u) != 0u || !(alike || some_see(u, pos + r))) sc[i] = 0;
+          bad |= (sc[i] & 0xffu) > kScaleTop || sc[i] >> 8 > kScaleTop;
+        }
+        if (!alike) {
+          // V rows whose scales are not finite: their tokens are added one by one.  The bits of the warp's ROWS rows.
+          auto name_apart = [&](int i, uint32_t rows) {
+            if (HD == 128) reinterpret_cast<uint8_t*>(bars->apart[s])[2 * i + half] = (uint8_t)rows;
+            else reinterpret_cast<uint16_t*>(bars->apart[s])[2 * i + half] = (uint16_t)rows;
+          };
+          if (!__any_sync(0xffffffffu, bad)) {
+            if (lane < ITEMS) name_apart(lane, 0);
+          } else {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+              // bit l of `odd`: lane l's chunk of its row
+              const uint32_t odd = __ballot_sync(0xffffffffu, (sc[i] & 0xffu) > kScaleTop || sc[i] >> 8 > kScaleTop);
+              uint32_t mine = 0;
+              for (int l = 0; odd && l < 32; l += CHUNKS)
+                if ((odd >> l) & ((1u << CHUNKS) - 1u)) mine |= 1u << row_in(l);
+              if ((mine >> row_in(lane)) & 1u) sc[i] = 0;
+              if (lane == 0) name_apart(i, mine);
             }
           }
-          if (none) now_sc[i] = 0;
         }
       }
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) {
         const int r = row_of(i);
-        const uint32_t x[4] = {box ? now[i].y : now[i].x, box ? now[i].x : now[i].y, box ? now[i].w : now[i].z, box ? now[i].z : now[i].w};
-        const uint32_t pair[2] = {scale4_pair(now_sc[i]), __byte_perm(now_sc[i], 0, 0x4141) << 7};
+        const uint32_t x[4] = {box ? codes[i].y : codes[i].x, box ? codes[i].x : codes[i].y, box ? codes[i].w : codes[i].z,
+                               box ? codes[i].z : codes[i].w};
+        const uint32_t pair[2] = {scale4_pair(sc[i]), __byte_perm(sc[i], 0, 0x4141) << 7};
         uint8_t* to = dst + box * BN * 128 + r * 128;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -1670,7 +1685,6 @@ cast_status launch_tiles(const cast_cache_attn_args& a, const TilesPlan& p, void
   k.pairs = p.pairs;
   k.most_pairs = (int)(((a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T) + 2 * p.tile_tokens - 1) / (2 * p.tile_tokens));
   k.whole = p.whole;
-  k.least = 12;   // three key tiles of two query tiles, six of one: fewer are not worth a part
   k.part_o = static_cast<float4*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
   k.cuts = reinterpret_cast<Cut*>(static_cast<char*>(ws) + p.part_o_bytes + p.part_ml_bytes);
