@@ -54,7 +54,8 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-template <int D, int NT>
+// SMALL: pages of 16 tokens, of which a block has two; else a block lies in one page
+template <int D, int NT, bool SMALL>
 __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
   using C = Cfg4<D, NT>;
   constexpr int KW = D / 32;   // words of a lane's part of a K row; a V row's part has D / 64
@@ -85,50 +86,68 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const int k0 = (int)(at - unit_at);
       const int k1 = (int)min((int64_t)nb, stop - unit_at);
 
-      // The pages of block i's halves (-1: out of range, reads as zeros; or, of pages of 16, seen by no row)
+      // The page of tokens p .. (-1: out of range, reads as zeros)
+      auto page_at = [&](int p) {
+        int page = __ldg(table + (p >> a.page_shift));
+        if ((unsigned)page >= (unsigned)a.n_pages) {
+          if (lane == 0) left_out();
+          page = -1;
+        }
+        return page;
+      };
+      // The pages of block i's halves (small pages: -1 too where no row sees any of it)
       auto pages_of = [&](int i) {
         const int base = z.block(i) * BT;
-        auto page_at = [&](int p) {
-          int page = __ldg(table + (p >> a.page_shift));
-          if (page < 0 || page >= a.n_pages) {
-            if (lane == 0) left_out();
-            page = -1;
-          }
-          return page;
-        };
-        auto some = [&](int p) { return p < z.hi && (p + 16 > z.lo || p < z.sinks); };
         int2 pages;
-        if (a.page_shift > 4) {
-          pages.x = pages.y = page_at(base);
-        } else {
+        if constexpr (SMALL) {
+          auto some = [&](int p) { return p < z.hi && (p + 16 > z.lo || p < z.sinks); };
           pages.x = some(base) ? page_at(base) : -1;
           pages.y = some(base + 16) ? page_at(base + 16) : -1;
+        } else {
+          pages.x = pages.y = page_at(base);
         }
         return pages;
       };
+      // A lane's part of a block: 16 bytes of each 512 of its codes (K's, and V's at the same distance), and of the
+      // scales: K's, behind them V's
+      const uint8_t* my_codes = a.k + (int64_t)h * a.page_size * C::ROWB + lane * 16;
+      const int64_t to_v = a.v - a.k;
+      constexpr int SCH = C::SBLOCK / 16;   // chunks of K's (V's) scales
+      const uint8_t* my_scales = (lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
+      const int page_scales = a.H * a.page_size * C::SROWB;
       // fetches block i of the unit into stage st
       auto fetch = [&](int i, int st, int2 pages) {
-        const int base = z.block(i) * BT;
+        const int row = (z.block(i) * BT) & (a.page_size - 1);
         const uint32_t dst = ring_at + st * C::STAGE + lane * 16;
+        if constexpr (SMALL) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int page = half ? pages.y : pages.x, row = (base + 16 * half) & (a.page_size - 1);
-          if (page >= 0) {
-            const int64_t from = page * page_bytes + (h * a.page_size + row) * C::ROWB + lane * 16;
+          for (int half = 0; half < 2; ++half) {
+            const int page = half ? pages.y : pages.x;
+            if (page < 0) continue;
+            const uint8_t* from = my_codes + page * page_bytes;
 #pragma unroll
             for (int c = 0; c < C::BLOCK / 2; c += 512) {
-              copy16(dst + half * (C::BLOCK / 2) + c, a.k + from + c);
-              copy16(dst + C::BLOCK + half * (C::BLOCK / 2) + c, a.v + from + c);
+              copy16(dst + half * (C::BLOCK / 2) + c, from + c);
+              copy16(dst + C::BLOCK + half * (C::BLOCK / 2) + c, from + to_v + c);
             }
           }
-        }
-        // scales: K's first half, its second, V's first, V's second
-        constexpr int CH = C::SBLOCK / 32;   // chunks of a half
-        if (lane < 4 * CH) {
-          const bool is_v = lane >= 2 * CH, second = (lane / CH) & 1;
-          const int page = second ? pages.y : pages.x, row = (base + (second ? 16 : 0)) & (a.page_size - 1);
-          const int64_t from = (((int64_t)max(page, 0) * a.H + h) * a.page_size + row) * C::SROWB + (lane & (CH - 1)) * 16;
-          copy16_or_zero(dst + 2 * C::BLOCK, (is_v ? vscale : kscale) + from, page >= 0);
+          if (lane < 2 * SCH) {
+            const bool second = (lane & (SCH - 1)) >= SCH / 2;
+            const int page = second ? pages.y : pages.x;
+            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (int64_t)max(page, 0) * page_scales - (second ? SCH / 2 * 16 : 0), page >= 0);
+          }
+        } else {
+          const int page = pages.x;
+          if (page >= 0) {
+            const uint8_t* from = my_codes + (page * page_bytes + row * C::ROWB);
+#pragma unroll
+            for (int c = 0; c < C::BLOCK; c += 512) {
+              copy16(dst + c, from + c);
+              copy16(dst + C::BLOCK + c, from + to_v + c);
+            }
+          }
+          if (lane < 2 * SCH)
+            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + ((int64_t)max(page, 0) * page_scales + row * C::SROWB), page >= 0);
         }
       };
       const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
@@ -435,30 +454,35 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
   }
 }
 
-template <int D, int NT>
-cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
+template <int D, int NT, bool SMALL>
+cast_status launch_pages(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
   using C = Cfg4<D, NT>;
   static std::atomic<uint64_t> attr_done{0};
   if (!once_per_device(attr_done, [&] {
-        return cudaFuncSetAttribute(k_cache_rows4<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
+        return cudaFuncSetAttribute(k_cache_rows4<D, NT, SMALL>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess;
       }))
     return check_launch("cache attention smem attribute");
-  k_cache_rows4<D, NT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
+  k_cache_rows4<D, NT, SMALL><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
   return launch_merge<D, C::ROWS, BT>(k, p.grid, st);
+}
+
+template <int D, int NT>
+cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
+  return k.page_size == 16 ? launch_pages<D, NT, true>(k, p, st) : launch_pages<D, NT, false>(k, p, st);
 }
 
 }  // namespace
 
 int rows4_ctas(int d, int mt) {
   if (d == 128) return mt == 1 ? Cfg4<128, 1>::CTAS : Cfg4<128, 2>::CTAS;
-  return mt == 1 ? Cfg4<64, 1>::CTAS : mt == 2 ? Cfg4<64, 2>::CTAS : Cfg4<64, 4>::CTAS;
+  return mt == 1 ? Cfg4<64, 1>::CTAS : Cfg4<64, 2>::CTAS;
 }
 
 cast_status launch_rows4(const RowsKArgs& k, const RowsPlan& p, int d, cudaStream_t st) {
   if (d == 128) return p.mt == 1 ? launch<128, 1>(k, p, st) : launch<128, 2>(k, p, st);
-  return p.mt == 1 ? launch<64, 1>(k, p, st) : p.mt == 2 ? launch<64, 2>(k, p, st) : launch<64, 4>(k, p, st);
+  return p.mt == 1 ? launch<64, 1>(k, p, st) : launch<64, 2>(k, p, st);
 }
 
 unsigned int cache_rows4_error_word(cudaStream_t st, bool clear) { return read_left_out(st, clear); }

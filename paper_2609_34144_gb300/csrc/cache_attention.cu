@@ -536,8 +536,8 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const bool f4 = a.cache.dtype == CAST_F4E2M1;
   const int64_t most_rows = (int64_t)max_new * group;
-  // 16 rows of a product, or two of them for the same keys; 4-bit pages: 8 rows, two or four times
-  p.mt = f4 ? (most_rows > 16 ? 4 : most_rows > 8 ? 2 : 1) : most_rows > 16 ? 2 : 1;
+  // 16 rows of a product, or two of them for the same keys; 4-bit pages: 8 rows, or two of them
+  p.mt = most_rows > (f4 ? 8 : 16) ? 2 : 1;
   const int rows = (f4 ? 8 : 16) * p.mt;
   p.row_tiles = (int)((most_rows + rows - 1) / rows);
   int dev = 0, nsm = 152;
@@ -634,6 +634,11 @@ extern "C" {
 static bool by_tiles(const cast_cache_attn_args& a) {
   const int max_new = a.batch.max_new < a.batch.T ? a.batch.max_new : a.batch.T;
   const int64_t rows = (int64_t)max_new * (a.H_q / a.cache.H);
+  // 4-bit pages: rows beyond 16 as further eights of the same keys lose too, since few warps are left an SM.  Measured,
+  // tiles / rows, us: heads of 128, 16 units of 60k with 20 rows 83 / 95, with 35 rows 81 / 136; 128 units of 8k with 32
+  // rows 98 / 94, with 40 rows 101 / 122; heads of 64, 16 units of 60k with 20 rows 66 / 68, with 35 rows 66 / 115; 128
+  // units of 8k with 64 rows 79 / 118
+  if (a.cache.dtype == CAST_F4E2M1) return rows > 16;
   return rows > 32 || (rows > 16 && (a.cache.d != 64 || (int64_t)a.batch.B * a.cache.H < 64));
 }
 

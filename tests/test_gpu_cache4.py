@@ -309,6 +309,11 @@ ROWS = [
     ([700] * 33, [1] * 33, 2, 2, 64, 16, False, 100, 0),
     ([500, 400], [8, 8], 33, 99, 64, 16, True, 0, 0),                     # 24 rows, 66 units
     ([1300, 400], [8, 3], 33, 132, 64, 64, True, 200, 17),                # 32 rows
+    ([3000, 950, 41], [10, 7, 10], 2, 8, 128, 16, True, 0, 0),            # 40 rows
+    ([1100, 950, 41], [5, 1, 5], 3, 15, 128, 64, True, 300, 20),          # 25 rows
+    ([2500, 64], [33, 33], 3, 3, 128, 32, False, 0, 0),                   # 33 rows
+    ([2500, 77, 8], [8, 8, 8], 2, 16, 64, 16, True, 0, 0),                # 64 rows
+    ([800, 50], [13, 50], 2, 2, 64, 128, False, 70, 3),                   # 50 rows
 ]
 
 
@@ -328,7 +333,7 @@ def test_attention_few_rows(lib, lens, new, H, H_q, d, page, causal, window, sin
 
 TILES = [
     # lens, new, H, H_q, d, page, causal, window, sinks
-    ([17], [17], 1, 1, 128, 16, True, 0, 0),
+    ([41], [41], 1, 1, 128, 16, True, 0, 0),
     ([301], [40], 2, 8, 64, 16, True, 0, 0),
     ([200, 500], [129, 77], 1, 3, 64, 16, True, 0, 0),
     ([300, 17, 1000], [130, 5, 64], 3, 3, 128, 32, True, 0, 0),
