@@ -65,6 +65,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
   const int g = lane >> 2, q4 = lane & 3;
   int entry;
   int64_t at, stop, entry_at;
+  // the joining may be put in place as CTAs leave (it waits for all of them)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!share_of<D, C::ROWS, BT>(a, entry, at, stop, entry_at)) return;
 
   uint8_t* ring = smem + warp * C::RING;
@@ -114,7 +116,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const int64_t to_v = a.v - a.k;
       constexpr int SCH = C::SBLOCK / 16;   // chunks of K's (V's) scales
       const uint8_t* my_scales = (lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
-      const int page_scales = a.H * a.page_size * C::SROWB;
+      const int64_t page_scales = (int64_t)a.H * a.page_size * C::SROWB;
       // fetches block i of the unit into stage st
       auto fetch = [&](int i, int st, int2 pages) {
         const int row = (z.block(i) * BT) & (a.page_size - 1);
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
           if (lane < 2 * SCH) {
             const bool second = (lane & (SCH - 1)) >= SCH / 2;
             const int page = second ? pages.y : pages.x;
-            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (int64_t)max(page, 0) * page_scales - (second ? SCH / 2 * 16 : 0), page >= 0);
+            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + max(page, 0) * page_scales - (second ? SCH / 2 * 16 : 0), page >= 0);
           }
         } else {
           const int page = pages.x;
@@ -147,7 +149,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             }
           }
           if (lane < 2 * SCH)
-            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + ((int64_t)max(page, 0) * page_scales + row * C::SROWB), page >= 0);
+            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (max(page, 0) * page_scales + row * C::SROWB), page >= 0);
         }
       };
       const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
