@@ -110,6 +110,12 @@ struct AppendKArgs {
 // Bound: memory (every channel read and written once).  Measured, GB300: 14080 tokens, 24 KV and 24 query
 // heads of 128, 8-bit pages (433 MB) 78 us, 5.5 TB/s, with three heads ahead (two 80, one 90 us) and
 // groups of 12 heads (24 79, 8 84, 4 104 us: what the angles cost).
+// Largest magnitude of three, NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 constexpr int kAhead = 4;
 template <int KIND>   // the pages' type
 __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendKArgs a,
@@ -248,9 +254,12 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
     if constexpr (F4) {
       // A scale's 16 channels are two runs of 8: both of this thread's unit or, where the half layout parts them,
       // one of this unit and one of another of the row, whose threads are neighbours in the warp
-      uint32_t top[2] = {0, 0};   // magnitudes order as their bits, NaN and infinity above all others
+      uint32_t top[2];   // magnitudes order as their bits, NaN and infinity above all others
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top[i >> 3] = max(top[i >> 3], __float_as_uint(fabsf(v[i])));
+      for (int i = 0; i < 2; ++i) {
+        const float* x = v + 8 * i;
+        top[i] = __float_as_uint(max3_nan(max3_nan(x[0], x[1], x[2]), max3_nan(x[3], x[4], x[5]), max3_nan(x[6], x[7], x[7])));
+      }
       const bool parted = c1 != c0 + 8;
       uint32_t both[2] = {max(top[0], top[1]), 0};
       both[1] = both[0];
@@ -280,9 +289,10 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const uint32_t code = scale4_code(both[i]);
-          const float s = scale4_value(code), r = code ? 1.f / s : 0.f;
+          // (of a scale of 0 or NaN no code matters)
+          const float s = scale4_value(code), r = code ? about_inverse(s) : 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[8 * i + e] = code == kScaleNan ? 0.f : over_scale(v[8 * i + e], s, r);
+          for (int e = 0; e < 8; ++e) v[8 * i + e] = over_scale(v[8 * i + e], s, r);
           word[i] = encode4(v + 8 * i);
           const int run = (i ? c1 : c0) >> 3;
           if (!(run & 1)) scales[run >> 1] = (uint8_t)code;

@@ -147,10 +147,22 @@ __device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) 
 constexpr uint32_t kScaleTop = 0xe2;    // 10240: six times it is the largest value within f16
 constexpr uint32_t kScaleNan = 0xff;
 
+// x / s for s of four bits or fewer and r = 1 / s to 2^-22: x r corrected once by its remainder, which is exact
+// (Markstein's correction).  Where the quotient is half way between two codes, or scales, it comes out exactly: the
+// correction is good to 2^-43 of it, and the halfway points have five bits at most.
+__device__ __forceinline__ float over_scale(float x, float s, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, s, x), r, q);
+}
+__device__ __forceinline__ float about_inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 // The scale of 16 channels whose largest magnitude has these bits, as its byte: max / 6 to nearest even
 __device__ __forceinline__ uint32_t scale4_code(uint32_t top) {
   if (top >= 0x7f800000u) return kScaleNan;
-  const float a = __fdiv_rn(__uint_as_float(top), 6.f);
+  const float a = over_scale(__uint_as_float(top), 6.f, 1.f / 6.f);
   if (a < 0x1p-14f) return (uint32_t)__float2int_rn(a * 0x1p17f);   // multiples of 2^-17
   uint32_t u = __float_as_uint(a);
   u += 0x7ffffu + ((u >> 20) & 1u);
@@ -164,13 +176,6 @@ __device__ __forceinline__ float value4(uint32_t code, uint32_t scale) {
   const uint32_t m = code & 7u;
   const float v = m < 2 ? 0.5f * m : (float)(2u + (m & 1u)) * pow2f((int)(m >> 1) - 2);
   return __half2float(__float2half_rn((code & 8u ? -v : v) * scale4_value(scale)));
-}
-// x / s for a scale s and r = 1 / s rounded: x r corrected once by its remainder, which is exact (Markstein's
-// correction).  Where the quotient is half way between two codes it comes out exactly: it differs from x r by 2^-23
-// of itself at most, the correction is good to 2^-47, and the halfway points have three bits.
-__device__ __forceinline__ float over_scale(float x, float s, float r) {
-  const float q = x * r;
-  return fmaf(fmaf(-q, s, x), r, q);
 }
 // Eight floats as codes, to nearest even (6 at most), the first in the lowest four bits
 __device__ __forceinline__ uint32_t encode4(const float* v) {

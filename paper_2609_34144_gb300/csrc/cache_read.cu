@@ -75,8 +75,7 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
   const int64_t out_stride = is_k ? a.k_stride : a.v_stride;
   const bool one = threadIdx.x == 0 && threadIdx.y == 0;
   const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto store = [&](int i, int h, const float* v) {
-    OUT* to = out + (int64_t)i * out_stride + (int64_t)h * a.d;
+  auto store = [&](OUT* to, const float* v) {
     if constexpr (sizeof(OUT) == 2) {
       *reinterpret_cast<uint4*>(to) = pack8(v);
     } else {
@@ -88,7 +87,7 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
     if (s.n_new > a.batch.max_new && one) left_out();
     // positions below 0
     for (int i = threadIdx.y; i < min(-p0, kept); i += blockDim.y)
-      for (int h = h0; h < h0 + heads; ++h) store(i, h, none);
+      for (int h = h0; h < h0 + heads; ++h) store(out + (int64_t)i * out_stride + (int64_t)h * a.d, none);
   }
   const int g = first / a.page_size + run;   // page of the sequence
   if ((int64_t)g * a.page_size >= end) return;
@@ -102,43 +101,63 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
   }
   const uint8_t* cache = is_k ? a.ck : a.cv;
   const uint8_t* scales = is_k ? a.k_scale : a.v_scale;
-  // pairs (row, head), heads fastest for pages whose rows hold all heads, else rows
-  const int rows = hi - lo, mine = (rows - (int)threadIdx.y + (int)blockDim.y - 1) / (int)blockDim.y;
-  const int items = mine > 0 ? mine * heads : 0;
-  for (int at = 0; at < items; at += kAtOnce) {
+  // (row, head) pairs: a head's rows in turn where they lie together, else a row's heads
+  constexpr bool ROWS_FIRST = KIND == CAST_F4E2M1;
+  const int step = blockDim.y, first_row = lo + threadIdx.y;
+  if (first_row >= hi) return;
+  int row = first_row, head = h0, left = ((hi - first_row + step - 1) / step) * heads;
+  const int64_t cell = KIND == CAST_F4E2M1 ? 0 : (int64_t)page * a.page_size * a.row_stride + threadIdx.x * 8;
+  const uint8_t* codes = cache + (int64_t)page * a.page_size * a.row_stride / 2 + threadIdx.x * 4;              // 4 bits
+  const uint8_t* scale4 = scales + (int64_t)page * a.H * a.page_size * (a.d / 16) + threadIdx.x / 2;
+  while (left > 0) {
     Eight<KIND> x[kAtOnce];
-    int row[kAtOnce], head[kAtOnce];
+    OUT* to[kAtOnce];
+    const int n = min(left, kAtOnce);
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
-      const int k = min(at + j, items - 1);
-      const int r = KIND == CAST_F4E2M1 ? k % mine : k / heads;
-      row[j] = lo + threadIdx.y + r * blockDim.y;
-      head[j] = h0 + (KIND == CAST_F4E2M1 ? k / mine : k % heads);
-      if (page < 0) continue;
-      if constexpr (KIND == CAST_F4E2M1) {
-        const int64_t of = (int64_t)head[j] * a.page_size + row[j];   // row of the page
-        x[j].w = __ldg(reinterpret_cast<const uint32_t*>(cache + (int64_t)page * a.page_size * a.row_stride / 2 + of * (a.d / 2)) + threadIdx.x);
-        x[j].scale = __ldg(scales + ((int64_t)page * a.H * a.page_size + of) * (a.d / 16) + threadIdx.x / 2);
-      } else {
-        const int64_t from = ((int64_t)page * a.page_size + row[j]) * a.row_stride + (int64_t)head[j] * a.d + threadIdx.x * 8;
-        if constexpr (KIND == CAST_F8E4M3) {
-          x[j].w = __ldg(reinterpret_cast<const uint2*>(cache + from));
-          x[j].scale = __ldg(reinterpret_cast<const float*>(scales) + (int64_t)page * a.H + head[j]);
+      to[j] = out + (int64_t)(base + row - p0) * out_stride + (int64_t)head * a.d;
+      if (page >= 0) {
+        if constexpr (KIND == CAST_F4E2M1) {
+          const int64_t of = (int64_t)head * a.page_size + row;   // row of the page
+          x[j].w = __ldg(reinterpret_cast<const uint32_t*>(codes + of * (a.d / 2)));
+          x[j].scale = __ldg(scale4 + of * (a.d / 16));
+        } else if constexpr (KIND == CAST_F8E4M3) {
+          x[j].w = __ldg(reinterpret_cast<const uint2*>(cache + cell + row * a.row_stride + (int64_t)head * a.d));
+          x[j].scale = __ldg(reinterpret_cast<const float*>(scales) + (int64_t)page * a.H + head);
         } else {
-          x[j].w = __ldg(reinterpret_cast<const uint4*>(cache + from * 2));
+          x[j].w = __ldg(reinterpret_cast<const uint4*>(cache + (cell + row * a.row_stride + (int64_t)head * a.d) * 2));
+        }
+      }
+      if (j + 1 < n) {   // (behind the last the same once more)
+        if (ROWS_FIRST) {
+          row += step;
+          if (row >= hi) row = first_row, ++head;
+        } else if (++head == h0 + heads) {
+          head = h0;
+          row += step;
         }
       }
     }
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
-      if (at + j >= items) break;
-      const int i = base + row[j] - p0;
+      if (j >= n) break;
+      float v[8];
       if (page < 0) {
-        store(i, head[j], none);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
       } else {
-        float v[8];
         x[j].values(v);
-        store(i, head[j], v);
+      }
+      store(to[j], v);
+    }
+    left -= n;
+    if (left > 0) {
+      if (ROWS_FIRST) {
+        row += step;
+        if (row >= hi) row = first_row, ++head;
+      } else if (++head == h0 + heads) {
+        head = h0;
+        row += step;
       }
     }
   }
