@@ -17,6 +17,7 @@ struct ReadKArgs {
   const uint8_t *k_scale, *v_scale;
   void *k, *v;
   int runs;        // page runs of a sequence that the grid has room for
+  int chunks;      // CTAs that share a page's rows
   int group;       // heads of one CTA
   int jobs;        // head groups of K (and of V)
 };
@@ -61,11 +62,11 @@ struct Eight<CAST_F4E2M1> {
   }
 };
 
-// One CTA: the wanted rows of one sequence in one page, for a group of heads of K or V.  blockDim = (runs of 8
-// channels of a row, rows).
+// One CTA: some rows of a page of a sequence, for a group of heads of K or V.  blockDim = (runs of 8 channels of a row,
+// rows).
 template <int KIND, class OUT>
 __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs a) {
-  const int b = blockIdx.x / a.runs, run = blockIdx.x - b * a.runs;
+  const int chunk = blockIdx.x % a.chunks, b = blockIdx.x / a.chunks / a.runs, run = blockIdx.x / a.chunks - b * a.runs;
   const Sequence s = sequence_of(a.batch, b);
   const int kept = min(s.n_new, a.batch.max_new);
   const int p0 = s.len - s.n_new, first = max(p0, 0), end = p0 + kept;
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
   const int h0 = (blockIdx.y - (is_k ? 0 : a.jobs)) * a.group, heads = min(a.group, a.H - h0);
   OUT* out = static_cast<OUT*>(is_k ? a.k : a.v) + (int64_t)s.t0 * (is_k ? a.k_stride : a.v_stride) + threadIdx.x * 8;
   const int64_t out_stride = is_k ? a.k_stride : a.v_stride;
-  const bool one = threadIdx.x == 0 && threadIdx.y == 0;
+  const bool one = threadIdx.x == 0 && threadIdx.y == 0 && chunk == 0;
   const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   auto store = [&](OUT* to, const float* v) {
     if constexpr (sizeof(OUT) == 2) {
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
       reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
   };
-  if (run == 0) {
+  if (run == 0 && chunk == 0) {
     if (s.n_new > a.batch.max_new && one) left_out();
     // positions below 0
     for (int i = threadIdx.y; i < min(-p0, kept); i += blockDim.y)
@@ -101,64 +102,51 @@ __global__ void __launch_bounds__(256) k_read(const __grid_constant__ ReadKArgs 
   }
   const uint8_t* cache = is_k ? a.ck : a.cv;
   const uint8_t* scales = is_k ? a.k_scale : a.v_scale;
-  // (row, head) pairs: a head's rows in turn where they lie together, else a row's heads
-  constexpr bool ROWS_FIRST = KIND == CAST_F4E2M1;
-  const int step = blockDim.y, first_row = lo + threadIdx.y;
-  if (first_row >= hi) return;
-  int row = first_row, head = h0, left = ((hi - first_row + step - 1) / step) * heads;
-  const int64_t cell = KIND == CAST_F4E2M1 ? 0 : (int64_t)page * a.page_size * a.row_stride + threadIdx.x * 8;
-  const uint8_t* codes = cache + (int64_t)page * a.page_size * a.row_stride / 2 + threadIdx.x * 4;              // 4 bits
-  const uint8_t* scale4 = scales + (int64_t)page * a.H * a.page_size * (a.d / 16) + threadIdx.x / 2;
-  while (left > 0) {
+  const int row = chunk * blockDim.y + threadIdx.y;
+  if (row < lo || row >= hi) return;
+  OUT* to = out + (int64_t)(base + row - p0) * out_stride + (int64_t)h0 * a.d;
+  if (page < 0) {
+    for (int h = 0; h < heads; ++h) store(to + h * a.d, none);
+    return;
+  }
+  // the row of head h0: codes, and the steps to the next head's
+  const int64_t in_page = (int64_t)h0 * a.page_size + row;
+  const uint8_t* from;
+  const uint8_t* scale;
+  int64_t step, scale_step;
+  if constexpr (KIND == CAST_F4E2M1) {
+    from = cache + (int64_t)page * a.page_size * a.row_stride / 2 + in_page * (a.d / 2) + threadIdx.x * 4;
+    scale = scales + ((int64_t)page * a.H * a.page_size + in_page) * (a.d / 16) + threadIdx.x / 2;
+    step = a.page_size * (a.d / 2);
+    scale_step = a.page_size * (a.d / 16);
+  } else {
+    const int elt = KIND == CAST_BF16 ? 2 : 1;
+    from = cache + (((int64_t)page * a.page_size + row) * a.row_stride + h0 * a.d + threadIdx.x * 8) * elt;
+    scale = scales + ((int64_t)page * a.H + h0) * 4;
+    step = a.d * elt;
+    scale_step = 4;
+  }
+  for (int h = 0; h < heads; h += kAtOnce) {
     Eight<KIND> x[kAtOnce];
-    OUT* to[kAtOnce];
-    const int n = min(left, kAtOnce);
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
-      to[j] = out + (int64_t)(base + row - p0) * out_stride + (int64_t)head * a.d;
-      if (page >= 0) {
-        if constexpr (KIND == CAST_F4E2M1) {
-          const int64_t of = (int64_t)head * a.page_size + row;   // row of the page
-          x[j].w = __ldg(reinterpret_cast<const uint32_t*>(codes + of * (a.d / 2)));
-          x[j].scale = __ldg(scale4 + of * (a.d / 16));
-        } else if constexpr (KIND == CAST_F8E4M3) {
-          x[j].w = __ldg(reinterpret_cast<const uint2*>(cache + cell + row * a.row_stride + (int64_t)head * a.d));
-          x[j].scale = __ldg(reinterpret_cast<const float*>(scales) + (int64_t)page * a.H + head);
-        } else {
-          x[j].w = __ldg(reinterpret_cast<const uint4*>(cache + (cell + row * a.row_stride + (int64_t)head * a.d) * 2));
-        }
-      }
-      if (j + 1 < n) {   // (behind the last the same once more)
-        if (ROWS_FIRST) {
-          row += step;
-          if (row >= hi) row = first_row, ++head;
-        } else if (++head == h0 + heads) {
-          head = h0;
-          row += step;
-        }
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kAtOnce; ++j) {
-      if (j >= n) break;
-      float v[8];
-      if (page < 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+      if (h + j >= heads) break;
+      if constexpr (KIND == CAST_F4E2M1) {
+        x[j].w = __ldg(reinterpret_cast<const uint32_t*>(from + (h + j) * step));
+        x[j].scale = __ldg(scale + (h + j) * scale_step);
+      } else if constexpr (KIND == CAST_F8E4M3) {
+        x[j].w = __ldg(reinterpret_cast<const uint2*>(from + (h + j) * step));
+        x[j].scale = __ldg(reinterpret_cast<const float*>(scale + (h + j) * scale_step));
       } else {
-        x[j].values(v);
+        x[j].w = __ldg(reinterpret_cast<const uint4*>(from + (h + j) * step));
       }
-      store(to[j], v);
     }
-    left -= n;
-    if (left > 0) {
-      if (ROWS_FIRST) {
-        row += step;
-        if (row >= hi) row = first_row, ++head;
-      } else if (++head == h0 + heads) {
-        head = h0;
-        row += step;
-      }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (h + j >= heads) break;
+      float v[8];
+      x[j].values(v);
+      store(to + (h + j) * a.d, v);
     }
   }
 }
@@ -210,12 +198,12 @@ extern "C" cast_status cast_cache_read(const cast_cache_read_args* a, void* stre
   k.v_stride = a->v_row_stride;
   const int max_new = a->batch.max_new < a->batch.T ? a->batch.max_new : a->batch.T;
   k.runs = (max_new + c.page_size - 2) / c.page_size + 1;
-  const int64_t gx = (int64_t)k.runs * a->batch.B;
-  if (gx > 0x7fffffff) return fail(CAST_ERR_UNSUPPORTED, "%s: %lld page runs", who, (long long)gx);
   const int lanes = c.d / 8, rows = 256 / lanes < c.page_size ? 256 / lanes : c.page_size;
-  // heads of one CTA: as many as keep every thread at 16 rows at most, fewer where the grid would not fill the SMs
-  int group = 16 * rows / c.page_size;
-  if (group < 1) group = 1;
+  k.chunks = c.page_size / rows;
+  const int64_t gx = (int64_t)k.runs * k.chunks * a->batch.B;
+  if (gx > 0x7fffffff) return fail(CAST_ERR_UNSUPPORTED, "%s: %lld page runs", who, (long long)gx);
+  // heads of one CTA: fewer where the grid would not fill the SMs
+  int group = 16;
   while (group > 1 && gx * (both ? 2 : 1) * ((c.H + group - 1) / group) < 4 * 152 * 4) group /= 2;
   if ((int64_t)((c.H + group - 1) / group) * 2 > 65535) group = (c.H + 32766) / 32767;
   k.group = group;
