@@ -3,7 +3,7 @@
 // at; attention over the cache itself reads the pages.
 //
 // Bound: memory (4-bit pages: 0.56 bytes a channel in, 2 out).  A thread has 8 channels of a row at a time, so that
-// eight lanes write 128 bytes of a bf16 row side by side, and up to four of its loads are on their way together.
+// eight lanes write 128 bytes of a bf16 row side by side, and up to eight heads' loads are on their way together.
 #include "cache.cuh"
 
 namespace cast {
@@ -22,7 +22,7 @@ struct ReadKArgs {
   int jobs;        // head groups of K (and of V)
 };
 
-constexpr int kAtOnce = 4;
+constexpr int kAtOnce = 8;
 
 // Eight channels, as floats
 template <int KIND>
