@@ -173,6 +173,29 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
     }
     copy_commit();
   };
+  // 4-bit pages: the row's codes and scales of head h0.  A unit of the half layout has its runs in two groups of 16
+  // channels; `parted`: the warp has such units.  The other half of run r = channel / 8, run r ^ 1, belongs to unit r
+  // (its first run), r - turned units (its second), or r / 2: to the next lane's same run where both are turned.
+  const bool parted_here = c1 != c0 + 8, parted = F4 && __any_sync(0xffffffffu, parted_here);
+  const bool pairs_up = tab.rot_dim % 32 == 0;
+  uint8_t *codes4 = nullptr, *scales4 = nullptr;
+  int owner[2] = {0, 0};
+  bool second[2] = {false, false};
+  if constexpr (F4) {
+    const int64_t at = ((int64_t)page * a.H + h0) * a.page_size + row;
+    codes4 = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv) + (int64_t)page * a.page_size * a.row_stride / 2 +
+             ((int64_t)h0 * a.page_size + row) * (a.d / 2);
+    scales4 = reinterpret_cast<uint8_t*>(kind == 0 ? a.k_scale : a.v_scale) + at * (a.d / 16);
+    if (parted && !pairs_up) {
+      const int units = tab.rot_dim / 16, row0 = (threadIdx.x & 31) & -per_row;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int run = ((i ? c1 : c0) >> 3) ^ 1;
+        owner[i] = row0 + (run < units ? run : run < 2 * units ? run - units : run >> 1);
+        second[i] = run < units ? false : run < 2 * units ? true : run & 1;
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < kAhead - 1; ++i) fetch(h0 + i);
   for (int h = h0; h < h1; ++h) {
@@ -252,58 +275,52 @@ __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendK
       if (threadIdx.x == 0) *scale = now;
     }
     if constexpr (F4) {
-      // A scale's 16 channels are two runs of 8: both of this thread's unit or, where the half layout parts them,
-      // one of this unit and one of another of the row, whose threads are neighbours in the warp
-      uint32_t top[2];   // magnitudes order as their bits, NaN and infinity above all others
+      float top[2];   // largest magnitudes of the unit's two runs of 8, NaN if one of them is
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const float* x = v + 8 * i;
-        top[i] = __float_as_uint(max3_nan(max3_nan(x[0], x[1], x[2]), max3_nan(x[3], x[4], x[5]), max3_nan(x[6], x[7], x[7])));
+        top[i] = max3_nan(max3_nan(x[0], x[1], x[2]), max3_nan(x[3], x[4], x[5]), max3_nan(x[6], x[7], x[7]));
       }
-      const bool parted = c1 != c0 + 8;
-      uint32_t both[2] = {max(top[0], top[1]), 0};
-      both[1] = both[0];
-      if (__any_sync(0xffffffffu, parted)) {
-        // run r = channel / 8 belongs to unit r (its first run), r - turned units (its second), or r / 2
-        const int turned_units = tab.rot_dim / 16, row0 = (threadIdx.x & 31) & -per_row;
-        uint32_t mate[2];
+      uint32_t code[2], word[2];
+      if (!parted) {
+        code[0] = code[1] = scale4_code(__float_as_uint(max3_nan(top[0], top[1], top[1])));
+        const float s = scale4_value(code[0]), r = about_inverse(s);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = over_scale(v[e], s, r);
+      } else {
+        // a scale's 16 channels are runs of two units, whose threads are neighbours in the warp
+        float mate[2];
+        if (pairs_up) {
+          mate[0] = __shfl_xor_sync(0xffffffffu, top[0], 1);
+          mate[1] = __shfl_xor_sync(0xffffffffu, top[1], 1);
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int run = ((i ? c1 : c0) >> 3) ^ 1;
-          const int owner = run < turned_units ? run : run < 2 * turned_units ? run - turned_units : run >> 1;
-          const bool second = run < turned_units ? false : run < 2 * turned_units ? true : run & 1;
-          const uint32_t a0 = __shfl_sync(0xffffffffu, top[0], row0 + owner), a1 = __shfl_sync(0xffffffffu, top[1], row0 + owner);
-          mate[i] = second ? a1 : a0;
-        }
-        if (parted) {
-          both[0] = max(top[0], mate[0]);
-          both[1] = max(top[1], mate[1]);
+          if (!pairs_up) {
+            const float a0 = __shfl_sync(0xffffffffu, top[0], owner[i]), a1 = __shfl_sync(0xffffffffu, top[1], owner[i]);
+            mate[i] = second[i] ? a1 : a0;
+          }
+          if (!parted_here) mate[i] = top[i ^ 1];
+          code[i] = scale4_code(__float_as_uint(max3_nan(top[i], mate[i], mate[i])));
+          const float s = scale4_value(code[i]), r = about_inverse(s);
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) v[e] = over_scale(v[e], s, r);
         }
       }
+      word[0] = encode4(v);
+      word[1] = encode4(v + 8);
       if (in) {
-        const int64_t first_row = ((int64_t)page * a.H + h) * a.page_size + row;   // of the scales
-        uint8_t* cache = static_cast<uint8_t*>(kind == 0 ? a.ck : a.cv) + (int64_t)page * a.page_size * a.row_stride / 2 +
-                         ((int64_t)h * a.page_size + row) * (a.d / 2);
-        uint8_t* scales = reinterpret_cast<uint8_t*>(kind == 0 ? a.k_scale : a.v_scale) + first_row * (a.d / 16);
-        uint32_t word[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t code = scale4_code(both[i]);
-          // (of a scale of 0 or NaN no code matters)
-          const float s = scale4_value(code), r = code ? about_inverse(s) : 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[8 * i + e] = over_scale(v[8 * i + e], s, r);
-          word[i] = encode4(v + 8 * i);
-          const int run = (i ? c1 : c0) >> 3;
-          if (!(run & 1)) scales[run >> 1] = (uint8_t)code;
-        }
-        if (parted) {
-          *reinterpret_cast<uint32_t*>(cache + c0 / 2) = word[0];
-          *reinterpret_cast<uint32_t*>(cache + c1 / 2) = word[1];
+        if (!(c0 & 8)) scales4[c0 >> 4] = (uint8_t)code[0];
+        if (!(c1 & 8)) scales4[c1 >> 4] = (uint8_t)code[1];
+        if (parted_here) {
+          *reinterpret_cast<uint32_t*>(codes4 + c0 / 2) = word[0];
+          *reinterpret_cast<uint32_t*>(codes4 + c1 / 2) = word[1];
         } else {
-          *reinterpret_cast<uint2*>(cache + c0 / 2) = make_uint2(word[0], word[1]);
+          *reinterpret_cast<uint2*>(codes4 + c0 / 2) = make_uint2(word[0], word[1]);
         }
       }
+      codes4 += a.page_size * (a.d / 2);
+      scales4 += a.page_size * (a.d / 16);
     }
   }
 }
