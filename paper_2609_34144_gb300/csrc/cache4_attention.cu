@@ -65,9 +65,12 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
   const int g = lane >> 2, q4 = lane & 3;
   int entry;
   int64_t at, stop, entry_at;
+  int share;
   // the joining may be put in place as CTAs leave (it waits for all of them)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (!share_of<D, C::ROWS, BT>(a, entry, at, stop, entry_at)) return;
+  // until the share is known no cut: the workspace may hold an earlier call's
+  if (!a.whole && threadIdx.x == 0) a.cuts[blockIdx.x].c0 = -1;
+  if (!share_of<D, C::ROWS, BT>(a, entry, at, stop, entry_at, &share)) return;
 
   uint8_t* ring = smem + warp * C::RING;
   const uint32_t ring_at = smem_u32(ring);
@@ -87,6 +90,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const int64_t unit_at = entry_at + (int64_t)h * nb;
       const int k0 = (int)(at - unit_at);
       const int k1 = (int)min((int64_t)nb, stop - unit_at);
+      // (k0 > 0: the share begins inside the unit)
+      if (k0 > 0 && threadIdx.x == 0)
+        a.cuts[blockIdx.x] = RowsCut{(int)blockIdx.x - (k0 + share - 1) / share, (int)blockIdx.x + (nb - 1 - k0) / share, h, tile, z.t0, z.n_rows};
 
       // The page of tokens p .. (-1: out of range, reads as zeros)
       auto page_at = [&](int p) {
@@ -467,7 +473,7 @@ cast_status launch_pages(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st)
   k_cache_rows4<D, NT, SMALL><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
-  return launch_merge<D, C::ROWS, BT>(k, p.grid, st);
+  return p.grid > 1 ? launch_joining(k_cuts_merge<D, C::ROWS>, p.grid - 1, st, k) : CAST_OK;
 }
 
 template <int D, int NT>

@@ -554,7 +554,11 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
     const int64_t seen = ((int64_t)a.window + rows) / 16 + 2 + ((int64_t)a.sinks + 15) / 16;
     if (seen < most) most = seen;
   }
-  p.whole = most <= 64;
+  // 4-bit pages: many units may be longer.  Measured, shares / whole, us, heads of 128: 8 units of 2000 tokens 13 / 19; 128
+  // of 2000 21 / 19, ragged 19 / 19, of 4000 28 / 34; 384 of 2000 39 / 32, of 4000 59 / 56, ragged 45 / 51; 1024 of
+  // 4000 131 / 118, ragged 94 / 93
+  const int64_t all = (int64_t)a.batch.B * p.row_tiles * a.cache.H;
+  p.whole = most <= 64 || (f4 && all >= 128 && most <= (all >= 384 ? 192 : 128));
   if (p.whole) {
     const int64_t units = (int64_t)a.batch.B * p.row_tiles * a.cache.H;
     p.grid = units > 0x7fffffff ? 0 : (int)units;
@@ -571,7 +575,8 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   p.two = !f4 && row <= 128 && a.cache.H % 2 == 0 && (int64_t)a.cache.H * row >= 512 && (int64_t)a.batch.B * p.row_tiles * a.cache.H >= 128;
   p.least >>= p.two;
   p.part_o_bytes = align_up(((size_t)2 * p.grid << p.two) * rows * a.cache.d * sizeof(float));
-  p.total_bytes = p.part_o_bytes + align_up(((size_t)2 * p.grid << p.two) * rows * sizeof(float2));
+  p.part_ml_bytes = align_up(((size_t)2 * p.grid << p.two) * rows * sizeof(float2));
+  p.total_bytes = p.part_o_bytes + p.part_ml_bytes + (f4 ? align_up((size_t)p.grid * sizeof(RowsCut)) : 0);
   return p;
 }
 
@@ -611,7 +616,7 @@ cast_status launch_rows(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) 
   k_cache_rows<D, F8, MT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
-  return launch_merge<D, C::ROWS>(k, p.grid, st);
+  return launch_joining(k_cache_merge<D, C::ROWS>, (int64_t)k.batch.B * k.row_tiles * k.H, st, k, p.grid);
 }
 
 }  // namespace
@@ -698,6 +703,7 @@ cast_status cast_cache_attention(const cast_cache_attn_args* a, void* ws, size_t
   k.units = c.H >> p.two;
   k.part_o = static_cast<float*>(ws);
   k.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ws) + p.part_o_bytes);
+  k.cuts = reinterpret_cast<RowsCut*>(static_cast<char*>(ws) + p.part_o_bytes + p.part_ml_bytes);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.dtype == CAST_F4E2M1) return launch_rows4(k, p, c.d, st);
   if (p.mt == 2)   // heads of 64 only

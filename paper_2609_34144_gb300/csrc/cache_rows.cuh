@@ -23,6 +23,12 @@ struct RowsKArgs {
   int two, units;     // 1: units of two KV heads side by side, else 0; units of an entry
   float* part_o;      // [2 * grid][1 + two][ROWS][D]
   float2* part_ml;    // [2 * grid][1 + two][ROWS]
+  struct RowsCut* cuts;   // 4-bit pages: [grid]
+};
+// What a CTA leaves for the joining (4-bit pages): the unit that its share begins inside of, which CTAs c0 .. c1 have
+// blocks of (c0 = -1: it begins with a unit, or has none)
+struct RowsCut {
+  int c0, c1, h, tile, t0, n_rows;
 };
 
 namespace {
@@ -116,14 +122,16 @@ __device__ __forceinline__ void zero_rows(const RowsKArgs& a, int e, int h0, int
 }
 
 // A CTA's share of the call's blocks: [at, stop), and the entry (sequence, row tile) it begins in, whose blocks
-// begin at entry_at.  False for a CTA without one.
+// begin at entry_at.  False for a CTA without one.  *size: blocks of a share (2^30 at most: no unit has as many).
 template <int D, int ROWS, int BT = 16>
-__device__ __forceinline__ bool share_of(const RowsKArgs& a, int& entry, int64_t& at, int64_t& stop, int64_t& entry_at) {
+__device__ __forceinline__ bool share_of(const RowsKArgs& a, int& entry, int64_t& at, int64_t& stop, int64_t& entry_at,
+                                         int* size = nullptr) {
   __shared__ int s_entry;
   __shared__ int64_t s_work[kWarps], s_before;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int entries = a.batch.B * a.row_tiles, units = a.units;
   entry_at = 0;
+  if (size) *size = 1;
   if (a.whole) {
     entry = blockIdx.x / units;
     const int h = blockIdx.x - entry * units;
@@ -150,6 +158,7 @@ __device__ __forceinline__ bool share_of(const RowsKArgs& a, int& entry, int64_t
   for (int w = 0; w < kWarps; ++w) total += s_work[w];
   total *= units;
   const int64_t share = max((int64_t)a.least, (total + gridDim.x - 1) / gridDim.x);
+  if (size) *size = (int)min(share, (int64_t)1 << 30);
   at = blockIdx.x * share;
   stop = min(at + share, total);
   if (none && blockIdx.x == 0) {
@@ -231,49 +240,17 @@ __device__ __forceinline__ void join_warps(const RowsKArgs& a, const Span& z, in
     }
 }
 
-// Joins the parts of the units that no single CTA of k_cache_rows or k_cache_rows4 had whole: one CTA a unit, one warp a
-// row and some of the parts (lanes: four channels each), then over the warps of a row.
+// Joins the parts of the unit (h, tile) of a sequence that CTAs c0 .. c1 left: one warp a row and some of the parts
+// (lanes: four channels each), then over the warps of a row.
 constexpr int kMergeWarps = 16;
-template <int D, int ROWS, int BT>
-__global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
+template <int D, int ROWS>
+__device__ __forceinline__ void merge_unit(const RowsKArgs& a, int c0, int c1, int h, int tile, int t0, int n_rows) {
   constexpr int LANES = D / 4, GROUPS = 32 / LANES;   // GROUPS parts at a time in a warp
-  __shared__ int64_t s_sum[kMergeWarps], s_before[kMergeWarps];
   __shared__ float4 s_o[kMergeWarps * GROUPS][LANES];
   __shared__ float2 s_ml[kMergeWarps * GROUPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int entries = a.batch.B * a.row_tiles;
-  const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  int64_t sum = 0, before = 0;
-  for (int e = threadIdx.x; e < entries; e += kMergeWarps * 32) {
-    const int n = span_of<BT>(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
-    sum += n;
-    before += e < entry ? n : 0;
-  }
-  sum = warp_sum(sum);
-  before = warp_sum(before);
-  if (lane == 0) {
-    s_sum[warp] = sum;
-    s_before[warp] = before;
-  }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  __syncthreads();
-  int64_t total = 0, at = 0;
-  for (int w = 0; w < kMergeWarps; ++w) {
-    total += s_sum[w];
-    at += s_before[w];
-  }
-  const int units = a.units;
-  total *= units;
-  const int64_t share = max((int64_t)a.least, (total + ctas - 1) / ctas);
-  const int tile = entry % a.row_tiles;
-  const Span z = span_of<BT>(a, entry / a.row_tiles, tile, ROWS);
-  const int nb = z.blocks();
-  at = at * units + (int64_t)(h >> a.two) * nb;
-  if (nb == 0) return;
-  const int c0 = (int)(at / share), c1 = (int)((at + nb - 1) / share);
-  if (c0 == c1) return;   // written whole
   // warps_per_row warps (a power of two) have every warps_per_row-th part of a row
-  const int rows = min(ROWS, z.n_rows - tile * ROWS), parts = c1 - c0 + 1;
+  const int rows = min(ROWS, n_rows - tile * ROWS), parts = c1 - c0 + 1;
   int per_row = 1;
   while (per_row * 2 * rows <= kMergeWarps && per_row * GROUPS < parts) per_row *= 2;
   for (int r0 = 0; r0 < rows; r0 += kMergeWarps / per_row) {
@@ -318,7 +295,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
       }
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const int r = tile * ROWS + rr;
-      const int64_t row = (int64_t)(z.t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
+      const int64_t row = (int64_t)(t0 + r / a.group) * a.H_q + h * a.group + r % a.group;
       if (a.o_f32) {
         *reinterpret_cast<float4*>(static_cast<float*>(a.o) + row * D + c * 4) =
             make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
@@ -332,11 +309,60 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
   }
 }
 
-// The joining's launch behind the kernel that left the parts
-template <int D, int ROWS, int BT = 16>
-cast_status launch_merge(const RowsKArgs& k, int ctas, cudaStream_t st) {
+// Joins the parts of the units that no single CTA of k_cache_rows had whole: one CTA a unit.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_constant__ RowsKArgs a, int ctas) {
+  __shared__ int64_t s_sum[kMergeWarps], s_before[kMergeWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int entries = a.batch.B * a.row_tiles;
+  const int entry = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  int64_t sum = 0, before = 0;
+  for (int e = threadIdx.x; e < entries; e += kMergeWarps * 32) {
+    const int n = span_of(a, e / a.row_tiles, e % a.row_tiles, ROWS).blocks();
+    sum += n;
+    before += e < entry ? n : 0;
+  }
+  sum = warp_sum(sum);
+  before = warp_sum(before);
+  if (lane == 0) {
+    s_sum[warp] = sum;
+    s_before[warp] = before;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  __syncthreads();
+  int64_t total = 0, at = 0;
+  for (int w = 0; w < kMergeWarps; ++w) {
+    total += s_sum[w];
+    at += s_before[w];
+  }
+  const int units = a.units;
+  total *= units;
+  const int64_t share = max((int64_t)a.least, (total + ctas - 1) / ctas);
+  const int tile = entry % a.row_tiles;
+  const Span z = span_of(a, entry / a.row_tiles, tile, ROWS);
+  const int nb = z.blocks();
+  at = at * units + (int64_t)(h >> a.two) * nb;
+  if (nb == 0) return;
+  const int c0 = (int)(at / share), c1 = (int)((at + nb - 1) / share);
+  if (c0 == c1) return;   // written whole
+  merge_unit<D, ROWS>(a, c0, c1, h, tile, z.t0, z.n_rows);
+}
+
+// The same by what the CTAs left of their shares' beginnings: CTA x takes the unit that the share of CTA x + 1 begins
+// inside of, if that is the first such share.  Nothing is searched for (48 sequences of 8 heads, windows of 4096 tokens
+// of 4 bits 68.6 -> 66.6 us; 128 of 1k to 4k tokens 94 -> 87 us).
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kMergeWarps * 32) k_cuts_merge(const __grid_constant__ RowsKArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const RowsCut u = a.cuts[blockIdx.x + 1];
+  if (u.c0 == (int)blockIdx.x) merge_unit<D, ROWS>(a, u.c0, u.c1, u.h, u.tile, u.t0, u.n_rows);
+}
+
+// A joining's launch behind the kernel that left the parts
+template <class... A>
+cast_status launch_joining(void (*kernel)(A...), int64_t grid, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(k.batch.B * k.row_tiles * k.H), 1, 1);
+  cfg.gridDim = dim3((unsigned)grid, 1, 1);
   cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -344,7 +370,7 @@ cast_status launch_merge(const RowsKArgs& k, int ctas, cudaStream_t st) {
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, k_cache_merge<D, ROWS, BT>, k, ctas) != cudaSuccess) return check_launch("cache attention merge");
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) return check_launch("cache attention merge");
   return check_launch("cache attention merge");
 }
 
@@ -353,7 +379,7 @@ cast_status launch_merge(const RowsKArgs& k, int ctas, cudaStream_t st) {
 struct RowsPlan {
   int mt, row_tiles, grid, least, two;   // mt: units of 16 * mt rows; 4-bit pages: of 8 * mt
   bool whole;            // a CTA takes a whole unit; else units may be split and are merged
-  size_t part_o_bytes, total_bytes;
+  size_t part_o_bytes, part_ml_bytes, total_bytes;
 };
 // 4-bit pages (cache4_attention.cu): CTAs that an SM holds, and the launch
 int rows4_ctas(int d, int mt);

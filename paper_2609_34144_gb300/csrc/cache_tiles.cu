@@ -218,14 +218,15 @@ __device__ __forceinline__ T scan(T x, int lane) {   // inclusive
 // How the call's work is dealt out.  Units of equal work are first dealt whole, a round of one for each
 // CTA (heads slowest: what runs together reads one head's keys); what is left, or everything where units
 // differ, is a row of work items from `base` on, of which CTA c has share * c .. share * (c + 1) - 1.
+template <int KIND>
 struct Deal {
   int64_t per_head;      // work of a head
   int each, rounds;      // of a unit that is dealt whole, and how many a CTA has
   int64_t base, share, total;
 };
 template <int KIND>
-__device__ __forceinline__ Deal deal(const TilesKArgs& a, int ctas, int lane) {   // one warp; every lane has it
-  Deal d{};
+__device__ __forceinline__ Deal<KIND> deal(const TilesKArgs& a, int ctas, int lane) {   // one warp; every lane has it
+  Deal<KIND> d{};
   if (a.batch.B == 1) {
     const Sequence s = sequence_of(a.batch, 0);
     const int n = min(s.n_new, a.batch.max_new), per = 2 * a.tile_tokens;
@@ -290,7 +291,7 @@ __device__ __forceinline__ Unit unit_of(const TilesKArgs& a, int x, int lane) {
 // unit's tile k is at item kBegin + k * tile_work.  Its first part (with tile 0) goes to the CTA's second
 // place, others to its first.
 template <int KIND>
-__device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal& d, int64_t at, int64_t stop, int lane, Cut* cut) {
+__device__ __forceinline__ Unit unit_at(const TilesKArgs& a, const Deal<KIND>& d, int64_t at, int64_t stop, int lane, Cut* cut) {
   Unit u{};
   if (cut && lane == 0) cut->c0 = -1;
   const int64_t from = at;
@@ -544,7 +545,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
     }
   }
   // warp 0: the CTA's share of the work, and its first unit
-  Deal d{};
+  Deal<KIND> d{};
   int64_t at = 0, stop = 0;
   int round = 0;
   if (warp == 0) {
@@ -559,7 +560,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
       at = d.rounds > 0 ? (int64_t)blockIdx.x * d.each : blockIdx.x * d.share;
       stop = d.rounds > 0 ? at + d.each : min(at + d.share, d.total);
       // with the share comes what it begins inside of, for the joining
-      u = unit_at<KIND>(a, d, at, stop, lane, d.rounds > 0 ? nullptr : a.cuts + blockIdx.x);
+      u = unit_at(a, d, at, stop, lane, d.rounds > 0 ? nullptr : a.cuts + blockIdx.x);
     }
     if (lane == 0) bars->unit = u;
   }
@@ -668,7 +669,7 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
           stop = round < d.rounds ? at + d.each : min(at + d.share, d.total);
         }
         if (at >= stop) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-        const Unit next = unit_at<KIND>(a, d, at, stop, lane, cut);
+        const Unit next = unit_at(a, d, at, stop, lane, cut);
         if (lane == 0) bars->next = next;
       }
     } else if (warp == 3 && !DECODED) {
@@ -843,7 +844,10 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
 #pragma unroll 1
       for (int j = max(issued - (1 << log_stages), 0); j < issued; ++j)
         mbar_wait(&full[j & ((1 << log_stages) - 1)], (uint32_t)(j >> log_stages) & 1u, lim);
-      if (warp == 0 && u.n_tiles > 0) mbar_wait(DECODED ? &bars->q_raw : &bars->q_full, 0, lim);
+      if (warp == 0 && u.n_tiles > 0) {
+        if (F4) mbar_wait(&bars->q_raw, 0, lim);
+        else mbar_wait(F8 ? &bars->q_raw : &bars->q_full, 0, lim);
+      }
     }
     if (warp == 1) tmem_dealloc(tmem, kTmemCols);
   } else if (warp < 12) {

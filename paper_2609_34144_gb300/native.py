@@ -723,13 +723,14 @@ def kv_cache(k, v, k_scale=None, v_scale=None):
 def _page_stride(t):
     """Elements (two a byte) a token row that lie between the pages of 4-bit pages [n_pages, H, page_size, d/2]."""
     n, H, ps, half = t.shape
-    if t.numel() == 0 or not t[0].is_contiguous():
+    s0, s1, s2, s3 = t.stride()
+    if (half > 1 and s3 != 1) or (ps > 1 and s2 != half) or (H > 1 and s1 != ps * half):
         raise ValueError("4-bit pages: heads, rows and channels of a page must be contiguous")
     if n < 2:
         return H * half * 2
-    if t.stride(0) * 2 % ps:
+    if s0 * 2 % ps:
         raise ValueError("4-bit pages: the page stride must be a multiple of page_size / 2 bytes")
-    return t.stride(0) * 2 // ps
+    return s0 * 2 // ps
 
 
 def _batch(page_table, kv_len, cu_new, T, max_new):

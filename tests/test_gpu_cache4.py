@@ -451,3 +451,283 @@ def test_attention_of_large_and_small_values(lib, new, H_q, d):
     q = randn(gen(2), new, H_q, d).to(torch.bfloat16) * 2e4
     o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, want_lse=True, out_dtype=torch.float32)
     check_attention(lib, c, [(k, v)], q, [new], o, lse)
+
+
+CUT = [
+    # units cut anywhere by the shares: at their first blocks, between units and at their last
+    ([20000, 131, 4100, 257], [2, 1, 2, 1], 2, 8, 64, 64, True, 0, 0),
+    ([9000] * 7, [1] * 7, 3, 15, 128, 16, True, 4000, 100),
+    ([0, 12000, 1], [0, 3, 1], 1, 4, 128, 128, True, 0, 0),
+    ([20000, 131, 4100, 257], [9, 20, 40, 64], 2, 8, 64, 64, True, 0, 0),
+    ([9000] * 7, [5] * 7, 3, 15, 128, 16, True, 4000, 100),
+    ([6000, 6100, 6200], [300, 129, 17], 2, 4, 128, 32, False, 0, 0),
+    ([0, 12000, 1], [6, 40, 6], 1, 24, 128, 128, True, 0, 0),
+    ([1100 + 130 * i for i in range(9)], [70 - 7 * i for i in range(9)], 5, 5, 64, 16, True, 0, 0),
+]
+
+
+@pytest.mark.parametrize("lens,new,H,H_q,d,page,causal,window,sinks", CUT)
+def test_units_cut_anywhere(lib, lens, new, H, H_q, d, page, causal, window, sinks):
+    """... also with rows of a sequence shorter than its new tokens, which see nothing."""
+    c = Pages4(lib, [max(n, 0) for n in lens], H, d, page, seed=8)
+    held = c.fill(seed=9)
+    q = (1.5 * randn(gen(3), sum(new), H_q, d)).to(torch.bfloat16)
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=i32(*np.concatenate([[0], np.cumsum(new)])), max_new=max(new),
+                                      want_lse=True, **kw)
+    lib.cast_check_device()
+    check_attention(lib, c, held, q, new, o, lse, **kw)
+
+
+@pytest.mark.parametrize("new", [1, 3, 8, 30])
+def test_many_sequences(lib, new):
+    """More sequences than a warp has lanes, of very different lengths; enough units that CTAs take whole ones, too."""
+    lens = [max(new, (37 * i * i) % 1700) for i in range(70)]
+    c = Pages4(lib, lens, 1, 64, 16, seed=2)
+    held = c.fill(seed=5)
+    n = [min(new, 1 + i % new) for i in range(70)]
+    q = randn(gen(1), sum(n), 4, 64).to(torch.bfloat16)
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=i32(*np.concatenate([[0], np.cumsum(n)])), max_new=new, want_lse=True)
+    lib.cast_check_device()
+    check_attention(lib, c, held, q, n, o, lse)
+
+
+@pytest.mark.parametrize("new", [2, 60])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_query_that_is_not_finite_stays_its_own(lib, new, bad):
+    c = Pages4(lib, [500], 2, 128, 32)
+    c.fill(seed=5)
+    q = randn(gen(1), new, 4, 128).to(torch.bfloat16)
+    want = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len)
+    q[1, 2, 77] = bad
+    got = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len)
+    got, want = got.view(new, 4, 128), want.view(new, 4, 128)
+    assert torch.isnan(got[1, 2]).all()
+    got[1, 2] = want[1, 2]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("new", [1, 90])
+def test_table_is_a_slice_shared_and_too_short(lib, new):
+    c = Pages4(lib, [900, 333], 2, 64, 16, seed=4)
+    held = c.fill(seed=5)
+    wide = torch.full((2, 5000), -7, dtype=torch.int32, device="cuda")
+    wide[:, 100:100 + c.table.shape[1]] = c.table
+    q = randn(gen(1), 2 * new, 4, 64).to(torch.bfloat16)
+    o = lib.cast_cache_attention(q, c.cache, wide[:, 100:4100], c.kv_len)
+    k, _ = lib.cast_cache_read(c.cache, wide[:, 100:4100], c.kv_len, 600)
+    lib.cast_check_device()
+    check_attention(lib, c, held, q, [new, new], o, None)
+    assert np.array_equal(f64(k[300:]), held[1][0][33:])
+    # one table for several sequences, of different lengths
+    one = c.table[:1].expand(2, -1)
+    o = lib.cast_cache_attention(q, c.cache, one, i32(900, 411))
+    lib.cast_check_device()
+    two = Pages4.__new__(Pages4)
+    two.lens = [900, 411]
+    check_attention(lib, two, [held[0], tuple(x[:411] for x in held[0])], q, [new, new], o, None)
+    lib.cast_cache_attention(q, c.cache, c.table[:, :30], c.kv_len, causal=False)   # room for 480 of 900
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+
+
+@pytest.mark.parametrize("said", [2, 60])
+def test_more_new_tokens_than_said_are_left_out(lib, said):
+    c = Pages4(lib, [300, 300], 1, 64, 16)
+    c.fill(seed=5)
+    n = [said, said + 5]
+    cu = i32(0, n[0], sum(n))
+    q = randn(gen(2), sum(n), 2, 64).to(torch.bfloat16)
+    out = torch.full((sum(n), 128), 5.0, dtype=torch.bfloat16, device="cuda")
+    lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, cu_new=cu, max_new=said, out=out)
+    with pytest.raises(lib.CastError):
+        lib.cast_check_device()
+    assert (out[n[0] + said:] == 5).all() and not (out[:n[0] + said] == 5).all(1).any()
+
+
+def test_append_leaves_out_what_is_out_of_range(lib):
+    """Pages outside the pool, positions past the table and below 0, tokens past max_new: nothing else is touched."""
+    x = randn(gen(1), 40, 2, 64).to(torch.bfloat16)
+    c = Pages4(lib, [40], 2, 64, 16, seed=3)
+    before = [t.clone() for t in (c.k, c.v, c.ks, c.vs)]
+    for table, n, said, rows in ((i32(-1, 5000, -7)[None], i32(40), 40, 0), (c.table[:, :1], i32(40), 40, 16), (c.table, i32(40), 7, 7),
+                                 (c.table, i32(9), 40, 9)):
+        cu = i32(0, 40)
+        lib.cast_cache_append(x, x, c.cache, table, n, cu_new=cu, max_new=said)
+        if n.item() == 40:
+            with pytest.raises(lib.CastError):
+                lib.cast_check_device()
+        else:
+            lib.cast_check_device()
+        p = c.table[0].long()
+        changed = (c.ks[p] != before[2][p]).any(-1).any(1).flatten()
+        assert int(changed.sum()) == rows and changed[:rows].all()
+        for t, was in zip((c.k, c.v, c.ks, c.vs), before):
+            t.copy_(was)
+
+
+def test_append_strided_in_place_and_on_another_stream(lib):
+    """Rows of a fused buffer, queries rotated where they lie, a stream of its own; as many heads as there are fetched
+    ahead and more."""
+    for H in (1, 3, 5, 13):
+        g = gen(H)
+        buf = randn(g, 50, 4 * H, 128).to(torch.bfloat16)
+        q, k, v = buf[:, :2 * H], buf[:, 2 * H:3 * H], buf[:, 3 * H:]
+        table = lib.rotary_table(128)
+        a, b = (Pages4(lib, [50], H, 128, 32, seed=1) for _ in range(2))
+        want = lib.cast_cache_append(k.contiguous(), v.contiguous(), a.cache, a.table, a.kv_len, rotary=table, q=q.contiguous())
+        rest = buf[:, 2 * H:].clone()
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        lib.cast_cache_append(k, v, b.cache, b.table, b.kv_len, rotary=table, q=q, q_out=q, stream=s)
+        read = lib.cast_cache_read(b.cache, b.table, b.kv_len, 50, stream=s)
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(q, want) and torch.equal(buf[:, 2 * H:], rest)
+        for x, y in zip(read, lib.cast_cache_read(a.cache, a.table, a.kv_len, 50)):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("new,H_q", [(1, 8), (30, 8), (300, 2)])
+def test_attention_again_strided_and_on_another_stream(lib, new, H_q):
+    c = Pages4(lib, [5000, 900], 2, 64, 16, seed=7)
+    c.fill(seed=8)
+    buf = randn(gen(2), 2 * new, 3 * H_q, 64).to(torch.bfloat16)
+    q = buf[:, H_q:2 * H_q]
+    want = lib.cast_cache_attention(q.contiguous(), c.cache, c.table, c.kv_len)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = [lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, stream=s) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(x, want) for x in got)
+
+
+def test_attention_with_a_workspace_of_earlier_calls(lib):
+    """Calls of every kind one after the other in one workspace that held anything."""
+    ws = torch.randint(0, 256, (1 << 28,), dtype=torch.uint8, device="cuda")
+    for lens, new, H, H_q, d, page, causal, window, sinks in ROWS[3:6] + CUT + TILES[3:6]:
+        c = Pages4(lib, lens, H, d, page, seed=1)
+        c.fill(seed=2)
+        q = randn(gen(d), sum(new), H_q, d).to(torch.bfloat16)
+        kw = dict(cu_new=i32(*np.concatenate([[0], np.cumsum(new)])), max_new=max(new), causal=causal, window=window, sinks=sinks)
+        want = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, **kw)
+        assert torch.equal(lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, workspace=ws, **kw), want)
+        ws.random_(0, 256)
+
+
+def test_offsets_beyond_32_bits(lib):
+    """Pages far into a pool of more than 2^32 bytes."""
+    H, d, page = 8, 128, 128
+    n = (1 << 32) // (H * page * d // 2) * 5 // 4 + 3
+    assert n * H * page * (d // 16) < 1 << 32 and n * H * page * d // 2 > 1 << 32
+    k, v = (torch.empty((n, H, page, d // 2), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.empty((n, H, page, d // 16), dtype=torch.uint8, device="cuda") for _ in range(2))
+    big = lib.kv_cache(k, v, ks, vs)
+    c = Pages4(lib, [300], H, d, page)
+    c.fill(seed=4)
+    far = torch.tensor([[n - 1, n - 3, n // 2 + 1]], dtype=torch.int32, device="cuda")
+    for t, x in ((k, c.k), (v, c.v), (ks, c.ks), (vs, c.vs)):
+        t[far[0].long()] = x[c.table[0].long()]
+    for new in (1, 50):
+        q = randn(gen(new), new, 16, d).to(torch.bfloat16)
+        assert torch.equal(lib.cast_cache_attention(q, big, far, c.kv_len), lib.cast_cache_attention(q, c.cache, c.table, c.kv_len))
+    x = randn(gen(9), 140, H, d).to(torch.bfloat16)
+    for cache, table in ((big, far), (c.cache, c.table)):
+        lib.cast_cache_append(x, x, cache, table, c.kv_len)
+    for a, b in zip(lib.cast_cache_read(big, far, c.kv_len, 300), lib.cast_cache_read(c.cache, c.table, c.kv_len, 300)):
+        assert torch.equal(a, b)
+    lib.cast_check_device()
+
+
+def test_a_session_in_a_graph(lib):
+    """What serving does: prompts appended and attended to, then token by token the append, the attention and the reading
+    of the last page in one captured graph, replayed as the lengths grow; against 64 bits and against eager calls."""
+    B, H, H_q, d, page = 3, 2, 8, 128, 16
+    c = Pages4(lib, [200] * B, H, d, page, seed=5)
+    table = lib.rotary_table(d)
+    g = gen(1)
+    new = [100, 31, 64]
+    c.lens, c.kv_len = new, i32(*new)
+    cu = i32(*np.concatenate([[0], np.cumsum(new)]))
+    qkv = randn(g, sum(new), H_q + 2 * H, d).to(torch.bfloat16)
+    split = lambda x: (x[:, :H_q], x[:, H_q:H_q + H], x[:, H_q + H:])
+    q, k, v = split(qkv)
+    turned = lib.cast_cache_append(k, v, c.cache, c.table, c.kv_len, cu_new=cu, rotary=table, q=q)
+    o, lse = lib.cast_cache_attention(turned, c.cache, c.table, c.kv_len, cu_new=cu, want_lse=True)
+    held = [tuple(c.held(x, b)[0] for x in "kv") for b in range(B)]
+    check_attention(lib, c, held, turned, new, o, lse)
+    x = randn(g, B, H_q + 2 * H, d).to(torch.bfloat16)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+
+    def step():
+        c.kv_len += 1
+        q, k, v = split(x)
+        turned = lib.cast_cache_append(k, v, c.cache, c.table, c.kv_len, rotary=table, q=q)
+        return (turned, lib.cast_cache_attention(turned, c.cache, c.table, c.kv_len, window=150, sinks=4, workspace=ws),
+                *lib.cast_cache_read(c.cache, c.table, c.kv_len, B * 7))
+
+    step()   # not captured: loads what a first call loads
+    x.copy_(randn(g, *x.shape))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(20):
+        x.copy_(randn(g, *x.shape))
+        graph.replay()
+        if i % 6:
+            continue
+        c.lens = [n + 2 + i for n in new]
+        assert c.kv_len.tolist() == c.lens
+        held = [tuple(c.held(y, b)[0] for y in "kv") for b in range(B)]
+        check_attention(lib, c, held, out[0], [1] * B, out[1], None, window=150, sinks=4)
+        for b in range(B):
+            for y, z in zip(out[2:], held[b]):
+                assert np.array_equal(f64(y[7 * b:7 * b + 7]), z[-7:])
+        again = [t.clone() for t in out]
+        c.kv_len -= 1
+        for a, b in zip(again, step()):
+            assert torch.equal(a, b)
+    lib.cast_check_device()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_rollout_example(lib, bits):
+    """The example's steps with 4-bit pages against 64 bits, and its chunk routed over pages that are read back."""
+    from examples.cache_rollout import Rollout
+    r = Rollout(H=2, H_q=4, d=64, grid=(8, 8), page=64, n_pages=16, bits=bits, window=150)
+    for tokens, causal in ((64, False), (64, False), (1, True), (64, False), (64, False), (1, True)):
+        (q, k, v, pos), turned, o = r.step(tokens, causal)
+        kk, vv = lib.cast_cache_read(r.cache, r.table, r.kv_len, r.len, dtype=torch.float32)
+        if bits == 4:
+            ref, err = R.rotate(f64(k), pos.cpu().numpy(), 64, sections=[32 - 2 * 12, 12, 12])
+            page = lambda t: t.transpose(1, 2).reshape(-1, 2, t.shape[-1])[r.len - tokens:r.len].cpu().numpy()
+            R4.check_quantised(f64(kk[r.len - tokens:]), page(r.cache._keep[2]), ref, err)
+            want, _, eo, _ = R4.attention(f64(turned), f64(kk), f64(vv), r.len, causal, 150, 64)
+            assert (np.abs(f64(o).reshape(want.shape) - want) <= eo + R.UBF * (np.abs(want) + eo)).all()
+    k, v = r.blocks()
+    assert k.shape == (r.len // 64, 64, 2, 64) and torch.equal(k.reshape(-1, 2, 64).float(), kk[:r.len // 64 * 64])
+    assert torch.isfinite(r.routed_chunk(n_frames=3, anchors=(0, 2), K=2).float()).all()
+    lib.cast_check_device()
+
+
+def test_pages_of_the_type_of_two_values(lib):
+    if not hasattr(torch, "float4_e2m1fn_x2"):
+        pytest.skip("no such type")
+    c = Pages4(lib, [100], 2, 64, 16)
+    c.fill()
+    other = lib.kv_cache(c.k.view(torch.float4_e2m1fn_x2), c.v.view(torch.float4_e2m1fn_x2), c.ks, c.vs)
+    for a, b in zip(lib.cast_cache_read(c.cache, c.table, c.kv_len, 100), lib.cast_cache_read(other, c.table, c.kv_len, 100)):
+        assert torch.equal(a, b)
+
+
+def test_binding_refuses_tensors_that_are_not_on_the_gpu(lib):
+    c = Pages4(lib, [100], 2, 64, 16)
+    host = lib.kv_cache(*(t.cpu() for t in (c.k, c.v, c.ks, c.vs)))
+    some = lib.kv_cache(c.k, c.v, c.ks, c.vs.cpu())
+    out = torch.empty((5, 2, 64), dtype=torch.bfloat16)
+    for call in (lambda: lib.cast_cache_read(host, c.table, c.kv_len, 5), lambda: lib.cast_cache_read(some, c.table, c.kv_len, 5),
+                 lambda: lib.cast_cache_read(c.cache, c.table.cpu(), c.kv_len, 5), lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len.cpu(), 5),
+                 lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len, 5, cu_new=torch.tensor([0, 5], dtype=torch.int32)),
+                 lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len, 5, k_out=out), lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len, 5, v_out=out)):
+        with pytest.raises(ValueError):
+            call()
