@@ -473,7 +473,10 @@ cast_status launch_pages(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st)
   k_cache_rows4<D, NT, SMALL><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
-  return p.grid > 1 ? launch_joining(k_cuts_merge<D, C::ROWS>, p.grid - 1, st, k) : CAST_OK;
+  if (p.grid < 2) return CAST_OK;
+  // two rows a CTA of the joining where units have 16 parts or more on average
+  const int64_t units = (int64_t)k.batch.B * k.row_tiles * k.H;
+  return launch_joining(k_cuts_merge<D, C::ROWS>, p.grid - 1, p.grid >= 16 * units ? C::ROWS / 2 : 1, st, k);
 }
 
 template <int D, int NT>

@@ -616,7 +616,7 @@ cast_status launch_rows(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) 
   k_cache_rows<D, F8, MT><<<p.grid, kWarps * 32, C::SMEM, st>>>(k);
   cast_status s = check_launch("cache attention");
   if (s || p.whole) return s;
-  return launch_joining(k_cache_merge<D, C::ROWS>, (int64_t)k.batch.B * k.row_tiles * k.H, st, k, p.grid);
+  return launch_joining(k_cache_merge<D, C::ROWS>, (int64_t)k.batch.B * k.row_tiles * k.H, 1, st, k, p.grid);
 }
 
 }  // namespace

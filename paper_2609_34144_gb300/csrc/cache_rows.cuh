@@ -240,20 +240,21 @@ __device__ __forceinline__ void join_warps(const RowsKArgs& a, const Span& z, in
     }
 }
 
-// Joins the parts of the unit (h, tile) of a sequence that CTAs c0 .. c1 left: one warp a row and some of the parts
+// Joins the parts of rows lo .. hi-1 of the unit (h, tile) of a sequence that CTAs c0 .. c1 left: one warp a row and some of the parts
 // (lanes: four channels each), then over the warps of a row.
 constexpr int kMergeWarps = 16;
 template <int D, int ROWS>
-__device__ __forceinline__ void merge_unit(const RowsKArgs& a, int c0, int c1, int h, int tile, int t0, int n_rows) {
+__device__ __forceinline__ void merge_unit(const RowsKArgs& a, int c0, int c1, int h, int tile, int t0, int n_rows, int lo = 0,
+                                           int hi = ROWS) {
   constexpr int LANES = D / 4, GROUPS = 32 / LANES;   // GROUPS parts at a time in a warp
   __shared__ float4 s_o[kMergeWarps * GROUPS][LANES];
   __shared__ float2 s_ml[kMergeWarps * GROUPS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // warps_per_row warps (a power of two) have every warps_per_row-th part of a row
-  const int rows = min(ROWS, n_rows - tile * ROWS), parts = c1 - c0 + 1;
+  const int rows = min(hi, n_rows - tile * ROWS), parts = c1 - c0 + 1;
   int per_row = 1;
-  while (per_row * 2 * rows <= kMergeWarps && per_row * GROUPS < parts) per_row *= 2;
-  for (int r0 = 0; r0 < rows; r0 += kMergeWarps / per_row) {
+  while (per_row * 2 * (rows - lo) <= kMergeWarps && per_row * GROUPS < parts) per_row *= 2;
+  for (int r0 = lo; r0 < rows; r0 += kMergeWarps / per_row) {
     const int rr = r0 + warp / per_row, mine = (warp % per_row) * GROUPS + lane / LANES, c = lane % LANES;
     const bool in = rr < rows;
     // CTA c0 began the unit (its second place), the others began inside it (their first place)
@@ -349,20 +350,22 @@ __global__ void __launch_bounds__(kMergeWarps * 32) k_cache_merge(const __grid_c
 }
 
 // The same by what the CTAs left of their shares' beginnings: CTA x takes the unit that the share of CTA x + 1 begins
-// inside of, if that is the first such share.  Nothing is searched for (48 sequences of 8 heads, windows of 4096 tokens
+// inside of, if that is the first such share; y: some of its rows, where units have many parts.  Nothing is searched for (48 sequences of 8 heads, windows of 4096 tokens
 // of 4 bits 68.6 -> 66.6 us; 128 of 1k to 4k tokens 94 -> 87 us).
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kMergeWarps * 32) k_cuts_merge(const __grid_constant__ RowsKArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const RowsCut u = a.cuts[blockIdx.x + 1];
-  if (u.c0 == (int)blockIdx.x) merge_unit<D, ROWS>(a, u.c0, u.c1, u.h, u.tile, u.t0, u.n_rows);
+  const int each = ROWS / gridDim.y, lo = blockIdx.y * each;
+  if (u.c0 == (int)blockIdx.x && lo < u.n_rows - u.tile * ROWS)
+    merge_unit<D, ROWS>(a, u.c0, u.c1, u.h, u.tile, u.t0, u.n_rows, lo, lo + each);
 }
 
 // A joining's launch behind the kernel that left the parts
 template <class... A>
-cast_status launch_joining(void (*kernel)(A...), int64_t grid, cudaStream_t st, A... args) {
+cast_status launch_joining(void (*kernel)(A...), int64_t grid, int rows, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid, 1, 1);
+  cfg.gridDim = dim3((unsigned)grid, rows, 1);
   cfg.blockDim = dim3(kMergeWarps * 32, 1, 1);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
