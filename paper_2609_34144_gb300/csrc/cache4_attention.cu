@@ -37,11 +37,15 @@ struct Cfg4 {
   static constexpr int BLOCK = BT * ROWB, SBLOCK = BT * SROWB;
   static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
   static constexpr int CTAS = D * NT <= 128 ? 4 : 3;      // of an SM
-  static constexpr int ROOM = (CTAS == 4 ? 13 * 1024 + 512 : 18 * 1024);   // a warp's ring at most
+  // 16 rows: their queries in shared memory, which leaves the registers to the loop (24 sequences of 8k to 32k tokens, 9
+  // rows a KV head, heads of 128 176 -> 169 us, of 64 120 -> 112); with 8 rows there are enough (130 -> 134 us)
+  static constexpr bool QS = NT > 1;
+  static constexpr int ROOM = CTAS == 4 ? 13 * 1024 + 512 - (QS ? 1024 : 0) : 17 * 1024;   // a warp's ring at most
   static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
   static constexpr int RING = STAGES * STAGE;
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
-  static constexpr int SMEM = kWarps * RING > MERGE ? kWarps * RING : MERGE;
+  static constexpr int OFF_Q = kWarps * RING > MERGE ? kWarps * RING : MERGE;
+  static constexpr int SMEM = OFF_Q + (QS ? NT * (D / 16) * 32 * 8 : 0);
   static_assert(STAGES >= 3 && (SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
 };
 
@@ -169,6 +173,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
 
       // Q^T fragments: row g of each 8 (product s takes channels (D / 4) q4 + 4 s .. + 3 of lane group q4)
       uint32_t qf[NT][D / 16][2];
+      uint2* qs = reinterpret_cast<uint2*>(smem + C::OFF_Q) + lane;   // [NT][D / 16][lane]
       float unit[NT][2];   // what the logits of rows 2 q4 and 2 q4 + 1 are multiplied by
       int pos[NT][2];      // their positions
 #pragma unroll
@@ -205,6 +210,12 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             const uint32_t w = qf[t][s][j];
             qf[t][s][j] = pack2h(__uint_as_float(w << 16) * down, __uint_as_float(w & 0xffff0000u) * down);
           }
+        if constexpr (C::QS) {
+          // the warps' are alike: each leaves some
+#pragma unroll
+          for (int s = 0; s < D / 16; ++s)
+            if ((s & (kWarps - 1)) == warp) qs[(t * (D / 16) + s) * 32] = make_uint2(qf[t][s][0], qf[t][s][1]);
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           unit[t][j] = __shfl_sync(0xffffffffu, up, (2 * q4 + j) * 4);
@@ -212,6 +223,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
           pos[t][j] = rr < z.n_rows ? z.p0 + rr / a.group : -1;
         }
       }
+      if constexpr (C::QS) __syncthreads();
       // positions that every row sees: [all_lo, all_hi); the others' blocks are masked
       int all_lo = 0, all_hi = z.hi;
       {
@@ -285,7 +297,14 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             for (int u = 0; u < 2; ++u) {
               const uint32_t f[4] = {x[2 * u], y[2 * u], x[2 * u + 1], y[2 * u + 1]};
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma16816h(s[t][half], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
+              for (int t = 0; t < NT; ++t) {
+                if constexpr (C::QS) {
+                  const uint2 q = qs[(t * (D / 16) + 2 * w + u) * 32];
+                  mma16816h(s[t][half], f, q.x, q.y);
+                } else {
+                  mma16816h(s[t][half], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
+                }
+              }
             }
           }
         }
