@@ -1,6 +1,6 @@
 // Attention over 4-bit pages for few rows a sequence (single tokens, drafts): k_cache_rows4.  Units, shares of the
 // work and the joining are those of k_cache_rows (cache_attention.cu); inside a CTA each warp works on its own blocks
-// of 32 tokens with its own running maximum, sum and o in registers.
+// of 32 (64) tokens with its own running maximum, sum and o in registers.
 //
 // The codes become f16 in registers (a conversion and a product with the scale for two, both exact), so the issue of
 // instructions is what bounds the kernel beside memory, and everything follows from it:
@@ -27,12 +27,12 @@
 namespace cast {
 namespace {
 
-constexpr int BT = 32;   // tokens of a block: two products' sixteen
-
 // NT: units of 8 NT rows
 template <int D, int NT>
 struct Cfg4 {
   static constexpr int ROWS = 8 * NT;
+  // tokens of a block: two products' sixteen, or four where that is no more bytes and registers
+  static constexpr int BT = D * NT == 64 ? 64 : 32, SUB = BT / 16;
   static constexpr int ROWB = D / 2, SROWB = D / 16;      // bytes of a token's codes and scales
   static constexpr int BLOCK = BT * ROWB, SBLOCK = BT * SROWB;
   static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
@@ -58,10 +58,11 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// SMALL: pages of 16 tokens, of which a block has two; else a block lies in one page
+// SMALL: a block has several pages; else it lies in one
 template <int D, int NT, bool SMALL>
 __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
   using C = Cfg4<D, NT>;
+  constexpr int BT = C::BT, SUB = C::SUB;
   constexpr int KW = D / 32;   // words of a lane's part of a K row; a V row's part has D / 64
   constexpr int VW = D / 64;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -107,16 +108,21 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         }
         return page;
       };
-      // The pages of block i's halves (small pages: -1 too where no row sees any of it)
+      // The pages of block i's sixteens, or its page (small pages: -1 too where no row sees any of the sixteen)
+      struct Pages {
+        int p[SMALL ? SUB : 1];
+      };
       auto pages_of = [&](int i) {
         const int base = z.block(i) * BT;
-        int2 pages;
+        Pages pages;
         if constexpr (SMALL) {
-          auto some = [&](int p) { return p < z.hi && (p + 16 > z.lo || p < z.sinks); };
-          pages.x = some(base) ? page_at(base) : -1;
-          pages.y = some(base + 16) ? page_at(base + 16) : -1;
+#pragma unroll
+          for (int k = 0; k < SUB; ++k) {
+            const int p = base + 16 * k;
+            pages.p[k] = p < z.hi && (p + 16 > z.lo || p < z.sinks) ? page_at(p) : -1;
+          }
         } else {
-          pages.x = pages.y = page_at(base);
+          pages.p[0] = page_at(base);
         }
         return pages;
       };
@@ -128,28 +134,30 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const uint8_t* my_scales = (lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
       const int64_t page_scales = (int64_t)a.H * a.page_size * C::SROWB;
       // fetches block i of the unit into stage st
-      auto fetch = [&](int i, int st, int2 pages) {
-        const int row = (z.block(i) * BT) & (a.page_size - 1);
+      auto fetch = [&](int i, int st, const Pages& pages) {
+        const int base = z.block(i) * BT;
         const uint32_t dst = ring_at + st * C::STAGE + lane * 16;
         if constexpr (SMALL) {
+          constexpr int PART = C::BLOCK / SUB, EACH = SCH / SUB;   // bytes of a sixteen's codes, chunks of its scales
+          const int mine = (lane & (SCH - 1)) / EACH;              // the sixteen whose scales this lane copies
+          auto row_of = [&](int k) { return BT == 32 ? 0 : (base + 16 * k) & (a.page_size - 1); };   // (32: pages of 16)
+          int page_mine = 0;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int page = half ? pages.y : pages.x;
+          for (int k = 0; k < SUB; ++k) {
+            const int page = pages.p[k];
+            if (mine == k) page_mine = page;
             if (page < 0) continue;
-            const uint8_t* from = my_codes + page * page_bytes;
+            const uint8_t* from = my_codes + (page * page_bytes + row_of(k) * C::ROWB);
 #pragma unroll
-            for (int c = 0; c < C::BLOCK / 2; c += 512) {
-              copy16(dst + half * (C::BLOCK / 2) + c, from + c);
-              copy16(dst + C::BLOCK + half * (C::BLOCK / 2) + c, from + to_v + c);
+            for (int c = 0; c < PART; c += 512) {
+              copy16(dst + k * PART + c, from + c);
+              copy16(dst + C::BLOCK + k * PART + c, from + to_v + c);
             }
           }
-          if (lane < 2 * SCH) {
-            const bool second = (lane & (SCH - 1)) >= SCH / 2;
-            const int page = second ? pages.y : pages.x;
-            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + max(page, 0) * page_scales - (second ? SCH / 2 * 16 : 0), page >= 0);
-          }
+          if (lane < 2 * SCH)
+            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (max(page_mine, 0) * page_scales + (row_of(mine) - 16 * mine) * C::SROWB), page_mine >= 0);
         } else {
-          const int page = pages.x;
+          const int page = pages.p[0], row = base & (a.page_size - 1);
           if (page >= 0) {
             const uint8_t* from = my_codes + (page * page_bytes + row * C::ROWB);
 #pragma unroll
@@ -169,7 +177,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         if (st < n) fetch(i0 + st * kWarps, st, pages_of(i0 + st * kWarps));
         copy_commit();
       }
-      int2 next_pages = C::STAGES - 1 < n ? pages_of(i0 + (C::STAGES - 1) * kWarps) : make_int2(-1, -1);
+      Pages next_pages{};
+      if (C::STAGES - 1 < n) next_pages = pages_of(i0 + (C::STAGES - 1) * kWarps);
 
       // Q^T fragments: row g of each 8 (product s takes channels (D / 4) q4 + 4 s .. + 3 of lane group q4)
       uint32_t qf[NT][D / 16][2];
@@ -258,18 +267,18 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         const uint8_t* ks = kt + 2 * C::BLOCK;
         const uint8_t* vs = ks + C::SBLOCK;
 
-        // ---- S^T = K Q^T, of 16 tokens and of the other 16
-        float s[NT][2][4];
+        // ---- S^T = K Q^T, 16 tokens after 16
+        float s[NT][SUB][4];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int part = 0; part < SUB; ++part) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][half][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s[t][part][e] = 0.f;
           uint32_t kw[2][KW], sc[2][2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int token = 16 * half + kt0 + 8 * j;
+            const int token = 16 * part + kt0 + 8 * j;
             const uint8_t* p = kt + token * C::ROWB + q4 * (D / 8);
             if constexpr (D == 128) {
               const uint4 w = *reinterpret_cast<const uint4*>(p);
@@ -300,9 +309,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
               for (int t = 0; t < NT; ++t) {
                 if constexpr (C::QS) {
                   const uint2 q = qs[(t * (D / 16) + 2 * w + u) * 32];
-                  mma16816h(s[t][half], f, q.x, q.y);
+                  mma16816h(s[t][part], f, q.x, q.y);
                 } else {
-                  mma16816h(s[t][half], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
+                  mma16816h(s[t][part], f, qf[t][2 * w + u][0], qf[t][2 * w + u][1]);
                 }
               }
             }
@@ -315,10 +324,10 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int part = 0; part < SUB; ++part)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                s[t][half][e] = sees(base + 16 * half + kt0 + (e & 2 ? 8 : 0), pos[t][e & 1]) ? s[t][half][e] * unit[t][e & 1] : -INFINITY;
+                s[t][part][e] = sees(base + 16 * part + kt0 + (e & 2 ? 8 : 0), pos[t][e & 1]) ? s[t][part][e] * unit[t][e & 1] : -INFINITY;
         }
 
         // ---- running maximum; what is left of a logit's factor
@@ -329,7 +338,10 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             times[t][j] = whole ? unit[t][j] : 1.f;
-            top[t][j] = fmaxf(fmaxf(s[t][0][j], s[t][0][2 + j]), fmaxf(s[t][1][j], s[t][1][2 + j])) * times[t][j];
+            float x = fmaxf(s[t][0][j], s[t][0][2 + j]);
+#pragma unroll
+            for (int k = 1; k < SUB; ++k) x = fmaxf(x, fmaxf(s[t][k][j], s[t][k][2 + j]));
+            top[t][j] = x * times[t][j];
             grows = grows || top[t][j] > m_ref[t][j] + kRescale;
           }
         if (__any_sync(0xffffffffu, grows)) {
@@ -354,7 +366,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             }
         }
         // ---- P^T, 2^kLift times the probabilities; l is the sum of them as they are before the rounding
-        uint32_t pf[NT][2][2];
+        uint32_t pf[NT][SUB][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -362,26 +374,29 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             // a row that has seen nothing yet: exp2(-inf - 0) = 0
             const float ref = kLift - (m_ref[t][j] == -INFINITY ? 0.f : m_ref[t][j]);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              s[t][half][j] = exp2_fast(fmaf(s[t][half][j], times[t][j], ref));
-              s[t][half][2 + j] = exp2_fast(fmaf(s[t][half][2 + j], times[t][j], ref));
+            for (int part = 0; part < SUB; ++part) {
+              s[t][part][j] = exp2_fast(fmaf(s[t][part][j], times[t][j], ref));
+              s[t][part][2 + j] = exp2_fast(fmaf(s[t][part][2 + j], times[t][j], ref));
             }
-            l[t][j] += (s[t][0][j] + s[t][0][2 + j]) + (s[t][1][j] + s[t][1][2 + j]);
+            float sum = s[t][0][j] + s[t][0][2 + j];
+#pragma unroll
+            for (int k = 1; k < SUB; ++k) sum += s[t][k][j] + s[t][k][2 + j];
+            l[t][j] += sum;
           }
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            pf[t][half][0] = transposed(pack2h(s[t][half][0], s[t][half][1]));
-            pf[t][half][1] = transposed(pack2h(s[t][half][2], s[t][half][3]));
+          for (int part = 0; part < SUB; ++part) {
+            pf[t][part][0] = transposed(pack2h(s[t][part][0], s[t][part][1]));
+            pf[t][part][1] = transposed(pack2h(s[t][part][2], s[t][part][3]));
           }
         }
 
         // ---- o^T += V^T P^T
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int part = 0; part < SUB; ++part) {
           uint32_t vw[4][VW], vc[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int token = 16 * half + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+            const int token = 16 * part + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
             const uint8_t* p = vt + token * C::ROWB + g * (D / 16);
             if constexpr (D == 128) {
               const uint2 w = *reinterpret_cast<const uint2*>(p);
@@ -397,7 +412,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
           if (!whole) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int p = base + 16 * half + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
+              const int p = base + 16 * part + (j & 1 ? vt1 : vt0) + (j & 2 ? 8 : 0);
               if (!(p < z.hi && (p >= z.lo || p < z.sinks))) vc[j] = 0;   // nobody's
               apart |= vc[j] > kScaleTop;
             }
@@ -409,18 +424,18 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
             for (int token = 0; token < 16; ++token) {
               // the lane group whose K token this is: row 2 q + j of token 4 j + (q ^ j)
               const int k = token & 7, from = (2 * ((k & 3) ^ (k >> 2)) + (k >> 2)) * 4 + q4;
-              const int p = base + 16 * half + token;
+              const int p = base + 16 * part + token;
 #pragma unroll
               for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                  const float w0 = __shfl_sync(0xffffffffu, s[t][half][j], from), w1 = __shfl_sync(0xffffffffu, s[t][half][2 + j], from);
+                  const float w0 = __shfl_sync(0xffffffffu, s[t][part][j], from), w1 = __shfl_sync(0xffffffffu, s[t][part][2 + j], from);
                   if (!sees(p, pos[t][j])) continue;
                   const float w = token < 8 ? w0 : w1;
-                  const uint32_t scale = vs[(16 * half + token) * C::SROWB + (D == 128 ? g : g >> 1)];
+                  const uint32_t scale = vs[(16 * part + token) * C::SROWB + (D == 128 ? g : g >> 1)];
 #pragma unroll
                   for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t two = vt[(16 * half + token) * C::ROWB + g * (D / 16) + i];
+                    const uint32_t two = vt[(16 * part + token) * C::ROWB + g * (D / 16) + i];
                     o[t][i][j] += w * value4(two, scale);
                     o[t][i][2 + j] += w * value4(two >> 4, scale);
                   }
@@ -441,7 +456,7 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
               for (int e = 0; e < 4; ++e) {
                 const uint32_t f[4] = {times2(x[e], s0), times2(y[e], s0), times2(u[e], s1), times2(v[e], s1)};
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma16816h(o[t][4 * w + e], f, pf[t][half][0], pf[t][half][1]);
+                for (int t = 0; t < NT; ++t) mma16816h(o[t][4 * w + e], f, pf[t][part][0], pf[t][part][1]);
               }
             }
           }
@@ -500,7 +515,7 @@ cast_status launch_pages(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st)
 
 template <int D, int NT>
 cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
-  return k.page_size == 16 ? launch_pages<D, NT, true>(k, p, st) : launch_pages<D, NT, false>(k, p, st);
+  return k.page_size < Cfg4<D, NT>::BT ? launch_pages<D, NT, true>(k, p, st) : launch_pages<D, NT, false>(k, p, st);
 }
 
 }  // namespace
@@ -508,6 +523,11 @@ cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
 int rows4_ctas(int d, int mt) {
   if (d == 128) return mt == 1 ? Cfg4<128, 1>::CTAS : Cfg4<128, 2>::CTAS;
   return mt == 1 ? Cfg4<64, 1>::CTAS : Cfg4<64, 2>::CTAS;
+}
+
+int rows4_block(int d, int mt) {
+  if (d == 128) return mt == 1 ? Cfg4<128, 1>::BT : Cfg4<128, 2>::BT;
+  return mt == 1 ? Cfg4<64, 1>::BT : Cfg4<64, 2>::BT;
 }
 
 cast_status launch_rows4(const RowsKArgs& k, const RowsPlan& p, int d, cudaStream_t st) {
