@@ -32,21 +32,21 @@ template <int D, int NT>
 struct Cfg4 {
   static constexpr int ROWS = 8 * NT;
   // tokens of a block: two products' sixteen, or four where that is no more bytes and registers
-  static constexpr int BT = D * NT == 64 ? 64 : 32, SUB = BT / 16;
+  static constexpr int BT = NT == 1 ? 64 : 32, SUB = BT / 16;
   static constexpr int ROWB = D / 2, SROWB = D / 16;      // bytes of a token's codes and scales
   static constexpr int BLOCK = BT * ROWB, SBLOCK = BT * SROWB;
   static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
-  static constexpr int CTAS = D * NT <= 128 ? 4 : 3;      // of an SM
+  static constexpr int CTAS = D == 128 ? 3 : 4;      // of an SM
   // 16 rows: their queries in shared memory, which leaves the registers to the loop (24 sequences of 8k to 32k tokens, 9
   // rows a KV head, heads of 128 176 -> 169 us, of 64 120 -> 112); with 8 rows there are enough (130 -> 134 us)
   static constexpr bool QS = NT > 1;
-  static constexpr int ROOM = CTAS == 4 ? 13 * 1024 + 512 - (QS ? 1024 : 0) : 17 * 1024;   // a warp's ring at most
+  static constexpr int ROOM = CTAS == 4 ? 13 * 1024 + 512 - (QS ? 1024 : 0) : D == 128 && NT == 1 ? 18 * 1024 + 256 : 17 * 1024;   // a warp's ring at most
   static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
   static constexpr int RING = STAGES * STAGE;
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
   static constexpr int OFF_Q = kWarps * RING > MERGE ? kWarps * RING : MERGE;
   static constexpr int SMEM = OFF_Q + (QS ? NT * (D / 16) * 32 * 8 : 0);
-  static_assert(STAGES >= 3 && (SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
+  static_assert(STAGES >= 2 && (SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
 };
 
 // The block's token that lane group g's row of a product is (and token + 8 that row g + 8 is): token 4 j + (q ^ j) for
@@ -131,7 +131,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       const uint8_t* my_codes = a.k + (int64_t)h * a.page_size * C::ROWB + lane * 16;
       const int64_t to_v = a.v - a.k;
       constexpr int SCH = C::SBLOCK / 16;   // chunks of K's (V's) scales
-      const uint8_t* my_scales = (lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
+      constexpr bool BOTH = SCH == 32;      // a lane copies a chunk of each
+      const int64_t to_vs = vscale - kscale;
+      const uint8_t* my_scales = (BOTH || lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
       const int64_t page_scales = (int64_t)a.H * a.page_size * C::SROWB;
       // fetches block i of the unit into stage st
       auto fetch = [&](int i, int st, const Pages& pages) {
@@ -154,8 +156,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
               copy16(dst + C::BLOCK + k * PART + c, from + to_v + c);
             }
           }
-          if (lane < 2 * SCH)
-            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (max(page_mine, 0) * page_scales + (row_of(mine) - 16 * mine) * C::SROWB), page_mine >= 0);
+          const uint8_t* from = my_scales + (max(page_mine, 0) * page_scales + (row_of(mine) - 16 * mine) * C::SROWB);
+          if (lane < 2 * SCH) copy16_or_zero(dst + 2 * C::BLOCK, from, page_mine >= 0);
+          if (BOTH) copy16_or_zero(dst + 2 * C::BLOCK + C::SBLOCK, from + to_vs, page_mine >= 0);
         } else {
           const int page = pages.p[0], row = base & (a.page_size - 1);
           if (page >= 0) {
@@ -166,8 +169,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
               copy16(dst + C::BLOCK + c, from + to_v + c);
             }
           }
-          if (lane < 2 * SCH)
-            copy16_or_zero(dst + 2 * C::BLOCK, my_scales + (max(page, 0) * page_scales + row * C::SROWB), page >= 0);
+          const uint8_t* from = my_scales + (max(page, 0) * page_scales + row * C::SROWB);
+          if (lane < 2 * SCH) copy16_or_zero(dst + 2 * C::BLOCK, from, page >= 0);
+          if (BOTH) copy16_or_zero(dst + 2 * C::BLOCK + C::SBLOCK, from + to_vs, page >= 0);
         }
       };
       const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
