@@ -99,90 +99,66 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
       if (k0 > 0 && threadIdx.x == 0)
         a.cuts[blockIdx.x] = RowsCut{(int)blockIdx.x - (k0 + share - 1) / share, (int)blockIdx.x + (nb - 1 - k0) / share, h, tile, z.t0, z.n_rows};
 
-      // The page of tokens p .. (-1: out of range, reads as zeros)
-      auto page_at = [&](int p) {
-        int page = __ldg(table + (p >> a.page_shift));
-        if ((unsigned)page >= (unsigned)a.n_pages) {
-          if (lane == 0) left_out();
-          page = -1;
+      // The page of block i (-1: out of range, reads as zeros); small pages: lane group lane / LANES has that of its
+      // sixteen tokens (-1 too where no row sees any of them)
+      constexpr int LANES = SMALL ? 32 / SUB : 32;
+      const int group = lane / LANES;
+      auto page_of = [&](int i) {
+        const int p = z.block(i) * BT + (SMALL ? 16 * group : 0);
+        int page = -1;
+        if (!SMALL || (p < z.hi && (p + 16 > z.lo || p < z.sinks))) {
+          page = __ldg(table + (p >> a.page_shift));
+          if ((unsigned)page >= (unsigned)a.n_pages) {
+            if (lane % LANES == 0) left_out();
+            page = -1;
+          }
         }
         return page;
       };
-      // The pages of block i's sixteens, or its page (small pages: -1 too where no row sees any of the sixteen)
-      struct Pages {
-        int p[SMALL ? SUB : 1];
-      };
-      auto pages_of = [&](int i) {
-        const int base = z.block(i) * BT;
-        Pages pages;
-        if constexpr (SMALL) {
-#pragma unroll
-          for (int k = 0; k < SUB; ++k) {
-            const int p = base + 16 * k;
-            pages.p[k] = p < z.hi && (p + 16 > z.lo || p < z.sinks) ? page_at(p) : -1;
-          }
-        } else {
-          pages.p[0] = page_at(base);
-        }
-        return pages;
-      };
-      // A lane's part of a block: 16 bytes of each 512 of its codes (K's, and V's at the same distance), and of the
-      // scales: K's, behind them V's
-      const uint8_t* my_codes = a.k + (int64_t)h * a.page_size * C::ROWB + lane * 16;
-      const int64_t to_v = a.v - a.k;
-      constexpr int SCH = C::SBLOCK / 16;   // chunks of K's (V's) scales
-      constexpr bool BOTH = SCH == 32;      // a lane copies a chunk of each
-      const int64_t to_vs = vscale - kscale;
+      // A lane's part of a block: 16 bytes of each 512 of its codes (small pages: of each 128 or 256 of its sixteen's), K's
+      // and V's at the same distance, and of the scales: K's, behind them V's
+      const int64_t to_v = a.v - a.k, to_vs = vscale - kscale;
+      constexpr int SCH = C::SBLOCK / 16, EACH = SCH / SUB;   // chunks of K's (V's) scales, and of a sixteen's
+      constexpr bool BOTH = SCH == 32;                        // a lane copies a chunk of each
+      const uint8_t* my_codes = a.k + (int64_t)h * a.page_size * C::ROWB + lane % LANES * 16;
       const uint8_t* my_scales = (BOTH || lane < SCH ? kscale : vscale) + (int64_t)h * a.page_size * C::SROWB + (lane & (SCH - 1)) * 16;
       const int64_t page_scales = (int64_t)a.H * a.page_size * C::SROWB;
+      const int scale_group = (lane & (SCH - 1)) / EACH;
       // fetches block i of the unit into stage st
-      auto fetch = [&](int i, int st, const Pages& pages) {
+      auto fetch = [&](int i, int st, int page) {
         const int base = z.block(i) * BT;
-        const uint32_t dst = ring_at + st * C::STAGE + lane * 16;
-        if constexpr (SMALL) {
-          constexpr int PART = C::BLOCK / SUB, EACH = SCH / SUB;   // bytes of a sixteen's codes, chunks of its scales
-          const int mine = (lane & (SCH - 1)) / EACH;              // the sixteen whose scales this lane copies
-          auto row_of = [&](int k) { return BT == 32 ? 0 : (base + 16 * k) & (a.page_size - 1); };   // (32: pages of 16)
-          int page_mine = 0;
+        const uint32_t dst = ring_at + st * C::STAGE;
+        // (small pages shorter than a block: its sixteens begin at rows 0, 16 or 32 of theirs)
+        const int row = (base + (SMALL ? 16 * group : 0)) & (a.page_size - 1);
+        constexpr int PART = SMALL ? C::BLOCK / SUB : C::BLOCK;
+        if (page >= 0) {
+          const uint8_t* from = my_codes + (page * page_bytes + row * C::ROWB);
+          const uint32_t to = dst + (SMALL ? group * PART : 0) + lane % LANES * 16;
 #pragma unroll
-          for (int k = 0; k < SUB; ++k) {
-            const int page = pages.p[k];
-            if (mine == k) page_mine = page;
-            if (page < 0) continue;
-            const uint8_t* from = my_codes + (page * page_bytes + row_of(k) * C::ROWB);
-#pragma unroll
-            for (int c = 0; c < PART; c += 512) {
-              copy16(dst + k * PART + c, from + c);
-              copy16(dst + C::BLOCK + k * PART + c, from + to_v + c);
-            }
+          for (int c = 0; c < PART; c += LANES * 16) {
+            copy16(to + c, from + c);
+            copy16(to + C::BLOCK + c, from + to_v + c);
           }
-          const uint8_t* from = my_scales + (max(page_mine, 0) * page_scales + (row_of(mine) - 16 * mine) * C::SROWB);
-          if (lane < 2 * SCH) copy16_or_zero(dst + 2 * C::BLOCK, from, page_mine >= 0);
-          if (BOTH) copy16_or_zero(dst + 2 * C::BLOCK + C::SBLOCK, from + to_vs, page_mine >= 0);
-        } else {
-          const int page = pages.p[0], row = base & (a.page_size - 1);
-          if (page >= 0) {
-            const uint8_t* from = my_codes + (page * page_bytes + row * C::ROWB);
-#pragma unroll
-            for (int c = 0; c < C::BLOCK; c += 512) {
-              copy16(dst + c, from + c);
-              copy16(dst + C::BLOCK + c, from + to_v + c);
-            }
-          }
-          const uint8_t* from = my_scales + (max(page, 0) * page_scales + row * C::SROWB);
-          if (lane < 2 * SCH) copy16_or_zero(dst + 2 * C::BLOCK, from, page >= 0);
-          if (BOTH) copy16_or_zero(dst + 2 * C::BLOCK + C::SBLOCK, from + to_vs, page >= 0);
         }
+        // the scales' page and row: this lane's, or, where a lane has one chunk of K or V, that of the chunk's sixteen
+        int s_page = page, s_row = row;
+        if constexpr (SMALL && !BOTH) {
+          s_page = __shfl_sync(0xffffffffu, page, scale_group * LANES);
+          s_row = (base + 16 * scale_group) & (a.page_size - 1);
+        }
+        const uint8_t* from = my_scales + (max(s_page, 0) * page_scales + (s_row - (SMALL ? 16 * scale_group : 0)) * C::SROWB);
+        const uint32_t to = dst + 2 * C::BLOCK + lane * 16;
+        if (lane < 2 * SCH) copy16_or_zero(to, from, s_page >= 0);
+        if (BOTH) copy16_or_zero(to + C::SBLOCK, from + to_vs, s_page >= 0);
       };
       const int n = k1 - k0 > warp ? (k1 - k0 - warp + kWarps - 1) >> kWarpsLog : 0;   // blocks of this warp
       const int i0 = k0 + warp;
       __syncwarp();
       for (int st = 0; st < C::STAGES - 1; ++st) {
-        if (st < n) fetch(i0 + st * kWarps, st, pages_of(i0 + st * kWarps));
+        if (st < n) fetch(i0 + st * kWarps, st, page_of(i0 + st * kWarps));
         copy_commit();
       }
-      Pages next_pages{};
-      if (C::STAGES - 1 < n) next_pages = pages_of(i0 + (C::STAGES - 1) * kWarps);
+      int next_page = C::STAGES - 1 < n ? page_of(i0 + (C::STAGES - 1) * kWarps) : -1;
 
       // Q^T fragments: row g of each 8 (product s takes channels (D / 4) q4 + 4 s .. + 3 of lane group q4)
       uint32_t qf[NT][D / 16][2];
@@ -263,9 +239,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         __syncwarp();
         // the stage used one block ago takes the block STAGES - 1 ahead
         const int ahead = it + C::STAGES - 1;
-        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_pages);
+        if (ahead < n) fetch(i0 + ahead * kWarps, into, next_page);
         copy_commit();
-        if (ahead + 1 < n) next_pages = pages_of(i0 + (ahead + 1) * kWarps);
+        if (ahead + 1 < n) next_page = page_of(i0 + (ahead + 1) * kWarps);
         const uint8_t* kt = ring + st * C::STAGE;
         const uint8_t* vt = kt + C::BLOCK;
         const uint8_t* ks = kt + 2 * C::BLOCK;
