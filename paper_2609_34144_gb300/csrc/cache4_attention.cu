@@ -1,6 +1,6 @@
 // Attention over 4-bit pages for few rows a sequence (single tokens, drafts): k_cache_rows4.  Units, shares of the
 // work and the joining are those of k_cache_rows (cache_attention.cu); inside a CTA each warp works on its own blocks
-// of 32 (64) tokens with its own running maximum, sum and o in registers.
+// of 64 tokens with its own running maximum, sum and o in registers.
 //
 // The codes become f16 in registers (a conversion and a product with the scale for two, both exact), so the issue of
 // instructions is what bounds the kernel beside memory, and everything follows from it:
@@ -27,20 +27,23 @@
 namespace cast {
 namespace {
 
+constexpr int BT = 64, SUB = BT / 16;   // tokens of a block: four products' sixteen
+
 // NT: units of 8 NT rows
 template <int D, int NT>
 struct Cfg4 {
   static constexpr int ROWS = 8 * NT;
-  // tokens of a block: two products' sixteen, or four where that is no more bytes and registers
-  static constexpr int BT = NT == 1 ? 64 : 32, SUB = BT / 16;
   static constexpr int ROWB = D / 2, SROWB = D / 16;      // bytes of a token's codes and scales
   static constexpr int BLOCK = BT * ROWB, SBLOCK = BT * SROWB;
   static constexpr int STAGE = 2 * (BLOCK + SBLOCK);      // codes of K, of V, scales of K, of V
-  static constexpr int CTAS = D == 128 ? 3 : 4;      // of an SM
-  // 16 rows: their queries in shared memory, which leaves the registers to the loop (24 sequences of 8k to 32k tokens, 9
-  // rows a KV head, heads of 128 176 -> 169 us, of 64 120 -> 112); with 8 rows there are enough (130 -> 134 us)
+  // Fewer CTAs and larger blocks: what a block costs besides its products is a third of the instructions at 32 tokens
+  // (24 sequences of 8k to 32k tokens, heads of 128, 32 tokens and four CTAs 130 us, 64 and three 115, and two 126;
+  // heads of 64 85 and 77; 9 rows a KV head 170 and 163, of 64 114 and 100)
+  static constexpr int CTAS = D == 128 ? (NT == 1 ? 3 : 2) : (NT == 1 ? 4 : 3);   // of an SM
+  // 16 rows: their queries in shared memory, which leaves the registers to the loop (at 32 tokens 176 -> 169 us, heads of
+  // 64 120 -> 112); with 8 rows there are enough (130 -> 134)
   static constexpr bool QS = NT > 1;
-  static constexpr int ROOM = CTAS == 4 ? 13 * 1024 + 512 - (QS ? 1024 : 0) : D == 128 && NT == 1 ? 18 * 1024 + 256 : 17 * 1024;   // a warp's ring at most
+  static constexpr int ROOM = D == 128 ? (NT == 1 ? 18 * 1024 + 256 : 25 * 1024) : (NT == 1 ? 13 * 1024 + 512 : 17 * 1024);   // a warp's ring
   static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
   static constexpr int RING = STAGES * STAGE;
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
@@ -62,7 +65,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 template <int D, int NT, bool SMALL>
 __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(const __grid_constant__ RowsKArgs a) {
   using C = Cfg4<D, NT>;
-  constexpr int BT = C::BT, SUB = C::SUB;
   constexpr int KW = D / 32;   // words of a lane's part of a K row; a V row's part has D / 64
   constexpr int VW = D / 64;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -495,7 +497,7 @@ cast_status launch_pages(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st)
 
 template <int D, int NT>
 cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
-  return k.page_size < Cfg4<D, NT>::BT ? launch_pages<D, NT, true>(k, p, st) : launch_pages<D, NT, false>(k, p, st);
+  return k.page_size < BT ? launch_pages<D, NT, true>(k, p, st) : launch_pages<D, NT, false>(k, p, st);
 }
 
 }  // namespace
@@ -503,11 +505,6 @@ cast_status launch(const RowsKArgs& k, const RowsPlan& p, cudaStream_t st) {
 int rows4_ctas(int d, int mt) {
   if (d == 128) return mt == 1 ? Cfg4<128, 1>::CTAS : Cfg4<128, 2>::CTAS;
   return mt == 1 ? Cfg4<64, 1>::CTAS : Cfg4<64, 2>::CTAS;
-}
-
-int rows4_block(int d, int mt) {
-  if (d == 128) return mt == 1 ? Cfg4<128, 1>::BT : Cfg4<128, 2>::BT;
-  return mt == 1 ? Cfg4<64, 1>::BT : Cfg4<64, 2>::BT;
 }
 
 cast_status launch_rows4(const RowsKArgs& k, const RowsPlan& p, int d, cudaStream_t st) {

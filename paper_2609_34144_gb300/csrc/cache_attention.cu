@@ -543,7 +543,7 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   int dev = 0, nsm = 152;
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev);
   p.grid = (f4 ? rows4_ctas(a.cache.d, p.mt) : a.cache.dtype == CAST_F8E4M3 ? Cfg<128, true, 1>::CTAS : Cfg<128, false, 1>::CTAS) * (nsm < 1 ? 1 : nsm);
-  p.least = f4 ? 256 / rows4_block(a.cache.d, p.mt) : 16;
+  p.least = f4 ? 4 : 16;   // blocks of 64 tokens, or of 16
   // Blocks that a unit has at most.  Up to 64 (a thousand tokens: four blocks' latency a warp's ring)
   // a CTA takes a whole unit and nothing is joined.  Measured, shares / whole units, us: one sequence of 301
   // tokens 12.5 / 6.9; 1000 tokens, 32 units 15.9 / 16.1, 384 units 48 / 46, ragged 38 / 34; but 4000 tokens (250

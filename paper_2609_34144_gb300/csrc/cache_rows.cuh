@@ -384,9 +384,8 @@ struct RowsPlan {
   bool whole;            // a CTA takes a whole unit; else units may be split and are merged
   size_t part_o_bytes, part_ml_bytes, total_bytes;
 };
-// 4-bit pages (cache4_attention.cu): CTAs that an SM holds, tokens of a block, and the launch
+// 4-bit pages (cache4_attention.cu): CTAs that an SM holds, and the launch
 int rows4_ctas(int d, int mt);
-int rows4_block(int d, int mt);
 cast_status launch_rows4(const RowsKArgs& k, const RowsPlan& p, int d, cudaStream_t st);
 
 }  // namespace cast
