@@ -102,6 +102,13 @@ struct AppendKArgs {
   int jobs_kv, jobs_q;    // head groups of K (and of V), of the queries
 };
 
+// Largest magnitude of three, NaN if one is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // One CTA: the new tokens of one sequence in one page (a run of rows lo .. hi-1), for a group of
 // heads of K, V or the queries.  A thread has one unit (row, 16 channels) of every head: it computes its
 // eight angles once, and a page's maximum is known before the values leave the registers.  The next three
@@ -109,13 +116,8 @@ struct AppendKArgs {
 // head's 32 KB on their way otherwise, which is what the copy rate times the memory's latency takes.
 // Bound: memory (every channel read and written once).  Measured, GB300: 14080 tokens, 24 KV and 24 query
 // heads of 128, 8-bit pages (433 MB) 78 us, 5.5 TB/s, with three heads ahead (two 80, one 90 us) and
-// groups of 12 heads (24 79, 8 84, 4 104 us: what the angles cost).
-// Largest magnitude of three, NaN if one is
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float d;
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
+// groups of 12 heads (24 79, 8 84, 4 104 us: what the angles cost).  4-bit pages (395 MB): 79 us, 5.0 TB/s, bound by issue
+// (72 % of the slots: 16 channels of K or V are about 350 instructions, of which 48 are the quotients).
 constexpr int kAhead = 4;
 template <int KIND>   // the pages' type
 __global__ void __launch_bounds__(1024) k_append(const __grid_constant__ AppendKArgs a,

@@ -17,6 +17,11 @@
 // Hidden tokens of a block that the rows do not all see: logits become -inf; their V scales, the only thing that can
 // make a value not finite, become 0, and tokens whose scales are not finite are added one by one where they are seen.
 // A page out of range is scales of 0.
+//
+// Bound: memory, and issue (530 instructions for 32 tokens, of which the conversions are 128 and the products with the
+// scales 128).  Measured, GB300: 24 sequences of 8k to 32k tokens, 8 KV heads of 128, 4 query heads each (626 MB) 111 us,
+// 5.6 TB/s; 48 sequences with windows of 4096 on pages of 16 (234 MB) 59 us, of which 20 are first loads, ends of units and
+// the joining; one sequence of 301 tokens 7 us.
 #include <cmath>
 
 #include "cache.cuh"

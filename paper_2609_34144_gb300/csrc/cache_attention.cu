@@ -554,9 +554,9 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
     const int64_t seen = ((int64_t)a.window + rows) / 16 + 2 + ((int64_t)a.sinks + 15) / 16;
     if (seen < most) most = seen;
   }
-  // 4-bit pages: many units may be longer.  Measured, shares / whole, us, heads of 128: 8 units of 2000 tokens 13 / 19; 128
-  // of 2000 21 / 19, ragged 19 / 19, of 4000 28 / 34; 384 of 2000 39 / 32, of 4000 59 / 56, ragged 45 / 51; 1024 of
-  // 4000 131 / 118, ragged 94 / 93
+  // 4-bit pages: many units may be longer.  Measured, shares / whole, us, heads of 128: 8 units of 2000 tokens 11 / 16; 128
+  // of 2000 20 / 17, ragged 18 / 17, of 3000 23 / 23, ragged 21 / 22; 384 of 2000 35 / 29, of 3000 44 / 39, ragged 36 / 35,
+  // of 4000 53 / 49, ragged 43 / 45; 1024 of 2000 67 / 71, ragged 60 / 54
   const int64_t all = (int64_t)a.batch.B * p.row_tiles * a.cache.H;
   p.whole = most <= 64 || (f4 && all >= 128 && most <= (all >= 384 ? 192 : 128));
   if (p.whole) {

@@ -3,7 +3,9 @@
 // at; attention over the cache itself reads the pages.
 //
 // Bound: memory (4-bit pages: 0.56 bytes a channel in, 2 out).  A thread has 8 channels of a row at a time, so that
-// eight lanes write 128 bytes of a bf16 row side by side, and up to eight heads' loads are on their way together.
+// eight lanes write 128 bytes of a bf16 row side by side, and up to eight heads' loads are on their way together (with
+// four 40 us where it is 35).  Measured, GB300, 24960 tokens of 12 heads of 128 to bf16: from 4 bits (196 MB) 33 us, 5.9 TB/s;
+// from 8 bits 40 us; from bf16 (307 MB) 50 us, 6.1 TB/s.
 #include "cache.cuh"
 
 namespace cast {
