@@ -199,7 +199,7 @@ extern "C" cast_status cast_cache_read(const cast_cache_read_args* a, void* stre
   k.k_stride = a->k_out ? a->k_row_stride : a->v_row_stride;
   k.v_stride = a->v_row_stride;
   const int max_new = a->batch.max_new < a->batch.T ? a->batch.max_new : a->batch.T;
-  k.runs = (max_new + c.page_size - 2) / c.page_size + 1;
+  k.runs = (int)(((int64_t)max_new + c.page_size - 2) / c.page_size + 1);
   const int lanes = c.d / 8, rows = 256 / lanes < c.page_size ? 256 / lanes : c.page_size;
   k.chunks = c.page_size / rows;
   const int64_t gx = (int64_t)k.runs * k.chunks * a->batch.B;

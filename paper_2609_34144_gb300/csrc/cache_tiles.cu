@@ -33,8 +33,8 @@
 // loses 2^-32 of what its codes would be at that scale, at most.
 //
 // 4-bit pages: K and V codes become f16 tiles, two warps a kind, each from a ring of its own that bulk copies fill
-// with a head's rows of a page and their scales; the products' operands take two thirds of shared memory's
-// bandwidth, and the codes' way through it the tenth by which frames are slower than from bf16 pages.  Queries are
+// with a head's rows of a page and their scales.  (Of a key tile of two query tiles the products read 192 KB of shared
+// memory and bf16 pages write 64; the codes add 36, which goes with the 8 % by which frames are slower.)  Queries are
 // turned into f16 in place of their split, P is f16 lifted by 2^7.
 //
 // A unit of one tile (few rows, or a sequence's odd last tile) gives even key tiles to one softmax
@@ -46,8 +46,9 @@
 // needs 0.73 us).  A CTA's first key tile is done 7 to 10 us after its start.  Measured, GB300: 3520 rows of 24
 // heads of 128 over 28160 positions, bf16 807 us, 1508 TFLOP/s, 8 bits 912 us, 1335 TFLOP/s; 1560 rows of 12 heads
 // over 12480 of 24960 positions, bf16 108 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
-// 76 us.  4 bits: the frames 878 us, 1387 TFLOP/s, over the window 121 us, the 35 rows (138 MB) 77 us.  Registers (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to
-// 1 % slower.
+// 76 us.  4 bits: the frames 878 us, 1387 TFLOP/s, over the window 121 us, the 35 rows (138 MB) 77 us.  Registers
+// (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to 1 % slower (4 bits: -2 % for
+// the 35 rows and 8 % for the window).
 #include <cmath>
 #include <type_traits>
 
