@@ -731,3 +731,31 @@ def test_binding_refuses_tensors_that_are_not_on_the_gpu(lib):
                  lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len, 5, k_out=out), lambda: lib.cast_cache_read(c.cache, c.table, c.kv_len, 5, v_out=out)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,H_q", [(1, 6), (2, 12), (3, 20), (50, 8)])
+def test_every_page_size_and_form(lib, page, d, new, H_q):
+    """Blocks and tiles of several pages and of parts of one, whole units and shares, sinks and windows that begin and end
+    inside pages, with whole pages between them that no row sees, whose table entries are out of range."""
+    H, lens, window, sinks = 2, [3001, 1400, 77], 333, 21
+    c = Pages4(lib, lens, H, d, page, seed=page + d)
+    held = c.fill(seed=page)
+    q = (1.5 * randn(gen(new), 3 * new, H_q, d)).to(torch.bfloat16)
+    for kw, table in ((dict(), c.table), (dict(window=window, sinks=sinks), c.table.clone())):
+        if kw:
+            for b, n in enumerate(lens):
+                first, last = -(-sinks // page), max(0, n - new - window + 1) // page   # pages that no row sees
+                if last > first:
+                    table[b, first:last] = -5
+        o, lse = lib.cast_cache_attention(q, c.cache, table, c.kv_len, want_lse=True, **kw)
+        lib.cast_check_device()
+        check_attention(lib, c, held, q, [new] * 3, o, lse, **kw)
+    # a short table: at most 1024 tokens, so that every CTA has a whole unit
+    short = [min(n, 1024) for n in lens]
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table[:, :1024 // page], i32(*short), want_lse=True)
+    lib.cast_check_device()
+    some = Pages4.__new__(Pages4)
+    some.lens = short
+    check_attention(lib, some, [tuple(x[:n] for x in h) for h, n in zip(held, short)], q, [new] * 3, o, lse)
