@@ -195,9 +195,9 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^-e with the largest channel in [2^14, 2^15); subnormal, zero and infinite rows as they are
-        const int e = (int)(top >> 23) - 127 - 14;
-        const bool plain = e < -126 || e > 113;
+        // 2^-e with the largest channel in [2^14, 2^15), 2^126 at most; rows that are not finite as they are
+        const int e = max((int)(top >> 23) - 127 - 14, -126);
+        const bool plain = e > 113;
         const float down = plain ? 1.f : pow2f(-e), up = a.scale_log2 * (plain ? 1.f : pow2f(e));
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)

@@ -945,8 +945,8 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
         mbar_arrive(&bars->q_full);
       }
       if constexpr (F4) {
-        // the row in f16, times the power of two that brings its largest channel below 2^15 (subnormal, zero and
-        // infinite rows as they are); without a second tile both warpgroups have the row, and write half of it each
+        // the row in f16, times the power of two that brings its largest channel below 2^15 (2^126 at most; rows that
+        // are not finite as they are); without a second tile both warpgroups have the row, and write half of it each
         if (n_tiles > 0 && __any_sync(0xffffffffu, live)) {
           bool w = !aborted(bars) && mbar_wait(&bars->q_raw, 0, lim);
           if (!__all_sync(0xffffffffu, w)) set_abort(bars);
@@ -960,8 +960,8 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
             top = max(top, max(max(x.x & 0x7fff0000u, (x.x << 16) & 0x7fff0000u), max(x.y & 0x7fff0000u, (x.y << 16) & 0x7fff0000u)));
             top = max(top, max(max(x.z & 0x7fff0000u, (x.z << 16) & 0x7fff0000u), max(x.w & 0x7fff0000u, (x.w << 16) & 0x7fff0000u)));
           }
-          const int ex = (int)(top >> 23) - 127 - 14;
-          const bool plain = ex < -126 || ex > 113;
+          const int ex = max((int)(top >> 23) - 127 - 14, -126);
+          const bool plain = ex > 113;
           const float down = plain ? 1.f : pow2f(-ex);
           // never 0 (a scale of 2^-25 under a row of 2^-112): a hidden column's -inf has to stay -inf
           unit = fmaxf(plain ? unit : unit * pow2f(ex), 0x1p-126f);

@@ -21,3 +21,14 @@ def test_a_row_whose_logits_are_next_to_nothing_is_the_mean(lib, new, H_q, d, kw
     q = (randn(gen(new), new, H_q, d) * size).to(torch.bfloat16)
     o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, scale=scale, want_lse=True, out_dtype=torch.float32, **kw)
     check_attention(lib, c, held, q, [new], o, lse, scale=scale, **kw)
+
+
+@pytest.mark.parametrize("new,H_q,d", FORMS)
+@pytest.mark.parametrize("scale,size", [(1e33, 1e-34), (1e35, 1e-36), (2e38, 1e-39), (1e-38, 1e38)])
+def test_queries_at_the_ends_of_bf16(lib, new, H_q, d, scale, size):
+    """Rows of subnormal numbers and of the largest, with a scale that makes ordinary logits of them."""
+    c = Pages4(lib, [700], 2, d, 32, seed=8)
+    held = c.fill(seed=9)
+    q = (randn(gen(new), new, H_q, d).clamp(-3, 3).double() * size).to(torch.bfloat16)
+    o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, scale=scale, want_lse=True, out_dtype=torch.float32)
+    check_attention(lib, c, held, q, [new], o, lse, scale=scale)
