@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kWarps * 32, Cfg4<D, NT>::CTAS) k_cache_rows4(
         // 2^-e with the largest channel in [2^14, 2^15), 2^126 at most; rows that are not finite as they are
         const int e = max((int)(top >> 23) - 127 - 14, -126);
         const bool plain = e > 113;
-        const float down = plain ? 1.f : pow2f(-e), up = a.scale_log2 * (plain ? 1.f : pow2f(e));
+        // (never infinite: keys of zeros give logits of 0)
+        const float down = plain ? 1.f : pow2f(-e), up = fminf(a.scale_log2 * (plain ? 1.f : pow2f(e)), 0x1.fffffep127f);
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
 #pragma unroll

@@ -963,8 +963,9 @@ __global__ void __launch_bounds__(Cfg<HD, KIND>::THREADS, 1)
           const int ex = max((int)(top >> 23) - 127 - 14, -126);
           const bool plain = ex > 113;
           const float down = plain ? 1.f : pow2f(-ex);
-          // never 0 (a scale of 2^-25 under a row of 2^-112): a hidden column's -inf has to stay -inf
-          unit = fmaxf(plain ? unit : unit * pow2f(ex), 0x1p-126f);
+          // never 0 (a scale of 2^-25 under a row of 2^-112): a hidden column's -inf has to stay -inf; and never
+          // infinite (2^16 over 2^127): keys of zeros give logits of 0
+          unit = fminf(fmaxf(plain ? unit : unit * pow2f(ex), 0x1p-126f), 0x1.fffffep127f);
           const int c0 = has_q1 ? 0 : t * (HD / 16), c1 = has_q1 ? HD / 8 : c0 + HD / 16;
 #pragma unroll 2
           for (int c = c0; c < c1; ++c) {

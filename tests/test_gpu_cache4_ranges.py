@@ -1,4 +1,5 @@
 """4-bit pages on the GPU at the ends of what scales and queries may be."""
+import numpy as np
 import pytest
 import torch
 
@@ -32,3 +33,16 @@ def test_queries_at_the_ends_of_bf16(lib, new, H_q, d, scale, size):
     q = (randn(gen(new), new, H_q, d).clamp(-3, 3).double() * size).to(torch.bfloat16)
     o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, scale=scale, want_lse=True, out_dtype=torch.float32)
     check_attention(lib, c, held, q, [new], o, lse, scale=scale)
+
+
+@pytest.mark.parametrize("new,H_q,d", FORMS)
+@pytest.mark.parametrize("kw", MASKS, ids=["causal", "window", "all"])
+def test_keys_of_zeros_under_the_largest_queries_and_scales(lib, new, H_q, d, kw):
+    """Every logit is 0 whatever multiplies it: the mean of the values."""
+    c = Pages4(lib, [700], 2, d, 32, seed=8)
+    (k, v), = c.fill(seed=9)
+    c.ks.zero_()
+    q = (randn(gen(new), new, H_q, d).clamp(-3, 3).double() * 1e38).to(torch.bfloat16)
+    for scale in (1e5, 3e38):
+        o, lse = lib.cast_cache_attention(q, c.cache, c.table, c.kv_len, scale=scale, want_lse=True, out_dtype=torch.float32, **kw)
+        check_attention(lib, c, [(np.zeros_like(k), v)], q, [new], o, lse, scale=scale, **kw)
