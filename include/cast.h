@@ -447,6 +447,19 @@ typedef struct {
  * strides, an unusable table; UNSUPPORTED for a head dim as above. */
 cast_status cast_rotary(const cast_rotary_args* args, void* stream);
 
+/* A pointer to scales: f32 numbers of 8-bit pages, bytes of 4-bit ones.  In C a void*; in C++ of the same size, set
+ * from any pointer and read as float*, or as `bytes`. */
+#ifdef __cplusplus
+struct cast_f32_or_u8 {
+  void* bytes;
+  cast_f32_or_u8() = default;
+  cast_f32_or_u8(void* p) : bytes(p) {}
+  operator float*() const { return static_cast<float*>(bytes); }
+};
+#else
+typedef void* cast_f32_or_u8;
+#endif
+
 typedef struct {
   int32_t dtype;                  /* CAST_BF16, CAST_F8E4M3 or CAST_F4E2M1 */
   int32_t n_pages, page_size;     /* page_size 16, 32, 64 or 128 tokens */
@@ -458,8 +471,8 @@ typedef struct {
   int64_t row_stride;             /* elements between token rows: >= H*d, a multiple of 16; a page
                                      is page_size consecutive rows.  CAST_F4E2M1: a page begins
                                      page_size * row_stride elements (two a byte) behind the one before */
-  void* k_scale;                  /* CAST_F8E4M3: device f32 [n_pages, H], powers of two: a row holds */
-  void* v_scale;                  /* code * scale.  CAST_F4E2M1: device [n_pages, H, page_size, d / 16] bytes, 16-byte
+  cast_f32_or_u8 k_scale;         /* CAST_F8E4M3: device f32 [n_pages, H], powers of two: a row holds */
+  cast_f32_or_u8 v_scale;         /* code * scale.  CAST_F4E2M1: device [n_pages, H, page_size, d / 16] bytes, 16-byte
                                      aligned, each a scale of 5 exponent and 3 mantissa bits: an f16 number's bits
                                      without sign, shifted right by 7 (0xf8 and above: not finite).  Appended ones are
                                      at most 10240, so that every value is exact in f16 and in bf16; the kernels form

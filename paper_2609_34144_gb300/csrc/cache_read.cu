@@ -192,8 +192,8 @@ extern "C" cast_status cast_cache_read(const cast_cache_read_args* a, void* stre
   const bool both = a->k_out && a->v_out;
   k.ck = static_cast<const uint8_t*>(a->k_out ? c.k : c.v);
   k.cv = static_cast<const uint8_t*>(c.v);
-  k.k_scale = static_cast<const uint8_t*>(a->k_out ? c.k_scale : c.v_scale);
-  k.v_scale = static_cast<const uint8_t*>(c.v_scale);
+  k.k_scale = static_cast<const uint8_t*>((a->k_out ? c.k_scale : c.v_scale).bytes);
+  k.v_scale = static_cast<const uint8_t*>(c.v_scale.bytes);
   k.k = a->k_out ? a->k_out : a->v_out;
   k.v = a->v_out;
   k.k_stride = a->k_out ? a->k_row_stride : a->v_row_stride;
