@@ -48,13 +48,12 @@ struct Cfg4 {
   // 16 rows: their queries in shared memory, which leaves the registers to the loop (at 32 tokens 176 -> 169 us, heads of
   // 64 120 -> 112); with 8 rows there are enough (130 -> 134)
   static constexpr bool QS = NT > 1;
-  static constexpr int ROOM = D == 128 ? (NT == 1 ? 18 * 1024 + 256 : 25 * 1024) : (NT == 1 ? 13 * 1024 + 512 : 17 * 1024);   // a warp's ring
-  static constexpr int STAGES = ROOM / STAGE > 8 ? 8 : ROOM / STAGE;
+  static constexpr int STAGES = D == 128 ? 2 : 3;   // of a warp's ring (16 rows: one more would fit; not measured)
   static constexpr int RING = STAGES * STAGE;
   static constexpr int MERGE = kWarps * ROWS * (D + 2) * 4;
   static constexpr int OFF_Q = kWarps * RING > MERGE ? kWarps * RING : MERGE;
   static constexpr int SMEM = OFF_Q + (QS ? NT * (D / 16) * 32 * 8 : 0);
-  static_assert(STAGES >= 2 && (SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
+  static_assert((SMEM + 1024 + 256) * CTAS <= 228 * 1024, "CTAs of an SM");
 };
 
 // The block's token that lane group g's row of a product is (and token + 8 that row g + 8 is): token 4 j + (q ^ j) for

@@ -556,7 +556,8 @@ RowsPlan rows_plan(const cast_cache_attn_args& a) {
   }
   // 4-bit pages: many units may be longer.  Measured, shares / whole, us, heads of 128: 8 units of 2000 tokens 11 / 16; 128
   // of 2000 20 / 17, ragged 18 / 17, of 3000 23 / 23, ragged 21 / 22; 384 of 2000 35 / 29, of 3000 44 / 39, ragged 36 / 35,
-  // of 4000 53 / 49, ragged 43 / 45; 1024 of 2000 67 / 71, ragged 60 / 54
+  // of 4000 53 / 49, ragged 43 / 45; 1024 of 2000 67 / 71, ragged 60 / 54.  The host does not know the lengths, and the
+  // limits are those for ragged ones: equal lengths lose by them at 1024 units of 2000 (whole) and at 384 of 4000 (shares).
   const int64_t all = (int64_t)a.batch.B * p.row_tiles * a.cache.H;
   p.whole = most <= 64 || (f4 && all >= 128 && most <= (all >= 384 ? 192 : 128));
   if (p.whole) {

@@ -44,9 +44,9 @@
 // Bound: products and exponentials, about 1 us each of the 1.6 us (8 bits: 1.9 us) that a key tile of two query
 // tiles takes; with one query tile of few rows the products of 128 rows (1 us a key tile, of which memory
 // needs 0.73 us).  A CTA's first key tile is done 7 to 10 us after its start.  Measured, GB300: 3520 rows of 24
-// heads of 128 over 28160 positions, bf16 807 us, 1508 TFLOP/s, 8 bits 912 us, 1335 TFLOP/s; 1560 rows of 12 heads
+// heads of 128 over 28160 positions, bf16 807 us, 1508 TFLOP/s, 8 bits 906 us, 1344 TFLOP/s; 1560 rows of 12 heads
 // over 12480 of 24960 positions, bf16 108 us; 4 sequences of 35 rows and 60011 positions, 4 heads, 8 bits (246 MB)
-// 76 us.  4 bits: the frames 878 us, 1387 TFLOP/s, over the window 121 us, the 35 rows (138 MB) 77 us.  Registers
+// 76 us.  4 bits: the frames 874 us, 1394 TFLOP/s, over the window 124 us, the 35 rows (138 MB) 77 us.  Registers
 // (control, softmax, decoding warps): the splits that fit and differ by one step are 0.4 to 1 % slower (4 bits: -2 % for
 // the 35 rows and 8 % for the window).
 #include <cmath>
@@ -377,8 +377,8 @@ struct Bars {
   uint32_t apart[kStages][4];          // V rows of a stage's tile that are added one by one
   float2 ml[BM];                       // maximum and sum of the second warpgroup's rows
   Unit unit, next;                     // of this segment and the next
-  // The codes' barriers come last: between the others they slowed every kind of pages down (frames of 3520 tokens, L2
-  // flushed, 8 bits 919 -> 908 us, bf16 824 -> 820, 4 bits 886 -> 882)
+  // (the order of the members changes the compiled code, and with it times by about 1 %: with these behind v_fixed frames of
+  // 3520 tokens take 916 us in 8 bits, 822 in bf16, 877 in 4 bits, with the window 127, and here 906, 815, 874 and 124)
   uint64_t raw_full[6], raw_empty[6];   // 8-bit pages: V codes; 4-bit pages: K and V codes and scales
   uint32_t absent[6];                  // 4-bit pages: pages of a stage's codes that were not fetched
 };

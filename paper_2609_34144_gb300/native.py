@@ -810,7 +810,8 @@ def cast_cache_read(cache, page_table, kv_len, rows, cu_new=None, max_new=None, 
                     dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
     """What the cache (of any type) holds of the last tokens of its sequences, in their order: `rows` of them in all,
     rows / B each or, with cu_new [B + 1], cu_new[b + 1] - cu_new[b]; kv_len [B] says where they end.  Returns (k, v),
-    each [rows, H, d] of `dtype` (bf16 or f32), None where keys or values is False and no output is given."""
+    each [rows, H, d] of `dtype` (bf16 or f32), None where keys or values is False and no output is given.  Rows that no
+    sequence has (behind cu_new[B], or a sequence's past max_new) are not written: as they were, or uninitialised."""
     H, d = cache.heads
     if cache.device < 0:
         raise ValueError("the cache must be on the GPU")
